@@ -11,7 +11,7 @@ With ``own`` false, ``run`` is the plain form: elementary torch operations in 32
 at the end.  With ``own`` true it calls the library's entry points.
 
 8-bit values are e4m3 with one power-of-two scale per 32 consecutive values: the smallest power
-for which no finite value of the block exceeds 448, kept between 2^-120 and 2^120 and stored as
+for which no finite value of the block exceeds 448, kept between 2^-120 and 2^119 and stored as
 its exponent plus 127.
 """
 import random
@@ -138,7 +138,7 @@ def _scale_bytes(amax):
     """Stored exponents of the scales for blocks of the given largest magnitudes (32-bit floats)."""
     mant, exp = torch.frexp(amax)                                       # amax = mant * 2^exp, 0.5 <= mant < 1
     k = torch.where(mant > 0.875, exp - 8, exp - 9)                     # 448 = 0.875 * 2^9
-    k = torch.where(amax > 0, k.clamp(-120, 120), -120)
+    k = torch.where(amax > 0, k.clamp(-120, 119), -120)
     return (k + 127).to(torch.uint8)
 
 
@@ -326,8 +326,8 @@ def _exact_codes(x):
     """Block scales and e4m3 values of 64-bit numbers, by logarithms corrected to the definition, and a rounding grid."""
     g = x.unflatten(-1, (-1, _GROUP))
     amax = g.abs().amax(-1, keepdim=True)
-    k = torch.ceil(torch.log2(amax.clamp_min(2.0 ** -140) / 448.0)).clamp(-120, 120)
-    k = torch.where(amax > 448.0 * 2.0 ** k, k + 1, torch.where(amax <= 448.0 * 2.0 ** (k - 1), k - 1, k)).clamp(-120, 120)
+    k = torch.ceil(torch.log2(amax.clamp_min(2.0 ** -140) / 448.0)).clamp(-120, 119)
+    k = torch.where(amax > 448.0 * 2.0 ** k, k + 1, torch.where(amax <= 448.0 * 2.0 ** (k - 1), k - 1, k)).clamp(-120, 119)
     z = g / 2.0 ** k
     step = torch.ldexp(torch.ones_like(z), torch.frexp(z.abs().clamp_min(2.0 ** -6)).exponent - 4)      # spacing of e4m3 at each magnitude
     return (torch.round(z / step) * step).flatten(-2), (2.0 ** k).squeeze(-1)     # round() takes ties to even
