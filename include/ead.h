@@ -53,6 +53,7 @@ extern "C" {
 #define EAD_STATUS_WAIT_EXPIRED 0x2u /* a bounded wait inside a kernel ran out                 */
 #define EAD_STATUS_BAD_COUNT   0x4u /* internal row counts inconsistent                       */
 #define EAD_STATUS_SHARD_MISMATCH 0x8u /* vocabulary shards disagree on the step or on a row's model */
+#define EAD_STATUS_BAD_PAGE    0x10u /* paged cache: page index out of range, or position not below max_len */
 
 typedef struct ead_ctx ead_ctx; /* opaque */
 
@@ -368,6 +369,144 @@ void ead_destroy(ead_ctx *ctx);
 int ead_head_entropy_static(const void *W, const void *h, int32_t B, int32_t V, int32_t H,
                             int32_t *tok, float *H_out, uint32_t *status, int32_t device,
                             void *stream);
+
+/*
+ * Decoder-side operators around the gate step: what M_S and M_L do between two gate steps with
+ * their contexts.  (The paper defines none of them: "l <- M_t(x + y)" is one line of Algorithm 1.
+ * A sequence that stays on its model brings one new token per step; one that was just switched
+ * brings every token its new model has not seen, which is why attention takes a CHUNK of new
+ * tokens per sequence, of a different length for every sequence of the batch.)
+ *
+ * Number formats.  EAD_FMT_BF16: bf16 values.  EAD_FMT_E4M3: 8-bit e4m3 codes, and for every 32
+ * consecutive values (along the head dimension, or along a hidden row) one scale byte e that
+ * stands for 2^(e - 127): value = code * 2^(e - 127).  The scale is the smallest power of two for
+ * which no finite value of the block exceeds 448, limited to 2^-120 .. 2^119 (a block of zeros
+ * has 2^-120; beyond 448 * 2^119 values saturate); codes are rounded to nearest, ties to even.  A block
+ * with a NaN or an infinity in it gets scale byte 255 and codes 0x7F, and reads as NaNs.  All
+ * other values are exact in bf16.  Code 0x7F does not occur under another scale byte; what is
+ * read for it there is unspecified.
+ *
+ * All four calls only enqueue work on `stream` of `device` (which they make current), allocate
+ * nothing and copy nothing to the host.  They own no state: every buffer is the caller's.
+ * Row strides are in elements; rows, pools and strides must keep 16-byte alignment.
+ */
+#define EAD_FMT_BF16 0
+#define EAD_FMT_E4M3 1
+#define EAD_FMT_BLOCK 32               /* values per scale byte */
+
+/*
+ * One layer's paged key/value cache.  Token slot s of page p of head h is the head_dim values at
+ * element p * page_stride + h * head_stride + s * slot_stride of k and of v (so pages may be laid
+ * out head by head or token by token, and k and v may be halves of one allocation).
+ */
+typedef struct ead_kv_cache {
+    int32_t format;          /* EAD_FMT_BF16 or EAD_FMT_E4M3                                    */
+    int32_t heads_kv;        /* 1 .. 128                                                        */
+    int32_t head_dim;        /* 64 or 128                                                       */
+    int32_t page_size;       /* token slots per page: 8, 16, 32, 64, 128 or 256                 */
+    int32_t n_pages;         /* pages in the pools                                              */
+    int32_t reserved;        /* 0                                                               */
+    int64_t page_stride, head_stride, slot_stride;   /* elements                                */
+    void *k, *v;             /* dev pools                                                       */
+    uint8_t *k_scale, *v_scale;   /* dev, EAD_FMT_E4M3 only: [n_pages, heads_kv, page_size,
+                                     head_dim / 32] bytes, contiguous; NULL for EAD_FMT_BF16    */
+} ead_kv_cache;
+
+/*
+ * The step's batch.  Sequence b brings the tokens new_start[b] .. new_start[b + 1] - 1 of the
+ * step (possibly none); they are the LAST tokens of its context of kv_len[b] tokens, i.e. token
+ * i of them has position kv_len[b] - n_b + i.  Position p lives in page
+ * page_table[b * table_stride + p / page_size], slot p % page_size.
+ * max_new and max_len are upper bounds of n_b and kv_len[b] known to the host; the arrays
+ * themselves stay on the device (a captured graph replays with new contents).  Positions at or
+ * beyond max_len have no place: no page table entry is read for them.
+ */
+typedef struct ead_kv_batch {
+    int32_t B;               /* sequences, 1 .. 4096                                            */
+    int32_t n_tokens;        /* new tokens of the step = new_start[B]; >= 0                     */
+    int32_t max_new;         /* >= every n_b                                                    */
+    int32_t max_len;         /* >= every kv_len[b], at most 2^30                                */
+    const int32_t *new_start;    /* dev [B + 1], ascending, new_start[0] = 0                    */
+    const int32_t *kv_len;       /* dev [B]                                                     */
+    const int32_t *page_table;   /* dev [B, table_stride]; entries beyond a context are not read */
+    int32_t table_stride;    /* entries per row, >= ceil(max_len / page_size)                   */
+    int32_t reserved;        /* 0                                                               */
+} ead_kv_batch;
+
+/*
+ * Writes the new tokens' keys and values into the cache, quantised where its format says so.
+ *   k_new, v_new  dev, bf16 [n_tokens, heads_kv, head_dim]; new_stride elements between tokens
+ *                 (heads of a token are contiguous), so both may be slices of one projection
+ *   status        dev uint32 or NULL; EAD_STATUS_BAD_PAGE is OR-ed in when a token has no valid
+ *                 place (its page index is out of range, its position negative or not below
+ *                 max_len); such a token is not written
+ * Two tokens of a step must not share a slot.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT,
+ * EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ */
+int ead_kv_write(const ead_kv_cache *cache, const ead_kv_batch *batch, const void *k_new, const void *v_new,
+                 int64_t new_stride, uint32_t *status, int32_t device, void *stream);
+
+/*
+ * Reads tokens back as bf16.  Row new_start[b] + i of the outputs is position first[b] + i of
+ * sequence b (first NULL: 0), for i < n_b; batch->kv_len is not used and may be NULL.
+ *   k_out, v_out  dev, bf16 [n_tokens, heads_kv, head_dim], out_stride elements between tokens
+ *   first         dev int32 [B] or NULL
+ * A token without a valid place reads as zeros and sets EAD_STATUS_BAD_PAGE in status.
+ * Errors as ead_kv_write.
+ */
+int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int32_t *first, void *k_out, void *v_out,
+                int64_t out_stride, uint32_t *status, int32_t device, void *stream);
+
+/*
+ * Attention of the step's new tokens over the paged cache (which already holds them:
+ * ead_kv_write comes first).  Query head hq reads cache head hq / (heads_q / heads_kv).  A query
+ * at position p sees key j iff j <= p and (window == 0 or j > p - window or j < sinks):
+ *   z_j = scale * q . k_j,  out = sum_j exp(z_j) v_j / sum_j exp(z_j),  lse = ln sum_j exp(z_j)
+ * with sums and maxima in 32 bits; probabilities are rounded to bf16 (the type of the values
+ * they weight) before the product with v.  A query that sees nothing (its position is negative)
+ * gets zeros and lse = -infinity.  Keys that no query of a sequence sees are not
+ * read, nor are the page table entries of pages that hold only such keys.
+ *   q          dev, bf16 [n_tokens, heads_q, head_dim], q_stride elements between tokens
+ *   heads_q    a multiple of heads_kv, at most 128 per cache head
+ *   scale      of the logits, finite and > 0
+ *   window     >= 0; 0 = all earlier tokens;  sinks  >= 0; used with a window
+ *   out        dev, bf16 [n_tokens, heads_q, head_dim], out_stride elements between tokens
+ *   lse        dev float [n_tokens, heads_q] or NULL
+ *   workspace  dev, EAD_KV_WORKSPACE_BYTES bytes, 256-byte aligned, zero-filled ONCE by the caller;
+ *              every call leaves it ready for the next one.  Calls that may overlap on the
+ *              device need a workspace each
+ *   status     dev uint32 or NULL.  EAD_STATUS_BAD_PAGE: a page index was out of range (its
+ *              tokens count as zeros) or a context is longer than max_len (the rest is not
+ *              seen); EAD_STATUS_BAD_COUNT: a sequence has more than max_new new tokens (its rows
+ *              may be unwritten); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out
+ * The result does not depend on the order in which blocks run: partial results are joined in a
+ * fixed order.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ */
+#define EAD_KV_WORKSPACE_BYTES (64u << 20)
+int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *batch, const void *q, int64_t q_stride,
+                     int32_t heads_q, float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride,
+                     float *lse, void *workspace, uint32_t *status, int32_t device, void *stream);
+
+/*
+ * Residual addition and root-mean-square norm of n_rows hidden rows of H elements:
+ *   s = x + residual (32 bits),  residual_out = bf16(s),
+ *   y = s / sqrt(mean(s^2) + eps) * weight,  out = y in `format`
+ * The sum of squares is taken over the unrounded s.  With EAD_FMT_BF16 the output is what
+ * ead_step takes as h_small / h_large.
+ *   x             dev, bf16 rows, x_stride elements apart
+ *   residual      dev, bf16 rows, residual_stride apart, or NULL (s = x)
+ *   residual_out  dev, bf16 rows, residual_out_stride apart, or NULL; may be residual itself
+ *   weight        dev, bf16 [H]
+ *   out           dev, bf16 or e4m3 rows, out_stride apart; may be x itself for EAD_FMT_BF16
+ *   out_scale     dev, uint8 [n_rows, H / 32], EAD_FMT_E4M3 only, else NULL
+ *   H             multiple of 8 (of 32 for EAD_FMT_E4M3), 8 .. 16384
+ * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (H), EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ */
+#define EAD_NORM_MAX_H 16384
+int ead_add_rmsnorm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                    void *residual_out, int64_t residual_out_stride, const void *weight, float eps, int32_t n_rows,
+                    int32_t H, int32_t format, void *out, int64_t out_stride, uint8_t *out_scale, int32_t device,
+                    void *stream);
 
 /* Static, NUL-terminated description of an EAD_E* code. */
 const char *ead_strerror(int code);

@@ -28,13 +28,19 @@ EAD_STATUS_BAD_COUNT = 0x4
 EAD_STATUS_SHARD_MISMATCH = 0x8
 EAD_SHARD_RECORD_BYTES = 32
 EAD_SHARD_MAX = 16
+EAD_STATUS_BAD_PAGE = 0x10
+EAD_FMT_BF16 = 0
+EAD_FMT_E4M3 = 1
+EAD_FMT_BLOCK = 32
+EAD_KV_WORKSPACE_BYTES = 64 << 20
+EAD_NORM_MAX_H = 16384
 
 SYMBOLS = ["ead_create", "ead_step", "ead_run", "ead_run_host", "ead_run_timed", "ead_reset", "ead_status",
            "ead_state_size", "ead_get_state", "ead_set_state", "ead_kernel_launches",
            "ead_launch_info", "ead_destroy", "ead_strerror", "ead_head_entropy_static",
            "ead_plan_split", "ead_plan_units", "ead_usage", "ead_parameter_ratio", "ead_set_done", "ead_get_done",
            "ead_shard_range", "ead_shard_partials", "ead_shard_gate", "ead_shard_connect",
-           "ead_shard_exchange_bytes"]
+           "ead_shard_exchange_bytes", "ead_kv_write", "ead_kv_read", "ead_kv_attention", "ead_add_rmsnorm"]
 
 
 class EadConfig(C.Structure):
@@ -44,6 +50,21 @@ class EadConfig(C.Structure):
                 ("temperature", C.c_float), ("seed", C.c_uint64), ("eos_token", C.c_int32),
                 ("V_large", C.c_int32), ("shard_count", C.c_int32), ("vocab_offset_small", C.c_int32),
                 ("vocab_offset_large", C.c_int32)]
+
+
+class EadKvCache(C.Structure):
+    """``struct ead_kv_cache``; made by ``ead_kv_cache``."""
+    _fields_ = [("format", C.c_int32), ("heads_kv", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("reserved", C.c_int32), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("slot_stride", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class EadKvBatch(C.Structure):
+    """``struct ead_kv_batch``; made by ``ead_kv_batch``."""
+    _fields_ = [("B", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32),
+                ("new_start", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p),
+                ("table_stride", C.c_int32), ("reserved", C.c_int32)]
 
 
 class EadError(RuntimeError):
@@ -116,6 +137,15 @@ def lib() -> C.CDLL:
         L.ead_shard_partials.argtypes = [vp, vp, vp, vp]
         L.ead_shard_gate.restype = C.c_int
         L.ead_shard_gate.argtypes = [vp, vp, C.c_int32, i32p, f32p, f32p, u8p, u8p]
+        i32, i64 = C.c_int32, C.c_int64
+        L.ead_kv_write.restype = C.c_int
+        L.ead_kv_write.argtypes = [vp, vp, vp, vp, i64, vp, i32, vp]
+        L.ead_kv_read.restype = C.c_int
+        L.ead_kv_read.argtypes = [vp, vp, vp, vp, vp, i64, vp, i32, vp]
+        L.ead_kv_attention.restype = C.c_int
+        L.ead_kv_attention.argtypes = [vp, vp, vp, i64, i32, C.c_float, i32, i32, vp, i64, vp, vp, vp, i32, vp]
+        L.ead_add_rmsnorm.restype = C.c_int
+        L.ead_add_rmsnorm.argtypes = [vp, i64, vp, i64, vp, i64, vp, C.c_float, i32, i32, i32, vp, i64, vp, i32, vp]
         L.ead_strerror.restype = C.c_char_p
         L.ead_strerror.argtypes = [C.c_int]
         _lib = L
@@ -293,6 +323,145 @@ def ead_shard_gate(ctx, all_records, n_shards, tok=None, H=None, Hbar=None, mode
                    next_model=None) -> None:
     _check(lib().ead_shard_gate(ctx, _ptr(all_records), int(n_shards), _ptr(tok), _ptr(H), _ptr(Hbar),
                                 _ptr(model_used), _ptr(next_model)), "ead_shard_gate")
+
+
+def _rows(t, dims: int, what: str) -> int:
+    """Elements between the rows (dimension 0) of a tensor whose other ``dims - 1`` dimensions are contiguous."""
+    if t.dim() != dims or (t.numel() and not t[0].is_contiguous()):
+        raise ValueError(f"{what}: want {dims} dimensions, contiguous within a row")
+    inner = 1
+    for n in t.shape[1:]:
+        inner *= n
+    return t.stride(0) if t.shape[0] > 1 else inner
+
+
+def _want(t, dtype: str, what: str) -> None:
+    if str(t.dtype) not in dtype:
+        raise ValueError(f"{what}: {t.dtype}, want {dtype}")
+
+
+def ead_kv_cache(k, v, k_scale=None, v_scale=None) -> EadKvCache:
+    """Describes a paged cache held in tensors; they are borrowed (the description keeps them alive).
+
+    ``k``, ``v``: ``[n_pages, heads_kv, page_size, head_dim]``, bf16, or 8-bit (``torch.float8_e4m3fn`` or
+    ``torch.uint8``) with ``*_scale`` uint8 ``[n_pages, heads_kv, page_size, head_dim / 32]``.  The last
+    dimension is contiguous, the others have any strides (a cache laid out token by token is a
+    ``transpose(1, 2)`` of its tensor), the same for both."""
+    e4m3 = k_scale is not None
+    for t, name in ((k, "k"), (v, "v")):
+        _want(t, "torch.float8_e4m3fn torch.uint8" if e4m3 else "torch.bfloat16", name)
+        if t.dim() != 4 or t.stride(3) != 1 or t.shape != k.shape or t.stride() != k.stride():
+            raise ValueError(f"{name}: want [n_pages, heads_kv, page_size, head_dim], contiguous in the last "
+                             "dimension, k and v alike")
+    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        if (t is not None) != e4m3:
+            raise ValueError("k_scale and v_scale come together")
+        if e4m3 and (str(t.dtype) != "torch.uint8" or not t.is_contiguous()
+                     or tuple(t.shape) != (*k.shape[:3], k.shape[3] // EAD_FMT_BLOCK)):
+            raise ValueError(f"{name}: want contiguous uint8 [n_pages, heads_kv, page_size, head_dim / 32]")
+    c = EadKvCache(EAD_FMT_E4M3 if e4m3 else EAD_FMT_BF16, k.shape[1], k.shape[3], k.shape[2], k.shape[0], 0,
+                   *k.stride()[:3], _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+    c.held = (k, v, k_scale, v_scale)
+    return c
+
+
+def ead_kv_batch(page_table, new_start, kv_len=None, *, n_tokens, max_new, max_len) -> EadKvBatch:
+    """Describes one step's batch: device int32 tensors ``page_table`` ``[B, entries]``, ``new_start``
+    ``[B + 1]``, ``kv_len`` ``[B]`` (borrowed; the description keeps them alive) and what the host knows
+    of them.  ``kv_len`` may be omitted for reading."""
+    for t, name in ((page_table, "page_table"), (new_start, "new_start"), (kv_len, "kv_len")):
+        if t is not None:
+            _want(t, "torch.int32", name)
+    B = page_table.shape[0]
+    if page_table.stride(1) != 1 or not new_start.is_contiguous() or new_start.numel() != B + 1:
+        raise ValueError("want page_table [B, entries] with contiguous rows and new_start [B + 1]")
+    if kv_len is not None and (not kv_len.is_contiguous() or kv_len.numel() != B):
+        raise ValueError("kv_len: want [B]")
+    c = EadKvBatch(B, int(n_tokens), int(max_new), int(max_len), _ptr(new_start), _ptr(kv_len), _ptr(page_table),
+                   page_table.stride(0) if B > 1 else page_table.shape[1], 0)
+    c.held = (page_table, new_start, kv_len)
+    return c
+
+
+def _shape(t, shape, what: str) -> None:
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, want {shape}")
+
+
+def ead_kv_write(cache: EadKvCache, batch: EadKvBatch, k_new, v_new, *, status=None, device=0, stream=0) -> None:
+    """Writes the step's keys and values, bf16 ``[n_tokens, heads_kv, head_dim]``, into the cache."""
+    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+        _want(t, "torch.bfloat16", name)
+        _shape(t, (batch.n_tokens, cache.heads_kv, cache.head_dim), name)
+    stride = _rows(k_new, 3, "k_new")
+    if _rows(v_new, 3, "v_new") != stride:
+        raise ValueError("k_new and v_new: want the same row stride")
+    _check(lib().ead_kv_write(C.byref(cache), C.byref(batch), _ptr(k_new), _ptr(v_new), stride, _ptr(status),
+                              device, stream or None), "ead_kv_write")
+
+
+def ead_kv_read(cache: EadKvCache, batch: EadKvBatch, k_out, v_out, *, first=None, status=None, device=0,
+                stream=0) -> None:
+    """Reads tokens back as bf16 ``[n_tokens, heads_kv, head_dim]``; ``first``: int32 ``[B]``, first positions."""
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        _want(t, "torch.bfloat16", name)
+        _shape(t, (batch.n_tokens, cache.heads_kv, cache.head_dim), name)
+    if first is not None:
+        _want(first, "torch.int32", "first")
+        _shape(first, (batch.B,), "first")
+    stride = _rows(k_out, 3, "k_out")
+    if _rows(v_out, 3, "v_out") != stride:
+        raise ValueError("k_out and v_out: want the same row stride")
+    _check(lib().ead_kv_read(C.byref(cache), C.byref(batch), _ptr(first), _ptr(k_out), _ptr(v_out), stride,
+                             _ptr(status), device, stream or None), "ead_kv_read")
+
+
+def ead_kv_attention(cache: EadKvCache, batch: EadKvBatch, q, out, *, scale, workspace, window=0, sinks=0, lse=None,
+                     status=None, device=0, stream=0) -> None:
+    """Attention of the step's new tokens over the paged cache; ``q`` and ``out`` are bf16
+    ``[n_tokens, heads_q, head_dim]``, ``lse`` float ``[n_tokens, heads_q]``; ``workspace`` is a zero-filled
+    buffer of ``EAD_KV_WORKSPACE_BYTES`` that calls which may overlap must not share."""
+    _want(q, "torch.bfloat16", "q")
+    _want(out, "torch.bfloat16", "out")
+    heads_q = q.shape[1]
+    _shape(q, (batch.n_tokens, heads_q, cache.head_dim), "q")
+    _shape(out, (batch.n_tokens, heads_q, cache.head_dim), "out")
+    if lse is not None:
+        _want(lse, "torch.float32", "lse")
+        _shape(lse, (batch.n_tokens, heads_q), "lse")
+        if not lse.is_contiguous():
+            raise ValueError("lse: want a contiguous tensor")
+    if workspace.numel() * workspace.element_size() < EAD_KV_WORKSPACE_BYTES:
+        raise ValueError("workspace: want EAD_KV_WORKSPACE_BYTES bytes")
+    _check(lib().ead_kv_attention(C.byref(cache), C.byref(batch), _ptr(q), _rows(q, 3, "q"), heads_q, scale, window,
+                                  sinks, _ptr(out), _rows(out, 3, "out"), _ptr(lse), _ptr(workspace), _ptr(status),
+                                  device, stream or None), "ead_kv_attention")
+
+
+def ead_add_rmsnorm(x, weight, out, *, residual=None, residual_out=None, out_scale=None, eps=1e-6, device=0,
+                    stream=0) -> None:
+    """``out = norm(x + residual) * weight`` over bf16 rows ``[n, H]``, ``residual_out = x + residual``; with
+    ``out_scale`` (uint8 ``[n, H / 32]``) the output is 8-bit (``torch.float8_e4m3fn`` or ``torch.uint8``)."""
+    n, H = x.shape
+    _want(x, "torch.bfloat16", "x")
+    _want(weight, "torch.bfloat16", "weight")
+    _shape(weight, (H,), "weight")
+    _want(out, "torch.float8_e4m3fn torch.uint8" if out_scale is not None else "torch.bfloat16", "out")
+    _shape(out, (n, H), "out")
+    for t, name in ((residual, "residual"), (residual_out, "residual_out")):
+        if t is not None:
+            _want(t, "torch.bfloat16", name)
+            _shape(t, (n, H), name)
+    if out_scale is not None:
+        _want(out_scale, "torch.uint8", "out_scale")
+        _shape(out_scale, (n, H // EAD_FMT_BLOCK), "out_scale")
+        if not out_scale.is_contiguous():
+            raise ValueError("out_scale: want a contiguous tensor")
+    _check(lib().ead_add_rmsnorm(_ptr(x), _rows(x, 2, "x"), _ptr(residual),
+                                 0 if residual is None else _rows(residual, 2, "residual"), _ptr(residual_out),
+                                 0 if residual_out is None else _rows(residual_out, 2, "residual_out"), _ptr(weight),
+                                 eps, n, H, EAD_FMT_BF16 if out_scale is None else EAD_FMT_E4M3, _ptr(out),
+                                 _rows(out, 2, "out"), _ptr(out_scale), device, stream or None), "ead_add_rmsnorm")
 
 
 def ead_destroy(ctx) -> None:

@@ -12,7 +12,7 @@ import sys
 _DIR = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_DIR, "csrc")
 LIB_PATH = os.path.join(_DIR, "libead_b200.so")
-SOURCES = [os.path.join(_CSRC, "ead_api.cu")]
+SOURCES = [os.path.join(_CSRC, f) for f in ("ead_api.cu", "ead_decoder_api.cu")]
 
 
 def _deps():

@@ -17,6 +17,7 @@
 #include "lmhead_kernel.cuh"
 #include "lmhead_dual_kernel.cuh"
 #include "lmhead_small_kernel.cuh"
+#include "tma_host.h"
 
 using namespace ead;
 
@@ -37,24 +38,6 @@ struct StateHeader {
     uint32_t magic;
     int32_t B, w, step;
 };
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled_fn()
-{
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
-    }
-    return fn;
-}
 
 // bf16 matrix [rows, cols] row major -> tiles of box_rows x 64 elements, 128-byte swizzle,
 // out-of-range elements read as zero.

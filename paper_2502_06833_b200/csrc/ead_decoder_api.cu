@@ -1,0 +1,266 @@
+// Host side of the decoder-side operators declared in include/ead.h: paged key/value cache, chunk
+// attention over it, residual norm.  Stateless: arguments are checked, kernels are enqueued.
+#include "../../include/ead.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "attention_kernels.cuh"
+#include "kv_cache_kernels.cuh"
+#include "rmsnorm_kernel.cuh"
+#include "tma_host.h"
+
+using namespace ead;
+
+namespace {
+
+#define EAD_CUDA(x)                          \
+    do {                                     \
+        if ((x) != cudaSuccess) {            \
+            cudaGetLastError();              \
+            return EAD_ECUDA;                \
+        }                                    \
+    } while (0)
+
+constexpr int kMaxDevices = 64;
+
+struct DeviceInfo {
+    bool ready = false;
+    int sms = 0;
+};
+
+std::mutex g_mu;
+DeviceInfo g_dev[kMaxDevices];
+
+// Makes `device` current; on its first use checks the architecture and sets kernel attributes.
+int use_device(int device, DeviceInfo **out)
+{
+    if (device < 0 || device >= kMaxDevices) return EAD_EINVALID_ARG;
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceInfo &d = g_dev[device];
+    if (!d.ready) {
+        int n = 0, major = 0;
+        EAD_CUDA(cudaGetDeviceCount(&n));
+        if (device >= n) return EAD_EINVALID_ARG;
+        EAD_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device));
+        if (major != 10) return EAD_EUNSUPPORTED_ARCH;
+        EAD_CUDA(cudaSetDevice(device));
+        EAD_CUDA(cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, device));
+        d.ready = true;
+    }
+    EAD_CUDA(cudaSetDevice(device));
+    *out = &d;
+    return EAD_OK;
+}
+
+int launched() { return cudaGetLastError() == cudaSuccess ? EAD_OK : EAD_ECUDA; }
+
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int check_cache(const ead_kv_cache *c, KvCacheView *v)
+{
+    if (!c || (c->format != EAD_FMT_BF16 && c->format != EAD_FMT_E4M3) || c->reserved) return EAD_EINVALID_ARG;
+    if (c->heads_kv < 1 || c->heads_kv > 128 || (c->head_dim != 64 && c->head_dim != 128)) return EAD_EINVALID_ARG;
+    if (c->page_size < 8 || c->page_size > 256 || (c->page_size & (c->page_size - 1)) || c->n_pages < 1)
+        return EAD_EINVALID_ARG;
+    if (!c->k || !c->v || c->page_stride < 0 || c->head_stride < 0 || c->slot_stride < c->head_dim) return EAD_EINVALID_ARG;
+    const bool e4m3 = c->format == EAD_FMT_E4M3;
+    if (e4m3 != (c->k_scale != nullptr) || e4m3 != (c->v_scale != nullptr)) return EAD_EINVALID_ARG;
+    const int per16 = e4m3 ? 16 : 8;                  // elements in 16 bytes
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || c->page_stride % per16 || c->head_stride % per16 ||
+        c->slot_stride % per16)
+        return EAD_EALIGNMENT;
+    if (e4m3 && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))) return EAD_EALIGNMENT;
+    v->k = static_cast<uint8_t *>(c->k);
+    v->v = static_cast<uint8_t *>(c->v);
+    v->k_scale = c->k_scale;
+    v->v_scale = c->v_scale;
+    v->page_stride = c->page_stride;
+    v->head_stride = c->head_stride;
+    v->slot_stride = c->slot_stride;
+    v->heads = c->heads_kv;
+    v->head_dim = c->head_dim;
+    v->page_size = c->page_size;
+    v->page_shift = __builtin_ctz(static_cast<unsigned>(c->page_size));
+    v->n_pages = c->n_pages;
+    return EAD_OK;
+}
+
+int check_batch(const ead_kv_batch *b, const KvCacheView &c, bool needs_len, KvBatchView *v)
+{
+    if (!b || b->reserved || b->B < 1 || b->B > 4096 || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0)
+        return EAD_EINVALID_ARG;
+    if (!b->new_start || (needs_len && !b->kv_len) || !b->page_table || b->table_stride < 1) return EAD_EINVALID_ARG;
+    if (b->n_tokens > static_cast<int64_t>(b->B) * b->max_new) return EAD_EINVALID_ARG;
+    if (b->max_len > static_cast<int64_t>(b->table_stride) * c.page_size) return EAD_EINVALID_ARG;
+    if (b->max_len > (1 << 30)) return EAD_EINVALID_ARG;   // positions stay within 32 bits
+    if (!aligned(b->new_start, 4) || !aligned(b->kv_len, 4) || !aligned(b->page_table, 4)) return EAD_EALIGNMENT;
+    v->new_start = b->new_start;
+    v->kv_len = b->kv_len;
+    v->page_table = b->page_table;
+    v->B = b->B;
+    v->n_tokens = b->n_tokens;
+    v->max_new = b->max_new;
+    v->max_len = b->max_len;
+    v->table_stride = b->table_stride;
+    return EAD_OK;
+}
+
+// Caller's bf16 rows of `elements` values, `stride` apart.
+int check_rows(const void *p, int64_t stride, int64_t elements)
+{
+    if (!p || stride < elements) return EAD_EINVALID_ARG;
+    if (!aligned(p, 16) || stride % 8) return EAD_EALIGNMENT;
+    return EAD_OK;
+}
+
+int move_setup(const ead_kv_cache *cache, const ead_kv_batch *batch, const void *k, const void *v, int64_t stride,
+               uint32_t *status, bool needs_len, int32_t device, KvMoveParams *p, DeviceInfo **d)
+{
+    int rc = check_cache(cache, &p->cache);
+    if (rc == EAD_OK) rc = check_batch(batch, p->cache, needs_len, &p->batch);
+    const int64_t row = static_cast<int64_t>(p->cache.heads) * p->cache.head_dim;
+    if (rc != EAD_OK || p->batch.n_tokens == 0) return rc;      // nothing to do: the rows may have no address
+    rc = check_rows(k, stride, row);
+    if (rc == EAD_OK) rc = check_rows(v, stride, row);
+    if (rc == EAD_OK && !aligned(status, 4)) rc = EAD_EALIGNMENT;
+    if (rc == EAD_OK) rc = use_device(device, d);
+    if (rc != EAD_OK) return rc;
+    p->rows_k = static_cast<uint8_t *>(const_cast<void *>(k));
+    p->rows_v = static_cast<uint8_t *>(const_cast<void *>(v));
+    p->row_stride = stride;
+    p->status = status;
+    return EAD_OK;
+}
+
+dim3 move_grid(const KvMoveParams &p, const DeviceInfo &d)
+{
+    const int per_block = kKvThreads / 32;
+    return dim3(std::min((p.batch.n_tokens + per_block - 1) / per_block, 8 * d.sms));
+}
+
+}  // namespace
+
+extern "C" int ead_kv_write(const ead_kv_cache *cache, const ead_kv_batch *batch, const void *k_new, const void *v_new,
+                            int64_t new_stride, uint32_t *status, int32_t device, void *stream)
+{
+    KvMoveParams p{};
+    DeviceInfo *d = nullptr;
+    const int rc = move_setup(cache, batch, k_new, v_new, new_stride, status, true, device, &p, &d);
+    if (rc != EAD_OK || p.batch.n_tokens == 0) return rc;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (cache->format == EAD_FMT_BF16)
+        ead_kv_write_kernel<kFmtBf16><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+    else
+        ead_kv_write_kernel<kFmtE4m3><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+    return launched();
+}
+
+extern "C" int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int32_t *first, void *k_out,
+                           void *v_out, int64_t out_stride, uint32_t *status, int32_t device, void *stream)
+{
+    KvMoveParams p{};
+    DeviceInfo *d = nullptr;
+    if (!aligned(first, 4)) return EAD_EALIGNMENT;
+    const int rc = move_setup(cache, batch, k_out, v_out, out_stride, status, false, device, &p, &d);
+    if (rc != EAD_OK || p.batch.n_tokens == 0) return rc;
+    p.first = first;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (cache->format == EAD_FMT_BF16)
+        ead_kv_read_kernel<kFmtBf16><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+    else
+        ead_kv_read_kernel<kFmtE4m3><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+    return launched();
+}
+
+extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *batch, const void *q, int64_t q_stride,
+                                int32_t heads_q, float scale, int32_t window, int32_t sinks, void *out,
+                                int64_t out_stride, float *lse, void *workspace, uint32_t *status, int32_t device,
+                                void *stream)
+{
+    AttnParams p{};
+    DeviceInfo *d = nullptr;
+    int rc = check_cache(cache, &p.cache);
+    if (rc == EAD_OK) rc = check_batch(batch, p.cache, true, &p.batch);
+    if (rc != EAD_OK) return rc;
+    if (heads_q < p.cache.heads || heads_q % p.cache.heads || heads_q / p.cache.heads > 128) return EAD_EINVALID_ARG;
+    if (!std::isfinite(scale) || !(scale > 0.f) || window < 0 || sinks < 0 || !workspace) return EAD_EINVALID_ARG;
+    if (p.batch.n_tokens == 0) return EAD_OK;
+    const int64_t row = static_cast<int64_t>(heads_q) * p.cache.head_dim;
+    rc = check_rows(q, q_stride, row);
+    if (rc == EAD_OK) rc = check_rows(out, out_stride, row);
+    if (rc == EAD_OK && (!aligned(lse, 4) || !aligned(workspace, 256) || !aligned(status, 4))) rc = EAD_EALIGNMENT;
+    if (rc == EAD_OK) rc = use_device(device, &d);
+    if (rc != EAD_OK) return rc;
+    p.q = static_cast<const uint8_t *>(q);
+    p.out = static_cast<uint8_t *>(out);
+    p.lse = lse;
+    p.q_stride = q_stride;
+    p.out_stride = out_stride;
+    p.heads_q = heads_q;
+    p.group = heads_q / p.cache.heads;
+    p.window = window;
+    p.sinks = window ? sinks : 0;
+    p.scale = scale;
+    p.status = status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const dim3 grid((p.batch.n_tokens + 3) / 4, heads_q);
+    if (cache->format == EAD_FMT_BF16)
+        ead_kv_attention_simple_kernel<kFmtBf16><<<grid, 128, 0, s>>>(p);
+    else
+        ead_kv_attention_simple_kernel<kFmtE4m3><<<grid, 128, 0, s>>>(p);
+    return launched();
+}
+
+extern "C" int ead_add_rmsnorm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                               void *residual_out, int64_t residual_out_stride, const void *weight, float eps,
+                               int32_t n_rows, int32_t H, int32_t format, void *out, int64_t out_stride,
+                               uint8_t *out_scale, int32_t device, void *stream)
+{
+    const bool e4m3 = format == EAD_FMT_E4M3;
+    if ((format != EAD_FMT_BF16 && !e4m3) || n_rows < 0 || H < 8 || !weight || e4m3 != (out_scale != nullptr))
+        return EAD_EINVALID_ARG;
+    if (!std::isfinite(eps) || eps < 0.f) return EAD_EINVALID_ARG;
+    if (H > EAD_NORM_MAX_H) return EAD_ELIMIT;
+    if (H % (e4m3 ? kFmtBlock : 8) || !aligned(weight, 16)) return EAD_EALIGNMENT;
+    if (n_rows == 0) return EAD_OK;
+    int rc = check_rows(x, x_stride, H);
+    if (rc == EAD_OK) rc = check_rows(out, out_stride, H);
+    if (rc == EAD_OK && residual) rc = check_rows(residual, residual_stride, H);
+    if (rc == EAD_OK && residual_out) rc = check_rows(residual_out, residual_out_stride, H);
+    DeviceInfo *d = nullptr;
+    if (rc == EAD_OK) rc = use_device(device, &d);
+    if (rc != EAD_OK) return rc;
+    NormParams p{};
+    p.x = static_cast<const uint8_t *>(x);
+    p.residual = static_cast<const uint8_t *>(residual);
+    p.weight = static_cast<const uint8_t *>(weight);
+    p.residual_out = static_cast<uint8_t *>(residual_out);
+    p.out = static_cast<uint8_t *>(out);
+    p.out_scale = out_scale;
+    p.x_stride = x_stride;
+    p.residual_stride = residual_stride;
+    p.residual_out_stride = residual_out_stride;
+    p.out_stride = out_stride;
+    p.H = H;
+    p.eps = eps;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int groups = H / 8;
+    const int nv = groups <= 512 ? 1 : groups <= 1024 ? 2 : 4;
+    const int threads = ((groups + nv - 1) / nv + 31) / 32 * 32;
+#define EAD_LAUNCH_NORM(NV)                                                                    \
+    (e4m3 ? ead_add_rmsnorm_kernel<kFmtE4m3, NV><<<n_rows, threads, 0, s>>>(p)                 \
+          : ead_add_rmsnorm_kernel<kFmtBf16, NV><<<n_rows, threads, 0, s>>>(p))
+    if (nv == 1)
+        EAD_LAUNCH_NORM(1);
+    else if (nv == 2)
+        EAD_LAUNCH_NORM(2);
+    else
+        EAD_LAUNCH_NORM(4);
+#undef EAD_LAUNCH_NORM
+    return launched();
+}
