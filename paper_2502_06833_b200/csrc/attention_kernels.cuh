@@ -1,22 +1,9 @@
 // Attention of the step's new tokens over the paged cache.  One warp per (token, query head):
 // 32 keys at a time, online softmax with a running maximum and sum.
 #pragma once
-#include "kv_format.cuh"
-#include "ptx_sm100.cuh"
+#include "attn_common.cuh"
 
 namespace ead {
-
-struct AttnParams {
-    KvCacheView cache;
-    KvBatchView batch;
-    const uint8_t *q;
-    uint8_t *out;
-    float *lse;
-    int64_t q_stride, out_stride;                 // elements between tokens
-    int32_t heads_q, group, window, sinks;
-    float scale;
-    uint32_t *status;
-};
 
 template <int FMT>
 __device__ __forceinline__ float pool_value(const KvCacheView &c, const uint8_t *pool, const uint8_t *scale, int page,
@@ -39,9 +26,10 @@ __global__ void __launch_bounds__(128) ead_kv_attention_simple_kernel(AttnParams
     const int b = find_sequence(p.batch.new_start, p.batch.B, t, lane);
     const int n_b = p.batch.new_start[b + 1] - p.batch.new_start[b];
     const int pos = p.batch.kv_len[b] - (p.batch.new_start[b + 1] - t);
+    if (n_b * p.group <= p.few_rows) return;
     if (n_b > p.batch.max_new && lane == 0) flag_status(p.status, kStatusBadCount);
     for (int d = lane; d < D; d += 32)
-        qs[w][d] = __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p.q)[t * p.q_stride + hq * D + d]) * p.scale;
+        qs[w][d] = __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p.q)[t * p.q_stride + hq * D + d]) * p.scale_log2;
     __syncwarp();
     const int cap = p.batch.max_len;
     if (p.batch.kv_len[b] > cap && lane == 0) flag_status(p.status, kStatusBadPage);
@@ -66,8 +54,8 @@ __global__ void __launch_bounds__(128) ead_kv_attention_simple_kernel(AttnParams
 #pragma unroll
         for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
         const float m_new = fmaxf(m, top);
-        const float f = m_new == -INFINITY ? 1.f : __expf(m - m_new);
-        const float e = seen ? __expf(z - m_new) : 0.f;
+        const float f = m_new == -INFINITY ? 1.f : exp2f(m - m_new);
+        const float e = seen ? exp2f(z - m_new) : 0.f;
         l = l * f + e;
         for (int i = 0; i < D / 32; ++i) o[i] *= f;
         for (int k = 0; k < 32; ++k) {
@@ -84,7 +72,7 @@ __global__ void __launch_bounds__(128) ead_kv_attention_simple_kernel(AttnParams
     const float inv = end > 0 ? 1.f / l : 0.f;
     for (int i = 0; i < D / 32; ++i)
         reinterpret_cast<__nv_bfloat16 *>(p.out)[t * p.out_stride + hq * D + lane + 32 * i] = __float2bfloat16(o[i] * inv);
-    if (p.lse && lane == 0) p.lse[static_cast<int64_t>(t) * p.heads_q + hq] = end > 0 ? m + logf(l) : -INFINITY;
+    if (p.lse && lane == 0) p.lse[static_cast<int64_t>(t) * p.heads_q + hq] = end > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 }  // namespace ead

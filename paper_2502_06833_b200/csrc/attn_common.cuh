@@ -1,0 +1,104 @@
+// What the attention kernels share: parameters, which keys a run of queries sees as a list of tiles,
+// how work is dealt out to blocks, and how parts of one result are joined.
+//
+// A UNIT is a run of query rows that share their keys: (sequence, cache head, run of new tokens), all
+// query heads of the group together.  Its keys are cut into tiles, all units' tiles are strung up one
+// after the other, and every block takes an equal stretch of that string.  A block whose stretch ends inside a
+// unit leaves its part (running maximum, sum, unnormalised output) in the workspace; the last block of a unit to arrive
+// joins the parts in the order of the blocks, so the result does not depend on who comes last.
+#pragma once
+#include "kv_format.cuh"
+#include "ptx_sm100.cuh"
+
+namespace ead {
+
+struct AttnParams {
+    KvCacheView cache;
+    KvBatchView batch;
+    const uint8_t *q;
+    uint8_t *out;
+    float *lse;
+    int64_t q_stride, out_stride;                 // elements between tokens
+    int32_t heads_q, group, window, sinks;
+    int32_t few_rows;                             // units of at most this many packed rows go to the few-rows kernel
+    float scale_log2;                             // scale * log2(e): logits are kept in units of log 2
+    uint32_t *status;
+    uint8_t *workspace;
+};
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Workspace: arrival counters of both kernels (zero between calls), then the partial results.
+constexpr size_t kAttnCounterBytes = 4096;        // 256 counters of 32 bits per kernel, 4 kernels at most
+constexpr int kAttnMaxCtas = 160;
+constexpr int kDecodeRows = 16;                   // most packed rows of a unit of the few-rows kernel
+constexpr size_t kDecodePartFloats = kDecodeRows * (128 + 2);
+constexpr size_t kDecodePartOffset = 2 * kAttnCounterBytes;
+
+// The new tokens and the readable context of a sequence.
+struct SeqInfo {
+    int n, p0, len;                               // new tokens, position of the first one, keys in the cache
+};
+__device__ __forceinline__ SeqInfo seq_info(const KvBatchView &bt, int b)
+{
+    SeqInfo s;
+    const int kv = __ldg(bt.kv_len + b);
+    s.n = __ldg(bt.new_start + b + 1) - __ldg(bt.new_start + b);
+    s.p0 = kv - s.n;
+    s.len = min(max(kv, 0), bt.max_len);
+    return s;
+}
+
+// Tiles of 2^shift keys that queries at positions pa .. pb see: those of the sinks, then those of
+// the window.  At least one tile, so that rows that see nothing are still written.
+struct KeyRange {
+    int lo, hi;                                   // window part [lo, hi); sinks are [0, min(sinks, lo))
+    int sink_tiles, first_tile, tiles;
+    __device__ __forceinline__ int base(int t, int shift) const
+    {
+        return (t < sink_tiles ? t : t - sink_tiles + first_tile) << shift;
+    }
+};
+__device__ __forceinline__ KeyRange key_range(int pa, int pb, int len, int window, int sinks, int shift)
+{
+    KeyRange r;
+    r.hi = min(max(pb + 1, 0), len);
+    r.lo = window ? min(max(pa - window + 1, 0), r.hi) : 0;
+    r.first_tile = r.lo >> shift;
+    r.sink_tiles = min((min(sinks, r.lo) + (1 << shift) - 1) >> shift, r.first_tile);
+    r.tiles = max(1, r.sink_tiles + ((r.hi + (1 << shift) - 1) >> shift) - r.first_tile);
+    return r;
+}
+// Whether any of the unit's queries sees key j, and whether one at position pos does.
+__device__ __forceinline__ bool seen_by_any(const KeyRange &r, int sinks, int j) { return j < r.hi && (j >= r.lo || j < sinks); }
+__device__ __forceinline__ bool seen_by(int pos, int window, int sinks, int j)
+{
+    return j <= pos && (window == 0 || j > pos - window || j < sinks);
+}
+
+// 2^x with 2^-inf = 0.
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Waits for a phase of an mbarrier; gives up after kWaitLimitNs and from then on does not wait again.
+__device__ __forceinline__ void wait_phase(uint32_t bar, uint32_t parity, uint32_t *status, bool *expired)
+{
+    if (*expired || mbar_try_wait(bar, parity)) return;
+    const uint64_t t0 = globaltimer_ns();
+    while (!mbar_try_wait_hint(bar, parity, 20000)) {
+        if (globaltimer_ns() - t0 > kWaitLimitNs) {
+            *expired = true;
+            flag_status(status, kStatusWaitExpired);
+            return;
+        }
+    }
+}
+
+// Orders the block's partial results in the workspace before an arrival, and the other blocks' before a read.
+__device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
+
+}  // namespace ead

@@ -1,0 +1,612 @@
+// Attention for units of at most 16 packed rows (new tokens x query heads of a cache head): single-token
+// decoding and very short chunks.
+//
+// Every key and value is read from HBM once and used for 8 or 16 rows only, so HBM bounds it; the
+// kernel is built to keep many bytes in flight and little else.  Seven or eight warps per SM work independently:
+// each has its own ring of 8 KiB stages (4 KiB of keys, 4 KiB of values) filled by TMA boxes of
+// one page each and takes every seventh or eighth tile of the block's stretch, so no barrier stands between the loads of
+// consecutive tiles or units.  Products are mma.sync with the keys (values) as the 16-row
+// operand and the packed query rows as the 8-column operand: a tensor-memory accumulator has 128 rows, of which
+// 8 would carry anything.  S^T = K Q^T has the layout that, transposed 8 x 8, is the second
+// operand of O^T = V^T P^T.
+//
+// 8-bit keys and values become bf16 in registers on their way from shared memory to the MMA: an e4m3 byte
+// placed 4 bits down in a bf16 is 2^-120 of its value, subnormals included, so one multiplication by
+// 2^(120 + k) is exact.
+#pragma once
+#include "attn_common.cuh"
+
+namespace ead {
+
+constexpr int kFewHalf = 4096;                    // bytes of keys (of values) per stage
+constexpr int kFewScaleBytes = 256;               // scale bytes of keys and values per stage
+constexpr float kLazyLog2 = 8.f;                  // the reference maximum moves when a logit exceeds it by 2^8
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Two of a register's four codes, chosen by `pick` (each goes to the high byte of a half), as bf16 times 2^-120.
+__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t codes, uint32_t pick)
+{
+    const uint32_t w = __byte_perm(codes, 0, pick);
+    return (w & 0x80008000u) | ((w >> 4) & 0x07F007F0u);
+}
+constexpr uint32_t kPick01 = 0x1404, kPick23 = 0x3424, kPick02 = 0x2404, kPick13 = 0x3414;
+
+// Factor of a scale byte for such a value, as bf16 bits: 2^(120 + byte - 127) up to the largest power of two a bf16
+// holds (byte 134, a scale of 2^7); what is above that is a second factor, which almost no cache needs.
+__device__ __forceinline__ uint32_t scale_factor(uint32_t byte) { return (min(byte, 134u) + 120u) << 7; }
+__device__ __forceinline__ uint32_t scale_rest(uint32_t byte)
+{
+    return byte == 255u ? 0x7FC0u : (byte > 134u ? byte - 134u + 127u : 127u) << 7;
+}
+
+// The NG scale bytes of one key, as the low bytes of a register.
+template <int NG>
+__device__ __forceinline__ uint32_t lds_scales(uint32_t addr)
+{
+    uint32_t v;
+    if (NG == 4) {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    } else {
+        asm volatile("{\n\t.reg .b16 t;\n\tld.shared.b16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(v) : "r"(addr) : "memory");
+    }
+    return v;
+}
+
+// A warp's place in the string of tiles: unit, its keys, and where the unit lies.
+struct FewCursor {
+    int b, h;                                     // sequence, cache head
+    int64_t begin;                                // the unit's first tile in the string
+    SeqInfo s;
+    KeyRange r;
+};
+
+__device__ __forceinline__ int few_tiles(const AttnParams &p, const SeqInfo &s, int shift, KeyRange *r)
+{
+    if (s.n < 1 || s.n * static_cast<int64_t>(p.group) > p.few_rows) return 0;
+    *r = key_range(s.p0, s.p0 + s.n - 1, s.len, p.window, p.sinks, shift);
+    return r->tiles;
+}
+// Moves on to the unit that holds tile g of the string (g is in this unit or a later one).
+__device__ __forceinline__ void few_seek(const AttnParams &p, int shift, int64_t g, FewCursor *c)
+{
+    while (g >= c->begin + c->r.tiles) {
+        c->begin += c->r.tiles;
+        if (c->r.tiles > 0 && c->h + 1 < p.cache.heads) {
+            ++c->h;
+        } else {
+            c->h = 0;
+            do {
+                ++c->b;
+                c->s = seq_info(p.batch, c->b);
+                c->r.tiles = few_tiles(p, c->s, shift, &c->r);
+            } while (c->r.tiles == 0);
+        }
+    }
+}
+
+// NB: packed rows in groups of 8 (1 or 2).
+template <int FMT, int D, int NB>
+struct FewLayout {
+    static constexpr int kRowBytes = FMT == kFmtBf16 ? 2 * D : D;           // bytes of one key
+    static constexpr int kTile = kFewHalf / kRowBytes;                      // keys per tile: 16, 32 or 64
+    static constexpr int kShift = kTile == 16 ? 4 : kTile == 32 ? 5 : 6;
+    static constexpr int kLine = kRowBytes < 128 ? kRowBytes : 128;         // bytes of a key in one box
+    static constexpr int kBoxes = kRowBytes / kLine;                        // boxes per key row (2 for 256-byte keys)
+    static constexpr int kRows = 8 * NB;
+    static constexpr int kWarps = FMT == kFmtE4m3 && D == 128 && NB == 1 ? 7 : 8;   // what shared memory has room for
+    static constexpr int kThreads = 32 * kWarps;
+    static constexpr int kMergeRow = D + 4;                                 // floats; the padding spreads the rows over the banks
+    static constexpr int kMergeWarp = kRows * kMergeRow + 2 * kRows;
+    static constexpr int kMergeBytes = kWarps * kMergeWarp * 4;
+    static constexpr int kStages = NB == 1 ? 3 : 2;
+    static constexpr int kRing = kWarps * kStages * 2 * kFewHalf;
+    static constexpr int kScales = FMT == kFmtE4m3 ? kWarps * kStages * kFewScaleBytes : 0;
+    static constexpr int kSmem = 1024 + kRing + kScales + kMergeBytes + kWarps * kStages * 8;
+};
+
+template <int FMT, int D, int NB>
+__global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
+    ead_attn_few_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, AttnParams p,
+                             int box_shift, int min_tiles)
+{
+    using L = FewLayout<FMT, D, NB>;
+    constexpr int S = L::kStages, TT = L::kTile, R = L::kRows, kFewWarps = L::kWarps, kFewThreads = L::kThreads;
+    const int box_keys = 1 << box_shift;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int64_t s_scan[kFewWarps];
+    __shared__ int s_b;
+    __shared__ int64_t s_before;
+    __shared__ int s_last;
+    const uint32_t raw = smem_u32(smem_raw), ring0 = (raw + 1023u) & ~1023u;
+    uint8_t *const ring_ptr = smem_raw + (ring0 - raw);
+    uint8_t *const scales_ptr = ring_ptr + L::kRing;
+    float *const merge = reinterpret_cast<float *>(scales_ptr + L::kScales);
+    const uint32_t bars = smem_u32(reinterpret_cast<uint8_t *>(merge) + L::kMergeBytes);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const KvCacheView &c = p.cache;
+
+    if (tid < kFewWarps * S) mbar_init(bars + 8 * tid, 1);
+    fence_mbar_init();
+
+    // ---- the string of tiles: its length, and the sequence in which this block's stretch begins
+    const int per = (p.batch.B + kFewThreads - 1) / kFewThreads;
+    const int b_lo = min(tid * per, p.batch.B), b_hi = min(b_lo + per, p.batch.B);
+    int64_t mine = 0;
+    KeyRange kr;
+    for (int b = b_lo; b < b_hi; ++b) {
+        const SeqInfo s = seq_info(p.batch, b);
+        mine += few_tiles(p, s, L::kShift, &kr);
+        if (blockIdx.x == 0) {
+            if (s.n > p.batch.max_new) flag_status(p.status, kStatusBadCount);
+            if (s.p0 + s.n > p.batch.max_len) flag_status(p.status, kStatusBadPage);
+        }
+    }
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) s_scan[warp] = upto;
+    __syncthreads();
+    int64_t total = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWarps; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+    }
+    upto += before;                                // tiles of one head up to and including this thread's sequences
+    const int64_t W = total * c.heads;
+    const int64_t ctas = min(static_cast<int64_t>(gridDim.x), max(static_cast<int64_t>(1), (W + min_tiles - 1) / min_tiles));
+    if (W == 0 || blockIdx.x >= ctas) return;
+    const int64_t g0 = W * blockIdx.x / ctas, g1 = W * (blockIdx.x + 1) / ctas;
+    if (mine > 0 && g0 >= (upto - mine) * c.heads && g0 < upto * c.heads) {
+        int64_t at = upto - mine;
+        for (int b = b_lo; b < b_hi; ++b) {
+            const int t = few_tiles(p, seq_info(p.batch, b), L::kShift, &kr);
+            if (g0 < (at + t) * c.heads) {
+                s_b = b;
+                s_before = at * c.heads;
+                break;
+            }
+            at += t;
+        }
+    }
+    __syncthreads();
+    FewCursor cur;
+    cur.b = s_b;
+    cur.s = seq_info(p.batch, cur.b);
+    cur.r.tiles = few_tiles(p, cur.s, L::kShift, &cur.r);
+    cur.h = static_cast<int>((g0 - s_before) / cur.r.tiles);
+    cur.begin = s_before + static_cast<int64_t>(cur.h) * cur.r.tiles;
+
+    // ---- loads: this warp's tiles are g0 + warp, g0 + warp + 8, ...
+    const uint32_t my_ring = ring0 + warp * S * 2 * kFewHalf;
+    const uint32_t my_scales = smem_u32(scales_ptr) + warp * S * kFewScaleBytes;
+    const uint32_t my_bars = bars + warp * S * 8;
+    FewCursor ahead = cur;
+    int64_t g_ahead = g0 + warp;
+    int page = -1, key0 = 0;                       // of this lane's box of the tile that is loaded next
+    const int boxes = TT >> box_shift;              // at most 8
+    auto look_up = [&]() {                         // one tile early, so that the load is there when the tile is issued
+        if (g_ahead >= g1) return;
+        few_seek(p, L::kShift, g_ahead, &ahead);
+        key0 = ahead.r.base(static_cast<int>(g_ahead - ahead.begin), L::kShift) + lane * box_keys;
+        page = -2;                                 // nothing of it is seen: not loaded
+        const bool any = key0 < ahead.r.hi && (key0 + box_keys > ahead.r.lo || key0 < p.sinks);
+        if (lane < boxes && any) {
+            page = find_page(c, p.batch, ahead.b, key0);
+            if (page < 0) {
+                flag_status(p.status, kStatusBadPage);
+                page = c.n_pages;                  // outside the pool: the copy delivers zeros
+            }
+        }
+    };
+    auto issue = [&](int stage) {
+        if (g_ahead >= g1) return;
+        const unsigned live = __ballot_sync(0xffffffffu, lane < boxes && page >= 0);
+        const uint32_t bar = my_bars + 8 * stage, dst = my_ring + stage * 2 * kFewHalf;
+        const uint32_t box_bytes = box_keys * L::kRowBytes;
+        const uint32_t sc_bytes = box_keys * (D / kFmtBlock);
+        if (FMT == kFmtE4m3) {
+            const unsigned scaled = __ballot_sync(0xffffffffu, lane < boxes && page >= 0 && page < c.n_pages);
+            if (lane == 0) mbar_arrive_expect_tx(bar, 2 * __popc(live) * box_bytes + 2 * __popc(scaled) * sc_bytes);
+        } else if (lane == 0) {
+            mbar_arrive_expect_tx(bar, 2 * __popc(live) * box_bytes);
+        }
+        __syncwarp();
+        if (lane < boxes && page >= 0) {
+            const int slot = key0 & (c.page_size - 1);
+            tma_load_5d(dst + lane * box_bytes, &tmK, 0, slot, 0, ahead.h, page, bar);
+            tma_load_5d(dst + kFewHalf + lane * box_bytes, &tmV, 0, slot, 0, ahead.h, page, bar);
+            if (FMT == kFmtE4m3) {
+                const uint32_t sc = my_scales + stage * kFewScaleBytes + lane * sc_bytes;
+                if (page < c.n_pages) {
+                    const int64_t at = scale_offset(c, page, ahead.h, slot);
+                    bulk_load(sc, c.k_scale + at, sc_bytes, bar);
+                    bulk_load(sc + kFewScaleBytes / 2, c.v_scale + at, sc_bytes, bar);
+                } else {
+                    for (uint32_t x = 0; x < sc_bytes; x += 4) {
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + x), "r"(0) : "memory");
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + kFewScaleBytes / 2 + x), "r"(0) : "memory");
+                    }
+                }
+            }
+        }
+        __syncwarp();
+        g_ahead += kFewWarps;
+    };
+    look_up();
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        issue(i);
+        look_up();
+    }
+
+    // ---- tiles, unit by unit
+    const int qc = (lane & 3) * 2;                 // this lane's packed rows: qc, qc + 1 (and 8 more)
+    int stage = 0;
+    uint32_t phase = 0;
+    int64_t g = g0 + warp;
+    int64_t unit_lo = g0;
+    bool first_unit = true, expired = false;
+    while (unit_lo < g1) {
+        const int64_t unit_end = cur.begin + cur.r.tiles, unit_hi = min(unit_end, g1);
+        const int rows = cur.s.n * p.group;
+        const int64_t token0 = __ldg(p.batch.new_start + cur.b);
+        // query rows as the 8-column operand: lane holds rows lane / 4 (+ 8), elements by the layout of the keys
+        uint32_t qf[D / 16][NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int row = nb * 8 + (lane >> 2);
+            const int i = row / p.group, gq = row - i * p.group;
+            const uint8_t *src = p.q + 2 * ((token0 + i) * p.q_stride + (static_cast<int64_t>(cur.h) * p.group + gq) * D);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                qf[ks][nb][0] = qf[ks][nb][1] = 0;
+                if (row < rows) {
+                    if (FMT == kFmtBf16) {
+                        qf[ks][nb][0] = __ldg(reinterpret_cast<const uint32_t *>(src + 2 * (16 * ks + qc)));
+                        qf[ks][nb][1] = __ldg(reinterpret_cast<const uint32_t *>(src + 2 * (16 * ks + qc + 8)));
+                    } else {                       // four consecutive codes per lane: elements 4c .. 4c + 3 of the step
+                        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src + 2 * (16 * ks + 2 * qc)));
+                        qf[ks][nb][0] = v.x;
+                        qf[ks][nb][1] = v.y;
+                    }
+                }
+            }
+        }
+        int pos[NB][2];                            // positions of this lane's rows
+        float m[NB][2], l[NB][2];
+        float o[D / 16][NB][4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                pos[nb][e] = cur.s.p0 + (nb * 8 + qc + e) / p.group;
+                m[nb][e] = -INFINITY;
+                l[nb][e] = 0.f;
+            }
+#pragma unroll
+        for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[mt][nb][e] = 0.f;
+        const int pb = cur.s.p0 + cur.s.n - 1;
+
+        for (; g < unit_hi; g += kFewWarps) {
+            const int base = cur.r.base(static_cast<int>(g - cur.begin), L::kShift);
+            const bool whole = base + TT - 1 <= cur.s.p0 && base + TT <= cur.s.len &&
+                               (p.window == 0 || base > pb - p.window || base + TT <= p.sinks);
+            const uint32_t kb = my_ring + stage * 2 * kFewHalf, vb = kb + kFewHalf;
+            wait_phase(my_bars + 8 * stage, phase, p.status, &expired);
+#pragma unroll 2
+            for (int st = 0; st < TT / 16; ++st) {
+                const int t0 = st * 16;
+                // address of 8 keys x 16 bytes: row `key`, 16-byte chunk `ch` of the key
+                auto chunk_at = [&](uint32_t tile, int key, int ch) -> uint32_t {
+                    if (L::kLine == 128) {
+                        const int bx = L::kBoxes == 1 ? 0 : key >> box_shift, in = key & (box_keys - 1), hb = ch >> 3;
+                        const uint32_t row = L::kBoxes == 1 ? key * 128u : (((bx * L::kBoxes + hb) << box_shift) + in) * 128u;
+                        return tile + row + (((ch & 7) ^ (key & 7)) << 4);
+                    }
+                    return tile + key * 64u + ((ch ^ ((key >> 1) & 3)) << 4);
+                };
+                float s[NB][4];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[nb][e] = 0.f;
+                const int mi = lane >> 3, mr = lane & 7;       // matrix and row this lane addresses
+                uint32_t rest_any = 0;
+                uint32_t ksc[2], vsc[4];
+                if (FMT == kFmtE4m3) {
+                    constexpr int NG = D / kFmtBlock;           // scale bytes per key
+                    const uint32_t sb = my_scales + stage * kFewScaleBytes;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) ksc[i] = lds_scales<NG>(sb + (t0 + (lane >> 2) + 8 * i) * NG);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vsc[i] = lds_scales<NG>(sb + 128 + (t0 + qc + (i & 1) + 8 * (i >> 1)) * NG);
+                    uint32_t over = 0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) over |= __vcmpgtu4(ksc[i], 0x86868686u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) over |= __vcmpgtu4(vsc[i], 0x86868686u);
+                    rest_any = __any_sync(0xffffffffu, over != 0);
+                }
+                if (FMT == kFmtBf16) {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        uint32_t a[4];
+                        ldsm4(a, chunk_at(kb, t0 + mr + (mi & 1) * 8, 2 * ks + (mi >> 1)));
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) mma16816(s[nb], a[0], a[1], a[2], a[3], qf[ks][nb][0], qf[ks][nb][1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int kp = 0; kp < D / 32; ++kp) {       // one scale block: two steps of 16
+                        uint32_t a[4];
+                        ldsm4(a, chunk_at(kb, t0 + mr + (mi & 1) * 8, 2 * kp + (mi >> 1)));
+                        uint32_t f[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t x = scale_factor((ksc[i] >> (8 * kp)) & 0xffu);
+                            f[i] = x | x << 16;
+                        }
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {           // matrices 2u (keys 0-7) and 2u + 1 (keys 8-15)
+                            uint32_t a0 = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick01), f[0]);
+                            uint32_t a1 = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick01), f[1]);
+                            uint32_t a2 = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick23), f[0]);
+                            uint32_t a3 = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick23), f[1]);
+                            if (rest_any) {
+                                const uint32_t x0 = scale_rest((ksc[0] >> (8 * kp)) & 0xffu) * 0x10001u;
+                                const uint32_t x1 = scale_rest((ksc[1] >> (8 * kp)) & 0xffu) * 0x10001u;
+                                a0 = mul_bf16x2(a0, x0); a2 = mul_bf16x2(a2, x0);
+                                a1 = mul_bf16x2(a1, x1); a3 = mul_bf16x2(a3, x1);
+                            }
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb)
+                                mma16816(s[nb], a0, a1, a2, a3, qf[2 * kp + u][nb][0], qf[2 * kp + u][nb][1]);
+                        }
+                    }
+                }
+                // logits in units of log 2; what is not seen is -inf
+                const int j0 = base + t0 + (lane >> 2);
+                float top = -INFINITY;                          // largest excess over the reference
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[nb][e] *= p.scale_log2;
+                        if (!whole) {
+                            const int j = j0 + 8 * (e >> 1);
+                            if (!(j < cur.s.len && seen_by(pos[nb][e & 1], p.window, p.sinks, j))) s[nb][e] = -INFINITY;
+                        }
+                        if (s[nb][e] > m[nb][e & 1] + kLazyLog2) top = INFINITY;
+                    }
+                if (__any_sync(0xffffffffu, top > 0.f)) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float x = fmaxf(s[nb][e], s[nb][e + 2]);
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                            x = fmaxf(x, m[nb][e]);
+                            const float f = x == -INFINITY ? 1.f : exp2_fast(m[nb][e] - x);
+                            m[nb][e] = x;
+                            l[nb][e] *= f;
+#pragma unroll
+                            for (int mt = 0; mt < D / 16; ++mt) {
+                                o[mt][nb][e] *= f;
+                                o[mt][nb][e + 2] *= f;
+                            }
+                        }
+                }
+                uint32_t pf[NB][2];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    float x[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float mm = m[nb][e & 1] == -INFINITY ? 0.f : m[nb][e & 1];
+                        x[e] = exp2_fast(s[nb][e] - mm);
+                        l[nb][e & 1] += x[e];
+                    }
+                    pf[nb][0] = transpose8x8(to_bf16x2(x[0], x[1]));
+                    pf[nb][1] = transpose8x8(to_bf16x2(x[2], x[3]));
+                }
+                // values no query sees may be anything, and were not even loaded: zeros, so that 0 * NaN cannot arise
+                uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int j = base + t0 + qc + 8 * i;
+                        keep[i] = (seen_by_any(cur.r, p.sinks, j) ? 0xffffu : 0u) | (seen_by_any(cur.r, p.sinks, j + 1) ? 0xffff0000u : 0u);
+                    }
+                }
+                if (FMT == kFmtBf16) {
+#pragma unroll
+                    for (int mt = 0; mt < D / 16; ++mt) {
+                        uint32_t a[4];
+                        ldsm4_t(a, chunk_at(vb, t0 + mr + (mi >> 1) * 8, 2 * mt + (mi & 1)));
+                        if (!whole) {
+                            a[0] &= keep[0]; a[1] &= keep[0];
+                            a[2] &= keep[1]; a[3] &= keep[1];
+                        }
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) mma16816(o[mt][nb], a[0], a[1], a[2], a[3], pf[nb][0], pf[nb][1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int mp = 0; mp < D / 32; ++mp) {
+                        uint32_t a[4];
+                        ldsm4_t(a, chunk_at(vb, t0 + mr + (mi & 1) * 8, 2 * mp + (mi >> 1)));
+                        uint32_t f[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            f[i] = scale_factor((vsc[2 * i] >> (8 * mp)) & 0xffu) | scale_factor((vsc[2 * i + 1] >> (8 * mp)) & 0xffu) << 16;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            uint32_t v[4];
+                            v[0] = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick02), f[0]);
+                            v[1] = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick13), f[0]);
+                            v[2] = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick02), f[1]);
+                            v[3] = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick13), f[1]);
+                            if (rest_any) {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const uint32_t x = scale_rest((vsc[2 * i] >> (8 * mp)) & 0xffu) | scale_rest((vsc[2 * i + 1] >> (8 * mp)) & 0xffu) << 16;
+                                    v[2 * i] = mul_bf16x2(v[2 * i], x);
+                                    v[2 * i + 1] = mul_bf16x2(v[2 * i + 1], x);
+                                }
+                            }
+                            if (!whole) {
+                                v[0] &= keep[0]; v[1] &= keep[0];
+                                v[2] &= keep[1]; v[3] &= keep[1];
+                            }
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) mma16816(o[2 * mp + u][nb], v[0], v[1], v[2], v[3], pf[nb][0], pf[nb][1]);
+                        }
+                    }
+                }
+            }
+            __syncwarp();                          // every lane has read the stage before it is filled again
+            issue(stage);
+            look_up();
+            if (++stage == S) {
+                stage = 0;
+                phase ^= 1;
+            }
+        }
+
+        // ---- the warps' parts of the unit come together
+        float *mw = merge + warp * L::kMergeWarp;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], x);
+                const int row = nb * 8 + qc + e;
+#pragma unroll
+                for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int d = 16 * mt + (FMT == kFmtBf16 ? (lane >> 2) + 8 * u : 2 * (lane >> 2) + u);
+                        mw[row * L::kMergeRow + d] = o[mt][nb][e + 2 * u];
+                    }
+                if (lane < 4) {
+                    mw[R * L::kMergeRow + row] = m[nb][e];
+                    mw[R * L::kMergeRow + R + row] = l[nb][e];
+                }
+            }
+        __syncthreads();
+        const bool begins = unit_lo == cur.begin, ends = unit_hi == unit_end;
+        float *const parts = reinterpret_cast<float *>(p.workspace + kDecodePartOffset);
+        uint32_t *const counters = reinterpret_cast<uint32_t *>(p.workspace);
+        float *const my_part = parts + (2 * blockIdx.x + (first_unit ? 0 : 1)) * kDecodePartFloats;
+        constexpr int kQuads = D / 4;
+        auto store = [&](int row, int dq, float M, float Lsum, float4 v) {
+            const int i = row / p.group, gq = row - i * p.group;
+            const float inv = Lsum == 0.f ? 0.f : 1.f / Lsum;
+            const int hq = cur.h * p.group + gq;
+            *reinterpret_cast<uint2 *>(p.out + 2 * ((token0 + i) * p.out_stride + static_cast<int64_t>(hq) * D + 4 * dq)) =
+                make_uint2(to_bf16x2(v.x * inv, v.y * inv), to_bf16x2(v.z * inv, v.w * inv));
+            if (p.lse && dq == 0) p.lse[(token0 + i) * p.heads_q + hq] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
+        };
+        for (int x = tid; x < rows * kQuads; x += kFewThreads) {
+            const int row = x / kQuads, dq = x - row * kQuads;
+            float M = -INFINITY, Lsum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) M = fmaxf(M, merge[w * L::kMergeWarp + R * L::kMergeRow + row]);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                const float *src = merge + w * L::kMergeWarp;
+                const float mm = src[R * L::kMergeRow + row];
+                const float f = mm == -INFINITY ? 0.f : exp2_fast(mm - M);
+                const float4 y = *reinterpret_cast<const float4 *>(src + row * L::kMergeRow + 4 * dq);
+                Lsum += f * src[R * L::kMergeRow + R + row];
+                v.x += f * y.x; v.y += f * y.y; v.z += f * y.z; v.w += f * y.w;
+            }
+            if (begins && ends) {
+                store(row, dq, M, Lsum, v);
+            } else {
+                *reinterpret_cast<float4 *>(my_part + row * D + 4 * dq) = v;
+                if (dq == 0) {
+                    my_part[kDecodeRows * 128 + row] = M;
+                    my_part[kDecodeRows * 128 + kDecodeRows + row] = Lsum;
+                }
+            }
+        }
+        if (!(begins && ends)) {
+            // blocks that hold a part of the unit: first .. last; the counter is the first one's
+            const int first = static_cast<int>(((cur.begin + 1) * ctas - 1) / W), last = static_cast<int>((unit_end * ctas - 1) / W);
+            fence_gpu();
+            __syncthreads();
+            if (tid == 0) {
+                const uint32_t seen = atomicAdd(counters + first, 1u);
+                s_last = seen == static_cast<uint32_t>(last - first);
+                if (s_last) counters[first] = 0;   // ready for the next call
+            }
+            __syncthreads();
+            if (s_last) {
+                fence_gpu();
+                const int first_slot = cur.begin == W * first / ctas ? 0 : 1;
+                for (int x = tid; x < rows * kQuads; x += kFewThreads) {
+                    const int row = x / kQuads, dq = x - row * kQuads;
+                    float M = -INFINITY, Lsum = 0.f;
+                    for (int k = first; k <= last; ++k)
+                        M = fmaxf(M, __ldcg(parts + (2 * k + (k == first ? first_slot : 0)) * kDecodePartFloats + kDecodeRows * 128 + row));
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int k = first; k <= last; ++k) {
+                        const float *src = parts + (2 * k + (k == first ? first_slot : 0)) * kDecodePartFloats;
+                        const float mm = __ldcg(src + kDecodeRows * 128 + row);
+                        const float f = mm == -INFINITY ? 0.f : exp2_fast(mm - M);
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + row * D + 4 * dq));
+                        Lsum += f * __ldcg(src + kDecodeRows * 128 + kDecodeRows + row);
+                        v.x += f * y.x; v.y += f * y.y; v.z += f * y.z; v.w += f * y.w;
+                    }
+                    store(row, dq, M, Lsum, v);
+                }
+            }
+        }
+        __syncthreads();                           // the merge buffer is free again
+        unit_lo = unit_hi;
+        first_unit = false;
+        if (unit_lo < g1) few_seek(p, L::kShift, unit_lo, &cur);
+    }
+}
+
+}  // namespace ead

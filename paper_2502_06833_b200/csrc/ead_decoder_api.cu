@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "attention_kernels.cuh"
+#include "attn_few_rows_kernel.cuh"
 #include "kv_cache_kernels.cuh"
 #include "rmsnorm_kernel.cuh"
 #include "tma_host.h"
@@ -27,6 +28,7 @@ namespace {
     } while (0)
 
 constexpr int kMaxDevices = 64;
+constexpr int kFewMinTiles = 16;          // tiles of 8 KiB per block before another block is worth its part in the join
 
 struct DeviceInfo {
     bool ready = false;
@@ -35,6 +37,59 @@ struct DeviceInfo {
 
 std::mutex g_mu;
 DeviceInfo g_dev[kMaxDevices];
+
+int launched() { return cudaGetLastError() == cudaSuccess ? EAD_OK : EAD_ECUDA; }
+
+// A pool as {128-byte (or 64-byte) line of a key, slot, line, head, page}; a box is `keys` consecutive slots of one
+// head of one page, line by line, with the swizzle that makes eight keys' chunks conflict-free.
+bool encode_pool(CUtensorMap *tm, const KvCacheView &c, int format, void *base, int keys)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const bool bf16 = format == EAD_FMT_BF16;
+    const int size = bf16 ? 2 : 1, row = c.head_dim * size, line = std::min(row, 128);
+    const cuuint64_t dims[5] = {static_cast<cuuint64_t>(line / size), static_cast<cuuint64_t>(c.page_size),
+                                static_cast<cuuint64_t>(row / line), static_cast<cuuint64_t>(c.heads),
+                                static_cast<cuuint64_t>(c.n_pages)};
+    const cuuint64_t strides[4] = {static_cast<cuuint64_t>(c.slot_stride * size), static_cast<cuuint64_t>(line),
+                                   static_cast<cuuint64_t>(c.head_stride * size),
+                                   static_cast<cuuint64_t>(c.page_stride * size)};
+    const cuuint32_t box[5] = {static_cast<cuuint32_t>(line / size), static_cast<cuuint32_t>(keys),
+                               static_cast<cuuint32_t>(row / line), 1, 1};
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    return fn(tm, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, base, dims, strides, box, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, line == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int FMT, int D, int NB>
+int launch_few_rows(const AttnParams &p, int sms, cudaStream_t s)
+{
+    using L = FewLayout<FMT, D, NB>;
+    const int keys = std::min(p.cache.page_size, L::kTile);
+    CUtensorMap tk, tv;
+    if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys)) return EAD_ECUDA;
+    ead_attn_few_rows_kernel<FMT, D, NB><<<std::min(sms, kAttnMaxCtas), L::kThreads, L::kSmem, s>>>(tk, tv, p, __builtin_ctz(keys), kFewMinTiles);
+    return launched();
+}
+
+template <int FMT, int D>
+int launch_few_rows(const AttnParams &p, int sms, cudaStream_t s)
+{
+    return p.few_rows <= 8 ? launch_few_rows<FMT, D, 1>(p, sms, s) : launch_few_rows<FMT, D, 2>(p, sms, s);
+}
+
+template <int FMT, int D, int NB>
+bool allow_smem()
+{
+    return cudaFuncSetAttribute(ead_attn_few_rows_kernel<FMT, D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                FewLayout<FMT, D, NB>::kSmem) == cudaSuccess;
+}
+template <int FMT, int D>
+bool allow_smem()
+{
+    return allow_smem<FMT, D, 1>() && allow_smem<FMT, D, 2>();
+}
 
 // Makes `device` current; on its first use checks the architecture and sets kernel attributes.
 int use_device(int device, DeviceInfo **out)
@@ -50,14 +105,17 @@ int use_device(int device, DeviceInfo **out)
         if (major != 10) return EAD_EUNSUPPORTED_ARCH;
         EAD_CUDA(cudaSetDevice(device));
         EAD_CUDA(cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, device));
+        if (!allow_smem<kFmtBf16, 64>() || !allow_smem<kFmtBf16, 128>() || !allow_smem<kFmtE4m3, 64>() ||
+            !allow_smem<kFmtE4m3, 128>()) {
+            cudaGetLastError();
+            return EAD_ECUDA;
+        }
         d.ready = true;
     }
     EAD_CUDA(cudaSetDevice(device));
     *out = &d;
     return EAD_OK;
 }
-
-int launched() { return cudaGetLastError() == cudaSuccess ? EAD_OK : EAD_ECUDA; }
 
 bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -205,9 +263,20 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
     p.group = heads_q / p.cache.heads;
     p.window = window;
     p.sinks = window ? sinks : 0;
-    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
+    p.workspace = static_cast<uint8_t *>(workspace);
     p.status = status;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // Units of up to 16 packed rows have a kernel of their own.  Where longer chunks are there as well, only up to 8:
+    // a second group of 8 rows costs every unit, and the other kernel runs anyway.
+    const int64_t most = static_cast<int64_t>(p.batch.max_new) * p.group;
+    p.few_rows = p.group > kDecodeRows ? 0 : most <= 8 || (most > kDecodeRows && p.group <= 8) ? 8 : kDecodeRows;
+    if (p.few_rows) {
+        const bool bf16 = cache->format == EAD_FMT_BF16, wide = p.cache.head_dim == 128;
+        rc = bf16 ? (wide ? launch_few_rows<kFmtBf16, 128>(p, d->sms, s) : launch_few_rows<kFmtBf16, 64>(p, d->sms, s))
+                  : (wide ? launch_few_rows<kFmtE4m3, 128>(p, d->sms, s) : launch_few_rows<kFmtE4m3, 64>(p, d->sms, s));
+        if (rc != EAD_OK || most <= p.few_rows) return rc;
+    }
     const dim3 grid((p.batch.n_tokens + 3) / 4, heads_q);
     if (cache->format == EAD_FMT_BF16)
         ead_kv_attention_simple_kernel<kFmtBf16><<<grid, 128, 0, s>>>(p);
