@@ -477,8 +477,8 @@ int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int3
  *              device need a workspace each
  *   status     dev uint32 or NULL.  EAD_STATUS_BAD_PAGE: a page index was out of range (its
  *              tokens count as zeros) or a context is longer than max_len (the rest is not
- *              seen); EAD_STATUS_BAD_COUNT: a sequence has more than max_new new tokens (its rows
- *              may be unwritten); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out
+ *              seen); EAD_STATUS_BAD_COUNT: new_start contradicts max_new or n_tokens (the rows
+ *              of such a sequence are not written); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out
  * The result does not depend on the order in which blocks run: partial results are joined in a
  * fixed order.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
  */

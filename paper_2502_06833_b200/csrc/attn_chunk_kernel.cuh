@@ -1,0 +1,742 @@
+// Attention for units of many packed rows (chunks of new tokens): tcgen05 MMAs with TMEM accumulators.
+//
+// A unit is up to 256 packed rows (new tokens x query heads of one cache head; consecutive rows are the heads of
+// a token), two tiles of 128 rows that share every key tile of 128 keys.  Per key tile and row tile: S = Q K^T (TMEM),
+// one thread per row turns S into probabilities P, which overwrite S as bf16 in TMEM, O += P V (TMEM).  While the tensor core
+// works on one row tile, the other's softmax runs; the two take turns.  A unit of at most 128 rows
+// gives both turns to the same rows instead: even key tiles go to the first accumulator, odd ones
+// to the second, and the two are joined at the end.
+//
+// Warps: 0-3 softmax and output of the first row tile, 4-7 of the second, 8 issues the MMAs, 9 loads key and value
+// tiles (TMA), 10-13 load the query rows and, for an 8-bit cache, turn codes into bf16 on their way into the MMA's
+// operand tiles (as in the few-rows kernel).
+#pragma once
+#include "attn_common.cuh"
+
+namespace ead {
+
+constexpr int kChunkThreads = 14 * 32;
+constexpr int kChunkMmaWarp = 8, kChunkLoadWarp = 9, kChunkFeedWarp = 10;
+constexpr int kChunkKeys = 128;                   // keys per tile
+constexpr int kChunkShift = 7;
+constexpr int kChunkRows = 256;                   // packed rows per unit
+constexpr size_t kChunkPartOffset = 4u << 20;     // the few-rows kernel's parts end below this
+
+// Two bf16 rows of a register's codes, chosen by `pick`, times 2^-120 (see the few-rows kernel).
+__device__ __forceinline__ uint32_t chunk_codes(uint32_t codes, uint32_t pick)
+{
+    const uint32_t w = __byte_perm(codes, 0, pick);
+    return (w & 0x80008000u) | ((w >> 4) & 0x07F007F0u);
+}
+
+template <int FMT, int D>
+struct ChunkLayout {
+    static constexpr int kHalves = D / 64;                               // 128-byte lines per bf16 row
+    static constexpr int kTileBytes = kChunkKeys * D * 2;                // a bf16 tile of keys, values or query rows
+    static constexpr int kQ = 2 * kTileBytes;
+    static constexpr int kStages = FMT == kFmtBf16 ? (D == 128 ? 5 : 8) : (D == 128 ? 4 : 8);
+    static constexpr int kRawTile = FMT == kFmtE4m3 ? kChunkKeys * D : 0;
+    static constexpr int kRawScale = FMT == kFmtE4m3 ? kChunkKeys * (D / kFmtBlock) : 0;
+    static constexpr int kRawStages = FMT == kFmtE4m3 ? 2 : 0;
+    static constexpr int kBars = 2 * kStages + 2 * 2 + 8;
+    static constexpr int kSmem = 1024 + kQ + kStages * kTileBytes + kRawStages * (kRawTile + kRawScale) + 8 * kBars;
+};
+
+// ---- the string of tiles: units in the order (sequence, cache head, run of rows); a tile of a two-tile unit
+// costs 2, one of a one-tile unit 1, and belongs to the block in whose stretch it begins
+struct ChunkCursor {
+    int b, h, blk;                                // sequence, cache head, run of 256 rows
+    int64_t begin;                                // the unit's place in the string
+    SeqInfo s;
+    int row0, rows;                               // packed rows of the unit
+    int pa, pb;                                   // positions of its first and last token
+    int cost;                                     // per tile
+    KeyRange r;
+};
+__device__ __forceinline__ int chunk_blocks(const AttnParams &p, const SeqInfo &s)
+{
+    const int rows = s.n * p.group;               // the host has checked that this fits
+    return rows <= p.few_rows ? 0 : (rows + kChunkRows - 1) / kChunkRows;
+}
+__device__ __forceinline__ void chunk_unit(const AttnParams &p, const SeqInfo &s, int blk, ChunkCursor *c)
+{
+    c->blk = blk;
+    c->row0 = blk * kChunkRows;
+    c->rows = min(kChunkRows, s.n * p.group - c->row0);
+    c->pa = s.p0 + c->row0 / p.group;
+    c->pb = s.p0 + (c->row0 + c->rows - 1) / p.group;
+    c->cost = c->rows > kChunkRows / 2 ? 2 : 1;
+    c->r = key_range(c->pa, c->pb, s.len, p.window, p.sinks, kChunkShift);
+}
+// Moves on to the next unit.
+__device__ __forceinline__ void chunk_next(const AttnParams &p, ChunkCursor *c)
+{
+    c->begin += static_cast<int64_t>(c->cost) * c->r.tiles;
+    int blk = c->blk + 1;
+    if (blk >= chunk_blocks(p, c->s)) {
+        blk = 0;
+        if (++c->h >= p.cache.heads) {
+            c->h = 0;
+            do {
+                ++c->b;
+                c->s = seq_info(p.batch, c->b);
+            } while (chunk_blocks(p, c->s) == 0);
+        }
+    }
+    chunk_unit(p, c->s, blk, c);
+}
+// The unit's tiles that begin within [g0, g1).
+__device__ __forceinline__ void chunk_stretch(const ChunkCursor &c, int64_t g0, int64_t g1, int *ta, int *tb)
+{
+    const int64_t a = (g0 - c.begin + c.cost - 1) / c.cost, b = (g1 - c.begin + c.cost - 1) / c.cost;
+    *ta = g0 <= c.begin ? 0 : static_cast<int>(a);
+    *tb = b < c.r.tiles ? static_cast<int>(b) : c.r.tiles;
+}
+
+// ---- tensor memory
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+}
+// Waits for every load of this thread; naming the registers keeps their uses behind it.
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
+                   "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
+                   "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
+                   "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Shared-memory writes of this thread become visible to the tensor core and to TMA.
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// D[tmem] (+)= A[tmem] * B[smem], A packed bf16.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Descriptor of a [rows of 64 elements, 128-byte swizzle] tile whose ROW index is the contraction (values: keys along K,
+// head dimension contiguous): leading offset = next 64 elements of the head dimension, stride offset = next 8 keys.
+__device__ __forceinline__ uint64_t umma_desc_mn(uint32_t saddr, uint32_t lead_bytes)
+{
+    const uint32_t lo = ((saddr >> 4) & 0x3FFFu) | ((lead_bytes >> 4) << 16);
+    const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+    return (static_cast<uint64_t>(hi) << 32) | lo;
+}
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+    ead_attn_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, AttnParams p,
+                          int box_shift, int min_cost)
+{
+    using L = ChunkLayout<FMT, D>;
+    constexpr int S = L::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int64_t s_scan[14];
+    __shared__ int s_b, s_last;
+    __shared__ int64_t s_before;
+    __shared__ uint32_t s_tmem;
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t *const base_ptr = smem_raw + (base - raw);
+    const uint32_t q_smem = base, ring = base + L::kQ, rawk = ring + S * L::kTileBytes;
+    const uint32_t raw_scale = rawk + L::kRawStages * L::kRawTile;
+    const uint32_t bars = raw_scale + L::kRawStages * L::kRawScale;
+    const uint32_t bar_full = bars, bar_empty = bars + 8 * S, bar_raw_full = bar_empty + 8 * S, bar_raw_empty = bar_raw_full + 16;
+    const uint32_t bar_s = bar_raw_empty + 16, bar_p = bar_s + 16, bar_o = bar_p + 16, bar_q_full = bar_o + 16, bar_q_empty = bar_q_full + 8;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const KvCacheView &c = p.cache;
+
+    if (tid == 0) {
+        for (int i = 0; i < S; ++i) {
+            mbar_init(bar_full + 8 * i, FMT == kFmtBf16 ? 1 : 128);
+            mbar_init(bar_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_raw_full + 8 * i, 1);
+            mbar_init(bar_raw_empty + 8 * i, 128);
+            mbar_init(bar_s + 8 * i, 1);
+            mbar_init(bar_p + 8 * i, 128);
+            mbar_init(bar_o + 8 * i, 1);
+        }
+        mbar_init(bar_q_full, 128);
+        mbar_init(bar_q_empty, 1);
+        fence_mbar_init();
+    }
+    if (warp == kChunkMmaWarp) {
+        tmem_alloc(smem_u32(&s_tmem), 512);
+        tmem_relinquish();
+    }
+
+    // ---- the string: cost of one cache head of every sequence, and where this block's stretch begins
+    int32_t *const s_cost = reinterpret_cast<int32_t *>(base_ptr);      // [B <= 4096], in the query rows' place for now
+    for (int b0 = warp * 32; b0 < p.batch.B; b0 += 14 * 32) {
+        const int b = b0 + lane;
+        SeqInfo s{};
+        int blocks = 0, cost = 0;
+        if (b < p.batch.B) {
+            bool bad;
+            s = seq_info(p.batch, b, &bad);
+            if (blockIdx.x == 0 && bad) flag_status(p.status, kStatusBadCount);
+            blocks = chunk_blocks(p, s);
+            if (blockIdx.x == 0 && blocks && s.p0 + s.n > p.batch.max_len) flag_status(p.status, kStatusBadPage);
+        }
+        unsigned many = __ballot_sync(0xffffffffu, blocks > 2);
+        ChunkCursor u;
+        if (blocks && blocks <= 2)
+            for (int k = 0; k < blocks; ++k) {
+                chunk_unit(p, s, k, &u);
+                cost += u.cost * u.r.tiles;
+            }
+        while (many) {                             // long chunks: the warp's lanes share the runs of one sequence
+            const int src = __ffs(many) - 1;
+            many &= many - 1;
+            SeqInfo t;
+            t.n = __shfl_sync(0xffffffffu, s.n, src);
+            t.p0 = __shfl_sync(0xffffffffu, s.p0, src);
+            t.len = __shfl_sync(0xffffffffu, s.len, src);
+            t.token0 = 0;
+            const int nb = __shfl_sync(0xffffffffu, blocks, src);
+            int part = 0;
+            for (int k = lane; k < nb; k += 32) {
+                chunk_unit(p, t, k, &u);
+                part += u.cost * u.r.tiles;
+            }
+            part = __reduce_add_sync(0xffffffffu, part);
+            if (lane == src) cost = part;
+        }
+        if (b < p.batch.B) s_cost[b] = cost;
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = s_tmem;
+    const int per = (p.batch.B + kChunkThreads - 1) / kChunkThreads;
+    const int b_lo = min(tid * per, p.batch.B), b_hi = min(b_lo + per, p.batch.B);
+    int64_t mine = 0;
+    for (int b = b_lo; b < b_hi; ++b) mine += s_cost[b];
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) s_scan[warp] = upto;
+    __syncthreads();
+    int64_t total = 0, before = 0;
+    for (int w = 0; w < 14; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+    }
+    upto += before;
+    const int64_t W = total * c.heads;
+    const int64_t ctas = min(static_cast<int64_t>(gridDim.x), max(static_cast<int64_t>(1), W / min_cost));
+    const bool idle = W == 0 || blockIdx.x >= ctas;
+    const int64_t g0 = idle ? 0 : W * blockIdx.x / ctas, g1 = idle ? 0 : W * (blockIdx.x + 1) / ctas;
+    if (!idle && mine > 0 && g0 >= (upto - mine) * c.heads && g0 < upto * c.heads) {
+        int64_t at = upto - mine;
+        for (int b = b_lo; b < b_hi; ++b) {
+            if (g0 < (at + s_cost[b]) * c.heads) {
+                s_b = b;
+                s_before = at * c.heads;
+                break;
+            }
+            at += s_cost[b];
+        }
+    }
+    __syncthreads();
+    ChunkCursor cur{};
+    if (!idle) {
+        cur.b = s_b;
+        cur.s = seq_info(p.batch, cur.b);
+        const int cost = s_cost[cur.b];
+        cur.h = static_cast<int>((g0 - s_before) / cost);
+        cur.begin = s_before + static_cast<int64_t>(cur.h) * cost;
+        chunk_unit(p, cur.s, 0, &cur);
+        // the first unit with a tile that begins at g0 or later
+        while (cur.begin + static_cast<int64_t>(cur.cost) * (cur.r.tiles - 1) < g0) chunk_next(p, &cur);
+    }
+    __syncthreads();                               // s_cost is done with; its place takes query rows now
+
+    bool expired = false;
+    if (idle) {
+        // nothing
+    } else if (warp == kChunkLoadWarp) {
+        // ================================================================ key and value tiles
+        const int boxes = kChunkKeys >> box_shift, box_keys = 1 << box_shift;     // at most 16
+        int t = 0;                                 // tiles so far
+        while (true) {
+            int ta, tb;
+            chunk_stretch(cur, g0, g1, &ta, &tb);
+            for (int k = ta; k < tb; ++k, ++t) {
+                const int key0 = cur.r.base(k, kChunkShift) + lane * box_keys, slot = key0 & (c.page_size - 1);
+                int page = -2;
+                if (lane < boxes && key0 < cur.r.hi && (key0 + box_keys > cur.r.lo || key0 < p.sinks)) {
+                    page = find_page(c, p.batch, cur.b, key0);
+                    if (page < 0) {
+                        flag_status(p.status, kStatusBadPage);
+                        page = c.n_pages;          // outside the pool: the copy delivers zeros
+                    }
+                }
+                const int live = __popc(__ballot_sync(0xffffffffu, page >= 0));
+                const int good = __popc(__ballot_sync(0xffffffffu, page >= 0 && page < c.n_pages));
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const int x = 2 * t + kv;
+                    const CUtensorMap *tm = kv ? &tmV : &tmK;
+                    if (FMT == kFmtBf16) {
+                        const int st = x % S;
+                        const uint32_t bar = bar_full + 8 * st, dst = ring + st * L::kTileBytes + lane * box_keys * 128;
+                        wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
+                        if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D * 2);
+                        __syncwarp();
+                        if (page >= 0) {
+#pragma unroll
+                            for (int hb = 0; hb < L::kHalves; ++hb)
+                                tma_load_5d(dst + hb * (kChunkKeys * 128), tm, 0, slot, hb, cur.h, page, bar);
+                        }
+                    } else {
+                        const int st = x % 2;
+                        const uint32_t bar = bar_raw_full + 8 * st;
+                        const uint32_t sc = raw_scale + st * L::kRawScale + lane * box_keys * (D / kFmtBlock);
+                        const uint32_t sc_bytes = box_keys * (D / kFmtBlock);
+                        wait_phase(bar_raw_empty + 8 * st, ((x / 2) & 1) ^ 1, p.status, &expired);
+                        if (page == c.n_pages)
+                            for (uint32_t y = 0; y < sc_bytes; y += 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + y), "r"(0) : "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D + good * sc_bytes);
+                        __syncwarp();
+                        if (page >= 0) {
+                            tma_load_5d(rawk + st * L::kRawTile + lane * box_keys * D, tm, 0, slot, 0, cur.h, page, bar);
+                            if (page < c.n_pages)
+                                bulk_load(sc, (kv ? c.v_scale : c.k_scale) + scale_offset(c, page, cur.h, slot), sc_bytes, bar);
+                        }
+                    }
+                }
+            }
+            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
+            chunk_next(p, &cur);
+        }
+    } else if (warp == kChunkMmaWarp) {
+        // ================================================================ MMAs
+        if (lane == 0) {
+            const uint32_t id_qk = umma_idesc_bf16_m128(kChunkKeys), id_pv = umma_idesc_bf16_m128(D) | (1u << 16);
+            int t = 0, segment = 0;
+            int np[2] = {0, 0};                    // probabilities taken so far per accumulator
+            while (true) {
+                int ta, tb;
+                chunk_stretch(cur, g0, g1, &ta, &tb);
+                const bool dual = cur.cost == 2;
+                const int nt = tb - ta;
+                int rounds[2];
+                rounds[0] = dual ? nt : (nt + 1) >> 1;
+                rounds[1] = dual ? nt : nt >> 1;
+                int left = rounds[0] + rounds[1];  // score products to come
+                wait_phase(bar_q_full, segment & 1, p.status, &expired);
+                tc_fence_after_sync();
+                auto scores = [&](int w, int i) {  // S_w = Q_w K^T of its i-th tile
+                    const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S;
+                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                    tc_fence_after_sync();
+                    const uint32_t a = q_smem + (dual ? w * L::kTileBytes : 0), b = ring + st * L::kTileBytes;
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        const uint32_t off = (ks >> 2) * (kChunkKeys * 128) + (ks & 3) * 32;
+                        umma_bf16(tmem + w * 128, umma_smem_desc(a + off), umma_smem_desc(b + off), id_qk, ks > 0);
+                    }
+                    if (!dual || w == 1) umma_commit(bar_empty + 8 * st);
+                    umma_commit(bar_s + 8 * w);
+                    if (--left == 0) umma_commit(bar_q_empty);                   // the query rows' place is free after the last one
+                };
+                for (int w = 0; w < 2; ++w)
+                    if (rounds[w] > 0) scores(w, 0);
+                for (int i = 0; i < rounds[0]; ++i)
+                    for (int w = 0; w < 2; ++w) {
+                        if (i >= rounds[w]) continue;
+                        const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S;
+                        wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                        wait_phase(bar_p + 8 * w, np[w] & 1, p.status, &expired);
+                        ++np[w];
+                        tc_fence_after_sync();
+#pragma unroll
+                        for (int ks = 0; ks < kChunkKeys / 16; ++ks)
+                            umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + ks * 8,
+                                         umma_desc_mn(ring + st * L::kTileBytes + ks * 2048, kChunkKeys * 128), id_pv, i > 0 || ks > 0);
+                        if (!dual || w == 1) umma_commit(bar_empty + 8 * st);
+                        if (i + 1 < rounds[w])
+                            scores(w, i + 1);
+                        else
+                            umma_commit(bar_o + 8 * w);
+                    }
+                t += nt;
+                ++segment;
+                if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
+                chunk_next(p, &cur);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= kChunkFeedWarp) {
+        // ================================================================ query rows; codes to bf16
+        const int ft = tid - kChunkFeedWarp * 32;  // 0 .. 127
+        int t = 0, segment = 0;
+        while (true) {
+            int ta, tb;
+            chunk_stretch(cur, g0, g1, &ta, &tb);
+            wait_phase(bar_q_empty, (segment & 1) ^ 1, p.status, &expired);
+            constexpr int kChunks = D / 8;         // 16-byte pieces per row
+            for (int y0 = ft; y0 < cur.cost * 128 * kChunks; y0 += 8 * 128) {     // eight loads in flight per thread
+                uint4 v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int y = y0 + u * 128, row = y / kChunks, ch = y - row * kChunks;
+                    v[u] = make_uint4(0, 0, 0, 0);
+                    if (row < cur.rows) {
+                        const int i = (cur.row0 + row) / p.group, gq = cur.row0 + row - i * p.group;
+                        v[u] = __ldg(reinterpret_cast<const uint4 *>(
+                            p.q + 2 * ((static_cast<int64_t>(cur.s.token0) + i) * p.q_stride + (static_cast<int64_t>(cur.h) * p.group + gq) * D + 8 * ch)));
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int y = y0 + u * 128, row = y / kChunks, ch = y - row * kChunks;
+                    const uint32_t dst = q_smem + (row >> 7) * L::kTileBytes + (ch >> 3) * (128 * 128) + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[u].x), "r"(v[u].y), "r"(v[u].z), "r"(v[u].w) : "memory");
+                }
+            }
+            fence_async_shared();
+            mbar_arrive(bar_q_full);
+            if (FMT == kFmtE4m3) {
+                for (int k = ta; k < tb; ++k, ++t)
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int x = 2 * t + kv, st = x % S, rs = x % 2;
+                        wait_phase(bar_raw_full + 8 * rs, (x / 2) & 1, p.status, &expired);
+                        uint32_t w[D / 4], sc;
+                        const uint32_t src = rawk + rs * L::kRawTile + ft * D;
+#pragma unroll
+                        for (int ch = 0; ch < D / 16; ++ch) {
+                            const uint32_t at = src + ((D == 128 ? ch ^ (ft & 7) : ch ^ ((ft >> 1) & 3)) << 4);
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(w[4 * ch]), "=r"(w[4 * ch + 1]), "=r"(w[4 * ch + 2]), "=r"(w[4 * ch + 3]) : "r"(at) : "memory");
+                        }
+                        const uint32_t sa = raw_scale + rs * L::kRawScale + ft * (D / kFmtBlock);
+                        if (D == 128)
+                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc) : "r"(sa) : "memory");
+                        else
+                            asm volatile("{\n\t.reg .b16 h;\n\tld.shared.b16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(sc) : "r"(sa) : "memory");
+                        // a key no query of the unit sees was perhaps not even loaded: zeros
+                        const bool keep = seen_by_any(cur.r, p.sinks, cur.r.base(k, kChunkShift) + ft);
+                        wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
+                        const uint32_t dst = ring + st * L::kTileBytes + ft * 128;
+#pragma unroll
+                        for (int g = 0; g < D / kFmtBlock; ++g) {
+                            const uint32_t byte = (sc >> (8 * g)) & 0xffu;
+                            const uint32_t f = ((min(byte, 134u) + 120u) << 7) * 0x10001u;       // see the few-rows kernel
+                            const uint32_t f2 = ((byte == 255u ? 0x7FC0u : (byte > 134u ? byte - 7u : 127u) << 7)) * 0x10001u;
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {                 // 8 values: 16 bytes of bf16
+                                uint32_t o[4];
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const uint32_t codes = w[8 * g + 2 * u + e];
+                                    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[2 * e]) : "r"(chunk_codes(codes, 0x1404)), "r"(f));
+                                    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[2 * e + 1]) : "r"(chunk_codes(codes, 0x3424)), "r"(f));
+                                }
+                                if (byte > 134u) {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[e]) : "r"(o[e]), "r"(f2));
+                                }
+                                if (!keep) o[0] = o[1] = o[2] = o[3] = 0;
+                                const int ch = 4 * g + u;
+                                const uint32_t at = dst + (ch >> 3) * (kChunkKeys * 128) + (((ch & 7) ^ (ft & 7)) << 4);
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                            }
+                        }
+                        fence_async_shared();
+                        mbar_arrive(bar_full + 8 * st);
+                        // not earlier: only the codes' use shows that their loads are done (released right after the loads, the
+                        // next tile's copy overtook loads that the tensor core's own reads had held up)
+                        mbar_arrive(bar_raw_empty + 8 * rs);
+                    }
+            }
+            ++segment;
+            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
+            chunk_next(p, &cur);
+        }
+    } else {
+        // ================================================================ softmax and output
+        const int w = warp >> 2, row = tid & 127;
+        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;            // this warp's 32 lanes of tensor memory
+        const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
+        int t = 0, ns = 0;
+        int outputs[2] = {0, 0};                   // finished outputs per accumulator
+        while (true) {
+            int ta, tb;
+            chunk_stretch(cur, g0, g1, &ta, &tb);
+            const bool dual = cur.cost == 2;
+            const int nt = tb - ta, rounds = dual ? nt : (nt + 1 - w) >> 1;
+            const int my_row = dual ? w * 128 + row : row;                       // packed row within the unit
+            const int pos = cur.s.p0 + (cur.row0 + min(my_row, cur.rows - 1)) / p.group;
+            // positions of this row tile's first and last row, for tiles that need no mask
+            const int row_a = dual ? w * 128 : 0, row_b = min(row_a + 127, cur.rows - 1);
+            const int pos_a = cur.s.p0 + (cur.row0 + row_a) / p.group, pos_b = cur.s.p0 + (cur.row0 + row_b) / p.group;
+            float m = -INFINITY, l = 0.f;
+            for (int i = 0; i < rounds; ++i) {
+                const int k = dual ? i : 2 * i + w;
+                const int key0 = cur.r.base(ta + k, kChunkShift);
+                const bool whole = key0 + kChunkKeys - 1 <= pos_a && key0 + kChunkKeys <= cur.s.len &&
+                                   (p.window == 0 || key0 > pos_b - p.window || key0 + kChunkKeys <= p.sinks);
+                if (FMT == kFmtBf16 && (dual ? w == 0 : true)) {
+                    // values no query sees may be anything, and were perhaps not even loaded: zeros, so that 0 * NaN cannot arise
+                    const bool clean = key0 + kChunkKeys <= cur.r.hi && (key0 >= cur.r.lo || key0 + kChunkKeys <= p.sinks);
+                    if (!clean) {
+                        const int x = 2 * (t + k) + 1, st = x % S;
+                        wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                        if (!seen_by_any(cur.r, p.sinks, key0 + row)) {
+                            const uint32_t dst = ring + st * L::kTileBytes + row * 128;
+#pragma unroll
+                            for (int hb = 0; hb < L::kHalves; ++hb)
+#pragma unroll
+                                for (int ch = 0; ch < 8; ++ch)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + hb * (kChunkKeys * 128) + ch * 16), "r"(0) : "memory");
+                        }
+                        fence_async_shared();
+                    }
+                }
+                wait_phase(bar_s + 8 * w, ns & 1, p.status, &expired);
+                ++ns;
+                __syncwarp();
+                tc_fence_after_sync();
+                uint32_t v[2][32];
+                const int limit = min(pos + 1, cur.s.len) - key0;                // columns from here on lie ahead or beyond the context
+                const int low = p.window ? pos - p.window + 1 - key0 : -0x40000000, sink = p.sinks - key0;
+                auto mask = [&](uint32_t (&x)[32], int c0) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int col = c0 + e;
+                        if (!(col < limit && (col >= low || col < sink))) x[e] = 0xff800000u;
+                    }
+                };
+                float top = -INFINITY;
+                tmem_ld32(t_s, v[0]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    tmem_wait_ld(v[q & 1]);
+                    if (q < 3) tmem_ld32(t_s + 32 * (q + 1), v[(q + 1) & 1]);
+                    if (!whole) mask(v[q & 1], 32 * q);
+                    float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[e & 3] = fmaxf(x[e & 3], __uint_as_float(v[q & 1][e]));
+                    top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+                }
+                tmem_ld32(t_s, v[0]);                                            // the scores once more, now for the exponentials
+                top *= p.scale_log2;
+                const bool raise = top > m + 8.f;
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float f = raise ? exp2_fast(m - top) : 1.f;
+                    if (raise) m = top;
+                    l *= f;
+                    if (i > 0) {                   // the products so far are complete: S of this tile was issued behind them
+                        uint32_t o[32];
+#pragma unroll
+                        for (int q = 0; q < D / 32; ++q) {
+                            tmem_wait_ld(v[0]);
+                            tmem_ld32(t_o + 32 * q, o);
+                            tmem_wait_ld(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st32(t_o + 32 * q, o);
+                        }
+                    }
+                }
+                const float mm = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    tmem_wait_ld(v[q & 1]);
+                    if (q < 3) tmem_ld32(t_s + 32 * (q + 1), v[(q + 1) & 1]);
+                    if (!whole) mask(v[q & 1], 32 * q);
+                    uint32_t pk[16];
+                    float sum[2] = {0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float a = exp2_fast(fmaf(__uint_as_float(v[q & 1][2 * e]), p.scale_log2, -mm));
+                        const float b = exp2_fast(fmaf(__uint_as_float(v[q & 1][2 * e + 1]), p.scale_log2, -mm));
+                        sum[0] += a;
+                        sum[1] += b;
+                        pk[e] = to_bf16x2(a, b);
+                    }
+                    l += sum[0] + sum[1];
+                    tmem_st16(t_s + 16 * q, pk);   // columns whose scores were read before
+                }
+                tmem_wait_st();
+                tc_fence_before_sync();
+                mbar_arrive(bar_p + 8 * w);
+            }
+
+            // ---- output: this thread's row
+            const int64_t unit_last = cur.begin + static_cast<int64_t>(cur.cost) * (cur.r.tiles - 1);
+            const bool alone = ta == 0 && tb == cur.r.tiles;
+            if (rounds > 0) {
+                wait_phase(bar_o + 8 * w, outputs[w] & 1, p.status, &expired);
+                __syncwarp();
+                tc_fence_after_sync();
+            }
+            float *const parts = reinterpret_cast<float *>(p.workspace + kChunkPartOffset);
+            constexpr size_t kPart = kChunkRows * (D + 2);
+            float *const my_part = parts + (2 * blockIdx.x + (cur.begin <= g0 ? 0 : 1)) * kPart;
+            float f0 = 1.f, f1 = 0.f;              // one-tile units: factors of the two accumulators
+            if (!dual) {
+                // through the places of rows 128 .. 255, which such a unit does not have
+                volatile float *const ml = my_part + kChunkRows * D + 128 + row;
+                if (w == 1) {
+                    ml[0] = m;
+                    ml[kChunkRows] = l;
+                }
+                named_sync(1, 256);
+                if (w == 0) {
+                    const float m1 = ml[0], l1 = ml[kChunkRows];
+                    const float M = fmaxf(m, m1);
+                    f0 = m == -INFINITY ? (M == -INFINITY ? 1.f : 0.f) : exp2_fast(m - M);
+                    f1 = m1 == -INFINITY ? 0.f : exp2_fast(m1 - M);
+                    l = l * f0 + l1 * f1;
+                    m = M;
+                    if (nt > 1) {                  // the second accumulator's products are complete, too
+                        wait_phase(bar_o + 8, outputs[1] & 1, p.status, &expired);
+                        __syncwarp();
+                        tc_fence_after_sync();
+                    }
+                }
+            }
+            const bool holds = dual || w == 0;
+            const bool live = holds && my_row < cur.rows;
+            const int pi = (cur.row0 + my_row) / p.group, hq = cur.h * p.group + (cur.row0 + my_row - pi * p.group);
+            const int64_t token = static_cast<int64_t>(cur.s.token0) + pi;
+            if (holds) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+                for (int q = 0; q < D / 32; ++q) {
+                    uint32_t o[32];
+                    __syncwarp();
+                    tmem_ld32(t_o + 32 * q, o);
+                    tmem_wait_ld(o);
+                    if (!dual) {
+                        uint32_t o1[32];
+                        tmem_ld32(t_o + 128 + 32 * q, o1);
+                        tmem_wait_ld(o1);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            o[e] = __float_as_uint(__uint_as_float(o[e]) * f0 + (nt > 1 ? __uint_as_float(o1[e]) * f1 : 0.f));
+                    }
+                    if (live && alone) {
+                        uint4 *dst = reinterpret_cast<uint4 *>(p.out + 2 * (token * p.out_stride + static_cast<int64_t>(hq) * D + 32 * q));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            dst[e] = make_uint4(to_bf16x2(__uint_as_float(o[8 * e]) * inv, __uint_as_float(o[8 * e + 1]) * inv),
+                                                to_bf16x2(__uint_as_float(o[8 * e + 2]) * inv, __uint_as_float(o[8 * e + 3]) * inv),
+                                                to_bf16x2(__uint_as_float(o[8 * e + 4]) * inv, __uint_as_float(o[8 * e + 5]) * inv),
+                                                to_bf16x2(__uint_as_float(o[8 * e + 6]) * inv, __uint_as_float(o[8 * e + 7]) * inv));
+                    } else if (live) {
+                        uint4 *dst = reinterpret_cast<uint4 *>(my_part + my_row * D + 32 * q);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                }
+                if (live) {
+                    if (alone) {
+                        if (p.lse) p.lse[token * p.heads_q + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+                    } else {
+                        my_part[kChunkRows * D + my_row] = m;
+                        my_part[kChunkRows * D + kChunkRows + my_row] = l;
+                    }
+                }
+                tc_fence_before_sync();
+            }
+            if (!dual) named_sync(1, 256);         // the second accumulator may be written again
+            if (!alone) {
+                // blocks that hold a part of the unit: first .. last; the counter is the first one's
+                uint32_t *const counters = reinterpret_cast<uint32_t *>(p.workspace + kAttnCounterBytes);
+                const int first = static_cast<int>(((cur.begin + 1) * ctas - 1) / W), last = static_cast<int>(((unit_last + 1) * ctas - 1) / W);
+                fence_gpu();
+                named_sync(1, 256);
+                if (tid == 0) {
+                    const uint32_t seen = atomicAdd(counters + first, 1u);
+                    s_last = seen == static_cast<uint32_t>(last - first);
+                    if (s_last) counters[first] = 0;                             // ready for the next call
+                }
+                named_sync(1, 256);
+                if (s_last) {
+                    fence_gpu();
+                    const int first_slot = cur.begin <= W * first / ctas ? 0 : 1;
+                    constexpr int kQuads = D / 4;
+                    for (int x = tid; x < cur.rows * kQuads; x += 256) {
+                        const int r = x / kQuads, dq = x - r * kQuads;
+                        float M = -INFINITY, Lsum = 0.f;
+                        for (int k = first; k <= last; ++k)
+                            M = fmaxf(M, __ldcg(parts + (2 * k + (k == first ? first_slot : 0)) * kPart + kChunkRows * D + r));
+                        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int k = first; k <= last; ++k) {
+                            const float *src = parts + (2 * k + (k == first ? first_slot : 0)) * kPart;
+                            const float mk = __ldcg(src + kChunkRows * D + r);
+                            const float f = mk == -INFINITY ? 0.f : exp2_fast(mk - M);
+                            const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + r * D + 4 * dq));
+                            Lsum += f * __ldcg(src + kChunkRows * D + kChunkRows + r);
+                            a.x += f * y.x; a.y += f * y.y; a.z += f * y.z; a.w += f * y.w;
+                        }
+                        const float inv = Lsum == 0.f ? 0.f : 1.f / Lsum;
+                        const int i = (cur.row0 + r) / p.group, hr = cur.h * p.group + (cur.row0 + r - i * p.group);
+                        const int64_t tok = static_cast<int64_t>(cur.s.token0) + i;
+                        *reinterpret_cast<uint2 *>(p.out + 2 * (tok * p.out_stride + static_cast<int64_t>(hr) * D + 4 * dq)) =
+                            make_uint2(to_bf16x2(a.x * inv, a.y * inv), to_bf16x2(a.z * inv, a.w * inv));
+                        if (p.lse && dq == 0) p.lse[tok * p.heads_q + hr] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
+                    }
+                }
+                named_sync(1, 256);                // s_last may be written again
+            }
+            t += nt;
+            outputs[0] += 1;                       // the first accumulator has a tile in every unit
+            outputs[1] += dual || nt > 1;
+            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
+            chunk_next(p, &cur);
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kChunkMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace ead

@@ -38,14 +38,20 @@ constexpr size_t kDecodePartOffset = 2 * kAttnCounterBytes;
 // The new tokens and the readable context of a sequence.
 struct SeqInfo {
     int n, p0, len;                               // new tokens, position of the first one, keys in the cache
+    int token0;                                   // first new token's row of the step
 };
-__device__ __forceinline__ SeqInfo seq_info(const KvBatchView &bt, int b)
+// A sequence whose new tokens contradict the host's bounds counts as one without any (`bad`).
+__device__ __forceinline__ SeqInfo seq_info(const KvBatchView &bt, int b, bool *bad = nullptr)
 {
     SeqInfo s;
-    const int kv = __ldg(bt.kv_len + b);
-    s.n = __ldg(bt.new_start + b + 1) - __ldg(bt.new_start + b);
+    const int kv = __ldg(bt.kv_len + b), end = __ldg(bt.new_start + b + 1);
+    s.token0 = __ldg(bt.new_start + b);
+    s.n = end - s.token0;
     s.p0 = kv - s.n;
     s.len = min(max(kv, 0), bt.max_len);
+    const bool wrong = s.n < 0 || s.n > bt.max_new || s.token0 < 0 || end > bt.n_tokens;
+    if (wrong) s.n = 0;
+    if (bad) *bad = wrong;
     return s;
 }
 
@@ -59,6 +65,7 @@ struct KeyRange {
         return (t < sink_tiles ? t : t - sink_tiles + first_tile) << shift;
     }
 };
+// (A negative pb + 1 leaves nothing; positions stay below 2^30 + 2^30.)
 __device__ __forceinline__ KeyRange key_range(int pa, int pb, int len, int window, int sinks, int shift)
 {
     KeyRange r;

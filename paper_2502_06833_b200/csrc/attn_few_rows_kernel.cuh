@@ -40,7 +40,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
 }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    // volatile: stays before the refill of the stage its operands came from
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
@@ -160,12 +161,11 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     int64_t mine = 0;
     KeyRange kr;
     for (int b = b_lo; b < b_hi; ++b) {
-        const SeqInfo s = seq_info(p.batch, b);
+        bool bad;
+        const SeqInfo s = seq_info(p.batch, b, &bad);
         mine += few_tiles(p, s, L::kShift, &kr);
-        if (blockIdx.x == 0) {
-            if (s.n > p.batch.max_new) flag_status(p.status, kStatusBadCount);
-            if (s.p0 + s.n > p.batch.max_len) flag_status(p.status, kStatusBadPage);
-        }
+        if (blockIdx.x == 0 && bad) flag_status(p.status, kStatusBadCount);
+        if (blockIdx.x == 0 && s.n > 0 && s.p0 + s.n > p.batch.max_len) flag_status(p.status, kStatusBadPage);
     }
     int64_t upto = mine;
 #pragma unroll
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     while (unit_lo < g1) {
         const int64_t unit_end = cur.begin + cur.r.tiles, unit_hi = min(unit_end, g1);
         const int rows = cur.s.n * p.group;
-        const int64_t token0 = __ldg(p.batch.new_start + cur.b);
+        const int64_t token0 = cur.s.token0;
         // query rows as the 8-column operand: lane holds rows lane / 4 (+ 8), elements by the layout of the keys
         uint32_t qf[D / 16][NB][2];
 #pragma unroll
@@ -327,6 +327,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                                (p.window == 0 || base > pb - p.window || base + TT <= p.sinks);
             const uint32_t kb = my_ring + stage * 2 * kFewHalf, vb = kb + kFewHalf;
             wait_phase(my_bars + 8 * stage, phase, p.status, &expired);
+            __syncwarp();
 #pragma unroll 2
             for (int st = 0; st < TT / 16; ++st) {
                 const int t0 = st * 16;

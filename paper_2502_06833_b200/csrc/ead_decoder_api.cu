@@ -9,7 +9,7 @@
 #include <cmath>
 #include <mutex>
 
-#include "attention_kernels.cuh"
+#include "attn_chunk_kernel.cuh"
 #include "attn_few_rows_kernel.cuh"
 #include "kv_cache_kernels.cuh"
 #include "rmsnorm_kernel.cuh"
@@ -28,6 +28,7 @@ namespace {
     } while (0)
 
 constexpr int kMaxDevices = 64;
+constexpr int kChunkMinCost = 8;          // tiles of 128 rows x 128 keys per block, likewise; at least 2
 constexpr int kFewMinTiles = 16;          // tiles of 8 KiB per block before another block is worth its part in the join
 
 struct DeviceInfo {
@@ -41,8 +42,8 @@ DeviceInfo g_dev[kMaxDevices];
 int launched() { return cudaGetLastError() == cudaSuccess ? EAD_OK : EAD_ECUDA; }
 
 // A pool as {128-byte (or 64-byte) line of a key, slot, line, head, page}; a box is `keys` consecutive slots of one
-// head of one page, line by line, with the swizzle that makes eight keys' chunks conflict-free.
-bool encode_pool(CUtensorMap *tm, const KvCacheView &c, int format, void *base, int keys)
+// head of one page, `lines` of its lines one after the other, with the swizzle that makes eight keys' chunks conflict-free.
+bool encode_pool(CUtensorMap *tm, const KvCacheView &c, int format, void *base, int keys, int lines)
 {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
@@ -55,7 +56,7 @@ bool encode_pool(CUtensorMap *tm, const KvCacheView &c, int format, void *base, 
                                    static_cast<cuuint64_t>(c.head_stride * size),
                                    static_cast<cuuint64_t>(c.page_stride * size)};
     const cuuint32_t box[5] = {static_cast<cuuint32_t>(line / size), static_cast<cuuint32_t>(keys),
-                               static_cast<cuuint32_t>(row / line), 1, 1};
+                               static_cast<cuuint32_t>(lines), 1, 1};
     const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     return fn(tm, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, base, dims, strides, box, ones,
               CU_TENSOR_MAP_INTERLEAVE_NONE, line == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
@@ -68,7 +69,8 @@ int launch_few_rows(const AttnParams &p, int sms, cudaStream_t s)
     using L = FewLayout<FMT, D, NB>;
     const int keys = std::min(p.cache.page_size, L::kTile);
     CUtensorMap tk, tv;
-    if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys)) return EAD_ECUDA;
+    if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys, L::kBoxes) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys, L::kBoxes))
+        return EAD_ECUDA;
     ead_attn_few_rows_kernel<FMT, D, NB><<<std::min(sms, kAttnMaxCtas), L::kThreads, L::kSmem, s>>>(tk, tv, p, __builtin_ctz(keys), kFewMinTiles);
     return launched();
 }
@@ -77,6 +79,17 @@ template <int FMT, int D>
 int launch_few_rows(const AttnParams &p, int sms, cudaStream_t s)
 {
     return p.few_rows <= 8 ? launch_few_rows<FMT, D, 1>(p, sms, s) : launch_few_rows<FMT, D, 2>(p, sms, s);
+}
+
+template <int FMT, int D>
+int launch_chunk(const AttnParams &p, int sms, cudaStream_t s)
+{
+    using L = ChunkLayout<FMT, D>;
+    const int keys = std::min(p.cache.page_size, kChunkKeys);
+    CUtensorMap tk, tv;
+    if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys, 1) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys, 1)) return EAD_ECUDA;
+    ead_attn_chunk_kernel<FMT, D><<<std::min(sms, kAttnMaxCtas), kChunkThreads, L::kSmem, s>>>(tk, tv, p, __builtin_ctz(keys), kChunkMinCost);
+    return launched();
 }
 
 template <int FMT, int D, int NB>
@@ -88,7 +101,9 @@ bool allow_smem()
 template <int FMT, int D>
 bool allow_smem()
 {
-    return allow_smem<FMT, D, 1>() && allow_smem<FMT, D, 2>();
+    return allow_smem<FMT, D, 1>() && allow_smem<FMT, D, 2>() &&
+           cudaFuncSetAttribute(ead_attn_chunk_kernel<FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                ChunkLayout<FMT, D>::kSmem) == cudaSuccess;
 }
 
 // Makes `device` current; on its first use checks the architecture and sets kernel attributes.
@@ -271,18 +286,17 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
     // a second group of 8 rows costs every unit, and the other kernel runs anyway.
     const int64_t most = static_cast<int64_t>(p.batch.max_new) * p.group;
     p.few_rows = p.group > kDecodeRows ? 0 : most <= 8 || (most > kDecodeRows && p.group <= 8) ? 8 : kDecodeRows;
+    if (most > 0x7fffffff) return EAD_EINVALID_ARG;
+    const bool bf16 = cache->format == EAD_FMT_BF16, wide = p.cache.head_dim == 128;
     if (p.few_rows) {
-        const bool bf16 = cache->format == EAD_FMT_BF16, wide = p.cache.head_dim == 128;
         rc = bf16 ? (wide ? launch_few_rows<kFmtBf16, 128>(p, d->sms, s) : launch_few_rows<kFmtBf16, 64>(p, d->sms, s))
                   : (wide ? launch_few_rows<kFmtE4m3, 128>(p, d->sms, s) : launch_few_rows<kFmtE4m3, 64>(p, d->sms, s));
-        if (rc != EAD_OK || most <= p.few_rows) return rc;
+        if (rc != EAD_OK) return rc;
     }
-    const dim3 grid((p.batch.n_tokens + 3) / 4, heads_q);
-    if (cache->format == EAD_FMT_BF16)
-        ead_kv_attention_simple_kernel<kFmtBf16><<<grid, 128, 0, s>>>(p);
-    else
-        ead_kv_attention_simple_kernel<kFmtE4m3><<<grid, 128, 0, s>>>(p);
-    return launched();
+    if (most > p.few_rows)
+        rc = bf16 ? (wide ? launch_chunk<kFmtBf16, 128>(p, d->sms, s) : launch_chunk<kFmtBf16, 64>(p, d->sms, s))
+                  : (wide ? launch_chunk<kFmtE4m3, 128>(p, d->sms, s) : launch_chunk<kFmtE4m3, 64>(p, d->sms, s));
+    return rc;
 }
 
 extern "C" int ead_add_rmsnorm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
