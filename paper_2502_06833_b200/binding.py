@@ -325,19 +325,40 @@ def ead_shard_gate(ctx, all_records, n_shards, tok=None, H=None, Hbar=None, mode
                                 _ptr(model_used), _ptr(next_model)), "ead_shard_gate")
 
 
-def _rows(t, dims: int, what: str) -> int:
-    """Elements between the rows (dimension 0) of a tensor whose other ``dims - 1`` dimensions are contiguous."""
-    if t.dim() != dims or (t.numel() and not t[0].is_contiguous()):
-        raise ValueError(f"{what}: want {dims} dimensions, contiguous within a row")
-    inner = 1
-    for n in t.shape[1:]:
-        inner *= n
-    return t.stride(0) if t.shape[0] > 1 else inner
+_torch = None
 
 
-def _want(t, dtype: str, what: str) -> None:
-    if str(t.dtype) not in dtype:
-        raise ValueError(f"{what}: {t.dtype}, want {dtype}")
+def _t():
+    """torch, on first use: the gate step's calls do not need it."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _rows3(t, shape, what: str) -> int:
+    """Checks a bf16 tensor ``[n, heads, dim]`` whose rows are contiguous; elements between rows."""
+    if t.dtype is not _t().bfloat16 or t.shape != shape:
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, want bfloat16 {tuple(shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (s1 != shape[2] and shape[1] != 1):
+        raise ValueError(f"{what}: want rows that are contiguous")
+    return s0 if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _rows2(t, shape, what: str, dtypes) -> int:
+    if t.dtype not in dtypes or t.shape != shape:
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, want {dtypes} {tuple(shape)}")
+    s0, s1 = t.stride()
+    if s1 != 1 and shape[1] != 1:
+        raise ValueError(f"{what}: want rows that are contiguous")
+    return s0 if shape[0] > 1 else shape[1]
+
+
+def _dense(t, shape, dtype, what: str) -> None:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, want contiguous {dtype} {tuple(shape)}")
 
 
 def ead_kv_cache(k, v, k_scale=None, v_scale=None) -> EadKvCache:
@@ -347,21 +368,23 @@ def ead_kv_cache(k, v, k_scale=None, v_scale=None) -> EadKvCache:
     ``torch.uint8``) with ``*_scale`` uint8 ``[n_pages, heads_kv, page_size, head_dim / 32]``.  The last
     dimension is contiguous, the others have any strides (a cache laid out token by token is a
     ``transpose(1, 2)`` of its tensor), the same for both."""
+    T = _t()
     e4m3 = k_scale is not None
     for t, name in ((k, "k"), (v, "v")):
-        _want(t, "torch.float8_e4m3fn torch.uint8" if e4m3 else "torch.bfloat16", name)
+        if t.dtype not in ((T.float8_e4m3fn, T.uint8) if e4m3 else (T.bfloat16,)):
+            raise ValueError(f"{name}: {t.dtype} does not fit a cache {'with' if e4m3 else 'without'} scales")
         if t.dim() != 4 or t.stride(3) != 1 or t.shape != k.shape or t.stride() != k.stride():
             raise ValueError(f"{name}: want [n_pages, heads_kv, page_size, head_dim], contiguous in the last "
                              "dimension, k and v alike")
     for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
         if (t is not None) != e4m3:
             raise ValueError("k_scale and v_scale come together")
-        if e4m3 and (str(t.dtype) != "torch.uint8" or not t.is_contiguous()
-                     or tuple(t.shape) != (*k.shape[:3], k.shape[3] // EAD_FMT_BLOCK)):
-            raise ValueError(f"{name}: want contiguous uint8 [n_pages, heads_kv, page_size, head_dim / 32]")
+        if e4m3:
+            _dense(t, (*k.shape[:3], k.shape[3] // EAD_FMT_BLOCK), T.uint8, name)
     c = EadKvCache(EAD_FMT_E4M3 if e4m3 else EAD_FMT_BF16, k.shape[1], k.shape[3], k.shape[2], k.shape[0], 0,
                    *k.stride()[:3], _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
     c.held = (k, v, k_scale, v_scale)
+    c.ref = C.byref(c)
     return c
 
 
@@ -369,51 +392,45 @@ def ead_kv_batch(page_table, new_start, kv_len=None, *, n_tokens, max_new, max_l
     """Describes one step's batch: device int32 tensors ``page_table`` ``[B, entries]``, ``new_start``
     ``[B + 1]``, ``kv_len`` ``[B]`` (borrowed; the description keeps them alive) and what the host knows
     of them.  ``kv_len`` may be omitted for reading."""
-    for t, name in ((page_table, "page_table"), (new_start, "new_start"), (kv_len, "kv_len")):
-        if t is not None:
-            _want(t, "torch.int32", name)
+    i32 = _t().int32
     B = page_table.shape[0]
-    if page_table.stride(1) != 1 or not new_start.is_contiguous() or new_start.numel() != B + 1:
-        raise ValueError("want page_table [B, entries] with contiguous rows and new_start [B + 1]")
-    if kv_len is not None and (not kv_len.is_contiguous() or kv_len.numel() != B):
-        raise ValueError("kv_len: want [B]")
+    if page_table.dtype is not i32 or page_table.dim() != 2 or page_table.stride(1) != 1:
+        raise ValueError("page_table: want int32 [B, entries] with contiguous rows")
+    _dense(new_start, (B + 1,), i32, "new_start")
+    if kv_len is not None:
+        _dense(kv_len, (B,), i32, "kv_len")
     c = EadKvBatch(B, int(n_tokens), int(max_new), int(max_len), _ptr(new_start), _ptr(kv_len), _ptr(page_table),
                    page_table.stride(0) if B > 1 else page_table.shape[1], 0)
     c.held = (page_table, new_start, kv_len)
+    c.ref = C.byref(c)
     return c
-
-
-def _shape(t, shape, what: str) -> None:
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, want {shape}")
 
 
 def ead_kv_write(cache: EadKvCache, batch: EadKvBatch, k_new, v_new, *, status=None, device=0, stream=0) -> None:
     """Writes the step's keys and values, bf16 ``[n_tokens, heads_kv, head_dim]``, into the cache."""
-    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-        _want(t, "torch.bfloat16", name)
-        _shape(t, (batch.n_tokens, cache.heads_kv, cache.head_dim), name)
-    stride = _rows(k_new, 3, "k_new")
-    if _rows(v_new, 3, "v_new") != stride:
+    shape = (batch.n_tokens, cache.heads_kv, cache.head_dim)
+    stride = _rows3(k_new, shape, "k_new")
+    if _rows3(v_new, shape, "v_new") != stride:
         raise ValueError("k_new and v_new: want the same row stride")
-    _check(lib().ead_kv_write(C.byref(cache), C.byref(batch), _ptr(k_new), _ptr(v_new), stride, _ptr(status),
-                              device, stream or None), "ead_kv_write")
+    rc = lib().ead_kv_write(cache.ref, batch.ref, k_new.data_ptr(), v_new.data_ptr(), stride, _ptr(status), device,
+                            stream)
+    if rc:
+        _check(rc, "ead_kv_write")
 
 
 def ead_kv_read(cache: EadKvCache, batch: EadKvBatch, k_out, v_out, *, first=None, status=None, device=0,
                 stream=0) -> None:
     """Reads tokens back as bf16 ``[n_tokens, heads_kv, head_dim]``; ``first``: int32 ``[B]``, first positions."""
-    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
-        _want(t, "torch.bfloat16", name)
-        _shape(t, (batch.n_tokens, cache.heads_kv, cache.head_dim), name)
-    if first is not None:
-        _want(first, "torch.int32", "first")
-        _shape(first, (batch.B,), "first")
-    stride = _rows(k_out, 3, "k_out")
-    if _rows(v_out, 3, "v_out") != stride:
+    shape = (batch.n_tokens, cache.heads_kv, cache.head_dim)
+    stride = _rows3(k_out, shape, "k_out")
+    if _rows3(v_out, shape, "v_out") != stride:
         raise ValueError("k_out and v_out: want the same row stride")
-    _check(lib().ead_kv_read(C.byref(cache), C.byref(batch), _ptr(first), _ptr(k_out), _ptr(v_out), stride,
-                             _ptr(status), device, stream or None), "ead_kv_read")
+    if first is not None:
+        _dense(first, (batch.B,), _t().int32, "first")
+    rc = lib().ead_kv_read(cache.ref, batch.ref, _ptr(first), k_out.data_ptr(), v_out.data_ptr(), stride,
+                           _ptr(status), device, stream)
+    if rc:
+        _check(rc, "ead_kv_read")
 
 
 def ead_kv_attention(cache: EadKvCache, batch: EadKvBatch, q, out, *, scale, workspace, window=0, sinks=0, lse=None,
@@ -421,47 +438,42 @@ def ead_kv_attention(cache: EadKvCache, batch: EadKvBatch, q, out, *, scale, wor
     """Attention of the step's new tokens over the paged cache; ``q`` and ``out`` are bf16
     ``[n_tokens, heads_q, head_dim]``, ``lse`` float ``[n_tokens, heads_q]``; ``workspace`` is a zero-filled
     buffer of ``EAD_KV_WORKSPACE_BYTES`` that calls which may overlap must not share."""
-    _want(q, "torch.bfloat16", "q")
-    _want(out, "torch.bfloat16", "out")
     heads_q = q.shape[1]
-    _shape(q, (batch.n_tokens, heads_q, cache.head_dim), "q")
-    _shape(out, (batch.n_tokens, heads_q, cache.head_dim), "out")
+    shape = (batch.n_tokens, heads_q, cache.head_dim)
+    q_stride, out_stride = _rows3(q, shape, "q"), _rows3(out, shape, "out")
     if lse is not None:
-        _want(lse, "torch.float32", "lse")
-        _shape(lse, (batch.n_tokens, heads_q), "lse")
-        if not lse.is_contiguous():
-            raise ValueError("lse: want a contiguous tensor")
-    if workspace.numel() * workspace.element_size() < EAD_KV_WORKSPACE_BYTES:
+        _dense(lse, shape[:2], _t().float32, "lse")
+    if workspace.nbytes < EAD_KV_WORKSPACE_BYTES:
         raise ValueError("workspace: want EAD_KV_WORKSPACE_BYTES bytes")
-    _check(lib().ead_kv_attention(C.byref(cache), C.byref(batch), _ptr(q), _rows(q, 3, "q"), heads_q, scale, window,
-                                  sinks, _ptr(out), _rows(out, 3, "out"), _ptr(lse), _ptr(workspace), _ptr(status),
-                                  device, stream or None), "ead_kv_attention")
+    rc = lib().ead_kv_attention(cache.ref, batch.ref, q.data_ptr(), q_stride, heads_q, scale, window, sinks,
+                                out.data_ptr(), out_stride, _ptr(lse), workspace.data_ptr(), _ptr(status), device,
+                                stream)
+    if rc:
+        _check(rc, "ead_kv_attention")
 
 
 def ead_add_rmsnorm(x, weight, out, *, residual=None, residual_out=None, out_scale=None, eps=1e-6, device=0,
                     stream=0) -> None:
     """``out = norm(x + residual) * weight`` over bf16 rows ``[n, H]``, ``residual_out = x + residual``; with
     ``out_scale`` (uint8 ``[n, H / 32]``) the output is 8-bit (``torch.float8_e4m3fn`` or ``torch.uint8``)."""
-    n, H = x.shape
-    _want(x, "torch.bfloat16", "x")
-    _want(weight, "torch.bfloat16", "weight")
-    _shape(weight, (H,), "weight")
-    _want(out, "torch.float8_e4m3fn torch.uint8" if out_scale is not None else "torch.bfloat16", "out")
-    _shape(out, (n, H), "out")
-    for t, name in ((residual, "residual"), (residual_out, "residual_out")):
-        if t is not None:
-            _want(t, "torch.bfloat16", name)
-            _shape(t, (n, H), name)
+    T = _t()
+    bf16 = (T.bfloat16,)
+    n, H = shape = x.shape
+    x_stride = _rows2(x, shape, "x", bf16)
+    _dense(weight, (H,), T.bfloat16, "weight")
+    out_stride = _rows2(out, shape, "out", bf16 if out_scale is None else (T.float8_e4m3fn, T.uint8))
+    r_stride = ro_stride = 0
+    if residual is not None:
+        r_stride = _rows2(residual, shape, "residual", bf16)
+    if residual_out is not None:
+        ro_stride = _rows2(residual_out, shape, "residual_out", bf16)
     if out_scale is not None:
-        _want(out_scale, "torch.uint8", "out_scale")
-        _shape(out_scale, (n, H // EAD_FMT_BLOCK), "out_scale")
-        if not out_scale.is_contiguous():
-            raise ValueError("out_scale: want a contiguous tensor")
-    _check(lib().ead_add_rmsnorm(_ptr(x), _rows(x, 2, "x"), _ptr(residual),
-                                 0 if residual is None else _rows(residual, 2, "residual"), _ptr(residual_out),
-                                 0 if residual_out is None else _rows(residual_out, 2, "residual_out"), _ptr(weight),
-                                 eps, n, H, EAD_FMT_BF16 if out_scale is None else EAD_FMT_E4M3, _ptr(out),
-                                 _rows(out, 2, "out"), _ptr(out_scale), device, stream or None), "ead_add_rmsnorm")
+        _dense(out_scale, (n, H // EAD_FMT_BLOCK), T.uint8, "out_scale")
+    rc = lib().ead_add_rmsnorm(x.data_ptr(), x_stride, _ptr(residual), r_stride, _ptr(residual_out), ro_stride,
+                               weight.data_ptr(), eps, n, H, EAD_FMT_BF16 if out_scale is None else EAD_FMT_E4M3,
+                               out.data_ptr(), out_stride, _ptr(out_scale), device, stream)
+    if rc:
+        _check(rc, "ead_add_rmsnorm")
 
 
 def ead_destroy(ctx) -> None:

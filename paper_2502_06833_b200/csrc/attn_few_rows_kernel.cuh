@@ -10,9 +10,13 @@
 // 8 would carry anything.  S^T = K Q^T has the layout that, transposed 8 x 8, is the second
 // operand of O^T = V^T P^T.
 //
-// 8-bit keys and values become bf16 in registers on their way from shared memory to the MMA: an e4m3 byte
-// placed 4 bits down in a bf16 is 2^-120 of its value, subnormals included, so one multiplication by
-// 2^(120 + k) is exact.
+// 8-bit keys and values are widened in registers on their way from shared memory to the MMA, and instructions, not
+// bytes, are what an 8-bit cache is short of, so the scales are applied where there is least to apply them to.
+// Keys: codes are exact in f16; the products of one scale block are summed apart and the four sums of a key are
+// scaled in 32 bits.  The query rows are f16 then, too: each row is first divided by a power of two that
+// brings its largest element to 1..2, so what an element loses is below 2^-25 of that.
+// Values: an e4m3 byte placed 4 bits down in a bf16 is 2^-120 of its value, subnormals included; the factor 2^(120 + k)
+// goes to the probabilities (an exact change of exponent), once per key and scale block instead of once per value.
 #pragma once
 #include "attn_common.cuh"
 
@@ -44,27 +48,45 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
     uint32_t r;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// Two of a register's four codes, chosen by `pick` (each goes to the high byte of a half), as bf16 times 2^-120.
-__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t codes, uint32_t pick)
+// Codes in bits 0-15 (16-31) as a pair of f16.
+__device__ __forceinline__ uint32_t codes_to_f16x2_lo(uint32_t codes)
 {
-    const uint32_t w = __byte_perm(codes, 0, pick);
-    return (w & 0x80008000u) | ((w >> 4) & 0x07F007F0u);
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(codes));
+    return r;
 }
-constexpr uint32_t kPick01 = 0x1404, kPick23 = 0x3424, kPick02 = 0x2404, kPick13 = 0x3414;
-
-// Factor of a scale byte for such a value, as bf16 bits: 2^(120 + byte - 127) up to the largest power of two a bf16
-// holds (byte 134, a scale of 2^7); what is above that is a second factor, which almost no cache needs.
-__device__ __forceinline__ uint32_t scale_factor(uint32_t byte) { return (min(byte, 134u) + 120u) << 7; }
-__device__ __forceinline__ uint32_t scale_rest(uint32_t byte)
+__device__ __forceinline__ uint32_t codes_to_f16x2_hi(uint32_t codes)
 {
-    return byte == 255u ? 0x7FC0u : (byte > 134u ? byte - 134u + 127u : 127u) << 7;
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(codes));
+    return r;
 }
+// Codes 0 and 2 (1 and 3) as a pair of bf16 times 2^-120.
+__device__ __forceinline__ uint32_t codes_to_bf16x2_even(uint32_t codes)
+{
+    return ((codes << 8) & 0x80008000u) | ((codes << 4) & 0x07F007F0u);
+}
+__device__ __forceinline__ uint32_t codes_to_bf16x2_odd(uint32_t codes)
+{
+    return (codes & 0x80008000u) | ((codes >> 4) & 0x07F007F0u);
+}
+// 2^(byte - 127) for byte `g` of a key's scale bytes (0 for byte 0, which the library never writes).
+__device__ __forceinline__ float key_scale(uint32_t bytes, int g)
+{
+    return __uint_as_float(__byte_perm(bytes, 0, 0x0444u | g << 12) >> 1);
+}
+constexpr uint32_t kValueScaleTop = 125;          // largest byte whose factor 2^(120 + k), times a probability of up to 2^8, is a bf16
 
 // The NG scale bytes of one key, as the low bytes of a register.
 template <int NG>
@@ -302,6 +324,34 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                 }
             }
         }
+        float row_scale[NB][2];                    // of this lane's rows' logits
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            row_scale[nb][0] = row_scale[nb][1] = p.scale_log2;
+            if (FMT == kFmtE4m3) {                 // the four lanes of a row bring it to f16
+                uint32_t top = 0;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        top = max(top, max(abs_bits(bf16_lo(qf[ks][nb][e])), abs_bits(bf16_hi(qf[ks][nb][e]))));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                // exponent of the largest element; a row of zeros or one that is not finite stays as it is
+                const int ex = top < 0x00800000u || top >= 0x7f800000u ? 127 : min(static_cast<int>(top >> 23), 253);
+                const float down = __uint_as_float(static_cast<uint32_t>(254 - ex) << 23);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const __half2 h = __floats2half2_rn(bf16_lo(qf[ks][nb][e]) * down, bf16_hi(qf[ks][nb][e]) * down);
+                        qf[ks][nb][e] = *reinterpret_cast<const uint32_t *>(&h);
+                    }
+                const float up = __uint_as_float(static_cast<uint32_t>(ex) << 23);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) row_scale[nb][e] = p.scale_log2 * __shfl_sync(0xffffffffu, up, (qc + e) * 4);
+            }
+        }
         int pos[NB][2];                            // positions of this lane's rows
         float m[NB][2], l[NB][2];
         float o[D / 16][NB][4];
@@ -346,7 +396,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[nb][e] = 0.f;
                 const int mi = lane >> 3, mr = lane & 7;       // matrix and row this lane addresses
-                uint32_t rest_any = 0;
+                bool far = false;                                // some value scale is too large for the probabilities to take it in
                 uint32_t ksc[2], vsc[4];
                 if (FMT == kFmtE4m3) {
                     constexpr int NG = D / kFmtBlock;           // scale bytes per key
@@ -357,10 +407,8 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                     for (int i = 0; i < 4; ++i) vsc[i] = lds_scales<NG>(sb + 128 + (t0 + qc + (i & 1) + 8 * (i >> 1)) * NG);
                     uint32_t over = 0;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) over |= __vcmpgtu4(ksc[i], 0x86868686u);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) over |= __vcmpgtu4(vsc[i], 0x86868686u);
-                    rest_any = __any_sync(0xffffffffu, over != 0);
+                    for (int i = 0; i < 4; ++i) over |= __vcmpgtu4(vsc[i], kValueScaleTop * 0x01010101u);
+                    far = __any_sync(0xffffffffu, over != 0);
                 }
                 if (FMT == kFmtBf16) {
 #pragma unroll
@@ -375,27 +423,22 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                     for (int kp = 0; kp < D / 32; ++kp) {       // one scale block: two steps of 16
                         uint32_t a[4];
                         ldsm4(a, chunk_at(kb, t0 + mr + (mi & 1) * 8, 2 * kp + (mi >> 1)));
-                        uint32_t f[2];
+                        float sb[NB][4];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t x = scale_factor((ksc[i] >> (8 * kp)) & 0xffu);
-                            f[i] = x | x << 16;
-                        }
+                        for (int nb = 0; nb < NB; ++nb) sb[nb][0] = sb[nb][1] = sb[nb][2] = sb[nb][3] = 0.f;
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {           // matrices 2u (keys 0-7) and 2u + 1 (keys 8-15)
-                            uint32_t a0 = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick01), f[0]);
-                            uint32_t a1 = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick01), f[1]);
-                            uint32_t a2 = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick23), f[0]);
-                            uint32_t a3 = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick23), f[1]);
-                            if (rest_any) {
-                                const uint32_t x0 = scale_rest((ksc[0] >> (8 * kp)) & 0xffu) * 0x10001u;
-                                const uint32_t x1 = scale_rest((ksc[1] >> (8 * kp)) & 0xffu) * 0x10001u;
-                                a0 = mul_bf16x2(a0, x0); a2 = mul_bf16x2(a2, x0);
-                                a1 = mul_bf16x2(a1, x1); a3 = mul_bf16x2(a3, x1);
-                            }
+                        for (int u = 0; u < 2; ++u)             // matrices 2u (keys 0-7) and 2u + 1 (keys 8-15)
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb)
-                                mma16816(s[nb], a0, a1, a2, a3, qf[2 * kp + u][nb][0], qf[2 * kp + u][nb][1]);
+                                mma16816_f16(sb[nb], codes_to_f16x2_lo(a[2 * u]), codes_to_f16x2_lo(a[2 * u + 1]), codes_to_f16x2_hi(a[2 * u]),
+                                             codes_to_f16x2_hi(a[2 * u + 1]), qf[2 * kp + u][nb][0], qf[2 * kp + u][nb][1]);
+                        const float f0 = key_scale(ksc[0], kp), f1 = key_scale(ksc[1], kp);
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) {
+                            s[nb][0] = fmaf(sb[nb][0], f0, s[nb][0]);
+                            s[nb][1] = fmaf(sb[nb][1], f0, s[nb][1]);
+                            s[nb][2] = fmaf(sb[nb][2], f1, s[nb][2]);
+                            s[nb][3] = fmaf(sb[nb][3], f1, s[nb][3]);
                         }
                     }
                 }
@@ -406,7 +449,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[nb][e] *= p.scale_log2;
+                        s[nb][e] *= row_scale[nb][e & 1];
                         if (!whole) {
                             const int j = j0 + 8 * (e >> 1);
                             if (!(j < cur.s.len && seen_by(pos[nb][e & 1], p.window, p.sinks, j))) s[nb][e] = -INFINITY;
@@ -468,35 +511,50 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                         for (int nb = 0; nb < NB; ++nb) mma16816(o[mt][nb], a[0], a[1], a[2], a[3], pf[nb][0], pf[nb][1]);
                     }
                 } else {
+                    // scale bytes 0 and 2 (1 and 3) of keys 2c, 2c + 1, then of keys 2c + 8, 2c + 9, one per half
+                    uint32_t pair[2][4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t e0 = vsc[2 * i] & 0x00ff00ffu, e1 = vsc[2 * i + 1] & 0x00ff00ffu;
+                        const uint32_t o0 = (vsc[2 * i] >> 8) & 0x00ff00ffu, o1 = (vsc[2 * i + 1] >> 8) & 0x00ff00ffu;
+                        pair[i][0] = __byte_perm(e0, e1, 0x5410);
+                        pair[i][1] = __byte_perm(o0, o1, 0x5410);
+                        pair[i][2] = __byte_perm(e0, e1, 0x7632);
+                        pair[i][3] = __byte_perm(o0, o1, 0x7632);
+                    }
+                    // the factors: 2^(120 + k), or 2^k where the values themselves are brought to size
+                    const uint32_t bias = far ? 0u : 0x3C003C00u;
 #pragma unroll
                     for (int mp = 0; mp < D / 32; ++mp) {
                         uint32_t a[4];
                         ldsm4_t(a, chunk_at(vb, t0 + mr + (mi & 1) * 8, 2 * mp + (mi >> 1)));
-                        uint32_t f[2];
+                        uint32_t w[NB][2];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            f[i] = scale_factor((vsc[2 * i] >> (8 * mp)) & 0xffu) | scale_factor((vsc[2 * i + 1] >> (8 * mp)) & 0xffu) << 16;
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t f = pair[i][mp] * 128u + bias;
+                            if (far) {             // byte 255 marks NaNs
+                                if ((f & 0xffffu) == 0x7f80u) f |= 0x40u;
+                                if ((f >> 16) == 0x7f80u) f |= 0x400000u;
+                            }
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) {
+                                w[nb][i] = mul_bf16x2(pf[nb][i], f);
+                                if (!whole) w[nb][i] &= keep[i];                // any code is finite so far: its factor decides
+                            }
+                        }
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             uint32_t v[4];
-                            v[0] = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick02), f[0]);
-                            v[1] = mul_bf16x2(codes_to_bf16x2(a[2 * u], kPick13), f[0]);
-                            v[2] = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick02), f[1]);
-                            v[3] = mul_bf16x2(codes_to_bf16x2(a[2 * u + 1], kPick13), f[1]);
-                            if (rest_any) {
+                            v[0] = codes_to_bf16x2_even(a[2 * u]);
+                            v[1] = codes_to_bf16x2_odd(a[2 * u]);
+                            v[2] = codes_to_bf16x2_even(a[2 * u + 1]);
+                            v[3] = codes_to_bf16x2_odd(a[2 * u + 1]);
+                            if (far) {
 #pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    const uint32_t x = scale_rest((vsc[2 * i] >> (8 * mp)) & 0xffu) | scale_rest((vsc[2 * i + 1] >> (8 * mp)) & 0xffu) << 16;
-                                    v[2 * i] = mul_bf16x2(v[2 * i], x);
-                                    v[2 * i + 1] = mul_bf16x2(v[2 * i + 1], x);
-                                }
-                            }
-                            if (!whole) {
-                                v[0] &= keep[0]; v[1] &= keep[0];
-                                v[2] &= keep[1]; v[3] &= keep[1];
+                                for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], 0x7B807B80u);       // 2^120
                             }
 #pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) mma16816(o[2 * mp + u][nb], v[0], v[1], v[2], v[3], pf[nb][0], pf[nb][1]);
+                            for (int nb = 0; nb < NB; ++nb) mma16816(o[2 * mp + u][nb], v[0], v[1], v[2], v[3], w[nb][0], w[nb][1]);
                         }
                     }
                 }

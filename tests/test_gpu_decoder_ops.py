@@ -196,6 +196,46 @@ def test_attention_e4m3_scales_over_their_whole_range(E, workspace):
         _check(_attend(E, ctx, q, workspace, 0.1), attention(ctx, q, 0.1, 0, 0))
 
 
+@pytest.mark.parametrize("new", [1, 2, 50])
+def test_attention_e4m3_small_codes_mixed_scales_and_large_queries(E, workspace, new):
+    """Blocks whose values but one are subnormal codes, neighbouring keys with scales 2^40 apart (also above
+    2^-2, where the probabilities cannot take them in), and query rows of very different size."""
+    def fill(name, b, x):
+        y = x.float()
+        if b == 0:
+            y = y * 2.0 ** -14
+            y[:, :, ::32] = 0.4
+        elif b == 1 and name == "v":
+            y = y * torch.where(torch.arange(len(y)) % 3 == 0, 2.0 ** -30, 2.0 ** 10)[:, None, None]
+        elif b == 2 and name == "v":
+            y = y * torch.where(torch.arange(len(y)) % 2 == 0, 2.0 ** 90, 1.0)[:, None, None]
+        elif b == 3 and name == "k":
+            y = y * torch.where(torch.arange(y.shape[2]) < 32, 2.0 ** -20, 2.0 ** -3)
+        return y.bfloat16()
+    ctx = Context([new] * 5, [333, 200, 77, 500, 140], 2, 128, 16, "e4m3", seed=14, fill=fill)
+    q = _q(ctx, 4)
+    q[4 * new:, :, 5] *= 2.0 ** 4                      # one element far above the rest of its row
+    q[4 * new:, :, 6:] *= 2.0 ** -20
+    _check(_attend(E, ctx, q, workspace, 0.02), attention(ctx, q, 0.02, 0, 0))
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_attention_nan_blocks_reach_only_their_sequence(E, workspace, new):
+    """A value block with an infinity is NaN for its 32 dimensions and its own sequence and head only."""
+    def fill(name, b, x):
+        if b == 1 and name == "v":
+            x[3, 1, 40] = float("inf")
+        return x
+    for fmt in ("e4m3",):
+        ctx = Context([new] * 3, [120, 130, 140], 2, 128, 16, fmt, seed=15, fill=fill)
+        q = _q(ctx, 4)
+        out, lse, st = _attend(E, ctx, q, workspace, 0.1)
+        assert st == 0 and torch.isfinite(lse).all()
+        nan = torch.zeros_like(out, dtype=torch.bool)
+        nan[new:2 * new, 4:, 32:64] = True
+        assert torch.equal(out.isnan(), nan)
+
+
 def test_attention_on_another_stream_and_in_a_graph(E, workspace):
     ctx = Context([1, 90], [900, 1000], 2, 128, 16, seed=11)
     q = _q(ctx, 4)
