@@ -160,6 +160,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
 {
     using L = FewLayout<FMT, D, NB>;
     constexpr int S = L::kStages, TT = L::kTile, R = L::kRows, kFewWarps = L::kWarps, kFewThreads = L::kThreads;
+    constexpr int NS = TT / 16, PER = 8 / NS;      // steps of 16 keys per tile, fragment loads per step
     const int box_keys = 1 << box_shift;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int64_t s_scan[kFewWarps];
@@ -378,51 +379,54 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             const uint32_t kb = my_ring + stage * 2 * kFewHalf, vb = kb + kFewHalf;
             wait_phase(my_bars + 8 * stage, phase, p.status, &expired);
             __syncwarp();
-#pragma unroll 2
-            for (int st = 0; st < TT / 16; ++st) {
-                const int t0 = st * 16;
-                // address of 8 keys x 16 bytes: row `key`, 16-byte chunk `ch` of the key
-                auto chunk_at = [&](uint32_t tile, int key, int ch) -> uint32_t {
-                    if (L::kLine == 128) {
-                        const int bx = L::kBoxes == 1 ? 0 : key >> box_shift, in = key & (box_keys - 1), hb = ch >> 3;
-                        const uint32_t row = L::kBoxes == 1 ? key * 128u : (((bx * L::kBoxes + hb) << box_shift) + in) * 128u;
-                        return tile + row + (((ch & 7) ^ (key & 7)) << 4);
-                    }
-                    return tile + key * 64u + ((ch ^ ((key >> 1) & 3)) << 4);
-                };
-                float s[NB][4];
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[nb][e] = 0.f;
-                const int mi = lane >> 3, mr = lane & 7;       // matrix and row this lane addresses
-                bool far = false;                                // some value scale is too large for the probabilities to take it in
-                uint32_t ksc[2], vsc[4];
-                if (FMT == kFmtE4m3) {
-                    constexpr int NG = D / kFmtBlock;           // scale bytes per key
-                    const uint32_t sb = my_scales + stage * kFewScaleBytes;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) ksc[i] = lds_scales<NG>(sb + (t0 + (lane >> 2) + 8 * i) * NG);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) vsc[i] = lds_scales<NG>(sb + 128 + (t0 + qc + (i & 1) + 8 * (i >> 1)) * NG);
-                    uint32_t over = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) over |= __vcmpgtu4(vsc[i], kValueScaleTop * 0x01010101u);
-                    far = __any_sync(0xffffffffu, over != 0);
+            // address of 8 keys x 16 bytes: row `key`, 16-byte chunk `ch` of the key
+            auto chunk_at = [&](uint32_t tile, int key, int ch) -> uint32_t {
+                if (L::kLine == 128) {
+                    const int bx = L::kBoxes == 1 ? 0 : key >> box_shift, in = key & (box_keys - 1), hb = ch >> 3;
+                    const uint32_t row = L::kBoxes == 1 ? key * 128u : (((bx * L::kBoxes + hb) << box_shift) + in) * 128u;
+                    return tile + row + (((ch & 7) ^ (key & 7)) << 4);
                 }
-                if (FMT == kFmtBf16) {
+                return tile + key * 64u + ((ch ^ ((key >> 1) & 3)) << 4);
+            };
+            // The tile is worked on as a whole, in steps of 16 keys side by side: eight fragment loads for the keys, all
+            // score products, eight loads for the values (their latency runs under the softmax), then the products with them.
+            const int mi = lane >> 3, mr = lane & 7;           // matrix and row this lane addresses
+            uint32_t frag[8][4];
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        uint32_t a[4];
-                        ldsm4(a, chunk_at(kb, t0 + mr + (mi & 1) * 8, 2 * ks + (mi >> 1)));
+            for (int x = 0; x < 8; ++x)
+                ldsm4(frag[x], chunk_at(kb, (x / PER) * 16 + mr + (mi & 1) * 8, 2 * (x % PER) + (mi >> 1)));
+            bool far = false;                                    // some value scale is too large for the probabilities to take it in
+            uint32_t ksc[NS][2], vsc[NS][4];
+            if (FMT == kFmtE4m3) {
+                constexpr int NG = D / kFmtBlock;               // scale bytes per key
+                const uint32_t sb = my_scales + stage * kFewScaleBytes;
+                uint32_t over = 0;
 #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) mma16816(s[nb], a[0], a[1], a[2], a[3], qf[ks][nb][0], qf[ks][nb][1]);
+                for (int st = 0; st < NS; ++st) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) ksc[st][i] = lds_scales<NG>(sb + (st * 16 + (lane >> 2) + 8 * i) * NG);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        vsc[st][i] = lds_scales<NG>(sb + 128 + (st * 16 + qc + (i & 1) + 8 * (i >> 1)) * NG);
+                        over |= __vcmpgtu4(vsc[st][i], kValueScaleTop * 0x01010101u);
                     }
-                } else {
+                }
+                far = __any_sync(0xffffffffu, over != 0);
+            }
+            float s[NS][NB][4];
 #pragma unroll
-                    for (int kp = 0; kp < D / 32; ++kp) {       // one scale block: two steps of 16
-                        uint32_t a[4];
-                        ldsm4(a, chunk_at(kb, t0 + mr + (mi & 1) * 8, 2 * kp + (mi >> 1)));
+            for (int st = 0; st < NS; ++st)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[st][nb][0] = s[st][nb][1] = s[st][nb][2] = s[st][nb][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int st = 0; st < NS; ++st) {
+                    const uint32_t(&a)[4] = frag[st * PER + j];
+                    if (FMT == kFmtBf16) {
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) mma16816(s[st][nb], a[0], a[1], a[2], a[3], qf[j][nb][0], qf[j][nb][1]);
+                    } else {                                    // one scale block: two steps of 16 dimensions
                         float sb[NB][4];
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) sb[nb][0] = sb[nb][1] = sb[nb][2] = sb[nb][3] = 0.f;
@@ -431,92 +435,107 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb)
                                 mma16816_f16(sb[nb], codes_to_f16x2_lo(a[2 * u]), codes_to_f16x2_lo(a[2 * u + 1]), codes_to_f16x2_hi(a[2 * u]),
-                                             codes_to_f16x2_hi(a[2 * u + 1]), qf[2 * kp + u][nb][0], qf[2 * kp + u][nb][1]);
-                        const float f0 = key_scale(ksc[0], kp), f1 = key_scale(ksc[1], kp);
+                                             codes_to_f16x2_hi(a[2 * u + 1]), qf[2 * j + u][nb][0], qf[2 * j + u][nb][1]);
+                        const float f0 = key_scale(ksc[st][0], j), f1 = key_scale(ksc[st][1], j);
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) {
-                            s[nb][0] = fmaf(sb[nb][0], f0, s[nb][0]);
-                            s[nb][1] = fmaf(sb[nb][1], f0, s[nb][1]);
-                            s[nb][2] = fmaf(sb[nb][2], f1, s[nb][2]);
-                            s[nb][3] = fmaf(sb[nb][3], f1, s[nb][3]);
+                            s[st][nb][0] = fmaf(sb[nb][0], f0, s[st][nb][0]);
+                            s[st][nb][1] = fmaf(sb[nb][1], f0, s[st][nb][1]);
+                            s[st][nb][2] = fmaf(sb[nb][2], f1, s[st][nb][2]);
+                            s[st][nb][3] = fmaf(sb[nb][3], f1, s[st][nb][3]);
                         }
                     }
                 }
-                // logits in units of log 2; what is not seen is -inf
-                const int j0 = base + t0 + (lane >> 2);
-                float top = -INFINITY;                          // largest excess over the reference
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int t0 = (x / PER) * 16, j = x % PER;
+                if (FMT == kFmtBf16)
+                    ldsm4_t(frag[x], chunk_at(vb, t0 + mr + (mi >> 1) * 8, 2 * j + (mi & 1)));
+                else
+                    ldsm4_t(frag[x], chunk_at(vb, t0 + mr + (mi & 1) * 8, 2 * j + (mi >> 1)));
+            }
+            // logits in units of log 2; what is not seen is -inf
+            bool above = false;                                 // some logit exceeds its row's reference by too much
+#pragma unroll
+            for (int st = 0; st < NS; ++st)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[nb][e] *= row_scale[nb][e & 1];
+                        float &z = s[st][nb][e];
+                        z *= row_scale[nb][e & 1];
                         if (!whole) {
-                            const int j = j0 + 8 * (e >> 1);
-                            if (!(j < cur.s.len && seen_by(pos[nb][e & 1], p.window, p.sinks, j))) s[nb][e] = -INFINITY;
+                            const int j = base + st * 16 + (lane >> 2) + 8 * (e >> 1);
+                            if (!(j < cur.s.len && seen_by(pos[nb][e & 1], p.window, p.sinks, j))) z = -INFINITY;
                         }
-                        if (s[nb][e] > m[nb][e & 1] + kLazyLog2) top = INFINITY;
+                        above |= z > m[nb][e & 1] + kLazyLog2;
                     }
-                if (__any_sync(0xffffffffu, top > 0.f)) {
+            if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
+                for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float x = fmaxf(s[nb][e], s[nb][e + 2]);
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                            x = fmaxf(x, m[nb][e]);
-                            const float f = x == -INFINITY ? 1.f : exp2_fast(m[nb][e] - x);
-                            m[nb][e] = x;
-                            l[nb][e] *= f;
+                    for (int e = 0; e < 2; ++e) {
+                        float x = m[nb][e];
 #pragma unroll
-                            for (int mt = 0; mt < D / 16; ++mt) {
-                                o[mt][nb][e] *= f;
-                                o[mt][nb][e + 2] *= f;
-                            }
+                        for (int st = 0; st < NS; ++st) x = fmaxf(x, fmaxf(s[st][nb][e], s[st][nb][e + 2]));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                        const float f = x == -INFINITY ? 1.f : exp2_fast(m[nb][e] - x);
+                        m[nb][e] = x;
+                        l[nb][e] *= f;
+#pragma unroll
+                        for (int mt = 0; mt < D / 16; ++mt) {
+                            o[mt][nb][e] *= f;
+                            o[mt][nb][e + 2] *= f;
                         }
-                }
-                uint32_t pf[NB][2];
+                    }
+            }
+            uint32_t pf[NS][NB][2];
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
+            for (int nb = 0; nb < NB; ++nb) {
+                const float mm[2] = {m[nb][0] == -INFINITY ? 0.f : m[nb][0], m[nb][1] == -INFINITY ? 0.f : m[nb][1]};
+#pragma unroll
+                for (int st = 0; st < NS; ++st) {
                     float x[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float mm = m[nb][e & 1] == -INFINITY ? 0.f : m[nb][e & 1];
-                        x[e] = exp2_fast(s[nb][e] - mm);
+                        x[e] = exp2_fast(s[st][nb][e] - mm[e & 1]);
                         l[nb][e & 1] += x[e];
                     }
-                    pf[nb][0] = transpose8x8(to_bf16x2(x[0], x[1]));
-                    pf[nb][1] = transpose8x8(to_bf16x2(x[2], x[3]));
+                    pf[st][nb][0] = transpose8x8(to_bf16x2(x[0], x[1]));
+                    pf[st][nb][1] = transpose8x8(to_bf16x2(x[2], x[3]));
                 }
+            }
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
                 // values no query sees may be anything, and were not even loaded: zeros, so that 0 * NaN cannot arise
                 uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
                 if (!whole) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int j = base + t0 + qc + 8 * i;
+                        const int j = base + st * 16 + qc + 8 * i;
                         keep[i] = (seen_by_any(cur.r, p.sinks, j) ? 0xffffu : 0u) | (seen_by_any(cur.r, p.sinks, j + 1) ? 0xffff0000u : 0u);
                     }
                 }
                 if (FMT == kFmtBf16) {
 #pragma unroll
                     for (int mt = 0; mt < D / 16; ++mt) {
-                        uint32_t a[4];
-                        ldsm4_t(a, chunk_at(vb, t0 + mr + (mi >> 1) * 8, 2 * mt + (mi & 1)));
+                        uint32_t(&a)[4] = frag[st * PER + mt];
                         if (!whole) {
                             a[0] &= keep[0]; a[1] &= keep[0];
                             a[2] &= keep[1]; a[3] &= keep[1];
                         }
 #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) mma16816(o[mt][nb], a[0], a[1], a[2], a[3], pf[nb][0], pf[nb][1]);
+                        for (int nb = 0; nb < NB; ++nb) mma16816(o[mt][nb], a[0], a[1], a[2], a[3], pf[st][nb][0], pf[st][nb][1]);
                     }
                 } else {
-                    // scale bytes 0 and 2 (1 and 3) of keys 2c, 2c + 1, then of keys 2c + 8, 2c + 9, one per half
+                    // scale bytes of keys 2c, 2c + 1, then of keys 2c + 8, 2c + 9, one per half, block by block
                     uint32_t pair[2][4];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const uint32_t e0 = vsc[2 * i] & 0x00ff00ffu, e1 = vsc[2 * i + 1] & 0x00ff00ffu;
-                        const uint32_t o0 = (vsc[2 * i] >> 8) & 0x00ff00ffu, o1 = (vsc[2 * i + 1] >> 8) & 0x00ff00ffu;
+                        const uint32_t e0 = vsc[st][2 * i] & 0x00ff00ffu, e1 = vsc[st][2 * i + 1] & 0x00ff00ffu;
+                        const uint32_t o0 = (vsc[st][2 * i] >> 8) & 0x00ff00ffu, o1 = (vsc[st][2 * i + 1] >> 8) & 0x00ff00ffu;
                         pair[i][0] = __byte_perm(e0, e1, 0x5410);
                         pair[i][1] = __byte_perm(o0, o1, 0x5410);
                         pair[i][2] = __byte_perm(e0, e1, 0x7632);
@@ -525,20 +544,19 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                     // the factors: 2^(120 + k), or 2^k where the values themselves are brought to size
                     const uint32_t bias = far ? 0u : 0x3C003C00u;
 #pragma unroll
-                    for (int mp = 0; mp < D / 32; ++mp) {
-                        uint32_t a[4];
-                        ldsm4_t(a, chunk_at(vb, t0 + mr + (mi & 1) * 8, 2 * mp + (mi >> 1)));
+                    for (int j = 0; j < D / 32; ++j) {
+                        const uint32_t(&a)[4] = frag[st * PER + j];
                         uint32_t w[NB][2];
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            uint32_t f = pair[i][mp] * 128u + bias;
+                            uint32_t f = pair[i][j] * 128u + bias;
                             if (far) {             // byte 255 marks NaNs
                                 if ((f & 0xffffu) == 0x7f80u) f |= 0x40u;
                                 if ((f >> 16) == 0x7f80u) f |= 0x400000u;
                             }
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb) {
-                                w[nb][i] = mul_bf16x2(pf[nb][i], f);
+                                w[nb][i] = mul_bf16x2(pf[st][nb][i], f);
                                 if (!whole) w[nb][i] &= keep[i];                // any code is finite so far: its factor decides
                             }
                         }
@@ -554,7 +572,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                                 for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], 0x7B807B80u);       // 2^120
                             }
 #pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) mma16816(o[2 * mp + u][nb], v[0], v[1], v[2], v[3], w[nb][0], w[nb][1]);
+                            for (int nb = 0; nb < NB; ++nb) mma16816(o[2 * j + u][nb], v[0], v[1], v[2], v[3], w[nb][0], w[nb][1]);
                         }
                     }
                 }
