@@ -2,9 +2,9 @@
 // decoding and very short chunks.
 //
 // Every key and value is read from HBM once and used for 8 or 16 rows only, so HBM bounds it; the
-// kernel is built to keep many bytes in flight and little else.  Seven or eight warps per SM work independently:
+// kernel is built to keep many bytes in flight and little else.  Eight warps per SM work independently:
 // each has its own ring of 8 KiB stages (4 KiB of keys, 4 KiB of values) filled by TMA boxes of
-// one page each and takes every seventh or eighth tile of the block's stretch, so no barrier stands between the loads of
+// one page each and takes every eighth tile of the block's stretch, so no barrier stands between the loads of
 // consecutive tiles or units.  Products are mma.sync with the keys (values) as the 16-row
 // operand and the packed query rows as the 8-column operand: a tensor-memory accumulator has 128 rows, of which
 // 8 would carry anything.  S^T = K Q^T has the layout that, transposed 8 x 8, is the second
@@ -104,7 +104,7 @@ __device__ __forceinline__ uint32_t lds_scales(uint32_t addr)
 // A warp's place in the string of tiles: unit, its keys, and where the unit lies.
 struct FewCursor {
     int b, h;                                     // sequence, cache head
-    int64_t begin;                                // the unit's first tile in the string
+    int begin;                                    // the unit's first tile, counted from the first of the block's stretch
     SeqInfo s;
     KeyRange r;
 };
@@ -116,7 +116,7 @@ __device__ __forceinline__ int few_tiles(const AttnParams &p, const SeqInfo &s, 
     return r->tiles;
 }
 // Moves on to the unit that holds tile g of the string (g is in this unit or a later one).
-__device__ __forceinline__ void few_seek(const AttnParams &p, int shift, int64_t g, FewCursor *c)
+__device__ __forceinline__ void few_seek(const AttnParams &p, int shift, int g, FewCursor *c)
 {
     while (g >= c->begin + c->r.tiles) {
         c->begin += c->r.tiles;
@@ -142,11 +142,11 @@ struct FewLayout {
     static constexpr int kLine = kRowBytes < 128 ? kRowBytes : 128;         // bytes of a key in one box
     static constexpr int kBoxes = kRowBytes / kLine;                        // boxes per key row (2 for 256-byte keys)
     static constexpr int kRows = 8 * NB;
-    static constexpr int kWarps = FMT == kFmtE4m3 && D == 128 && NB == 1 ? 7 : 8;   // what shared memory has room for
+    static constexpr int kWarps = 8;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kMergeRow = D + 4;                                 // floats; the padding spreads the rows over the banks
     static constexpr int kMergeWarp = kRows * kMergeRow + 2 * kRows;
-    static constexpr int kMergeBytes = kWarps * kMergeWarp * 4;
+    static constexpr int kMergeBytes = kWarps / 2 * kMergeWarp * 4;
     static constexpr int kStages = NB == 1 ? 3 : 2;
     static constexpr int kRing = kWarps * kStages * 2 * kFewHalf;
     static constexpr int kScales = FMT == kFmtE4m3 ? kWarps * kStages * kFewScaleBytes : 0;
@@ -167,6 +167,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     __shared__ int s_b;
     __shared__ int64_t s_before;
     __shared__ int s_last;
+    __shared__ float s_ml[NB * 4 * 4 * 32];        // maxima and sums of warps 4-7, lane by lane
     const uint32_t raw = smem_u32(smem_raw), ring0 = (raw + 1023u) & ~1023u;
     uint8_t *const ring_ptr = smem_raw + (ring0 - raw);
     uint8_t *const scales_ptr = ring_ptr + L::kRing;
@@ -227,20 +228,21 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     cur.s = seq_info(p.batch, cur.b);
     cur.r.tiles = few_tiles(p, cur.s, L::kShift, &cur.r);
     cur.h = static_cast<int>((g0 - s_before) / cur.r.tiles);
-    cur.begin = s_before + static_cast<int64_t>(cur.h) * cur.r.tiles;
+    cur.begin = static_cast<int>(s_before + static_cast<int64_t>(cur.h) * cur.r.tiles - g0);
+    const int n_tiles = static_cast<int>(g1 - g0);  // from here on tiles are counted from g0
 
-    // ---- loads: this warp's tiles are g0 + warp, g0 + warp + 8, ...
+    // ---- loads: this warp's tiles are warp, warp + 8, ...
     const uint32_t my_ring = ring0 + warp * S * 2 * kFewHalf;
     const uint32_t my_scales = smem_u32(scales_ptr) + warp * S * kFewScaleBytes;
     const uint32_t my_bars = bars + warp * S * 8;
     FewCursor ahead = cur;
-    int64_t g_ahead = g0 + warp;
+    int g_ahead = warp;
     int page = -1, key0 = 0;                       // of this lane's box of the tile that is loaded next
     const int boxes = TT >> box_shift;              // at most 8
     auto look_up = [&]() {                         // one tile early, so that the load is there when the tile is issued
-        if (g_ahead >= g1) return;
+        if (g_ahead >= n_tiles) return;
         few_seek(p, L::kShift, g_ahead, &ahead);
-        key0 = ahead.r.base(static_cast<int>(g_ahead - ahead.begin), L::kShift) + lane * box_keys;
+        key0 = ahead.r.base(g_ahead - ahead.begin, L::kShift) + lane * box_keys;
         page = -2;                                 // nothing of it is seen: not loaded
         const bool any = key0 < ahead.r.hi && (key0 + box_keys > ahead.r.lo || key0 < p.sinks);
         if (lane < boxes && any) {
@@ -252,7 +254,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         }
     };
     auto issue = [&](int stage) {
-        if (g_ahead >= g1) return;
+        if (g_ahead >= n_tiles) return;
         const unsigned live = __ballot_sync(0xffffffffu, lane < boxes && page >= 0);
         const uint32_t bar = my_bars + 8 * stage, dst = my_ring + stage * 2 * kFewHalf;
         const uint32_t box_bytes = box_keys * L::kRowBytes;
@@ -294,13 +296,27 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
 
     // ---- tiles, unit by unit
     const int qc = (lane & 3) * 2;                 // this lane's packed rows: qc, qc + 1 (and 8 more)
+    // Where this lane's row of an 8 x 16-byte matrix lies within a tile, for the first four fragment loads of a step;
+    // later ones are a line (256-byte keys), later steps 16 keys further on.
+    const int mi = lane >> 3, mr = lane & 7;       // matrix and row this lane addresses
+    const uint32_t line_step = L::kBoxes == 2 ? box_keys * 128u : 0u;
+    auto chunk_at = [&](int key, int ch) -> uint32_t {
+        if (L::kLine == 64) return key * 64u + ((ch ^ ((key >> 1) & 3)) << 4);
+        const uint32_t row = L::kBoxes == 2 ? (key >> box_shift) * 2u * box_keys + (key & (box_keys - 1)) : key;
+        return row * 128u + ((ch ^ (key & 7)) << 4);
+    };
+    uint32_t off_k[4], off_v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        off_k[j] = chunk_at(mr + (mi & 1) * 8, 2 * j + (mi >> 1));
+        off_v[j] = FMT == kFmtBf16 ? chunk_at(mr + (mi >> 1) * 8, 2 * j + (mi & 1)) : off_k[j];
+    }
     int stage = 0;
     uint32_t phase = 0;
-    int64_t g = g0 + warp;
-    int64_t unit_lo = g0;
+    int g = warp, unit_lo = 0;
     bool first_unit = true, expired = false;
-    while (unit_lo < g1) {
-        const int64_t unit_end = cur.begin + cur.r.tiles, unit_hi = min(unit_end, g1);
+    while (unit_lo < n_tiles) {
+        const int unit_end = cur.begin + cur.r.tiles, unit_hi = min(unit_end, n_tiles);
         const int rows = cur.s.n * p.group;
         const int64_t token0 = cur.s.token0;
         // query rows as the 8-column operand: lane holds rows lane / 4 (+ 8), elements by the layout of the keys
@@ -373,28 +389,18 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         const int pb = cur.s.p0 + cur.s.n - 1;
 
         for (; g < unit_hi; g += kFewWarps) {
-            const int base = cur.r.base(static_cast<int>(g - cur.begin), L::kShift);
+            const int base = cur.r.base(g - cur.begin, L::kShift);
             const bool whole = base + TT - 1 <= cur.s.p0 && base + TT <= cur.s.len &&
                                (p.window == 0 || base > pb - p.window || base + TT <= p.sinks);
             const uint32_t kb = my_ring + stage * 2 * kFewHalf, vb = kb + kFewHalf;
             wait_phase(my_bars + 8 * stage, phase, p.status, &expired);
             __syncwarp();
-            // address of 8 keys x 16 bytes: row `key`, 16-byte chunk `ch` of the key
-            auto chunk_at = [&](uint32_t tile, int key, int ch) -> uint32_t {
-                if (L::kLine == 128) {
-                    const int bx = L::kBoxes == 1 ? 0 : key >> box_shift, in = key & (box_keys - 1), hb = ch >> 3;
-                    const uint32_t row = L::kBoxes == 1 ? key * 128u : (((bx * L::kBoxes + hb) << box_shift) + in) * 128u;
-                    return tile + row + (((ch & 7) ^ (key & 7)) << 4);
-                }
-                return tile + key * 64u + ((ch ^ ((key >> 1) & 3)) << 4);
-            };
             // The tile is worked on as a whole, in steps of 16 keys side by side: eight fragment loads for the keys, all
             // score products, eight loads for the values (their latency runs under the softmax), then the products with them.
-            const int mi = lane >> 3, mr = lane & 7;           // matrix and row this lane addresses
             uint32_t frag[8][4];
 #pragma unroll
             for (int x = 0; x < 8; ++x)
-                ldsm4(frag[x], chunk_at(kb, (x / PER) * 16 + mr + (mi & 1) * 8, 2 * (x % PER) + (mi >> 1)));
+                ldsm4(frag[x], kb + off_k[x % PER & 3] + (x / PER) * 16 * L::kRowBytes + (x % PER >> 2) * line_step);
             bool far = false;                                    // some value scale is too large for the probabilities to take it in
             uint32_t ksc[NS][2], vsc[NS][4];
             if (FMT == kFmtE4m3) {
@@ -408,10 +414,10 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         vsc[st][i] = lds_scales<NG>(sb + 128 + (st * 16 + qc + (i & 1) + 8 * (i >> 1)) * NG);
-                        over |= __vcmpgtu4(vsc[st][i], kValueScaleTop * 0x01010101u);
+                        over |= vsc[st][i] | (vsc[st][i] + (127u - kValueScaleTop) * 0x01010101u);   // bit 7 of a byte above 125
                     }
                 }
-                far = __any_sync(0xffffffffu, over != 0);
+                far = __any_sync(0xffffffffu, (over & 0x80808080u) != 0);
             }
             float s[NS][NB][4];
 #pragma unroll
@@ -448,11 +454,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                 }
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                const int t0 = (x / PER) * 16, j = x % PER;
-                if (FMT == kFmtBf16)
-                    ldsm4_t(frag[x], chunk_at(vb, t0 + mr + (mi >> 1) * 8, 2 * j + (mi & 1)));
-                else
-                    ldsm4_t(frag[x], chunk_at(vb, t0 + mr + (mi & 1) * 8, 2 * j + (mi >> 1)));
+                ldsm4_t(frag[x], vb + off_v[x % PER & 3] + (x / PER) * 16 * L::kRowBytes + (x % PER >> 2) * line_step);
             }
             // logits in units of log 2; what is not seen is -inf
             bool above = false;                                 // some logit exceeds its row's reference by too much
@@ -586,27 +588,69 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             }
         }
 
-        // ---- the warps' parts of the unit come together
-        float *mw = merge + warp * L::kMergeWarp;
+        // ---- the warps' parts of the unit come together: warps 4-7 hand theirs to 0-3 lane by lane, those lay them out by rows
+        constexpr int kHalf = kFewWarps / 2;
+        if (warp >= kHalf) {
+            float *mw = merge + (warp - kHalf) * L::kMergeWarp + lane;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], x);
-                const int row = nb * 8 + qc + e;
+            for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
                 for (int mt = 0; mt < D / 16; ++mt)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int d = 16 * mt + (FMT == kFmtBf16 ? (lane >> 2) + 8 * u : 2 * (lane >> 2) + u);
-                        mw[row * L::kMergeRow + d] = o[mt][nb][e + 2 * u];
-                    }
-                if (lane < 4) {
-                    mw[R * L::kMergeRow + row] = m[nb][e];
-                    mw[R * L::kMergeRow + R + row] = l[nb][e];
-                }
+                    for (int e = 0; e < 4; ++e) mw[((mt * NB + nb) * 4 + e) * 32] = o[mt][nb][e];
             }
+            float *ml = s_ml + (warp - kHalf) * NB * 4 * 32 + lane;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    ml[(nb * 4 + e) * 32] = m[nb][e];
+                    ml[(nb * 4 + 2 + e) * 32] = l[nb][e];
+                }
+        }
+        __syncthreads();
+        if (warp < kHalf) {
+            const float *src = merge + warp * L::kMergeWarp + lane, *ml = s_ml + warp * NB * 4 * 32 + lane;
+            float f[NB][2], f2[NB][2];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float m2 = ml[(nb * 4 + e) * 32], l2 = ml[(nb * 4 + 2 + e) * 32], M = fmaxf(m[nb][e], m2);
+                    f[nb][e] = m[nb][e] == -INFINITY ? 0.f : exp2_fast(m[nb][e] - M);
+                    f2[nb][e] = m2 == -INFINITY ? 0.f : exp2_fast(m2 - M);
+                    l[nb][e] = l[nb][e] * f[nb][e] + l2 * f2[nb][e];
+                    m[nb][e] = M;
+                }
+#pragma unroll
+            for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[mt][nb][e] = o[mt][nb][e] * f[nb][e & 1] + src[((mt * NB + nb) * 4 + e) * 32] * f2[nb][e & 1];
+            __syncwarp();
+            float *mw = merge + warp * L::kMergeWarp;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], x);
+                    const int row = nb * 8 + qc + e;
+#pragma unroll
+                    for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int d = 16 * mt + (FMT == kFmtBf16 ? (lane >> 2) + 8 * u : 2 * (lane >> 2) + u);
+                            mw[row * L::kMergeRow + d] = o[mt][nb][e + 2 * u];
+                        }
+                    if (lane < 4) {
+                        mw[R * L::kMergeRow + row] = m[nb][e];
+                        mw[R * L::kMergeRow + R + row] = l[nb][e];
+                    }
+                }
+        }
         __syncthreads();
         const bool begins = unit_lo == cur.begin, ends = unit_hi == unit_end;
         float *const parts = reinterpret_cast<float *>(p.workspace + kDecodePartOffset);
@@ -625,10 +669,10 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             const int row = x / kQuads, dq = x - row * kQuads;
             float M = -INFINITY, Lsum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) M = fmaxf(M, merge[w * L::kMergeWarp + R * L::kMergeRow + row]);
+            for (int w = 0; w < kHalf; ++w) M = fmaxf(M, merge[w * L::kMergeWarp + R * L::kMergeRow + row]);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) {
+            for (int w = 0; w < kHalf; ++w) {
                 const float *src = merge + w * L::kMergeWarp;
                 const float mm = src[R * L::kMergeRow + row];
                 const float f = mm == -INFINITY ? 0.f : exp2_fast(mm - M);
@@ -648,7 +692,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         }
         if (!(begins && ends)) {
             // blocks that hold a part of the unit: first .. last; the counter is the first one's
-            const int first = static_cast<int>(((cur.begin + 1) * ctas - 1) / W), last = static_cast<int>((unit_end * ctas - 1) / W);
+            const int first = static_cast<int>(((g0 + cur.begin + 1) * ctas - 1) / W), last = static_cast<int>(((g0 + unit_end) * ctas - 1) / W);
             fence_gpu();
             __syncthreads();
             if (tid == 0) {
@@ -659,7 +703,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             __syncthreads();
             if (s_last) {
                 fence_gpu();
-                const int first_slot = cur.begin == W * first / ctas ? 0 : 1;
+                const int first_slot = g0 + cur.begin == W * first / ctas ? 0 : 1;
                 for (int x = tid; x < rows * kQuads; x += kFewThreads) {
                     const int row = x / kQuads, dq = x - row * kQuads;
                     float M = -INFINITY, Lsum = 0.f;
@@ -682,7 +726,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         __syncthreads();                           // the merge buffer is free again
         unit_lo = unit_hi;
         first_unit = false;
-        if (unit_lo < g1) few_seek(p, L::kShift, unit_lo, &cur);
+        if (unit_lo < n_tiles) few_seek(p, L::kShift, unit_lo, &cur);
     }
 }
 
