@@ -142,14 +142,20 @@ struct FewLayout {
     static constexpr int kLine = kRowBytes < 128 ? kRowBytes : 128;         // bytes of a key in one box
     static constexpr int kBoxes = kRowBytes / kLine;                        // boxes per key row (2 for 256-byte keys)
     static constexpr int kRows = 8 * NB;
-    static constexpr int kWarps = 8;
+    // An 8-bit cache is bound by instructions, not bytes: three warps per scheduler, a tile's steps one after the other.
+    // Otherwise two warps per scheduler and a tile's steps side by side.
+    static constexpr bool kManyWarps = FMT == kFmtE4m3 && NB == 1;
+    static constexpr int kWarps = kManyWarps ? 12 : 8;
+    static constexpr int kSide = kManyWarps ? 1 : kTile / 16;               // steps of 16 keys worked on at once
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kMergeRow = D + 4;                                 // floats; the padding spreads the rows over the banks
-    static constexpr int kMergeWarp = kRows * kMergeRow + 2 * kRows;
+    static constexpr int kByRows = kRows * kMergeRow + 2 * kRows, kByLanes = kRows * D + NB * 128;   // output, maxima and sums
+    static constexpr int kMergeWarp = kByRows > kByLanes ? kByRows : kByLanes;
     static constexpr int kMergeBytes = kWarps / 2 * kMergeWarp * 4;
-    static constexpr int kStages = NB == 1 ? 3 : 2;
+    static constexpr int kStages = NB == 1 && !kManyWarps ? 3 : 2;
     static constexpr int kRing = kWarps * kStages * 2 * kFewHalf;
     static constexpr int kScales = FMT == kFmtE4m3 ? kWarps * kStages * kFewScaleBytes : 0;
+    static_assert(kMergeWarp % 4 == 0, "rows are read 16 bytes at a time");
     static constexpr int kSmem = 1024 + kRing + kScales + kMergeBytes + kWarps * kStages * 8;
 };
 
@@ -160,14 +166,13 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
 {
     using L = FewLayout<FMT, D, NB>;
     constexpr int S = L::kStages, TT = L::kTile, R = L::kRows, kFewWarps = L::kWarps, kFewThreads = L::kThreads;
-    constexpr int NS = TT / 16, PER = 8 / NS;      // steps of 16 keys per tile, fragment loads per step
+    constexpr int NS = L::kSide, PER = 8 / (TT / 16);   // steps of 16 keys at once, fragment loads per step
     const int box_keys = 1 << box_shift;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int64_t s_scan[kFewWarps];
     __shared__ int s_b;
     __shared__ int64_t s_before;
     __shared__ int s_last;
-    __shared__ float s_ml[NB * 4 * 4 * 32];        // maxima and sums of warps 4-7, lane by lane
     const uint32_t raw = smem_u32(smem_raw), ring0 = (raw + 1023u) & ~1023u;
     uint8_t *const ring_ptr = smem_raw + (ring0 - raw);
     uint8_t *const scales_ptr = ring_ptr + L::kRing;
@@ -392,20 +397,22 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             const int base = cur.r.base(g - cur.begin, L::kShift);
             const bool whole = base + TT - 1 <= cur.s.p0 && base + TT <= cur.s.len &&
                                (p.window == 0 || base > pb - p.window || base + TT <= p.sinks);
-            const uint32_t kb = my_ring + stage * 2 * kFewHalf, vb = kb + kFewHalf;
+            uint32_t kb = my_ring + stage * 2 * kFewHalf, vb = kb + kFewHalf;
             wait_phase(my_bars + 8 * stage, phase, p.status, &expired);
             __syncwarp();
-            // The tile is worked on as a whole, in steps of 16 keys side by side: eight fragment loads for the keys, all
-            // score products, eight loads for the values (their latency runs under the softmax), then the products with them.
-            uint32_t frag[8][4];
+            // Steps of 16 keys, NS of them side by side: the fragment loads for the keys, all score products, the loads
+            // for the values (their latency runs under the softmax), then the products with them.
+#pragma unroll 1
+            for (int t0 = 0; t0 < TT; t0 += 16 * NS, kb += 16 * NS * L::kRowBytes, vb += 16 * NS * L::kRowBytes) {
+            uint32_t frag[NS * PER][4];
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
+            for (int x = 0; x < NS * PER; ++x)
                 ldsm4(frag[x], kb + off_k[x % PER & 3] + (x / PER) * 16 * L::kRowBytes + (x % PER >> 2) * line_step);
             bool far = false;                                    // some value scale is too large for the probabilities to take it in
             uint32_t ksc[NS][2], vsc[NS][4];
             if (FMT == kFmtE4m3) {
                 constexpr int NG = D / kFmtBlock;               // scale bytes per key
-                const uint32_t sb = my_scales + stage * kFewScaleBytes;
+                const uint32_t sb = my_scales + stage * kFewScaleBytes + t0 * NG;
                 uint32_t over = 0;
 #pragma unroll
                 for (int st = 0; st < NS; ++st) {
@@ -453,7 +460,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                     }
                 }
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
+            for (int x = 0; x < NS * PER; ++x) {
                 ldsm4_t(frag[x], vb + off_v[x % PER & 3] + (x / PER) * 16 * L::kRowBytes + (x % PER >> 2) * line_step);
             }
             // logits in units of log 2; what is not seen is -inf
@@ -467,7 +474,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                         float &z = s[st][nb][e];
                         z *= row_scale[nb][e & 1];
                         if (!whole) {
-                            const int j = base + st * 16 + (lane >> 2) + 8 * (e >> 1);
+                            const int j = base + t0 + st * 16 + (lane >> 2) + 8 * (e >> 1);
                             if (!(j < cur.s.len && seen_by(pos[nb][e & 1], p.window, p.sinks, j))) z = -INFINITY;
                         }
                         above |= z > m[nb][e & 1] + kLazyLog2;
@@ -516,7 +523,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                 if (!whole) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int j = base + st * 16 + qc + 8 * i;
+                        const int j = base + t0 + st * 16 + qc + 8 * i;
                         keep[i] = (seen_by_any(cur.r, p.sinks, j) ? 0xffffu : 0u) | (seen_by_any(cur.r, p.sinks, j + 1) ? 0xffff0000u : 0u);
                     }
                 }
@@ -579,6 +586,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                     }
                 }
             }
+            }
             __syncwarp();                          // every lane has read the stage before it is filled again
             issue(stage);
             look_up();
@@ -599,7 +607,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) mw[((mt * NB + nb) * 4 + e) * 32] = o[mt][nb][e];
             }
-            float *ml = s_ml + (warp - kHalf) * NB * 4 * 32 + lane;
+            float *ml = mw + R * D;                // behind the fragments
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -610,7 +618,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         }
         __syncthreads();
         if (warp < kHalf) {
-            const float *src = merge + warp * L::kMergeWarp + lane, *ml = s_ml + warp * NB * 4 * 32 + lane;
+            const float *src = merge + warp * L::kMergeWarp + lane, *ml = src + R * D;
             float f[NB][2], f2[NB][2];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
