@@ -1,24 +1,28 @@
 // Attention for units of many packed rows (chunks of new tokens): tcgen05 MMAs with TMEM accumulators.
 //
 // A unit is up to 256 packed rows (new tokens x query heads of one cache head; consecutive rows are the heads of
-// a token), two tiles of 128 rows that share every key tile of 128 keys.  Per key tile and row tile: S = Q K^T (TMEM),
-// one thread per row turns S into probabilities P, which overwrite S as bf16 in TMEM, O += P V (TMEM).  While the tensor core
-// works on one row tile, the other's softmax runs; the two take turns.  A unit of at most 128 rows
+// a token), two tiles of 128 rows that share every key tile of 64 keys.  Per key tile and row tile: S = Q K^T (TMEM),
+// one thread per row turns S into probabilities P, which overwrite S as bf16 in TMEM, O += P V (TMEM).  Every row tile has two
+// S buffers, so the scores of the next key tile are there when the softmax of this one ends: tensor core and softmax do not
+// wait for each other's round trip.  (With 128-key tiles TMEM has room for one S per row tile: 5860 cycles per 256 x 128
+// scores instead of the ~2560 that the operands' reads from shared memory take.)  A unit of at most 128 rows
 // gives both turns to the same rows instead: even key tiles go to the first accumulator, odd ones
 // to the second, and the two are joined at the end.
 //
 // Warps: 0-3 softmax and output of the first row tile, 4-7 of the second, 8 issues the MMAs, 9 loads key and value
-// tiles (TMA), 10-13 load the query rows and, for an 8-bit cache, turn codes into bf16 on their way into the MMA's
-// operand tiles (as in the few-rows kernel).
+// tiles (TMA), 12-15 load the query rows and, for an 8-bit cache, turn codes into bf16 on their way into the MMA's
+// operand tiles (as in the few-rows kernel).  10 and 11 complete the warpgroup: registers are dealt out by warpgroups, most
+// of them to the softmax, which keeps a row of 128 scores in them.
 #pragma once
 #include "attn_common.cuh"
 
 namespace ead {
 
-constexpr int kChunkThreads = 14 * 32;
-constexpr int kChunkMmaWarp = 8, kChunkLoadWarp = 9, kChunkFeedWarp = 10;
-constexpr int kChunkKeys = 128;                   // keys per tile
-constexpr int kChunkShift = 7;
+constexpr int kChunkWarps = 16;
+constexpr int kChunkThreads = 32 * kChunkWarps;
+constexpr int kChunkMmaWarp = 8, kChunkLoadWarp = 9, kChunkFeedWarp = 12;
+constexpr int kChunkKeys = 64;                    // keys per tile
+constexpr int kChunkShift = 6;
 constexpr int kChunkRows = 256;                   // packed rows per unit
 constexpr size_t kChunkPartOffset = 4u << 20;     // the few-rows kernel's parts end below this
 
@@ -32,14 +36,19 @@ __device__ __forceinline__ uint32_t chunk_codes(uint32_t codes, uint32_t pick)
 template <int FMT, int D>
 struct ChunkLayout {
     static constexpr int kHalves = D / 64;                               // 128-byte lines per bf16 row
-    static constexpr int kTileBytes = kChunkKeys * D * 2;                // a bf16 tile of keys, values or query rows
-    static constexpr int kQ = 2 * kTileBytes;
-    static constexpr int kStages = FMT == kFmtBf16 ? (D == 128 ? 5 : 8) : (D == 128 ? 4 : 8);
+    static constexpr int kTileBytes = kChunkKeys * D * 2;                // a bf16 tile of keys or values
+    static constexpr int kLine = kChunkKeys * 128;                       // ... of 64 dimensions of them
+    static constexpr int kQTile = 128 * D * 2;                           // a tile of query rows
+    static constexpr int kStages = D == 64 ? 16 : FMT == kFmtBf16 ? 10 : 8;   // at least 8: see the order of the MMAs
     static constexpr int kRawTile = FMT == kFmtE4m3 ? kChunkKeys * D : 0;
     static constexpr int kRawScale = FMT == kFmtE4m3 ? kChunkKeys * (D / kFmtBlock) : 0;
-    static constexpr int kRawStages = FMT == kFmtE4m3 ? 2 : 0;
-    static constexpr int kBars = 2 * kStages + 2 * 2 + 8;
-    static constexpr int kSmem = 1024 + kQ + kStages * kTileBytes + kRawStages * (kRawTile + kRawScale) + 8 * kBars;
+    static constexpr int kRaw = 4;                                       // stages of codes
+    static constexpr int kRawBytes = kRaw * (kRawTile + kRawScale);
+    static constexpr int kBars = 2 * kStages + 2 * kRaw + 14;
+    static constexpr int kSmem = 1024 + 2 * kQTile + kStages * kTileBytes + kRawBytes + 8 * kBars;
+    // registers per thread: two softmax warpgroups, MMA and loads, feeders; together the 4 x 128 of the launch
+    static constexpr int kSoftmaxRegs = FMT == kFmtBf16 ? 184 : 160, kIssueRegs = 72, kFeedRegs = FMT == kFmtBf16 ? 72 : 120;
+    static_assert(2 * kSoftmaxRegs + kIssueRegs + kFeedRegs <= 512, "more than the block was launched with");
 };
 
 // ---- the string of tiles: units in the order (sequence, cache head, run of rows); a tile of a two-tile unit
@@ -117,18 +126,6 @@ __device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[32])
                    "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
                    "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
-        : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
 {
     asm volatile(
@@ -137,6 +134,54 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]
         "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
         : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
+// Pairs of floats in one 64-bit register, two operations per instruction.
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pack_u32x2(uint32_t a, uint32_t b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Shared-memory writes of this thread become visible to the tensor core and to TMA.
@@ -151,13 +196,20 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
         "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// Descriptor of a [rows of 64 elements, 128-byte swizzle] tile whose ROW index is the contraction (values: keys along K,
-// head dimension contiguous): leading offset = next 64 elements of the head dimension, stride offset = next 8 keys.
-__device__ __forceinline__ uint64_t umma_desc_mn(uint32_t saddr, uint32_t lead_bytes)
+// Shared-memory descriptor from its low word: start address / 16 in bits 0-13 and leading offset / 16 in bits 16-29; 128-byte
+// swizzle, 8-row groups 1024 bytes apart.  Tiles are rows of 64 elements.  Query rows and keys are contracted along the row
+// (leading offset unused, 16 bytes).  Values are contracted along the ROW INDEX, their head dimension is the
+// contiguous one: leading offset = next 64 elements of the head dimension, stride offset = next 8 keys.
+__device__ __forceinline__ uint64_t umma_desc_of(uint32_t lo)
 {
-    const uint32_t lo = ((saddr >> 4) & 0x3FFFu) | ((lead_bytes >> 4) << 16);
     const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
     return (static_cast<uint64_t>(hi) << 32) | lo;
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
@@ -169,17 +221,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     using L = ChunkLayout<FMT, D>;
     constexpr int S = L::kStages;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ int64_t s_scan[14];
+    __shared__ int64_t s_scan[kChunkWarps];
     __shared__ int s_b, s_last;
     __shared__ int64_t s_before;
     __shared__ uint32_t s_tmem;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - raw);
-    const uint32_t q_smem = base, ring = base + L::kQ, rawk = ring + S * L::kTileBytes;
-    const uint32_t raw_scale = rawk + L::kRawStages * L::kRawTile;
-    const uint32_t bars = raw_scale + L::kRawStages * L::kRawScale;
-    const uint32_t bar_full = bars, bar_empty = bars + 8 * S, bar_raw_full = bar_empty + 8 * S, bar_raw_empty = bar_raw_full + 16;
-    const uint32_t bar_s = bar_raw_empty + 16, bar_p = bar_s + 16, bar_o = bar_p + 16, bar_q_full = bar_o + 16, bar_q_empty = bar_q_full + 8;
+    const uint32_t q_smem = base, ring = base + 2 * L::kQTile, rawk = ring + S * L::kTileBytes;
+    const uint32_t raw_scale = rawk + L::kRaw * L::kRawTile;
+    const uint32_t bars = rawk + L::kRawBytes;
+    const uint32_t bar_full = bars, bar_empty = bars + 8 * S, bar_raw_full = bar_empty + 8 * S, bar_raw_empty = bar_raw_full + 8 * L::kRaw;
+    // scores and probabilities: one barrier per row tile (16 bytes apart) and buffer
+    const uint32_t bar_s = bar_raw_empty + 8 * L::kRaw, bar_p = bar_s + 32, bar_o = bar_p + 32, bar_v = bar_o + 16, bar_q_full = bar_v + 16, bar_q_empty = bar_q_full + 8;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvCacheView &c = p.cache;
 
@@ -188,12 +241,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             mbar_init(bar_full + 8 * i, FMT == kFmtBf16 ? 1 : 128);
             mbar_init(bar_empty + 8 * i, 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < L::kRaw; ++i) {
             mbar_init(bar_raw_full + 8 * i, 1);
             mbar_init(bar_raw_empty + 8 * i, 128);
+        }
+        for (int i = 0; i < 4; ++i) {
             mbar_init(bar_s + 8 * i, 1);
             mbar_init(bar_p + 8 * i, 128);
+        }
+        for (int i = 0; i < 2; ++i) {
             mbar_init(bar_o + 8 * i, 1);
+            mbar_init(bar_v + 8 * i, 1);
         }
         mbar_init(bar_q_full, 128);
         mbar_init(bar_q_empty, 1);
@@ -206,7 +264,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 
     // ---- the string: cost of one cache head of every sequence, and where this block's stretch begins
     int32_t *const s_cost = reinterpret_cast<int32_t *>(base_ptr);      // [B <= 4096], in the query rows' place for now
-    for (int b0 = warp * 32; b0 < p.batch.B; b0 += 14 * 32) {
+    for (int b0 = warp * 32; b0 < p.batch.B; b0 += kChunkThreads) {
         const int b = b0 + lane;
         SeqInfo s{};
         int blocks = 0, cost = 0;
@@ -260,7 +318,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     if (lane == 31) s_scan[warp] = upto;
     __syncthreads();
     int64_t total = 0, before = 0;
-    for (int w = 0; w < 14; ++w) {
+    for (int w = 0; w < kChunkWarps; ++w) {
         if (w < warp) before += s_scan[w];
         total += s_scan[w];
     }
@@ -297,9 +355,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     bool expired = false;
     if (idle) {
         // nothing
-    } else if (warp == kChunkLoadWarp) {
+    } else if (warp >= kChunkMmaWarp && warp < kChunkFeedWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kIssueRegs));
+        if (warp == kChunkLoadWarp) {
         // ================================================================ key and value tiles
-        const int boxes = kChunkKeys >> box_shift, box_keys = 1 << box_shift;     // at most 16
+        const int boxes = kChunkKeys >> box_shift, box_keys = 1 << box_shift;     // at most 8
         int t = 0;                                 // tiles so far
         while (true) {
             int ta, tb;
@@ -329,14 +389,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                         if (page >= 0) {
 #pragma unroll
                             for (int hb = 0; hb < L::kHalves; ++hb)
-                                tma_load_5d(dst + hb * (kChunkKeys * 128), tm, 0, slot, hb, cur.h, page, bar);
+                                tma_load_5d(dst + hb * L::kLine, tm, 0, slot, hb, cur.h, page, bar);
                         }
                     } else {
-                        const int st = x % 2;
+                        const int st = x % L::kRaw;
                         const uint32_t bar = bar_raw_full + 8 * st;
                         const uint32_t sc = raw_scale + st * L::kRawScale + lane * box_keys * (D / kFmtBlock);
                         const uint32_t sc_bytes = box_keys * (D / kFmtBlock);
-                        wait_phase(bar_raw_empty + 8 * st, ((x / 2) & 1) ^ 1, p.status, &expired);
+                        wait_phase(bar_raw_empty + 8 * st, ((x / L::kRaw) & 1) ^ 1, p.status, &expired);
                         if (page == c.n_pages)
                             for (uint32_t y = 0; y < sc_bytes; y += 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + y), "r"(0) : "memory");
                         __syncwarp();
@@ -353,65 +413,81 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
             chunk_next(p, &cur);
         }
-    } else if (warp == kChunkMmaWarp) {
+        } else if (warp == kChunkMmaWarp) {
         // ================================================================ MMAs
-        if (lane == 0) {
-            const uint32_t id_qk = umma_idesc_bf16_m128(kChunkKeys), id_pv = umma_idesc_bf16_m128(D) | (1u << 16);
-            int t = 0, segment = 0;
-            int np[2] = {0, 0};                    // probabilities taken so far per accumulator
-            while (true) {
-                int ta, tb;
-                chunk_stretch(cur, g0, g1, &ta, &tb);
-                const bool dual = cur.cost == 2;
-                const int nt = tb - ta;
-                int rounds[2];
-                rounds[0] = dual ? nt : (nt + 1) >> 1;
-                rounds[1] = dual ? nt : nt >> 1;
-                int left = rounds[0] + rounds[1];  // score products to come
-                wait_phase(bar_q_full, segment & 1, p.status, &expired);
+        // The whole warp walks through the loop, one lane issues.  It is chosen by elect.sync, not by its number: only then
+        // does the compiler know that one lane is active, and eight 128 x 128 x 16 MMAs take 513 cycles to issue
+        // instead of 663 (measured alone; the tensor core needs 512).
+        const uint32_t id_qk = umma_idesc_bf16_m128(kChunkKeys), id_pv = umma_idesc_bf16_m128(D) | (1u << 16);
+        const uint32_t q_lo = (q_smem >> 4) | (1u << 16), k_lo = (ring >> 4) | (1u << 16), v_lo = (ring >> 4) | ((L::kLine >> 4) << 16);
+        int t = 0, segment = 0;
+        int ns[2] = {0, 0}, np[2] = {0, 0};        // scores issued and probabilities taken so far per row tile
+        while (true) {
+            int ta, tb;
+            chunk_stretch(cur, g0, g1, &ta, &tb);
+            const bool dual = __shfl_sync(0xffffffffu, cur.cost, 0) == 2;
+            const int nt = __shfl_sync(0xffffffffu, tb - ta, 0);
+            int rounds[2];
+            rounds[0] = dual ? nt : (nt + 1) >> 1;
+            rounds[1] = dual ? nt : nt >> 1;
+            int left = rounds[0] + rounds[1];      // score products to come
+            wait_phase(bar_q_full, segment & 1, p.status, &expired);
+            auto scores = [&](int w, int i) {      // S_w = Q_w K^T of its i-th tile
+                const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S, buf = ns[w] & 1;
+                wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                __syncwarp();
                 tc_fence_after_sync();
-                auto scores = [&](int w, int i) {  // S_w = Q_w K^T of its i-th tile
-                    const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S;
-                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                    tc_fence_after_sync();
-                    const uint32_t a = q_smem + (dual ? w * L::kTileBytes : 0), b = ring + st * L::kTileBytes;
+                const uint32_t a = q_lo + (dual ? w * (L::kQTile >> 4) : 0), b = k_lo + st * (L::kTileBytes >> 4);
+                --left;
+                if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        const uint32_t off = (ks >> 2) * (kChunkKeys * 128) + (ks & 3) * 32;
-                        umma_bf16(tmem + w * 128, umma_smem_desc(a + off), umma_smem_desc(b + off), id_qk, ks > 0);
-                    }
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        umma_bf16(tmem + w * 128 + buf * 64, umma_desc_of(a + (ks >> 2) * ((128 * 128) >> 4) + (ks & 3) * 2),
+                                  umma_desc_of(b + (ks >> 2) * (L::kLine >> 4) + (ks & 3) * 2), id_qk, ks > 0);
+                    umma_commit(bar_s + 16 * w + 8 * buf);
                     if (!dual || w == 1) umma_commit(bar_empty + 8 * st);
-                    umma_commit(bar_s + 8 * w);
-                    if (--left == 0) umma_commit(bar_q_empty);                   // the query rows' place is free after the last one
-                };
+                    if (left == 0) umma_commit(bar_q_empty);                     // the query rows' place is free after the last one
+                }
+                __syncwarp();
+                ++ns[w];
+            };
+            // Order: two tiles' scores ahead; a buffer's next scores are issued behind the product that reads its probabilities.
+            // With one-tile units the keys of tile k + 4 are waited for while tile k's values are unread: 8 stages at least.
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
                 for (int w = 0; w < 2; ++w)
-                    if (rounds[w] > 0) scores(w, 0);
-                for (int i = 0; i < rounds[0]; ++i)
-                    for (int w = 0; w < 2; ++w) {
-                        if (i >= rounds[w]) continue;
-                        const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S;
-                        wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                        wait_phase(bar_p + 8 * w, np[w] & 1, p.status, &expired);
-                        ++np[w];
-                        tc_fence_after_sync();
+                    if (i < rounds[w]) scores(w, i);
+            for (int i = 0; i < rounds[0]; ++i)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    if (i >= rounds[w]) continue;
+                    const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S, buf = np[w] & 1;
+                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                    wait_phase(bar_p + 16 * w + 8 * buf, (np[w] >> 1) & 1, p.status, &expired);
+                    __syncwarp();
+                    tc_fence_after_sync();
+                    const uint32_t b = v_lo + st * (L::kTileBytes >> 4);
+                    if (elect_one()) {
 #pragma unroll
                         for (int ks = 0; ks < kChunkKeys / 16; ++ks)
-                            umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + ks * 8,
-                                         umma_desc_mn(ring + st * L::kTileBytes + ks * 2048, kChunkKeys * 128), id_pv, i > 0 || ks > 0);
+                            umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + buf * 64 + ks * 8, umma_desc_of(b + ks * (2048 >> 4)), id_pv,
+                                         i > 0 || ks > 0);
                         if (!dual || w == 1) umma_commit(bar_empty + 8 * st);
-                        if (i + 1 < rounds[w])
-                            scores(w, i + 1);
-                        else
-                            umma_commit(bar_o + 8 * w);
+                        umma_commit(bar_v + 8 * w);
+                        if (i + 1 == rounds[w]) umma_commit(bar_o + 8 * w);
                     }
-                t += nt;
-                ++segment;
-                if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
-                chunk_next(p, &cur);
-            }
+                    __syncwarp();
+                    ++np[w];
+                    if (i + 2 < rounds[w]) scores(w, i + 2);
+                }
+            t += nt;
+            ++segment;
+            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
+            chunk_next(p, &cur);
         }
-        __syncwarp();
+        }
     } else if (warp >= kChunkFeedWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kFeedRegs));
         // ================================================================ query rows; codes to bf16
         const int ft = tid - kChunkFeedWarp * 32;  // 0 .. 127
         int t = 0, segment = 0;
@@ -435,7 +511,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const int y = y0 + u * 128, row = y / kChunks, ch = y - row * kChunks;
-                    const uint32_t dst = q_smem + (row >> 7) * L::kTileBytes + (ch >> 3) * (128 * 128) + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                    const uint32_t dst = q_smem + (row >> 7) * L::kQTile + (ch >> 3) * (128 * 128) + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[u].x), "r"(v[u].y), "r"(v[u].z), "r"(v[u].w) : "memory");
                 }
             }
@@ -444,27 +520,29 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             if (FMT == kFmtE4m3) {
                 for (int k = ta; k < tb; ++k, ++t)
                     for (int kv = 0; kv < 2; ++kv) {
-                        const int x = 2 * t + kv, st = x % S, rs = x % 2;
-                        wait_phase(bar_raw_full + 8 * rs, (x / 2) & 1, p.status, &expired);
-                        uint32_t w[D / 4], sc;
-                        const uint32_t src = rawk + rs * L::kRawTile + ft * D;
+                        // half a key per thread: threads 0-63 the first half of the dimensions, 64-127 the second
+                        const int x = 2 * t + kv, st = x % S, rs = x % L::kRaw, key = ft & 63, part = ft >> 6;
+                        wait_phase(bar_raw_full + 8 * rs, (x / L::kRaw) & 1, p.status, &expired);
+                        uint32_t w[D / 8], sc;
+                        const uint32_t src = rawk + rs * L::kRawTile + key * D;
 #pragma unroll
-                        for (int ch = 0; ch < D / 16; ++ch) {
-                            const uint32_t at = src + ((D == 128 ? ch ^ (ft & 7) : ch ^ ((ft >> 1) & 3)) << 4);
+                        for (int c16 = 0; c16 < D / 32; ++c16) {
+                            const int ch = part * (D / 32) + c16;
+                            const uint32_t at = src + ((D == 128 ? ch ^ (key & 7) : ch ^ ((key >> 1) & 3)) << 4);
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(w[4 * ch]), "=r"(w[4 * ch + 1]), "=r"(w[4 * ch + 2]), "=r"(w[4 * ch + 3]) : "r"(at) : "memory");
+                                         : "=r"(w[4 * c16]), "=r"(w[4 * c16 + 1]), "=r"(w[4 * c16 + 2]), "=r"(w[4 * c16 + 3]) : "r"(at) : "memory");
                         }
-                        const uint32_t sa = raw_scale + rs * L::kRawScale + ft * (D / kFmtBlock);
+                        const uint32_t sa = raw_scale + rs * L::kRawScale + key * (D / kFmtBlock) + part * (D / 64);
                         if (D == 128)
-                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc) : "r"(sa) : "memory");
-                        else
                             asm volatile("{\n\t.reg .b16 h;\n\tld.shared.b16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(sc) : "r"(sa) : "memory");
+                        else
+                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(sa) : "memory");
                         // a key no query of the unit sees was perhaps not even loaded: zeros
-                        const bool keep = seen_by_any(cur.r, p.sinks, cur.r.base(k, kChunkShift) + ft);
+                        const bool keep = seen_by_any(cur.r, p.sinks, cur.r.base(k, kChunkShift) + key);
                         wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
-                        const uint32_t dst = ring + st * L::kTileBytes + ft * 128;
+                        const uint32_t dst = ring + st * L::kTileBytes + key * 128;
 #pragma unroll
-                        for (int g = 0; g < D / kFmtBlock; ++g) {
+                        for (int g = 0; g < D / 64; ++g) {
                             const uint32_t byte = (sc >> (8 * g)) & 0xffu;
                             const uint32_t f = ((min(byte, 134u) + 120u) << 7) * 0x10001u;       // see the few-rows kernel
                             const uint32_t f2 = ((byte == 255u ? 0x7FC0u : (byte > 134u ? byte - 7u : 127u) << 7)) * 0x10001u;
@@ -482,8 +560,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                                     for (int e = 0; e < 4; ++e) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[e]) : "r"(o[e]), "r"(f2));
                                 }
                                 if (!keep) o[0] = o[1] = o[2] = o[3] = 0;
-                                const int ch = 4 * g + u;
-                                const uint32_t at = dst + (ch >> 3) * (kChunkKeys * 128) + (((ch & 7) ^ (ft & 7)) << 4);
+                                const int ch = part * (D / 16) + 4 * g + u;
+                                const uint32_t at = dst + (ch >> 3) * L::kLine + (((ch & 7) ^ (key & 7)) << 4);
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                             }
                         }
@@ -499,10 +577,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             chunk_next(p, &cur);
         }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kSoftmaxRegs));
         // ================================================================ softmax and output
         const int w = warp >> 2, row = tid & 127;
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;            // this warp's 32 lanes of tensor memory
-        const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
+        const uint32_t t_o = tmem + lanes + 256 + w * 128;
         int t = 0, ns = 0;
         int outputs[2] = {0, 0};                   // finished outputs per accumulator
         while (true) {
@@ -527,85 +606,82 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                     if (!clean) {
                         const int x = 2 * (t + k) + 1, st = x % S;
                         wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                        if (!seen_by_any(cur.r, p.sinks, key0 + row)) {
-                            const uint32_t dst = ring + st * L::kTileBytes + row * 128;
+                        if (row < kChunkKeys * L::kHalves && !seen_by_any(cur.r, p.sinks, key0 + (row & 63))) {
+                            const uint32_t dst = ring + st * L::kTileBytes + (row >> 6) * L::kLine + (row & 63) * 128;
 #pragma unroll
-                            for (int hb = 0; hb < L::kHalves; ++hb)
-#pragma unroll
-                                for (int ch = 0; ch < 8; ++ch)
-                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + hb * (kChunkKeys * 128) + ch * 16), "r"(0) : "memory");
+                            for (int ch = 0; ch < 8; ++ch)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + ch * 16), "r"(0) : "memory");
                         }
                         fence_async_shared();
                     }
                 }
-                wait_phase(bar_s + 8 * w, ns & 1, p.status, &expired);
+                const uint32_t t_s = tmem + lanes + w * 128 + (ns & 1) * 64, done = bar_p + 16 * w + 8 * (ns & 1);
+                wait_phase(bar_s + 16 * w + 8 * (ns & 1), (ns >> 1) & 1, p.status, &expired);
                 ++ns;
                 __syncwarp();
                 tc_fence_after_sync();
                 uint32_t v[2][32];
-                const int limit = min(pos + 1, cur.s.len) - key0;                // columns from here on lie ahead or beyond the context
-                const int low = p.window ? pos - p.window + 1 - key0 : -0x40000000, sink = p.sinks - key0;
-                auto mask = [&](uint32_t (&x)[32], int c0) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int col = c0 + e;
-                        if (!(col < limit && (col >= low || col < sink))) x[e] = 0xff800000u;
-                    }
-                };
-                float top = -INFINITY;
                 tmem_ld32(t_s, v[0]);
+                tmem_ld32(t_s + 32, v[1]);
+                tmem_wait_ld(v[0]);
+                tmem_wait_ld(v[1]);
+                if (!whole) {
+                    const int limit = min(pos + 1, cur.s.len) - key0;            // columns from here on lie ahead or beyond the context
+                    const int low = p.window ? pos - p.window + 1 - key0 : -0x40000000, sink = p.sinks - key0;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    tmem_wait_ld(v[q & 1]);
-                    if (q < 3) tmem_ld32(t_s + 32 * (q + 1), v[(q + 1) & 1]);
-                    if (!whole) mask(v[q & 1], 32 * q);
-                    float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e & 3] = fmaxf(x[e & 3], __uint_as_float(v[q & 1][e]));
-                    top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+                    for (int col = 0; col < kChunkKeys; ++col)
+                        if (!(col < limit && (col >= low || col < sink))) v[col >> 5][col & 31] = 0xff800000u;
                 }
-                tmem_ld32(t_s, v[0]);                                            // the scores once more, now for the exponentials
-                top *= p.scale_log2;
-                const bool raise = top > m + 8.f;
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int col = 0; col < kChunkKeys; col += 2)
+                    top[(col >> 1) & 3] = max3(top[(col >> 1) & 3], __uint_as_float(v[col >> 5][col & 31]), __uint_as_float(v[col >> 5][(col & 31) + 1]));
+                const float mx = max3(top[0], top[1], fmaxf(top[2], top[3])) * p.scale_log2;
+                const bool raise = mx > m + 8.f;   // the reference stays while no probability exceeds 2^8
                 if (__any_sync(0xffffffffu, raise)) {
-                    const float f = raise ? exp2_fast(m - top) : 1.f;
-                    if (raise) m = top;
+                    const float f = raise ? exp2_fast(m - mx) : 1.f;
+                    if (raise) m = mx;
                     l *= f;
-                    if (i > 0) {                   // the products so far are complete: S of this tile was issued behind them
-                        uint32_t o[32];
+                    if (i > 0) {
+                        // the product of the tile before may still be running (the one before that is not: S came behind it)
+                        wait_phase(bar_v + 8 * w, (ns - 2) & 1, p.status, &expired);
+                        __syncwarp();
+                        tc_fence_after_sync();
 #pragma unroll
-                        for (int q = 0; q < D / 32; ++q) {
-                            tmem_wait_ld(v[0]);
-                            tmem_ld32(t_o + 32 * q, o);
-                            tmem_wait_ld(o);
+                        for (int q = 0; q < D / 16; ++q) {
+                            uint32_t o[16];
+                            tmem_ld16(t_o + 16 * q, o);
+                            tmem_wait_ld16(o);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_st32(t_o + 32 * q, o);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st16(t_o + 16 * q, o);
                         }
                     }
                 }
                 const float mm = m == -INFINITY ? 0.f : m;
+                const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2), minus2 = pack_f32x2(-mm, -mm);
+                uint64_t sum2[2] = {0, 0};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    tmem_wait_ld(v[q & 1]);
-                    if (q < 3) tmem_ld32(t_s + 32 * (q + 1), v[(q + 1) & 1]);
-                    if (!whole) mask(v[q & 1], 32 * q);
+                for (int q = 0; q < 2; ++q) {
                     uint32_t pk[16];
-                    float sum[2] = {0.f, 0.f};
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float a = exp2_fast(fmaf(__uint_as_float(v[q & 1][2 * e]), p.scale_log2, -mm));
-                        const float b = exp2_fast(fmaf(__uint_as_float(v[q & 1][2 * e + 1]), p.scale_log2, -mm));
-                        sum[0] += a;
-                        sum[1] += b;
+                        const uint64_t x = fma_f32x2(pack_u32x2(v[q][2 * e], v[q][2 * e + 1]), scale2, minus2);
+                        float a, b;
+                        unpack_f32x2(x, a, b);
+                        a = exp2_fast(a);
+                        b = exp2_fast(b);
+                        sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(a, b));
                         pk[e] = to_bf16x2(a, b);
                     }
-                    l += sum[0] + sum[1];
-                    tmem_st16(t_s + 16 * q, pk);   // columns whose scores were read before
+                    tmem_st16(t_s + 16 * q, pk);   // columns whose scores are in registers
                 }
                 tmem_wait_st();
                 tc_fence_before_sync();
-                mbar_arrive(bar_p + 8 * w);
+                mbar_arrive(done);
+                float s0, s1;
+                unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
+                l += s0 + s1;
             }
 
             // ---- output: this thread's row
@@ -671,9 +747,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                                                 to_bf16x2(__uint_as_float(o[8 * e + 4]) * inv, __uint_as_float(o[8 * e + 5]) * inv),
                                                 to_bf16x2(__uint_as_float(o[8 * e + 6]) * inv, __uint_as_float(o[8 * e + 7]) * inv));
                     } else if (live) {
-                        uint4 *dst = reinterpret_cast<uint4 *>(my_part + my_row * D + 32 * q);
+                        uint4 *dst = reinterpret_cast<uint4 *>(my_part) + 8 * q * kChunkRows + my_row;       // four columns by rows: consecutive lanes are adjacent
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        for (int e = 0; e < 8; ++e) dst[e * kChunkRows] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                     }
                 }
                 if (live) {
@@ -702,27 +778,41 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 if (s_last) {
                     fence_gpu();
                     const int first_slot = cur.begin <= W * first / ctas ? 0 : 1;
-                    constexpr int kQuads = D / 4;
-                    for (int x = tid; x < cur.rows * kQuads; x += 256) {
-                        const int r = x / kQuads, dq = x - r * kQuads;
+                    if (tid < cur.rows) {          // one row per thread, 32 columns at a time
+                        const int r = tid;
+                        auto part_of = [&](int k) { return parts + (2 * k + (k == first ? first_slot : 0)) * kPart; };
                         float M = -INFINITY, Lsum = 0.f;
-                        for (int k = first; k <= last; ++k)
-                            M = fmaxf(M, __ldcg(parts + (2 * k + (k == first ? first_slot : 0)) * kPart + kChunkRows * D + r));
-                        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int k = first; k <= last; ++k) M = fmaxf(M, __ldcg(part_of(k) + kChunkRows * D + r));
                         for (int k = first; k <= last; ++k) {
-                            const float *src = parts + (2 * k + (k == first ? first_slot : 0)) * kPart;
-                            const float mk = __ldcg(src + kChunkRows * D + r);
-                            const float f = mk == -INFINITY ? 0.f : exp2_fast(mk - M);
-                            const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + r * D + 4 * dq));
-                            Lsum += f * __ldcg(src + kChunkRows * D + kChunkRows + r);
-                            a.x += f * y.x; a.y += f * y.y; a.z += f * y.z; a.w += f * y.w;
+                            const float mk = __ldcg(part_of(k) + kChunkRows * D + r);
+                            Lsum += (mk == -INFINITY ? 0.f : exp2_fast(mk - M)) * __ldcg(part_of(k) + kChunkRows * D + kChunkRows + r);
                         }
                         const float inv = Lsum == 0.f ? 0.f : 1.f / Lsum;
                         const int i = (cur.row0 + r) / p.group, hr = cur.h * p.group + (cur.row0 + r - i * p.group);
                         const int64_t tok = static_cast<int64_t>(cur.s.token0) + i;
-                        *reinterpret_cast<uint2 *>(p.out + 2 * (tok * p.out_stride + static_cast<int64_t>(hr) * D + 4 * dq)) =
-                            make_uint2(to_bf16x2(a.x * inv, a.y * inv), to_bf16x2(a.z * inv, a.w * inv));
-                        if (p.lse && dq == 0) p.lse[tok * p.heads_q + hr] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
+                        if (p.lse) p.lse[tok * p.heads_q + hr] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
+                        for (int q = 0; q < D / 32; ++q) {
+                            float4 a[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) a[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            for (int k = first; k <= last; ++k) {
+                                const float mk = __ldcg(part_of(k) + kChunkRows * D + r);
+                                const float4 *src = reinterpret_cast<const float4 *>(part_of(k)) + 8 * q * kChunkRows + r;
+                                float4 y[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) y[e] = __ldcg(src + e * kChunkRows);
+                                const float f = (mk == -INFINITY ? 0.f : exp2_fast(mk - M)) * inv;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    a[e].x += f * y[e].x; a[e].y += f * y[e].y; a[e].z += f * y[e].z; a[e].w += f * y[e].w;
+                                }
+                            }
+                            uint4 *dst = reinterpret_cast<uint4 *>(p.out + 2 * (tok * p.out_stride + static_cast<int64_t>(hr) * D + 32 * q));
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                dst[e] = make_uint4(to_bf16x2(a[2 * e].x, a[2 * e].y), to_bf16x2(a[2 * e].z, a[2 * e].w),
+                                                    to_bf16x2(a[2 * e + 1].x, a[2 * e + 1].y), to_bf16x2(a[2 * e + 1].z, a[2 * e + 1].w));
+                        }
                     }
                 }
                 named_sync(1, 256);                // s_last may be written again

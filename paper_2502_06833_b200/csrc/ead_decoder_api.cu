@@ -28,7 +28,7 @@ namespace {
     } while (0)
 
 constexpr int kMaxDevices = 64;
-constexpr int kChunkMinCost = 8;          // tiles of 128 rows x 128 keys per block, likewise; at least 2
+constexpr int kChunkMinCost = 16;         // tiles of 128 rows x 64 keys per block, likewise; at least 2
 constexpr int kFewMinTiles = 16;          // tiles of 8 KiB per block before another block is worth its part in the join
 
 struct DeviceInfo {
