@@ -9,10 +9,11 @@
 // gives both turns to the same rows instead: even key tiles go to the first accumulator, odd ones
 // to the second, and the two are joined at the end.
 //
-// Warps: 0-3 softmax and output of the first row tile, 4-7 of the second, 8 issues the MMAs, 9 loads key and value
+// Warps: 0-3 softmax and output of the first row tile, 4-7 of the second, 8 and 10 issue their MMAs (the instructions
+// around the MMAs take longer than the MMAs: one warp for both row tiles took twice the time), 9 loads key and value
 // tiles (TMA), 12-15 load the query rows and, for an 8-bit cache, turn codes into bf16 on their way into the MMA's
-// operand tiles (as in the few-rows kernel).  10 and 11 complete the warpgroup: registers are dealt out by warpgroups, most
-// of them to the softmax, which keeps a row of 128 scores in them.
+// operand tiles (as in the few-rows kernel).  11 completes the warpgroup: registers are dealt out by warpgroups, most
+// of them to the softmax, which keeps a row's scores in them.
 #pragma once
 #include "attn_common.cuh"
 
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     if (tid == 0) {
         for (int i = 0; i < S; ++i) {
             mbar_init(bar_full + 8 * i, FMT == kFmtBf16 ? 1 : 128);
-            mbar_init(bar_empty + 8 * i, 1);
+            mbar_init(bar_empty + 8 * i, 2);
         }
         for (int i = 0; i < L::kRaw; ++i) {
             mbar_init(bar_raw_full + 8 * i, 1);
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             mbar_init(bar_v + 8 * i, 1);
         }
         mbar_init(bar_q_full, 128);
-        mbar_init(bar_q_empty, 1);
+        mbar_init(bar_q_empty, 2);
         fence_mbar_init();
     }
     if (warp == kChunkMmaWarp) {
@@ -413,73 +414,69 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
             chunk_next(p, &cur);
         }
-        } else if (warp == kChunkMmaWarp) {
+        } else if (warp == kChunkMmaWarp || warp == kChunkMmaWarp + 2) {
         // ================================================================ MMAs
         // The whole warp walks through the loop, one lane issues.  It is chosen by elect.sync, not by its number: only then
         // does the compiler know that one lane is active, and eight 128 x 128 x 16 MMAs take 513 cycles to issue
         // instead of 663 (measured alone; the tensor core needs 512).
+        const int w = __shfl_sync(0xffffffffu, (warp - kChunkMmaWarp) >> 1, 0);  // row tile
         const uint32_t id_qk = umma_idesc_bf16_m128(kChunkKeys), id_pv = umma_idesc_bf16_m128(D) | (1u << 16);
         const uint32_t q_lo = (q_smem >> 4) | (1u << 16), k_lo = (ring >> 4) | (1u << 16), v_lo = (ring >> 4) | ((L::kLine >> 4) << 16);
+        const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
         int t = 0, segment = 0;
-        int ns[2] = {0, 0}, np[2] = {0, 0};        // scores issued and probabilities taken so far per row tile
+        int ns = 0, np = 0;                        // scores issued and probabilities taken so far
         while (true) {
             int ta, tb;
             chunk_stretch(cur, g0, g1, &ta, &tb);
             const bool dual = __shfl_sync(0xffffffffu, cur.cost, 0) == 2;
             const int nt = __shfl_sync(0xffffffffu, tb - ta, 0);
-            int rounds[2];
-            rounds[0] = dual ? nt : (nt + 1) >> 1;
-            rounds[1] = dual ? nt : nt >> 1;
-            int left = rounds[0] + rounds[1];      // score products to come
+            const int rounds = dual ? nt : (nt + 1 - w) >> 1;
             wait_phase(bar_q_full, segment & 1, p.status, &expired);
-            auto scores = [&](int w, int i) {      // S_w = Q_w K^T of its i-th tile
-                const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S, buf = ns[w] & 1;
+            const uint32_t a = q_lo + (dual ? w * (L::kQTile >> 4) : 0);
+            auto scores = [&](int i) {             // S = Q K^T of the i-th tile
+                const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S;
                 wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
                 __syncwarp();
                 tc_fence_after_sync();
-                const uint32_t a = q_lo + (dual ? w * (L::kQTile >> 4) : 0), b = k_lo + st * (L::kTileBytes >> 4);
-                --left;
+                const uint32_t d = t_s + (ns & 1) * 64, b = k_lo + st * (L::kTileBytes >> 4);
                 if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks)
-                        umma_bf16(tmem + w * 128 + buf * 64, umma_desc_of(a + (ks >> 2) * ((128 * 128) >> 4) + (ks & 3) * 2),
+                        umma_bf16(d, umma_desc_of(a + (ks >> 2) * ((128 * 128) >> 4) + (ks & 3) * 2),
                                   umma_desc_of(b + (ks >> 2) * (L::kLine >> 4) + (ks & 3) * 2), id_qk, ks > 0);
-                    umma_commit(bar_s + 16 * w + 8 * buf);
-                    if (!dual || w == 1) umma_commit(bar_empty + 8 * st);
-                    if (left == 0) umma_commit(bar_q_empty);                     // the query rows' place is free after the last one
+                    umma_commit(bar_s + 16 * w + 8 * (ns & 1));
+                    umma_commit(bar_empty + 8 * st);
+                    if (!dual) umma_commit(bar_empty + 8 * st);                  // for the row tile that is not there
+                    if (i + 1 == rounds) umma_commit(bar_q_empty);               // the query rows' place is free after the last one
                 }
                 __syncwarp();
-                ++ns[w];
+                ++ns;
             };
             // Order: two tiles' scores ahead; a buffer's next scores are issued behind the product that reads its probabilities.
             // With one-tile units the keys of tile k + 4 are waited for while tile k's values are unread: 8 stages at least.
+            if (rounds == 0 && elect_one()) mbar_arrive(bar_q_empty);
             for (int i = 0; i < 2; ++i)
+                if (i < rounds) scores(i);
+            for (int i = 0; i < rounds; ++i) {
+                const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S;
+                const uint32_t pr = t_s + (np & 1) * 64, b = v_lo + st * (L::kTileBytes >> 4);
+                wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                wait_phase(bar_p + 16 * w + 8 * (np & 1), (np >> 1) & 1, p.status, &expired);
+                __syncwarp();
+                tc_fence_after_sync();
+                if (elect_one()) {
 #pragma unroll
-                for (int w = 0; w < 2; ++w)
-                    if (i < rounds[w]) scores(w, i);
-            for (int i = 0; i < rounds[0]; ++i)
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    if (i >= rounds[w]) continue;
-                    const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S, buf = np[w] & 1;
-                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                    wait_phase(bar_p + 16 * w + 8 * buf, (np[w] >> 1) & 1, p.status, &expired);
-                    __syncwarp();
-                    tc_fence_after_sync();
-                    const uint32_t b = v_lo + st * (L::kTileBytes >> 4);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int ks = 0; ks < kChunkKeys / 16; ++ks)
-                            umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + buf * 64 + ks * 8, umma_desc_of(b + ks * (2048 >> 4)), id_pv,
-                                         i > 0 || ks > 0);
-                        if (!dual || w == 1) umma_commit(bar_empty + 8 * st);
-                        umma_commit(bar_v + 8 * w);
-                        if (i + 1 == rounds[w]) umma_commit(bar_o + 8 * w);
-                    }
-                    __syncwarp();
-                    ++np[w];
-                    if (i + 2 < rounds[w]) scores(w, i + 2);
+                    for (int ks = 0; ks < kChunkKeys / 16; ++ks)
+                        umma_bf16_ts(t_o, pr + ks * 8, umma_desc_of(b + ks * (2048 >> 4)), id_pv, i > 0 || ks > 0);
+                    umma_commit(bar_v + 8 * w);
+                    umma_commit(bar_empty + 8 * st);
+                    if (!dual) umma_commit(bar_empty + 8 * st);
+                    if (i + 1 == rounds) umma_commit(bar_o + 8 * w);
                 }
+                __syncwarp();
+                ++np;
+                if (i + 2 < rounds) scores(i + 2);
+            }
             t += nt;
             ++segment;
             if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
@@ -600,8 +597,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 const int key0 = cur.r.base(ta + k, kChunkShift);
                 const bool whole = key0 + kChunkKeys - 1 <= pos_a && key0 + kChunkKeys <= cur.s.len &&
                                    (p.window == 0 || key0 > pos_b - p.window || key0 + kChunkKeys <= p.sinks);
-                if (FMT == kFmtBf16 && (dual ? w == 0 : true)) {
+                if (FMT == kFmtBf16) {
                     // values no query sees may be anything, and were perhaps not even loaded: zeros, so that 0 * NaN cannot arise
+                    // (both row tiles' threads write them: each has its own product to come)
                     const bool clean = key0 + kChunkKeys <= cur.r.hi && (key0 >= cur.r.lo || key0 + kChunkKeys <= p.sinks);
                     if (!clean) {
                         const int x = 2 * (t + k) + 1, st = x % S;
