@@ -12,8 +12,9 @@
 // Warps: 0-3 softmax and output of the first row tile, 4-7 of the second, 8 and 10 issue their MMAs (the instructions
 // around the MMAs take longer than the MMAs: one warp for both row tiles took twice the time), 9 loads key and value
 // tiles (TMA), 12-15 load the query rows and, for an 8-bit cache, turn codes into bf16 on their way into the MMA's
-// operand tiles (as in the few-rows kernel).  11 completes the warpgroup: registers are dealt out by warpgroups, most
-// of them to the softmax, which keeps a row's scores in them.
+// operand tiles (as in the few-rows kernel).  11 walks through the block's units and describes each to the others in shared
+// memory, two ahead at most.  Registers are dealt out by warpgroups, most of them to the softmax, which keeps a row's
+// scores in them.
 #pragma once
 #include "attn_common.cuh"
 
@@ -21,7 +22,7 @@ namespace ead {
 
 constexpr int kChunkWarps = 16;
 constexpr int kChunkThreads = 32 * kChunkWarps;
-constexpr int kChunkMmaWarp = 8, kChunkLoadWarp = 9, kChunkFeedWarp = 12;
+constexpr int kChunkMmaWarp = 8, kChunkLoadWarp = 9, kChunkUnitWarp = 11, kChunkFeedWarp = 12;
 constexpr int kChunkKeys = 64;                    // keys per tile
 constexpr int kChunkShift = 6;
 constexpr int kChunkRows = 256;                   // packed rows per unit
@@ -45,10 +46,10 @@ struct ChunkLayout {
     static constexpr int kRawScale = FMT == kFmtE4m3 ? kChunkKeys * (D / kFmtBlock) : 0;
     static constexpr int kRaw = 4;                                       // stages of codes
     static constexpr int kRawBytes = kRaw * (kRawTile + kRawScale);
-    static constexpr int kBars = 2 * kStages + 2 * kRaw + 14;
+    static constexpr int kBars = 2 * kStages + 2 * kRaw + 18;
     static constexpr int kSmem = 1024 + 2 * kQTile + kStages * kTileBytes + kRawBytes + 8 * kBars;
     // registers per thread: two softmax warpgroups, MMA and loads, feeders; together the 4 x 128 of the launch
-    static constexpr int kSoftmaxRegs = FMT == kFmtBf16 ? 184 : 160, kIssueRegs = 72, kFeedRegs = FMT == kFmtBf16 ? 72 : 120;
+    static constexpr int kSoftmaxRegs = FMT == kFmtBf16 ? 168 : 152, kIssueRegs = 88, kFeedRegs = FMT == kFmtBf16 ? 88 : 120;
     static_assert(2 * kSoftmaxRegs + kIssueRegs + kFeedRegs <= 512, "more than the block was launched with");
 };
 
@@ -102,6 +103,24 @@ __device__ __forceinline__ void chunk_stretch(const ChunkCursor &c, int64_t g0, 
     *ta = g0 <= c.begin ? 0 : static_cast<int>(a);
     *tb = b < c.r.tiles ? static_cast<int>(b) : c.r.tiles;
 }
+
+// A block's part of a unit, as warp 11 describes it to the others.
+struct ChunkUnit {
+    int b, h, token0;                             // sequence, cache head, first row of the sequence in the step
+    int row0, rows;                               // packed rows
+    int p0, len;                                  // position of the sequence's first new token, keys in the cache
+    int lo, hi, sink_tiles, first_tile;           // keys (KeyRange)
+    int ta, nt;                                   // first tile, tiles
+    int dual;                                     // two row tiles?
+    int last;                                     // the block's last unit?
+    int part;                                     // place of its result in the workspace (0, 1), or -1: the unit is this block's alone
+    int first, blocks, first_part;                // blocks that hold a part of it; the first one's place
+    __device__ __forceinline__ int base(int t) const
+    {
+        return (t < sink_tiles ? t : t - sink_tiles + first_tile) << kChunkShift;
+    }
+    __device__ __forceinline__ bool seen(int sinks, int j) const { return j < hi && (j >= lo || j < sinks); }
+};
 
 // ---- tensor memory
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
@@ -224,6 +243,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     __shared__ int64_t s_scan[kChunkWarps];
     __shared__ int s_b, s_last;
+    __shared__ ChunkUnit s_unit[2];
     __shared__ int64_t s_before;
     __shared__ uint32_t s_tmem;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -234,6 +254,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const uint32_t bar_full = bars, bar_empty = bars + 8 * S, bar_raw_full = bar_empty + 8 * S, bar_raw_empty = bar_raw_full + 8 * L::kRaw;
     // scores and probabilities: one barrier per row tile (16 bytes apart) and buffer
     const uint32_t bar_s = bar_raw_empty + 8 * L::kRaw, bar_p = bar_s + 32, bar_o = bar_p + 32, bar_v = bar_o + 16, bar_q_full = bar_v + 16, bar_q_empty = bar_q_full + 8;
+    const uint32_t bar_u_full = bar_q_empty + 8, bar_u_empty = bar_u_full + 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvCacheView &c = p.cache;
 
@@ -253,6 +274,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_o + 8 * i, 1);
             mbar_init(bar_v + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_u_full + 8 * i, 1);
+            mbar_init(bar_u_empty + 8 * i, kChunkWarps - 1);
         }
         mbar_init(bar_q_full, 128);
         mbar_init(bar_q_empty, 2);
@@ -354,155 +379,192 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     __syncthreads();                               // s_cost is done with; its place takes query rows now
 
     bool expired = false;
+    // Every role takes the units one by one: waits for the description, works, releases it (one arrival per warp).
+    auto unit_wait = [&](int n) -> const ChunkUnit & {
+        wait_phase(bar_u_full + 8 * (n & 1), (n >> 1) & 1, p.status, &expired);
+        __syncwarp();
+        return s_unit[n & 1];
+    };
+    auto unit_done = [&](int n) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_u_empty + 8 * (n & 1));
+    };
     if (idle) {
         // nothing
     } else if (warp >= kChunkMmaWarp && warp < kChunkFeedWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kIssueRegs));
-        if (warp == kChunkLoadWarp) {
-        // ================================================================ key and value tiles
-        const int boxes = kChunkKeys >> box_shift, box_keys = 1 << box_shift;     // at most 8
-        int t = 0;                                 // tiles so far
-        while (true) {
-            int ta, tb;
-            chunk_stretch(cur, g0, g1, &ta, &tb);
-            for (int k = ta; k < tb; ++k, ++t) {
-                const int key0 = cur.r.base(k, kChunkShift) + lane * box_keys, slot = key0 & (c.page_size - 1);
-                int page = -2;
-                if (lane < boxes && key0 < cur.r.hi && (key0 + box_keys > cur.r.lo || key0 < p.sinks)) {
-                    page = find_page(c, p.batch, cur.b, key0);
-                    if (page < 0) {
-                        flag_status(p.status, kStatusBadPage);
-                        page = c.n_pages;          // outside the pool: the copy delivers zeros
-                    }
+        if (warp == kChunkUnitWarp) {
+            // ============================================================ units
+            for (int n = 0;; ++n) {
+                int ta, tb;
+                chunk_stretch(cur, g0, g1, &ta, &tb);
+                const int64_t end = cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles;
+                wait_phase(bar_u_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, p.status, &expired);
+                __syncwarp();
+                if (lane == 0) {
+                    ChunkUnit &u = s_unit[n & 1];
+                    u.b = cur.b; u.h = cur.h; u.token0 = cur.s.token0;
+                    u.row0 = cur.row0; u.rows = cur.rows;
+                    u.p0 = cur.s.p0; u.len = cur.s.len;
+                    u.lo = cur.r.lo; u.hi = cur.r.hi; u.sink_tiles = cur.r.sink_tiles; u.first_tile = cur.r.first_tile;
+                    u.ta = ta; u.nt = tb - ta;
+                    u.dual = cur.cost == 2;
+                    u.last = end >= g1;
+                    u.part = ta == 0 && tb == cur.r.tiles ? -1 : cur.begin <= g0 ? 0 : 1;
+                    // blocks in whose stretch its first and its last tile begin
+                    u.first = static_cast<int>(((cur.begin + 1) * ctas - 1) / W);
+                    u.blocks = static_cast<int>(((end - cur.cost + 1) * ctas - 1) / W) - u.first + 1;
+                    u.first_part = cur.begin <= W * u.first / ctas ? 0 : 1;
+                    mbar_arrive(bar_u_full + 8 * (n & 1));
                 }
-                const int live = __popc(__ballot_sync(0xffffffffu, page >= 0));
-                const int good = __popc(__ballot_sync(0xffffffffu, page >= 0 && page < c.n_pages));
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    const int x = 2 * t + kv;
-                    const CUtensorMap *tm = kv ? &tmV : &tmK;
-                    if (FMT == kFmtBf16) {
-                        const int st = x % S;
-                        const uint32_t bar = bar_full + 8 * st, dst = ring + st * L::kTileBytes + lane * box_keys * 128;
-                        wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
-                        if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D * 2);
-                        __syncwarp();
-                        if (page >= 0) {
-#pragma unroll
-                            for (int hb = 0; hb < L::kHalves; ++hb)
-                                tma_load_5d(dst + hb * L::kLine, tm, 0, slot, hb, cur.h, page, bar);
-                        }
-                    } else {
-                        const int st = x % L::kRaw;
-                        const uint32_t bar = bar_raw_full + 8 * st;
-                        const uint32_t sc = raw_scale + st * L::kRawScale + lane * box_keys * (D / kFmtBlock);
-                        const uint32_t sc_bytes = box_keys * (D / kFmtBlock);
-                        wait_phase(bar_raw_empty + 8 * st, ((x / L::kRaw) & 1) ^ 1, p.status, &expired);
-                        if (page == c.n_pages)
-                            for (uint32_t y = 0; y < sc_bytes; y += 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + y), "r"(0) : "memory");
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D + good * sc_bytes);
-                        __syncwarp();
-                        if (page >= 0) {
-                            tma_load_5d(rawk + st * L::kRawTile + lane * box_keys * D, tm, 0, slot, 0, cur.h, page, bar);
-                            if (page < c.n_pages)
-                                bulk_load(sc, (kv ? c.v_scale : c.k_scale) + scale_offset(c, page, cur.h, slot), sc_bytes, bar);
+                if (end >= g1) break;
+                chunk_next(p, &cur);
+            }
+        } else if (warp == kChunkLoadWarp) {
+            // ============================================================ key and value tiles
+            const int boxes = kChunkKeys >> box_shift, box_keys = 1 << box_shift;     // at most 8
+            int t = 0;                             // tiles so far
+            for (int n = 0;; ++n) {
+                const ChunkUnit &u = unit_wait(n);
+                const int ta = u.ta, nt = u.nt, last = u.last, b = u.b, h = u.h;
+                KeyRange r;
+                r.lo = u.lo; r.hi = u.hi; r.sink_tiles = u.sink_tiles; r.first_tile = u.first_tile; r.tiles = 0;
+                unit_done(n);
+                for (int k = ta; k < ta + nt; ++k, ++t) {
+                    const int key0 = r.base(k, kChunkShift) + lane * box_keys, slot = key0 & (c.page_size - 1);
+                    int page = -2;
+                    if (lane < boxes && key0 < r.hi && (key0 + box_keys > r.lo || key0 < p.sinks)) {
+                        page = find_page(c, p.batch, b, key0);
+                        if (page < 0) {
+                            flag_status(p.status, kStatusBadPage);
+                            page = c.n_pages;      // outside the pool: the copy delivers zeros
                         }
                     }
-                }
-            }
-            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
-            chunk_next(p, &cur);
-        }
-        } else if (warp == kChunkMmaWarp || warp == kChunkMmaWarp + 2) {
-        // ================================================================ MMAs
-        // The whole warp walks through the loop, one lane issues.  It is chosen by elect.sync, not by its number: only then
-        // does the compiler know that one lane is active, and eight 128 x 128 x 16 MMAs take 513 cycles to issue
-        // instead of 663 (measured alone; the tensor core needs 512).
-        const int w = __shfl_sync(0xffffffffu, (warp - kChunkMmaWarp) >> 1, 0);  // row tile
-        const uint32_t id_qk = umma_idesc_bf16_m128(kChunkKeys), id_pv = umma_idesc_bf16_m128(D) | (1u << 16);
-        const uint32_t q_lo = (q_smem >> 4) | (1u << 16), k_lo = (ring >> 4) | (1u << 16), v_lo = (ring >> 4) | ((L::kLine >> 4) << 16);
-        const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
-        int t = 0, segment = 0;
-        int ns = 0, np = 0;                        // scores issued and probabilities taken so far
-        while (true) {
-            int ta, tb;
-            chunk_stretch(cur, g0, g1, &ta, &tb);
-            const bool dual = __shfl_sync(0xffffffffu, cur.cost, 0) == 2;
-            const int nt = __shfl_sync(0xffffffffu, tb - ta, 0);
-            const int rounds = dual ? nt : (nt + 1 - w) >> 1;
-            wait_phase(bar_q_full, segment & 1, p.status, &expired);
-            const uint32_t a = q_lo + (dual ? w * (L::kQTile >> 4) : 0);
-            auto scores = [&](int i) {             // S = Q K^T of the i-th tile
-                const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S;
-                wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                __syncwarp();
-                tc_fence_after_sync();
-                const uint32_t d = t_s + (ns & 1) * 64, b = k_lo + st * (L::kTileBytes >> 4);
-                if (elect_one()) {
+                    const int live = __popc(__ballot_sync(0xffffffffu, page >= 0));
+                    const int good = __popc(__ballot_sync(0xffffffffu, page >= 0 && page < c.n_pages));
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-                        umma_bf16(d, umma_desc_of(a + (ks >> 2) * ((128 * 128) >> 4) + (ks & 3) * 2),
-                                  umma_desc_of(b + (ks >> 2) * (L::kLine >> 4) + (ks & 3) * 2), id_qk, ks > 0);
-                    umma_commit(bar_s + 16 * w + 8 * (ns & 1));
-                    umma_commit(bar_empty + 8 * st);
-                    if (!dual) umma_commit(bar_empty + 8 * st);                  // for the row tile that is not there
-                    if (i + 1 == rounds) umma_commit(bar_q_empty);               // the query rows' place is free after the last one
-                }
-                __syncwarp();
-                ++ns;
-            };
-            // Order: two tiles' scores ahead; a buffer's next scores are issued behind the product that reads its probabilities.
-            // With one-tile units the keys of tile k + 4 are waited for while tile k's values are unread: 8 stages at least.
-            if (rounds == 0 && elect_one()) mbar_arrive(bar_q_empty);
-            for (int i = 0; i < 2; ++i)
-                if (i < rounds) scores(i);
-            for (int i = 0; i < rounds; ++i) {
-                const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S;
-                const uint32_t pr = t_s + (np & 1) * 64, b = v_lo + st * (L::kTileBytes >> 4);
-                wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                wait_phase(bar_p + 16 * w + 8 * (np & 1), (np >> 1) & 1, p.status, &expired);
-                __syncwarp();
-                tc_fence_after_sync();
-                if (elect_one()) {
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int x = 2 * t + kv;
+                        const CUtensorMap *tm = kv ? &tmV : &tmK;
+                        if (FMT == kFmtBf16) {
+                            const int st = x % S;
+                            const uint32_t bar = bar_full + 8 * st, dst = ring + st * L::kTileBytes + lane * box_keys * 128;
+                            wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
+                            if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D * 2);
+                            __syncwarp();
+                            if (page >= 0) {
 #pragma unroll
-                    for (int ks = 0; ks < kChunkKeys / 16; ++ks)
-                        umma_bf16_ts(t_o, pr + ks * 8, umma_desc_of(b + ks * (2048 >> 4)), id_pv, i > 0 || ks > 0);
-                    umma_commit(bar_v + 8 * w);
-                    umma_commit(bar_empty + 8 * st);
-                    if (!dual) umma_commit(bar_empty + 8 * st);
-                    if (i + 1 == rounds) umma_commit(bar_o + 8 * w);
+                                for (int hb = 0; hb < L::kHalves; ++hb)
+                                    tma_load_5d(dst + hb * L::kLine, tm, 0, slot, hb, h, page, bar);
+                            }
+                        } else {
+                            const int st = x % L::kRaw;
+                            const uint32_t bar = bar_raw_full + 8 * st;
+                            const uint32_t sc = raw_scale + st * L::kRawScale + lane * box_keys * (D / kFmtBlock);
+                            const uint32_t sc_bytes = box_keys * (D / kFmtBlock);
+                            wait_phase(bar_raw_empty + 8 * st, ((x / L::kRaw) & 1) ^ 1, p.status, &expired);
+                            if (page == c.n_pages)
+                                for (uint32_t y = 0; y < sc_bytes; y += 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + y), "r"(0) : "memory");
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D + good * sc_bytes);
+                            __syncwarp();
+                            if (page >= 0) {
+                                tma_load_5d(rawk + st * L::kRawTile + lane * box_keys * D, tm, 0, slot, 0, h, page, bar);
+                                if (page < c.n_pages)
+                                    bulk_load(sc, (kv ? c.v_scale : c.k_scale) + scale_offset(c, page, h, slot), sc_bytes, bar);
+                            }
+                        }
+                    }
                 }
-                __syncwarp();
-                ++np;
-                if (i + 2 < rounds) scores(i + 2);
+                if (last) break;
             }
-            t += nt;
-            ++segment;
-            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
-            chunk_next(p, &cur);
-        }
+        } else {
+            // ============================================================ MMAs
+            // The whole warp walks through the loop, one lane issues.  It is chosen by elect.sync, not by its number: only then
+            // does the compiler know that one lane is active, and eight 128 x 128 x 16 MMAs take 513 cycles to issue
+            // instead of 663 (measured alone; the tensor core needs 512).
+            const int w = __shfl_sync(0xffffffffu, (warp - kChunkMmaWarp) >> 1, 0);  // row tile
+            const uint32_t id_qk = umma_idesc_bf16_m128(kChunkKeys), id_pv = umma_idesc_bf16_m128(D) | (1u << 16);
+            const uint32_t q_lo = (q_smem >> 4) | (1u << 16), k_lo = (ring >> 4) | (1u << 16), v_lo = (ring >> 4) | ((L::kLine >> 4) << 16);
+            const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
+            int t = 0;
+            int ns = 0, np = 0;                    // scores issued and probabilities taken so far
+            for (int n = 0;; ++n) {
+                const ChunkUnit &u = unit_wait(n);
+                const bool dual = __shfl_sync(0xffffffffu, u.dual, 0) != 0;
+                const int nt = __shfl_sync(0xffffffffu, u.nt, 0), last = __shfl_sync(0xffffffffu, u.last, 0);
+                unit_done(n);
+                const int rounds = dual ? nt : (nt + 1 - w) >> 1;
+                wait_phase(bar_q_full, n & 1, p.status, &expired);
+                const uint32_t a = q_lo + (dual ? w * (L::kQTile >> 4) : 0);
+                auto scores = [&](int i) {         // S = Q K^T of the i-th tile
+                    const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S;
+                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                    __syncwarp();
+                    tc_fence_after_sync();
+                    const uint32_t d = t_s + (ns & 1) * 64, b = k_lo + st * (L::kTileBytes >> 4);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks)
+                            umma_bf16(d, umma_desc_of(a + (ks >> 2) * ((128 * 128) >> 4) + (ks & 3) * 2),
+                                      umma_desc_of(b + (ks >> 2) * (L::kLine >> 4) + (ks & 3) * 2), id_qk, ks > 0);
+                        umma_commit(bar_s + 16 * w + 8 * (ns & 1));
+                        umma_commit(bar_empty + 8 * st);
+                        if (!dual) umma_commit(bar_empty + 8 * st);              // for the row tile that is not there
+                        if (i + 1 == rounds) umma_commit(bar_q_empty);           // the query rows' place is free after the last one
+                    }
+                    __syncwarp();
+                    ++ns;
+                };
+                // Order: two tiles' scores ahead; a buffer's next scores are issued behind the product that reads its probabilities.
+                // With one-tile units the keys of tile k + 4 are waited for while tile k's values are unread: 8 stages at least.
+                if (rounds == 0 && elect_one()) mbar_arrive(bar_q_empty);
+                for (int i = 0; i < 2; ++i)
+                    if (i < rounds) scores(i);
+                for (int i = 0; i < rounds; ++i) {
+                    const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S;
+                    const uint32_t pr = t_s + (np & 1) * 64, b = v_lo + st * (L::kTileBytes >> 4);
+                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                    wait_phase(bar_p + 16 * w + 8 * (np & 1), (np >> 1) & 1, p.status, &expired);
+                    __syncwarp();
+                    tc_fence_after_sync();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < kChunkKeys / 16; ++ks)
+                            umma_bf16_ts(t_o, pr + ks * 8, umma_desc_of(b + ks * (2048 >> 4)), id_pv, i > 0 || ks > 0);
+                        umma_commit(bar_v + 8 * w);
+                        umma_commit(bar_empty + 8 * st);
+                        if (!dual) umma_commit(bar_empty + 8 * st);
+                        if (i + 1 == rounds) umma_commit(bar_o + 8 * w);
+                    }
+                    __syncwarp();
+                    ++np;
+                    if (i + 2 < rounds) scores(i + 2);
+                }
+                t += nt;
+                if (last) break;
+            }
         }
     } else if (warp >= kChunkFeedWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kFeedRegs));
         // ================================================================ query rows; codes to bf16
         const int ft = tid - kChunkFeedWarp * 32;  // 0 .. 127
-        int t = 0, segment = 0;
-        while (true) {
-            int ta, tb;
-            chunk_stretch(cur, g0, g1, &ta, &tb);
-            wait_phase(bar_q_empty, (segment & 1) ^ 1, p.status, &expired);
+        int t = 0;
+        for (int n = 0;; ++n) {
+            const ChunkUnit &un = unit_wait(n);
+            const int last = un.last;
+            wait_phase(bar_q_empty, (n & 1) ^ 1, p.status, &expired);
             constexpr int kChunks = D / 8;         // 16-byte pieces per row
-            for (int y0 = ft; y0 < cur.cost * 128 * kChunks; y0 += 8 * 128) {     // eight loads in flight per thread
+            for (int y0 = ft; y0 < (un.dual ? 256 : 128) * kChunks; y0 += 8 * 128) {     // eight loads in flight per thread
                 uint4 v[8];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const int y = y0 + u * 128, row = y / kChunks, ch = y - row * kChunks;
                     v[u] = make_uint4(0, 0, 0, 0);
-                    if (row < cur.rows) {
-                        const int i = (cur.row0 + row) / p.group, gq = cur.row0 + row - i * p.group;
+                    if (row < un.rows) {
+                        const int i = (un.row0 + row) / p.group, gq = un.row0 + row - i * p.group;
                         v[u] = __ldg(reinterpret_cast<const uint4 *>(
-                            p.q + 2 * ((static_cast<int64_t>(cur.s.token0) + i) * p.q_stride + (static_cast<int64_t>(cur.h) * p.group + gq) * D + 8 * ch)));
+                            p.q + 2 * ((static_cast<int64_t>(un.token0) + i) * p.q_stride + (static_cast<int64_t>(un.h) * p.group + gq) * D + 8 * ch)));
                     }
                 }
 #pragma unroll
@@ -515,7 +577,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             fence_async_shared();
             mbar_arrive(bar_q_full);
             if (FMT == kFmtE4m3) {
-                for (int k = ta; k < tb; ++k, ++t)
+                for (int k = un.ta, end = un.ta + un.nt; k < end; ++k, ++t)
                     for (int kv = 0; kv < 2; ++kv) {
                         // half a key per thread: threads 0-63 the first half of the dimensions, 64-127 the second
                         const int x = 2 * t + kv, st = x % S, rs = x % L::kRaw, key = ft & 63, part = ft >> 6;
@@ -535,7 +597,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                         else
                             asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(sa) : "memory");
                         // a key no query of the unit sees was perhaps not even loaded: zeros
-                        const bool keep = seen_by_any(cur.r, p.sinks, cur.r.base(k, kChunkShift) + key);
+                        const bool keep = un.seen(p.sinks, un.base(k) + key);
                         wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
                         const uint32_t dst = ring + st * L::kTileBytes + key * 128;
 #pragma unroll
@@ -569,9 +631,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                         mbar_arrive(bar_raw_empty + 8 * rs);
                     }
             }
-            ++segment;
-            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
-            chunk_next(p, &cur);
+            unit_done(n);
+            if (last) break;
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kSoftmaxRegs));
@@ -581,30 +642,31 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         const uint32_t t_o = tmem + lanes + 256 + w * 128;
         int t = 0, ns = 0;
         int outputs[2] = {0, 0};                   // finished outputs per accumulator
-        while (true) {
-            int ta, tb;
-            chunk_stretch(cur, g0, g1, &ta, &tb);
-            const bool dual = cur.cost == 2;
-            const int nt = tb - ta, rounds = dual ? nt : (nt + 1 - w) >> 1;
+        for (int n = 0;; ++n) {
+            const ChunkUnit &u = unit_wait(n);
+            const bool dual = u.dual != 0;
+            const int ta = u.ta, nt = u.nt, rounds = dual ? nt : (nt + 1 - w) >> 1;
             const int my_row = dual ? w * 128 + row : row;                       // packed row within the unit
-            const int pos = cur.s.p0 + (cur.row0 + min(my_row, cur.rows - 1)) / p.group;
-            // positions of this row tile's first and last row, for tiles that need no mask
-            const int row_a = dual ? w * 128 : 0, row_b = min(row_a + 127, cur.rows - 1);
-            const int pos_a = cur.s.p0 + (cur.row0 + row_a) / p.group, pos_b = cur.s.p0 + (cur.row0 + row_b) / p.group;
+            const int pos = u.p0 + (u.row0 + min(my_row, u.rows - 1)) / p.group;
+            // A tile needs no mask if its last key is no later than the row tile's first position (and in the cache), and its first
+            // key is in the window of the row tile's last one, or all of it are sinks.
+            const int row_a = dual ? w * 128 : 0, row_b = min(row_a + 127, u.rows - 1);
+            const int no_later = min(u.p0 + (u.row0 + row_a) / p.group, u.len - 1) - (kChunkKeys - 1);
+            const int no_sooner = p.window ? u.p0 + (u.row0 + row_b) / p.group - p.window + 1 : -0x40000000;
+            const int sink_tiles = u.sink_tiles, first_tile = u.first_tile - sink_tiles;
             float m = -INFINITY, l = 0.f;
             for (int i = 0; i < rounds; ++i) {
                 const int k = dual ? i : 2 * i + w;
-                const int key0 = cur.r.base(ta + k, kChunkShift);
-                const bool whole = key0 + kChunkKeys - 1 <= pos_a && key0 + kChunkKeys <= cur.s.len &&
-                                   (p.window == 0 || key0 > pos_b - p.window || key0 + kChunkKeys <= p.sinks);
-                if (FMT == kFmtBf16) {
+                const int kt = ta + k, key0 = (kt < sink_tiles ? kt : kt + first_tile) << kChunkShift;
+                const bool whole = key0 <= no_later && (key0 >= no_sooner || key0 + kChunkKeys <= p.sinks);
+                if (FMT == kFmtBf16 && !whole) {
                     // values no query sees may be anything, and were perhaps not even loaded: zeros, so that 0 * NaN cannot arise
                     // (both row tiles' threads write them: each has its own product to come)
-                    const bool clean = key0 + kChunkKeys <= cur.r.hi && (key0 >= cur.r.lo || key0 + kChunkKeys <= p.sinks);
+                    const bool clean = key0 + kChunkKeys <= u.hi && (key0 >= u.lo || key0 + kChunkKeys <= p.sinks);
                     if (!clean) {
                         const int x = 2 * (t + k) + 1, st = x % S;
                         wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                        if (row < kChunkKeys * L::kHalves && !seen_by_any(cur.r, p.sinks, key0 + (row & 63))) {
+                        if (row < kChunkKeys * L::kHalves && !u.seen(p.sinks, key0 + (row & 63))) {
                             const uint32_t dst = ring + st * L::kTileBytes + (row >> 6) * L::kLine + (row & 63) * 128;
 #pragma unroll
                             for (int ch = 0; ch < 8; ++ch)
@@ -624,7 +686,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 tmem_wait_ld(v[0]);
                 tmem_wait_ld(v[1]);
                 if (!whole) {
-                    const int limit = min(pos + 1, cur.s.len) - key0;            // columns from here on lie ahead or beyond the context
+                    const int limit = min(pos + 1, u.len) - key0;            // columns from here on lie ahead or beyond the context
                     const int low = p.window ? pos - p.window + 1 - key0 : -0x40000000, sink = p.sinks - key0;
 #pragma unroll
                     for (int col = 0; col < kChunkKeys; ++col)
@@ -683,8 +745,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
 
             // ---- output: this thread's row
-            const int64_t unit_last = cur.begin + static_cast<int64_t>(cur.cost) * (cur.r.tiles - 1);
-            const bool alone = ta == 0 && tb == cur.r.tiles;
+            const bool alone = u.part < 0;
             if (rounds > 0) {
                 wait_phase(bar_o + 8 * w, outputs[w] & 1, p.status, &expired);
                 __syncwarp();
@@ -692,7 +753,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
             float *const parts = reinterpret_cast<float *>(p.workspace + kChunkPartOffset);
             constexpr size_t kPart = kChunkRows * (D + 2);
-            float *const my_part = parts + (2 * blockIdx.x + (cur.begin <= g0 ? 0 : 1)) * kPart;
+            // (a unit of this block alone has no place; its two accumulators' statistics meet in the second)
+            float *const my_part = parts + (2 * blockIdx.x + (u.part < 0 ? 1 : u.part)) * kPart;
             float f0 = 1.f, f1 = 0.f;              // one-tile units: factors of the two accumulators
             if (!dual) {
                 // through the places of rows 128 .. 255, which such a unit does not have
@@ -717,9 +779,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 }
             }
             const bool holds = dual || w == 0;
-            const bool live = holds && my_row < cur.rows;
-            const int pi = (cur.row0 + my_row) / p.group, hq = cur.h * p.group + (cur.row0 + my_row - pi * p.group);
-            const int64_t token = static_cast<int64_t>(cur.s.token0) + pi;
+            const bool live = holds && my_row < u.rows;
+            const int pi = (u.row0 + my_row) / p.group, hq = u.h * p.group + (u.row0 + my_row - pi * p.group);
+            const int64_t token = static_cast<int64_t>(u.token0) + pi;
             if (holds) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -764,19 +826,19 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             if (!alone) {
                 // blocks that hold a part of the unit: first .. last; the counter is the first one's
                 uint32_t *const counters = reinterpret_cast<uint32_t *>(p.workspace + kAttnCounterBytes);
-                const int first = static_cast<int>(((cur.begin + 1) * ctas - 1) / W), last = static_cast<int>(((unit_last + 1) * ctas - 1) / W);
+                const int first = u.first, blocks = u.blocks;
                 fence_gpu();
                 named_sync(1, 256);
                 if (tid == 0) {
                     const uint32_t seen = atomicAdd(counters + first, 1u);
-                    s_last = seen == static_cast<uint32_t>(last - first);
+                    s_last = seen == static_cast<uint32_t>(blocks - 1);
                     if (s_last) counters[first] = 0;                             // ready for the next call
                 }
                 named_sync(1, 256);
                 if (s_last) {
                     fence_gpu();
-                    const int first_slot = cur.begin <= W * first / ctas ? 0 : 1;
-                    if (tid < cur.rows) {          // one row per thread, 32 columns at a time
+                    const int first_slot = u.first_part, last = first + blocks - 1;
+                    if (tid < u.rows) {          // one row per thread, 32 columns at a time
                         const int r = tid;
                         auto part_of = [&](int k) { return parts + (2 * k + (k == first ? first_slot : 0)) * kPart; };
                         float M = -INFINITY, Lsum = 0.f;
@@ -786,8 +848,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                             Lsum += (mk == -INFINITY ? 0.f : exp2_fast(mk - M)) * __ldcg(part_of(k) + kChunkRows * D + kChunkRows + r);
                         }
                         const float inv = Lsum == 0.f ? 0.f : 1.f / Lsum;
-                        const int i = (cur.row0 + r) / p.group, hr = cur.h * p.group + (cur.row0 + r - i * p.group);
-                        const int64_t tok = static_cast<int64_t>(cur.s.token0) + i;
+                        const int i = (u.row0 + r) / p.group, hr = u.h * p.group + (u.row0 + r - i * p.group);
+                        const int64_t tok = static_cast<int64_t>(u.token0) + i;
                         if (p.lse) p.lse[tok * p.heads_q + hr] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
                         for (int q = 0; q < D / 32; ++q) {
                             float4 a[8];
@@ -818,8 +880,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             t += nt;
             outputs[0] += 1;                       // the first accumulator has a tile in every unit
             outputs[1] += dual || nt > 1;
-            if (cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles >= g1) break;
-            chunk_next(p, &cur);
+            const int last = u.last;
+            unit_done(n);
+            if (last) break;
         }
     }
     tc_fence_before_sync();
