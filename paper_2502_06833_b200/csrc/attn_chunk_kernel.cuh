@@ -44,7 +44,7 @@ struct ChunkLayout {
     static constexpr int kStages = D == 64 ? 16 : FMT == kFmtBf16 ? 10 : 8;   // at least 8: see the order of the MMAs
     static constexpr int kRawTile = FMT == kFmtE4m3 ? kChunkKeys * D : 0;
     static constexpr int kRawScale = FMT == kFmtE4m3 ? kChunkKeys * (D / kFmtBlock) : 0;
-    static constexpr int kRaw = 4;                                       // stages of codes
+    static constexpr int kRaw = 3;                                       // stages of codes
     static constexpr int kRawBytes = kRaw * (kRawTile + kRawScale);
     static constexpr int kBars = 2 * kStages + 2 * kRaw + 18;
     static constexpr int kSmem = 1024 + 2 * kQTile + kStages * kTileBytes + kRawBytes + 8 * kBars;
@@ -53,8 +53,10 @@ struct ChunkLayout {
     static_assert(2 * kSoftmaxRegs + kIssueRegs + kFeedRegs <= 512, "more than the block was launched with");
 };
 
-// ---- the string of tiles: units in the order (sequence, cache head, run of rows); a tile of a two-tile unit
-// costs 2, one of a one-tile unit 1, and belongs to the block in whose stretch it begins
+// ---- the string of tiles: units in the order (sequence, cache head, run of rows); a unit costs kChunkUnitCost (query rows
+// in, output out: about 20 000 cycles against 2 100 per key tile of two row tiles), then 2 per tile of a two-tile unit,
+// 1 of a one-tile unit; a tile belongs to the block in whose stretch it begins
+constexpr int kChunkUnitCost = 12;
 struct ChunkCursor {
     int b, h, blk;                                // sequence, cache head, run of 256 rows
     int64_t begin;                                // the unit's place in the string
@@ -63,6 +65,9 @@ struct ChunkCursor {
     int pa, pb;                                   // positions of its first and last token
     int cost;                                     // per tile
     KeyRange r;
+    __device__ __forceinline__ int length() const { return kChunkUnitCost + cost * r.tiles; }
+    // where the first tile begins
+    __device__ __forceinline__ int64_t tiles_at() const { return begin + kChunkUnitCost; }
 };
 __device__ __forceinline__ int chunk_blocks(const AttnParams &p, const SeqInfo &s)
 {
@@ -82,7 +87,7 @@ __device__ __forceinline__ void chunk_unit(const AttnParams &p, const SeqInfo &s
 // Moves on to the next unit.
 __device__ __forceinline__ void chunk_next(const AttnParams &p, ChunkCursor *c)
 {
-    c->begin += static_cast<int64_t>(c->cost) * c->r.tiles;
+    c->begin += c->length();
     int blk = c->blk + 1;
     if (blk >= chunk_blocks(p, c->s)) {
         blk = 0;
@@ -99,8 +104,8 @@ __device__ __forceinline__ void chunk_next(const AttnParams &p, ChunkCursor *c)
 // The unit's tiles that begin within [g0, g1).
 __device__ __forceinline__ void chunk_stretch(const ChunkCursor &c, int64_t g0, int64_t g1, int *ta, int *tb)
 {
-    const int64_t a = (g0 - c.begin + c.cost - 1) / c.cost, b = (g1 - c.begin + c.cost - 1) / c.cost;
-    *ta = g0 <= c.begin ? 0 : static_cast<int>(a);
+    const int64_t at = c.tiles_at(), a = (g0 - at + c.cost - 1) / c.cost, b = (g1 - at + c.cost - 1) / c.cost;
+    *ta = g0 <= at ? 0 : static_cast<int>(a);
     *tb = b < c.r.tiles ? static_cast<int>(b) : c.r.tiles;
 }
 
@@ -244,6 +249,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     __shared__ int64_t s_scan[kChunkWarps];
     __shared__ int s_b, s_last;
     __shared__ ChunkUnit s_unit[2];
+    __shared__ float s_stat[2][128];               // maxima and sums of a one-tile unit's second accumulator
     __shared__ int64_t s_before;
     __shared__ uint32_t s_tmem;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -306,7 +312,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         if (blocks && blocks <= 2)
             for (int k = 0; k < blocks; ++k) {
                 chunk_unit(p, s, k, &u);
-                cost += u.cost * u.r.tiles;
+                cost += u.length();
             }
         while (many) {                             // long chunks: the warp's lanes share the runs of one sequence
             const int src = __ffs(many) - 1;
@@ -320,7 +326,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             int part = 0;
             for (int k = lane; k < nb; k += 32) {
                 chunk_unit(p, t, k, &u);
-                part += u.cost * u.r.tiles;
+                part += u.length();
             }
             part = __reduce_add_sync(0xffffffffu, part);
             if (lane == src) cost = part;
@@ -374,7 +380,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         cur.begin = s_before + static_cast<int64_t>(cur.h) * cost;
         chunk_unit(p, cur.s, 0, &cur);
         // the first unit with a tile that begins at g0 or later
-        while (cur.begin + static_cast<int64_t>(cur.cost) * (cur.r.tiles - 1) < g0) chunk_next(p, &cur);
+        while (cur.tiles_at() + static_cast<int64_t>(cur.cost) * (cur.r.tiles - 1) < g0) chunk_next(p, &cur);
     }
     __syncthreads();                               // s_cost is done with; its place takes query rows now
 
@@ -398,7 +404,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             for (int n = 0;; ++n) {
                 int ta, tb;
                 chunk_stretch(cur, g0, g1, &ta, &tb);
-                const int64_t end = cur.begin + static_cast<int64_t>(cur.cost) * cur.r.tiles;
+                const int64_t at = cur.tiles_at(), end = at + static_cast<int64_t>(cur.cost) * cur.r.tiles;
                 wait_phase(bar_u_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, p.status, &expired);
                 __syncwarp();
                 if (lane == 0) {
@@ -409,15 +415,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                     u.lo = cur.r.lo; u.hi = cur.r.hi; u.sink_tiles = cur.r.sink_tiles; u.first_tile = cur.r.first_tile;
                     u.ta = ta; u.nt = tb - ta;
                     u.dual = cur.cost == 2;
-                    u.last = end >= g1;
-                    u.part = ta == 0 && tb == cur.r.tiles ? -1 : cur.begin <= g0 ? 0 : 1;
+                    u.last = end + kChunkUnitCost >= g1;   // where the next unit's first tile would begin
+                    u.part = ta == 0 && tb == cur.r.tiles ? -1 : at <= g0 ? 0 : 1;
                     // blocks in whose stretch its first and its last tile begin
-                    u.first = static_cast<int>(((cur.begin + 1) * ctas - 1) / W);
+                    u.first = static_cast<int>(((at + 1) * ctas - 1) / W);
                     u.blocks = static_cast<int>(((end - cur.cost + 1) * ctas - 1) / W) - u.first + 1;
-                    u.first_part = cur.begin <= W * u.first / ctas ? 0 : 1;
+                    u.first_part = at <= W * u.first / ctas ? 0 : 1;
                     mbar_arrive(bar_u_full + 8 * (n & 1));
                 }
-                if (end >= g1) break;
+                if (end + kChunkUnitCost >= g1) break;
                 chunk_next(p, &cur);
             }
         } else if (warp == kChunkLoadWarp) {
@@ -430,16 +436,22 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 KeyRange r;
                 r.lo = u.lo; r.hi = u.hi; r.sink_tiles = u.sink_tiles; r.first_tile = u.first_tile; r.tiles = 0;
                 unit_done(n);
+                // this lane's box of a tile: its page as the table has it, or -2 if no query sees any of it
+                auto look_up = [&](int k) {
+                    const int at = r.base(k, kChunkShift) + lane * box_keys;
+                    const bool any = lane < boxes && at < r.hi && (at + box_keys > r.lo || at < p.sinks);
+                    return any ? max(__ldg(p.batch.page_table + static_cast<int64_t>(b) * p.batch.table_stride + (at >> c.page_shift)), -1) : -2;
+                };
+                int entry = look_up(ta);
                 for (int k = ta; k < ta + nt; ++k, ++t) {
-                    const int key0 = r.base(k, kChunkShift) + lane * box_keys, slot = key0 & (c.page_size - 1);
-                    int page = -2;
-                    if (lane < boxes && key0 < r.hi && (key0 + box_keys > r.lo || key0 < p.sinks)) {
-                        page = find_page(c, p.batch, b, key0);
-                        if (page < 0) {
-                            flag_status(p.status, kStatusBadPage);
-                            page = c.n_pages;      // outside the pool: the copy delivers zeros
-                        }
+                    const int slot = (r.base(k, kChunkShift) + lane * box_keys) & (c.page_size - 1);
+                    const int next = k + 1 < ta + nt ? look_up(k + 1) : -2;       // its latency runs under this tile's waits
+                    int page = entry;
+                    if (page != -2 && (page < 0 || page >= c.n_pages)) {
+                        flag_status(p.status, kStatusBadPage);
+                        page = c.n_pages;          // outside the pool: the copy delivers zeros
                     }
+                    entry = next;
                     const int live = __popc(__ballot_sync(0xffffffffu, page >= 0));
                     const int good = __popc(__ballot_sync(0xffffffffu, page >= 0 && page < c.n_pages));
 #pragma unroll
@@ -555,25 +567,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             const int last = un.last;
             wait_phase(bar_q_empty, (n & 1) ^ 1, p.status, &expired);
             constexpr int kChunks = D / 8;         // 16-byte pieces per row
-            for (int y0 = ft; y0 < (un.dual ? 256 : 128) * kChunks; y0 += 8 * 128) {     // eight loads in flight per thread
-                uint4 v[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int y = y0 + u * 128, row = y / kChunks, ch = y - row * kChunks;
-                    v[u] = make_uint4(0, 0, 0, 0);
-                    if (row < un.rows) {
-                        const int i = (un.row0 + row) / p.group, gq = un.row0 + row - i * p.group;
-                        v[u] = __ldg(reinterpret_cast<const uint4 *>(
-                            p.q + 2 * ((static_cast<int64_t>(un.token0) + i) * p.q_stride + (static_cast<int64_t>(un.h) * p.group + gq) * D + 8 * ch)));
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int y = y0 + u * 128, row = y / kChunks, ch = y - row * kChunks;
-                    const uint32_t dst = q_smem + (row >> 7) * L::kQTile + (ch >> 3) * (128 * 128) + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[u].x), "r"(v[u].y), "r"(v[u].z), "r"(v[u].w) : "memory");
-                }
+            const uint8_t *const q0 = p.q + 2 * (static_cast<int64_t>(un.token0) * p.q_stride + static_cast<int64_t>(un.h) * p.group * D);
+            const int rows = un.rows, row0 = un.row0;
+#pragma unroll 4
+            for (int y = ft; y < (un.dual ? 256 : 128) * kChunks; y += 128) {        // all copies in flight at once
+                const int row = y / kChunks, ch = y - row * kChunks, i = (row0 + row) / p.group, gq = row0 + row - i * p.group;
+                const uint8_t *src = row < rows ? q0 + 2 * (i * p.q_stride + gq * D + 8 * ch) : p.q;   // zeros behind the last row
+                const uint32_t dst = q_smem + (row >> 7) * L::kQTile + (ch >> 3) * (128 * 128) + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(row < rows ? 16 : 0) : "memory");
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
             fence_async_shared();
             mbar_arrive(bar_q_full);
             if (FMT == kFmtE4m3) {
@@ -753,19 +756,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
             float *const parts = reinterpret_cast<float *>(p.workspace + kChunkPartOffset);
             constexpr size_t kPart = kChunkRows * (D + 2);
-            // (a unit of this block alone has no place; its two accumulators' statistics meet in the second)
-            float *const my_part = parts + (2 * blockIdx.x + (u.part < 0 ? 1 : u.part)) * kPart;
+            float *const my_part = parts + (2 * blockIdx.x + (u.part < 0 ? 0 : u.part)) * kPart;   // not used by a unit of this block alone
             float f0 = 1.f, f1 = 0.f;              // one-tile units: factors of the two accumulators
             if (!dual) {
-                // through the places of rows 128 .. 255, which such a unit does not have
-                volatile float *const ml = my_part + kChunkRows * D + 128 + row;
                 if (w == 1) {
-                    ml[0] = m;
-                    ml[kChunkRows] = l;
+                    s_stat[0][row] = m;
+                    s_stat[1][row] = l;
                 }
                 named_sync(1, 256);
                 if (w == 0) {
-                    const float m1 = ml[0], l1 = ml[kChunkRows];
+                    const float m1 = s_stat[0][row], l1 = s_stat[1][row];
                     const float M = fmaxf(m, m1);
                     f0 = m == -INFINITY ? (M == -INFINITY ? 1.f : 0.f) : exp2_fast(m - M);
                     f1 = m1 == -INFINITY ? 0.f : exp2_fast(m1 - M);
@@ -822,7 +822,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 }
                 tc_fence_before_sync();
             }
-            if (!dual) named_sync(1, 256);         // the second accumulator may be written again
+            if (!dual) named_sync(1, 256);         // the second accumulator and s_stat may be written again
             if (!alone) {
                 // blocks that hold a part of the unit: first .. last; the counter is the first one's
                 uint32_t *const counters = reinterpret_cast<uint32_t *>(p.workspace + kAttnCounterBytes);

@@ -28,7 +28,8 @@ namespace {
     } while (0)
 
 constexpr int kMaxDevices = 64;
-constexpr int kChunkMinCost = 16;         // tiles of 128 rows x 64 keys per block, likewise; at least 2
+constexpr int kChunkMinCost = 24;         // cost per block (a tile of 128 rows x 64 keys: 1), likewise
+static_assert(kChunkMinCost >= kChunkUnitCost + 2, "every block's stretch has to hold the beginning of a tile");
 constexpr int kFewMinTiles = 16;          // tiles of 8 KiB per block before another block is worth its part in the join
 
 struct DeviceInfo {
