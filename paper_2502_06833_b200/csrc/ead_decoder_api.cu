@@ -28,6 +28,8 @@ namespace {
     } while (0)
 
 constexpr int kMaxDevices = 64;
+constexpr int kKvRun = 4;                 // tokens per warp of the cache's write and read ...
+constexpr int kKvLongRunTokens = 1024;    // ... from this many tokens on; before, one
 constexpr int kChunkMinCost = 24;         // cost per block (a tile of 128 rows x 64 keys: 1), likewise
 static_assert(kChunkMinCost >= kChunkUnitCost + 2, "every block's stretch has to hold the beginning of a tile");
 constexpr int kFewMinTiles = 16;          // tiles of 8 KiB per block before another block is worth its part in the join
@@ -211,10 +213,11 @@ int move_setup(const ead_kv_cache *cache, const ead_kv_batch *batch, const void 
     return EAD_OK;
 }
 
-dim3 move_grid(const KvMoveParams &p, const DeviceInfo &d)
+// One warp per run of tokens and stretch of a token's values.
+dim3 move_grid(const KvMoveParams &p, int run)
 {
-    const int per_block = kKvThreads / 32;
-    return dim3(std::min((p.batch.n_tokens + per_block - 1) / per_block, 8 * d.sms));
+    const int warps = (p.batch.n_tokens + run - 1) / run, per_block = kKvThreads / 32;
+    return dim3((warps + per_block - 1) / per_block, (2 * p.cache.heads * p.cache.head_dim + kKvPass - 1) / kKvPass);
 }
 
 }  // namespace
@@ -227,10 +230,13 @@ extern "C" int ead_kv_write(const ead_kv_cache *cache, const ead_kv_batch *batch
     const int rc = move_setup(cache, batch, k_new, v_new, new_stride, status, true, device, &p, &d);
     if (rc != EAD_OK || p.batch.n_tokens == 0) return rc;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cache->format == EAD_FMT_BF16)
-        ead_kv_write_kernel<kFmtBf16><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+    const bool bf16 = cache->format == EAD_FMT_BF16;
+    if (p.batch.n_tokens < kKvLongRunTokens)
+        bf16 ? ead_kv_write_kernel<kFmtBf16, 1><<<move_grid(p, 1), kKvThreads, 0, s>>>(p)
+             : ead_kv_write_kernel<kFmtE4m3, 1><<<move_grid(p, 1), kKvThreads, 0, s>>>(p);
     else
-        ead_kv_write_kernel<kFmtE4m3><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+        bf16 ? ead_kv_write_kernel<kFmtBf16, kKvRun><<<move_grid(p, kKvRun), kKvThreads, 0, s>>>(p)
+             : ead_kv_write_kernel<kFmtE4m3, kKvRun><<<move_grid(p, kKvRun), kKvThreads, 0, s>>>(p);
     return launched();
 }
 
@@ -244,10 +250,13 @@ extern "C" int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch,
     if (rc != EAD_OK || p.batch.n_tokens == 0) return rc;
     p.first = first;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cache->format == EAD_FMT_BF16)
-        ead_kv_read_kernel<kFmtBf16><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+    const bool bf16 = cache->format == EAD_FMT_BF16;
+    if (p.batch.n_tokens < kKvLongRunTokens)
+        bf16 ? ead_kv_read_kernel<kFmtBf16, 1><<<move_grid(p, 1), kKvThreads, 0, s>>>(p)
+             : ead_kv_read_kernel<kFmtE4m3, 1><<<move_grid(p, 1), kKvThreads, 0, s>>>(p);
     else
-        ead_kv_read_kernel<kFmtE4m3><<<move_grid(p, *d), kKvThreads, 0, s>>>(p);
+        bf16 ? ead_kv_read_kernel<kFmtBf16, kKvRun><<<move_grid(p, kKvRun), kKvThreads, 0, s>>>(p)
+             : ead_kv_read_kernel<kFmtE4m3, kKvRun><<<move_grid(p, kKvRun), kKvThreads, 0, s>>>(p);
     return launched();
 }
 

@@ -1,8 +1,8 @@
 // Writing new tokens into the paged cache and reading tokens back.  Both move every byte once and
 // compute next to nothing, so HBM bounds them at size and the launch bounds them at one step.
-// One warp serves one token at a time: its row of 2 x heads x head_dim values is contiguous on the
-// caller's side (except between k and v), its place is looked up once, and in passes of 512 values
-// every lane moves 16 consecutive ones, which is one 16-byte store of codes and half a scale block.
+// A warp moves one stretch of 512 of a token's 2 x heads x head_dim values, 16 consecutive ones per lane (one 16-byte
+// store of codes, half a scale block), for a run of consecutive tokens: its lanes look up the places of all of
+// them at once, so the chain new_start -> kv_len -> page table -> data costs its latency once per run.
 #pragma once
 #include "kv_format.cuh"
 #include "ptx_sm100.cuh"
@@ -11,7 +11,7 @@ namespace ead {
 
 constexpr int kKvThreads = 256;
 constexpr int kKvLaneValues = 16;
-constexpr int kKvPass = 32 * kKvLaneValues;       // values a warp moves per pass
+constexpr int kKvPass = 32 * kKvLaneValues;       // values a warp moves of a token
 
 struct KvMoveParams {
     KvCacheView cache;
@@ -22,134 +22,139 @@ struct KvMoveParams {
     uint32_t *status;
 };
 
-template <int FMT>
+// Data that is used once.
+__device__ __forceinline__ uint4 load_once(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// Page and slot of token t0 + lane for the lanes below n (page -1: no valid place).
+template <bool WRITE>
+__device__ __forceinline__ void find_places(const KvMoveParams &p, int t0, int n, int lane, int *page, int *slot)
+{
+    int b = find_sequence(p.batch.new_start, p.batch.B, t0, lane);
+    const int t = t0 + lane;
+    *page = -1;
+    *slot = 0;
+    if (lane < n) {
+        while (b + 1 < p.batch.B && __ldg(p.batch.new_start + b + 1) <= t) ++b;
+        const int pos = WRITE ? __ldg(p.batch.kv_len + b) - (__ldg(p.batch.new_start + b + 1) - t)
+                              : (p.first ? __ldg(p.first + b) : 0) + t - __ldg(p.batch.new_start + b);
+        *page = find_page(p.cache, p.batch, b, pos);
+        *slot = pos & (p.cache.page_size - 1);
+        if (*page < 0) flag_status(p.status, kStatusBadPage);
+    }
+    __syncwarp();
+}
+
+// RUN tokens per warp, all their loads in flight before the first store.
+template <int FMT, int RUN>
 __global__ void __launch_bounds__(kKvThreads) ead_kv_write_kernel(KvMoveParams p)
 {
     const int lane = threadIdx.x & 31;
-    const int warp = (blockIdx.x * kKvThreads + threadIdx.x) >> 5, warps = (gridDim.x * kKvThreads) >> 5;
+    const int t0 = ((blockIdx.x * kKvThreads + threadIdx.x) >> 5) * RUN, n = min(RUN, p.batch.n_tokens - t0);
+    if (n <= 0) return;
     const KvCacheView &c = p.cache;
-    const int per_half = c.heads * c.head_dim, total = 2 * per_half;
-    for (int t = warp; t < p.batch.n_tokens; t += warps) {
-        const int b = find_sequence(p.batch.new_start, p.batch.B, t, lane);
-        const int pos = __ldg(p.batch.kv_len + b) - (__ldg(p.batch.new_start + b + 1) - t);
-        const int page = find_page(c, p.batch, b, pos);
-        if (page < 0) {
-            if (lane == 0) flag_status(p.status, kStatusBadPage);
-            continue;
+    const int per_half = c.heads * c.head_dim, off = blockIdx.y * kKvPass + lane * kKvLaneValues;
+    const bool live = off < 2 * per_half, is_v = off >= per_half;
+    const int x = off - (is_v ? per_half : 0), head = x / c.head_dim, d = x - head * c.head_dim;
+    const uint8_t *const row0 = (is_v ? p.rows_v : p.rows_k) + 2 * (t0 * p.row_stride + x);
+    uint8_t *const pool = is_v ? c.v : c.k, *const scales = is_v ? c.v_scale : c.k_scale;
+    uint4 in[RUN][2];
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) {
+        in[i][0] = in[i][1] = make_uint4(0, 0, 0, 0);
+        if (live && i < n) {
+            in[i][0] = load_once(row0 + 2 * i * p.row_stride);
+            in[i][1] = load_once(row0 + 2 * i * p.row_stride + 16);
         }
-        const int slot = pos & (c.page_size - 1);
-        for (int base = 0; base < total; base += 2 * kKvPass) {      // two passes' loads in flight
-            uint4 in[2][2];
-            int off[2];
+    }
+    int pages, slots;
+    find_places<true>(p, t0, n, lane, &pages, &slots);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                off[u] = base + u * kKvPass + lane * kKvLaneValues;
-                if (off[u] < total) {
-                    const bool is_v = off[u] >= per_half;
-                    const uint8_t *row = (is_v ? p.rows_v : p.rows_k) + 2 * (t * p.row_stride + off[u] - (is_v ? per_half : 0));
-                    in[u][0] = __ldg(reinterpret_cast<const uint4 *>(row));
-                    in[u][1] = __ldg(reinterpret_cast<const uint4 *>(row) + 1);
-                } else {
-                    in[u][0] = in[u][1] = make_uint4(0, 0, 0, 0);
-                }
+    for (int i = 0; i < RUN; ++i) {
+        const int page = __shfl_sync(0xffffffffu, pages, i), slot = __shfl_sync(0xffffffffu, slots, i);
+        if (FMT == kFmtBf16) {
+            if (live && page >= 0) {
+                uint4 *dst = reinterpret_cast<uint4 *>(pool + 2 * (pool_offset(c, page, head, slot) + d));
+                dst[0] = in[i][0];
+                dst[1] = in[i][1];
             }
+        } else {
+            const uint32_t w[8] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w, in[i][1].x, in[i][1].y, in[i][1].z, in[i][1].w};
+            uint32_t amax = 0;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const bool live = off[u] < total, is_v = off[u] >= per_half;
-                const int x = off[u] - (is_v ? per_half : 0), head = x / c.head_dim, d = x - head * c.head_dim;
-                const uint32_t w[8] = {in[u][0].x, in[u][0].y, in[u][0].z, in[u][0].w,
-                                       in[u][1].x, in[u][1].y, in[u][1].z, in[u][1].w};
-                uint8_t *pool = is_v ? c.v : c.k;
-                if (FMT == kFmtBf16) {
-                    if (live) {
-                        uint4 *dst = reinterpret_cast<uint4 *>(pool + 2 * (pool_offset(c, page, head, slot) + d));
-                        dst[0] = in[u][0];
-                        dst[1] = in[u][1];
-                    }
-                } else {
-                    uint32_t amax = 0;
+            for (int k = 0; k < 8; ++k) amax = max(amax, max(abs_bits(bf16_lo(w[k])), abs_bits(bf16_hi(w[k]))));
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            const int byte = scale_byte(amax);
+            const float inv = inverse_scale(byte);
+            uint32_t o[4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) amax = max(amax, max(abs_bits(bf16_lo(w[i])), abs_bits(bf16_hi(w[i]))));
-                    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-                    const int byte = scale_byte(amax);
-                    const float inv = inverse_scale(byte);
-                    uint32_t o[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        o[i] = to_e4m3x2(bf16_lo(w[2 * i]) * inv, bf16_hi(w[2 * i]) * inv) |
-                               to_e4m3x2(bf16_lo(w[2 * i + 1]) * inv, bf16_hi(w[2 * i + 1]) * inv) << 16;
-                    if (live) {
-                        *reinterpret_cast<uint4 *>(pool + pool_offset(c, page, head, slot) + d) =
-                            make_uint4(o[0], o[1], o[2], o[3]);
-                        if ((lane & 1) == 0)
-                            (is_v ? c.v_scale : c.k_scale)[scale_offset(c, page, head, slot) + d / kFmtBlock] =
-                                static_cast<uint8_t>(byte);
-                    }
-                }
+            for (int k = 0; k < 4; ++k)
+                o[k] = to_e4m3x2(bf16_lo(w[2 * k]) * inv, bf16_hi(w[2 * k]) * inv) |
+                       to_e4m3x2(bf16_lo(w[2 * k + 1]) * inv, bf16_hi(w[2 * k + 1]) * inv) << 16;
+            if (live && page >= 0) {
+                *reinterpret_cast<uint4 *>(pool + pool_offset(c, page, head, slot) + d) = make_uint4(o[0], o[1], o[2], o[3]);
+                if ((lane & 1) == 0) scales[scale_offset(c, page, head, slot) + d / kFmtBlock] = static_cast<uint8_t>(byte);
             }
         }
     }
 }
 
-template <int FMT>
+template <int FMT, int RUN>
 __global__ void __launch_bounds__(kKvThreads) ead_kv_read_kernel(KvMoveParams p)
 {
     const int lane = threadIdx.x & 31;
-    const int warp = (blockIdx.x * kKvThreads + threadIdx.x) >> 5, warps = (gridDim.x * kKvThreads) >> 5;
+    const int t0 = ((blockIdx.x * kKvThreads + threadIdx.x) >> 5) * RUN, n = min(RUN, p.batch.n_tokens - t0);
+    if (n <= 0) return;
     const KvCacheView &c = p.cache;
-    const int per_half = c.heads * c.head_dim, total = 2 * per_half;
-    for (int t = warp; t < p.batch.n_tokens; t += warps) {
-        const int b = find_sequence(p.batch.new_start, p.batch.B, t, lane);
-        const int pos = (p.first ? __ldg(p.first + b) : 0) + t - __ldg(p.batch.new_start + b);
-        const int page = find_page(c, p.batch, b, pos);
-        if (page < 0 && lane == 0) flag_status(p.status, kStatusBadPage);
-        const int slot = pos & (c.page_size - 1);
-        for (int base = 0; base < total; base += 2 * kKvPass) {
-            uint4 in[2][2];
-            int byte[2];
-            int off[2];
+    const int per_half = c.heads * c.head_dim, off = blockIdx.y * kKvPass + lane * kKvLaneValues;
+    const bool live = off < 2 * per_half, is_v = off >= per_half;
+    const int x = off - (is_v ? per_half : 0), head = x / c.head_dim, d = x - head * c.head_dim;
+    uint8_t *const row0 = (is_v ? p.rows_v : p.rows_k) + 2 * (t0 * p.row_stride + x);
+    const uint8_t *const pool = is_v ? c.v : c.k, *const scales = is_v ? c.v_scale : c.k_scale;
+    int pages, slots;
+    find_places<false>(p, t0, n, lane, &pages, &slots);
+    uint4 in[RUN][FMT == kFmtBf16 ? 2 : 1];
+    uint32_t byte[RUN];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                off[u] = base + u * kKvPass + lane * kKvLaneValues;
-                in[u][0] = in[u][1] = make_uint4(0, 0, 0, 0);
-                byte[u] = 127;
-                if (off[u] < total && page >= 0) {
-                    const bool is_v = off[u] >= per_half;
-                    const int x = off[u] - (is_v ? per_half : 0), head = x / c.head_dim, d = x - head * c.head_dim;
-                    const uint8_t *pool = is_v ? c.v : c.k;
-                    if (FMT == kFmtBf16) {
-                        const uint4 *src = reinterpret_cast<const uint4 *>(pool + 2 * (pool_offset(c, page, head, slot) + d));
-                        in[u][0] = __ldg(src);
-                        in[u][1] = __ldg(src + 1);
-                    } else {
-                        in[u][0] = __ldg(reinterpret_cast<const uint4 *>(pool + pool_offset(c, page, head, slot) + d));
-                        byte[u] = __ldg((is_v ? c.v_scale : c.k_scale) + scale_offset(c, page, head, slot) + d / kFmtBlock);
-                    }
-                }
+    for (int i = 0; i < RUN; ++i) {
+        const int page = __shfl_sync(0xffffffffu, pages, i), slot = __shfl_sync(0xffffffffu, slots, i);
+        in[i][0] = make_uint4(0, 0, 0, 0);         // no place: zeros
+        if (FMT == kFmtBf16) in[i][FMT == kFmtBf16] = in[i][0];
+        byte[i] = 127;
+        if (live && page >= 0) {
+            if (FMT == kFmtBf16) {
+                const uint8_t *src = pool + 2 * (pool_offset(c, page, head, slot) + d);
+                in[i][0] = load_once(src);
+                in[i][FMT == kFmtBf16] = load_once(src + 16);
+            } else {
+                in[i][0] = load_once(pool + pool_offset(c, page, head, slot) + d);
+                byte[i] = __ldg(scales + scale_offset(c, page, head, slot) + d / kFmtBlock);
             }
+        }
+    }
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (off[u] >= total) continue;
-                const bool is_v = off[u] >= per_half;
-                uint4 *row = reinterpret_cast<uint4 *>((is_v ? p.rows_v : p.rows_k) +
-                                                       2 * (t * p.row_stride + off[u] - (is_v ? per_half : 0)));
-                if (FMT == kFmtBf16) {
-                    row[0] = in[u][0];
-                    row[1] = in[u][1];
-                } else {
-                    const float s = scale_value(byte[u]);
-                    const uint32_t w[4] = {in[u][0].x, in[u][0].y, in[u][0].z, in[u][0].w};
-                    uint32_t o[8];
+    for (int i = 0; i < RUN; ++i) {
+        if (!live || i >= n) continue;
+        uint4 *const row = reinterpret_cast<uint4 *>(row0 + 2 * i * p.row_stride);
+        if (FMT == kFmtBf16) {
+            row[0] = in[i][0];
+            row[1] = in[i][FMT == kFmtBf16];
+        } else {
+            const float s = scale_value(byte[i]);
+            const uint32_t w[4] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w};
+            uint32_t o[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 a = from_e4m3x2(w[i] & 0xffffu), e = from_e4m3x2(w[i] >> 16);
-                        o[2 * i] = to_bf16x2(a.x * s, a.y * s);
-                        o[2 * i + 1] = to_bf16x2(e.x * s, e.y * s);
-                    }
-                    row[0] = make_uint4(o[0], o[1], o[2], o[3]);
-                    row[1] = make_uint4(o[4], o[5], o[6], o[7]);
-                }
+            for (int k = 0; k < 4; ++k) {
+                const float2 a = from_e4m3x2(w[k] & 0xffffu), e = from_e4m3x2(w[k] >> 16);
+                o[2 * k] = to_bf16x2(a.x * s, a.y * s);
+                o[2 * k + 1] = to_bf16x2(e.x * s, e.y * s);
             }
+            row[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            row[1] = make_uint4(o[4], o[5], o[6], o[7]);
         }
     }
 }
