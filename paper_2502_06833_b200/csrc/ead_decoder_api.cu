@@ -28,6 +28,7 @@ namespace {
     } while (0)
 
 constexpr int kMaxDevices = 64;
+constexpr int kNormThreadsPerSm = 2048;
 constexpr int kKvRun = 4;                 // tokens per warp of the cache's write and read ...
 constexpr int kKvLongRunTokens = 1024;    // ... from this many tokens on; before, one
 constexpr int kChunkMinCost = 24;         // cost per block (a tile of 128 rows x 64 keys: 1), likewise
@@ -345,9 +346,10 @@ extern "C" int ead_add_rmsnorm(const void *x, int64_t x_stride, const void *resi
     const int groups = H / 8;
     const int nv = groups <= 512 ? 1 : groups <= 1024 ? 2 : 4;
     const int threads = ((groups + nv - 1) / nv + 31) / 32 * 32;
+    const int blocks = std::min(n_rows, kNormThreadsPerSm / threads * d->sms);
 #define EAD_LAUNCH_NORM(NV)                                                                    \
-    (e4m3 ? ead_add_rmsnorm_kernel<kFmtE4m3, NV><<<n_rows, threads, 0, s>>>(p)                 \
-          : ead_add_rmsnorm_kernel<kFmtBf16, NV><<<n_rows, threads, 0, s>>>(p))
+    (e4m3 ? ead_add_rmsnorm_kernel<kFmtE4m3, NV><<<blocks, threads, 0, s>>>(p, n_rows)         \
+          : ead_add_rmsnorm_kernel<kFmtBf16, NV><<<blocks, threads, 0, s>>>(p, n_rows))
     if (nv == 1)
         EAD_LAUNCH_NORM(1);
     else if (nv == 2)

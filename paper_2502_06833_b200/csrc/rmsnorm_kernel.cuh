@@ -1,6 +1,6 @@
 // Residual addition and root-mean-square norm of hidden rows, output in bf16 or in 8-bit blocks:
 //   s = x + residual,  y = s * rsqrt(mean(s^2) + eps) * weight
-// One block per row; the row stays in registers between the sum of squares and the output, so every
+// A block works on a row at a time; the row stays in registers between the sum of squares and the output, so every
 // input is read once and every output written once.  HBM bounds it at size, the launch at one step.
 #pragma once
 #include "kv_format.cuh"
@@ -27,70 +27,83 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8])
 }
 
 // NV: groups of 8 consecutive elements per thread; thread i takes groups i, i + blockDim.x, ...
+// A block takes every gridDim.x-th row and has the next one's loads in flight while it reduces this one; the weights,
+// the same for every row, stay in registers.
 template <int FMT, int NV>
-__global__ void __launch_bounds__(512) ead_add_rmsnorm_kernel(NormParams p)
+__global__ void __launch_bounds__(512) ead_add_rmsnorm_kernel(NormParams p, int n_rows)
 {
-    __shared__ float part[16];
-    const int64_t row = blockIdx.x;
+    __shared__ float part[2][16];
     const int groups = p.H >> 3, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    float s[NV][8];
-    float sum = 0.f;
+    uint4 w[NV], x[NV], r[NV];
+    auto fetch = [&](int64_t row) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int g = threadIdx.x + i * blockDim.x;
-        if (g < groups) {
-            unpack8(*(reinterpret_cast<const uint4 *>(p.x + 2 * row * p.x_stride) + g), s[i]);
-            if (p.residual) {
-                float r[8];
-                unpack8(*(reinterpret_cast<const uint4 *>(p.residual + 2 * row * p.residual_stride) + g), r);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) s[i][k] += r[k];
+        for (int i = 0; i < NV; ++i) {
+            const int g = threadIdx.x + i * blockDim.x;
+            x[i] = r[i] = make_uint4(0, 0, 0, 0);
+            if (g < groups) {
+                x[i] = *(reinterpret_cast<const uint4 *>(p.x + 2 * row * p.x_stride) + g);
+                if (p.residual) r[i] = *(reinterpret_cast<const uint4 *>(p.residual + 2 * row * p.residual_stride) + g);
             }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) s[i][k] = 0.f;
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum = fmaf(s[i][k], s[i][k], sum);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (warps > 1) {
-        if (lane == 0) part[warp] = sum;
-        __syncthreads();
-        sum = lane < warps ? part[lane] : 0.f;
-#pragma unroll
-        for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        sum = __shfl_sync(0xffffffffu, sum, 0);
-    }
-    const float r = rsqrtf(sum / static_cast<float>(p.H) + p.eps);
+    };
+    fetch(blockIdx.x);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int g = threadIdx.x + i * blockDim.x;
-        const bool live = g < groups;
-        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live) {
-            if (p.residual_out) *(reinterpret_cast<uint4 *>(p.residual_out + 2 * row * p.residual_out_stride) + g) = pack8(s[i]);
-            float w[8];
-            unpack8(__ldg(reinterpret_cast<const uint4 *>(p.weight) + g), w);
+        w[i] = g < groups ? __ldg(reinterpret_cast<const uint4 *>(p.weight) + g) : make_uint4(0, 0, 0, 0);
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < n_rows; row += gridDim.x, turn ^= 1) {
+        float s[NV][8];
+        float sum = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = s[i][k] * r * w[k];
+        for (int i = 0; i < NV; ++i) {
+            float b[8];
+            unpack8(x[i], s[i]);
+            unpack8(r[i], b);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                s[i][k] += b[k];
+                sum = fmaf(s[i][k], s[i][k], sum);
+            }
         }
-        if (FMT == kFmtBf16) {
-            if (live) *(reinterpret_cast<uint4 *>(p.out + 2 * row * p.out_stride) + g) = pack8(y);
-        } else {
-            uint32_t amax = 0;
+        if (row + gridDim.x < n_rows) fetch(row + gridDim.x);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) amax = max(amax, abs_bits(y[k]));
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));         // 4 lanes hold a block of 32
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            const int byte = scale_byte(amax);
-            const float inv = inverse_scale(byte);
-            if (live) {
-                *(reinterpret_cast<uint2 *>(p.out + row * p.out_stride) + g) =
-                    make_uint2(to_e4m3x2(y[0] * inv, y[1] * inv) | to_e4m3x2(y[2] * inv, y[3] * inv) << 16,
-                               to_e4m3x2(y[4] * inv, y[5] * inv) | to_e4m3x2(y[6] * inv, y[7] * inv) << 16);
-                if ((lane & 3) == 0) p.out_scale[row * (p.H / kFmtBlock) + (g >> 2)] = static_cast<uint8_t>(byte);
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (warps > 1) {                           // two turns' sums in turn: one barrier per row
+            if (lane == 0) part[turn][warp] = sum;
+            __syncthreads();
+            sum = lane < warps ? part[turn][lane] : 0.f;
+#pragma unroll
+            for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            sum = __shfl_sync(0xffffffffu, sum, 0);
+        }
+        const float scale = rsqrtf(sum / static_cast<float>(p.H) + p.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int g = threadIdx.x + i * blockDim.x;
+            const bool live = g < groups;
+            if (live && p.residual_out) *(reinterpret_cast<uint4 *>(p.residual_out + 2 * row * p.residual_out_stride) + g) = pack8(s[i]);
+            float y[8], v[8];
+            unpack8(w[i], v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = s[i][k] * scale * v[k];
+            if (FMT == kFmtBf16) {
+                if (live) *(reinterpret_cast<uint4 *>(p.out + 2 * row * p.out_stride) + g) = pack8(y);
+            } else {
+                uint32_t amax = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) amax = max(amax, abs_bits(y[k]));
+                amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));     // 4 lanes hold a block of 32
+                amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+                const int byte = scale_byte(amax);
+                const float inv = inverse_scale(byte);
+                if (live) {
+                    *(reinterpret_cast<uint2 *>(p.out + row * p.out_stride) + g) =
+                        make_uint2(to_e4m3x2(y[0] * inv, y[1] * inv) | to_e4m3x2(y[2] * inv, y[3] * inv) << 16,
+                                   to_e4m3x2(y[4] * inv, y[5] * inv) | to_e4m3x2(y[6] * inv, y[7] * inv) << 16);
+                    if ((lane & 3) == 0) p.out_scale[row * (p.H / kFmtBlock) + (g >> 2)] = static_cast<uint8_t>(byte);
+                }
             }
         }
     }
