@@ -83,6 +83,27 @@ __device__ __forceinline__ bool seen_by(int pos, int window, int sinks, int j)
     return j <= pos && (window == 0 || j > pos - window || j < sinks);
 }
 
+// W items dealt out to `blocks` stretches of nearly equal length, the longer ones first.
+struct Stretches {
+    int64_t len;
+    int longer;                                   // stretches of len + 1
+    __device__ __forceinline__ Stretches(int64_t W, int blocks)
+    {
+        len = W < 0x7fffffff ? static_cast<int>(W) / blocks : W / blocks;
+        longer = static_cast<int>(W - len * blocks);
+    }
+    __device__ __forceinline__ int64_t begin(int i) const { return i * len + min(i, longer); }
+    __device__ __forceinline__ int block_of(int64_t item) const
+    {
+        const int64_t head = longer * (len + 1);
+        return item < head ? div(item, len + 1) : longer + div(item - head, len);
+    }
+    static __device__ __forceinline__ int div(int64_t a, int64_t b)
+    {
+        return a < 0x7fffffff && b < 0x7fffffff ? static_cast<int>(a) / static_cast<int>(b) : static_cast<int>(a / b);
+    }
+};
+
 // 2^x with 2^-inf = 0.
 __device__ __forceinline__ float exp2_fast(float x)
 {

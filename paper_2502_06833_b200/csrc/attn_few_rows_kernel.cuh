@@ -133,6 +133,9 @@ __device__ __forceinline__ void few_seek(const AttnParams &p, int shift, int g, 
     }
 }
 
+// Units of at most so many tiles are not divided among blocks (joining parts costs more than the imbalance).
+constexpr int kFewWholeTiles = 48;
+
 // NB: packed rows in groups of 8 (1 or 2).
 template <int FMT, int D, int NB>
 struct FewLayout {
@@ -170,8 +173,8 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     const int box_keys = 1 << box_shift;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int64_t s_scan[kFewWarps];
-    __shared__ int s_b;
-    __shared__ int64_t s_before;
+    __shared__ int s_b[2];
+    __shared__ int64_t s_before[2];
     __shared__ int s_last;
     const uint32_t raw = smem_u32(smem_raw), ring0 = (raw + 1023u) & ~1023u;
     uint8_t *const ring_ptr = smem_raw + (ring0 - raw);
@@ -214,27 +217,48 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     const int64_t W = total * c.heads;
     const int64_t ctas = min(static_cast<int64_t>(gridDim.x), max(static_cast<int64_t>(1), (W + min_tiles - 1) / min_tiles));
     if (W == 0 || blockIdx.x >= ctas) return;
-    const int64_t g0 = W * blockIdx.x / ctas, g1 = W * (blockIdx.x + 1) / ctas;
-    if (mine > 0 && g0 >= (upto - mine) * c.heads && g0 < upto * c.heads) {
-        int64_t at = upto - mine;
-        for (int b = b_lo; b < b_hi; ++b) {
-            const int t = few_tiles(p, seq_info(p.batch, b), L::kShift, &kr);
-            if (g0 < (at + t) * c.heads) {
-                s_b = b;
-                s_before = at * c.heads;
-                break;
+    const Stretches even(W, static_cast<int>(ctas));
+    // The sequences in which the two ends of the block's stretch lie.  (The code up to the first loads runs once and
+    // from a cold instruction cache: loops stay loops.)
+#pragma unroll 1
+    for (int64_t b = b_lo, at = upto - mine; b < b_hi; ++b) {
+        const int t = per == 1 ? static_cast<int>(mine) : few_tiles(p, seq_info(p.batch, b), L::kShift, &kr);
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {
+            const int64_t g = even.begin(blockIdx.x + e);
+            if (g >= at * c.heads && g < (at + t) * c.heads) {
+                s_b[e] = b;
+                s_before[e] = at * c.heads;
             }
-            at += t;
         }
+        at += t;
     }
     __syncthreads();
     FewCursor cur;
-    cur.b = s_b;
-    cur.s = seq_info(p.batch, cur.b);
-    cur.r.tiles = few_tiles(p, cur.s, L::kShift, &cur.r);
-    cur.h = static_cast<int>((g0 - s_before) / cur.r.tiles);
-    cur.begin = static_cast<int>(s_before + static_cast<int64_t>(cur.h) * cur.r.tiles - g0);
+    int64_t cur_begin = 0, g0 = 0, g1 = W;
+    bool next_unit = false;
+#pragma unroll 1
+    for (int e = 1; e >= 0; --e) {                 // a short unit is not divided: an end within it moves to its nearer end
+        int64_t g = even.begin(blockIdx.x + e);
+        if (g < W) {
+            cur.b = s_b[e];
+            cur.s = seq_info(p.batch, cur.b);
+            cur.r.tiles = few_tiles(p, cur.s, L::kShift, &cur.r);
+            const int64_t off = g - s_before[e];
+            cur.h = off < 0x7fffffff ? static_cast<int>(off) / cur.r.tiles : static_cast<int>(off / cur.r.tiles);
+            cur_begin = s_before[e] + static_cast<int64_t>(cur.h) * cur.r.tiles;
+            next_unit = false;
+            if (cur.r.tiles <= kFewWholeTiles && g > cur_begin) {
+                next_unit = 2 * (g - cur_begin) >= cur.r.tiles;
+                g = next_unit ? cur_begin + cur.r.tiles : cur_begin;
+            }
+        }
+        (e ? g1 : g0) = g;
+    }
+    if (g0 >= g1) return;
+    cur.begin = static_cast<int>(cur_begin - g0);
     const int n_tiles = static_cast<int>(g1 - g0);  // from here on tiles are counted from g0
+    if (next_unit) few_seek(p, L::kShift, 0, &cur);
 
     // ---- loads: this warp's tiles are warp, warp + 8, ...
     const uint32_t my_ring = ring0 + warp * S * 2 * kFewHalf;
@@ -242,24 +266,34 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     const uint32_t my_bars = bars + warp * S * 8;
     FewCursor ahead = cur;
     int g_ahead = warp;
-    int page = -1, key0 = 0;                       // of this lane's box of the tile that is loaded next
     const int boxes = TT >> box_shift;              // at most 8
-    auto look_up = [&]() {                         // one tile early, so that the load is there when the tile is issued
-        if (g_ahead >= n_tiles) return;
-        few_seek(p, L::kShift, g_ahead, &ahead);
-        key0 = ahead.r.base(g_ahead - ahead.begin, L::kShift) + lane * box_keys;
-        page = -2;                                 // nothing of it is seen: not loaded
-        const bool any = key0 < ahead.r.hi && (key0 + box_keys > ahead.r.lo || key0 < p.sinks);
-        if (lane < boxes && any) {
-            page = find_page(c, p.batch, ahead.b, key0);
-            if (page < 0) {
-                flag_status(p.status, kStatusBadPage);
-                page = c.n_pages;                  // outside the pool: the copy delivers zeros
-            }
-        }
+    // This lane's box of a tile that is to be loaded.
+    struct Box {
+        int entry;                                 // page as the table has it, or -2 if no query sees any of it
+        int key0, h;
+        bool tile;                                 // is there such a tile?
     };
-    auto issue = [&](int stage) {
-        if (g_ahead >= n_tiles) return;
+    // One tile early, so that the entry is there when the tile is issued (nothing here waits for it).
+    auto look_up = [&]() {
+        Box x{-2, 0, 0, g_ahead < n_tiles};
+        if (x.tile) {
+            few_seek(p, L::kShift, g_ahead, &ahead);
+            x.key0 = ahead.r.base(g_ahead - ahead.begin, L::kShift) + lane * box_keys;
+            x.h = ahead.h;
+            if (lane < boxes && x.key0 < ahead.r.hi && (x.key0 + box_keys > ahead.r.lo || x.key0 < p.sinks))
+                x.entry = max(__ldg(p.batch.page_table + static_cast<int64_t>(ahead.b) * p.batch.table_stride + (x.key0 >> c.page_shift)), -1);
+            g_ahead += kFewWarps;
+        }
+        return x;
+    };
+    auto issue = [&](int stage, const Box &x) {
+        if (!x.tile) return;
+        int page = x.entry;
+        if (page != -2 && (page < 0 || page >= c.n_pages)) {
+            flag_status(p.status, kStatusBadPage);
+            page = c.n_pages;                      // outside the pool: the copy delivers zeros
+        }
+        const int key0 = x.key0;
         const unsigned live = __ballot_sync(0xffffffffu, lane < boxes && page >= 0);
         const uint32_t bar = my_bars + 8 * stage, dst = my_ring + stage * 2 * kFewHalf;
         const uint32_t box_bytes = box_keys * L::kRowBytes;
@@ -273,30 +307,29 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         __syncwarp();
         if (lane < boxes && page >= 0) {
             const int slot = key0 & (c.page_size - 1);
-            tma_load_5d(dst + lane * box_bytes, &tmK, 0, slot, 0, ahead.h, page, bar);
-            tma_load_5d(dst + kFewHalf + lane * box_bytes, &tmV, 0, slot, 0, ahead.h, page, bar);
+            tma_load_5d(dst + lane * box_bytes, &tmK, 0, slot, 0, x.h, page, bar);
+            tma_load_5d(dst + kFewHalf + lane * box_bytes, &tmV, 0, slot, 0, x.h, page, bar);
             if (FMT == kFmtE4m3) {
                 const uint32_t sc = my_scales + stage * kFewScaleBytes + lane * sc_bytes;
                 if (page < c.n_pages) {
-                    const int64_t at = scale_offset(c, page, ahead.h, slot);
+                    const int64_t at = scale_offset(c, page, x.h, slot);
                     bulk_load(sc, c.k_scale + at, sc_bytes, bar);
                     bulk_load(sc + kFewScaleBytes / 2, c.v_scale + at, sc_bytes, bar);
                 } else {
-                    for (uint32_t x = 0; x < sc_bytes; x += 4) {
-                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + x), "r"(0) : "memory");
-                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + kFewScaleBytes / 2 + x), "r"(0) : "memory");
+                    for (uint32_t y = 0; y < sc_bytes; y += 4) {
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + y), "r"(0) : "memory");
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + kFewScaleBytes / 2 + y), "r"(0) : "memory");
                     }
                 }
             }
         }
         __syncwarp();
-        g_ahead += kFewWarps;
     };
-    look_up();
-#pragma unroll
+    Box next_box = look_up();
+#pragma unroll 1
     for (int i = 0; i < S; ++i) {
-        issue(i);
-        look_up();
+        issue(i, next_box);
+        next_box = look_up();
     }
 
     // ---- tiles, unit by unit
@@ -316,36 +349,48 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         off_k[j] = chunk_at(mr + (mi & 1) * 8, 2 * j + (mi >> 1));
         off_v[j] = FMT == kFmtBf16 ? chunk_at(mr + (mi >> 1) * 8, 2 * j + (mi & 1)) : off_k[j];
     }
-    int stage = 0;
-    uint32_t phase = 0;
-    int g = warp, unit_lo = 0;
-    bool first_unit = true, expired = false;
-    while (unit_lo < n_tiles) {
-        const int unit_end = cur.begin + cur.r.tiles, unit_hi = min(unit_end, n_tiles);
-        const int rows = cur.s.n * p.group;
-        const int64_t token0 = cur.s.token0;
-        // query rows as the 8-column operand: lane holds rows lane / 4 (+ 8), elements by the layout of the keys
-        uint32_t qf[D / 16][NB][2];
+    // Query rows as the 8-column operand: a lane holds rows lane / 4 (+ 8), elements by the layout of the keys.  With one
+    // group of rows those of the next unit are fetched while this one's parts are joined.
+    uint32_t q_next[D / 16][NB][2];
+    auto query_rows = [&](const FewCursor &u) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const int row = nb * 8 + (lane >> 2);
             const int i = row / p.group, gq = row - i * p.group;
-            const uint8_t *src = p.q + 2 * ((token0 + i) * p.q_stride + (static_cast<int64_t>(cur.h) * p.group + gq) * D);
+            const uint8_t *src = p.q + 2 * ((static_cast<int64_t>(u.s.token0) + i) * p.q_stride + (static_cast<int64_t>(u.h) * p.group + gq) * D);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
-                qf[ks][nb][0] = qf[ks][nb][1] = 0;
-                if (row < rows) {
+                q_next[ks][nb][0] = q_next[ks][nb][1] = 0;
+                if (row < u.s.n * p.group) {
                     if (FMT == kFmtBf16) {
-                        qf[ks][nb][0] = __ldg(reinterpret_cast<const uint32_t *>(src + 2 * (16 * ks + qc)));
-                        qf[ks][nb][1] = __ldg(reinterpret_cast<const uint32_t *>(src + 2 * (16 * ks + qc + 8)));
+                        q_next[ks][nb][0] = __ldg(reinterpret_cast<const uint32_t *>(src + 2 * (16 * ks + (lane & 3) * 2)));
+                        q_next[ks][nb][1] = __ldg(reinterpret_cast<const uint32_t *>(src + 2 * (16 * ks + (lane & 3) * 2 + 8)));
                     } else {                       // four consecutive codes per lane: elements 4c .. 4c + 3 of the step
-                        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src + 2 * (16 * ks + 2 * qc)));
-                        qf[ks][nb][0] = v.x;
-                        qf[ks][nb][1] = v.y;
+                        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src + 2 * (16 * ks + (lane & 3) * 4)));
+                        q_next[ks][nb][0] = v.x;
+                        q_next[ks][nb][1] = v.y;
                     }
                 }
             }
         }
+    };
+    int stage = 0;
+    uint32_t phase = 0;
+    int g = warp, unit_lo = 0;
+    bool expired = false;
+    while (unit_lo < n_tiles) {
+        const int unit_end = cur.begin + cur.r.tiles, unit_hi = min(unit_end, n_tiles);
+        const int rows = cur.s.n * p.group;
+        const int64_t token0 = cur.s.token0;
+        if (NB == 2 || unit_lo == 0) query_rows(cur);
+        uint32_t qf[D / 16][NB][2];
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                qf[ks][nb][0] = q_next[ks][nb][0];
+                qf[ks][nb][1] = q_next[ks][nb][1];
+            }
         float row_scale[NB][2];                    // of this lane's rows' logits
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -588,14 +633,19 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             }
             }
             __syncwarp();                          // every lane has read the stage before it is filled again
-            issue(stage);
-            look_up();
+            issue(stage, next_box);
+            next_box = look_up();
             if (++stage == S) {
                 stage = 0;
                 phase ^= 1;
             }
         }
 
+        FewCursor after = cur;
+        if (unit_hi < n_tiles) {
+            few_seek(p, L::kShift, unit_hi, &after);
+            if (NB == 1) query_rows(after);
+        }
         // ---- the warps' parts of the unit come together: warps 4-7 hand theirs to 0-3 lane by lane, those lay them out by rows
         constexpr int kHalf = kFewWarps / 2;
         if (warp >= kHalf) {
@@ -663,7 +713,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         const bool begins = unit_lo == cur.begin, ends = unit_hi == unit_end;
         float *const parts = reinterpret_cast<float *>(p.workspace + kDecodePartOffset);
         uint32_t *const counters = reinterpret_cast<uint32_t *>(p.workspace);
-        float *const my_part = parts + (2 * blockIdx.x + (first_unit ? 0 : 1)) * kDecodePartFloats;
+        float *const my_part = parts + (2 * blockIdx.x + (begins ? 1 : 0)) * kDecodePartFloats;   // a block has one part of each kind at most
         constexpr int kQuads = D / 4;
         auto store = [&](int row, int dq, float M, float Lsum, float4 v) {
             const int i = row / p.group, gq = row - i * p.group;
@@ -700,7 +750,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         }
         if (!(begins && ends)) {
             // blocks that hold a part of the unit: first .. last; the counter is the first one's
-            const int first = static_cast<int>(((g0 + cur.begin + 1) * ctas - 1) / W), last = static_cast<int>(((g0 + unit_end) * ctas - 1) / W);
+            const int first = even.block_of(g0 + cur.begin), last = even.block_of(g0 + unit_end - 1);
             fence_gpu();
             __syncthreads();
             if (tid == 0) {
@@ -711,16 +761,15 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             __syncthreads();
             if (s_last) {
                 fence_gpu();
-                const int first_slot = g0 + cur.begin == W * first / ctas ? 0 : 1;
                 for (int x = tid; x < rows * kQuads; x += kFewThreads) {
                     const int row = x / kQuads, dq = x - row * kQuads;
                     float M = -INFINITY, Lsum = 0.f;
                     for (int k = first; k <= last; ++k)
-                        M = fmaxf(M, __ldcg(parts + (2 * k + (k == first ? first_slot : 0)) * kDecodePartFloats + kDecodeRows * 128 + row));
+                        M = fmaxf(M, __ldcg(parts + (2 * k + (k == first ? 1 : 0)) * kDecodePartFloats + kDecodeRows * 128 + row));
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
                     for (int k = first; k <= last; ++k) {
-                        const float *src = parts + (2 * k + (k == first ? first_slot : 0)) * kDecodePartFloats;
+                        const float *src = parts + (2 * k + (k == first ? 1 : 0)) * kDecodePartFloats;
                         const float mm = __ldcg(src + kDecodeRows * 128 + row);
                         const float f = mm == -INFINITY ? 0.f : exp2_fast(mm - M);
                         const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + row * D + 4 * dq));
@@ -733,8 +782,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
         }
         __syncthreads();                           // the merge buffer is free again
         unit_lo = unit_hi;
-        first_unit = false;
-        if (unit_lo < n_tiles) few_seek(p, L::kShift, unit_lo, &cur);
+        cur = after;
     }
 }
 
