@@ -236,6 +236,17 @@ __device__ __forceinline__ bool elect_one()
     asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(p));
     return p != 0;
 }
+// 32 bytes to global memory, in one store if `wide` (the address is a multiple of 32 then).
+__device__ __forceinline__ void store_32(uint8_t *dst, const uint32_t (&v)[8], bool wide)
+{
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                     "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4 *>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 template <int FMT, int D>
@@ -264,6 +275,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvCacheView &c = p.cache;
 
+    if (tid == 32) {
+        tma_prefetch_desc(&tmK);
+        tma_prefetch_desc(&tmV);
+    }
     if (tid == 0) {
         for (int i = 0; i < S; ++i) {
             mbar_init(bar_full + 8 * i, FMT == kFmtBf16 ? 1 : 128);
@@ -645,6 +660,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         const uint32_t t_o = tmem + lanes + 256 + w * 128;
         int t = 0, ns = 0;
         int outputs[2] = {0, 0};                   // finished outputs per accumulator
+        // a thread writes a row: 32 bytes at a time, a whole sector each, if every row begins at one
+        const bool whole_sectors = ((reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(2 * p.out_stride)) & 31) == 0;
         for (int n = 0;; ++n) {
             const ChunkUnit &u = unit_wait(n);
             const bool dual = u.dual != 0;
@@ -799,13 +816,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                             o[e] = __float_as_uint(__uint_as_float(o[e]) * f0 + (nt > 1 ? __uint_as_float(o1[e]) * f1 : 0.f));
                     }
                     if (live && alone) {
-                        uint4 *dst = reinterpret_cast<uint4 *>(p.out + 2 * (token * p.out_stride + static_cast<int64_t>(hq) * D + 32 * q));
+                        uint8_t *dst = p.out + 2 * (token * p.out_stride + static_cast<int64_t>(hq) * D + 32 * q);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            dst[e] = make_uint4(to_bf16x2(__uint_as_float(o[8 * e]) * inv, __uint_as_float(o[8 * e + 1]) * inv),
-                                                to_bf16x2(__uint_as_float(o[8 * e + 2]) * inv, __uint_as_float(o[8 * e + 3]) * inv),
-                                                to_bf16x2(__uint_as_float(o[8 * e + 4]) * inv, __uint_as_float(o[8 * e + 5]) * inv),
-                                                to_bf16x2(__uint_as_float(o[8 * e + 6]) * inv, __uint_as_float(o[8 * e + 7]) * inv));
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t v8[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                v8[e] = to_bf16x2(__uint_as_float(o[16 * h + 2 * e]) * inv, __uint_as_float(o[16 * h + 2 * e + 1]) * inv);
+                            store_32(dst + 32 * h, v8, whole_sectors);
+                        }
                     } else if (live) {
                         uint4 *dst = reinterpret_cast<uint4 *>(my_part) + 8 * q * kChunkRows + my_row;       // four columns by rows: consecutive lanes are adjacent
 #pragma unroll
@@ -842,36 +861,42 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                         const int r = tid;
                         auto part_of = [&](int k) { return parts + (2 * k + (k == first ? first_slot : 0)) * kPart; };
                         float M = -INFINITY, Lsum = 0.f;
-                        for (int k = first; k <= last; ++k) M = fmaxf(M, __ldcg(part_of(k) + kChunkRows * D + r));
+#pragma unroll 4
                         for (int k = first; k <= last; ++k) {
-                            const float mk = __ldcg(part_of(k) + kChunkRows * D + r);
-                            Lsum += (mk == -INFINITY ? 0.f : exp2_fast(mk - M)) * __ldcg(part_of(k) + kChunkRows * D + kChunkRows + r);
+                            const float mk = __ldcg(part_of(k) + kChunkRows * D + r), lk = __ldcg(part_of(k) + kChunkRows * D + kChunkRows + r);
+                            const float top = fmaxf(M, mk), base = top == -INFINITY ? 0.f : top;
+                            Lsum = Lsum * exp2_fast(M - base) + lk * exp2_fast(mk - base);
+                            M = top;
                         }
                         const float inv = Lsum == 0.f ? 0.f : 1.f / Lsum;
                         const int i = (u.row0 + r) / p.group, hr = u.h * p.group + (u.row0 + r - i * p.group);
                         const int64_t tok = static_cast<int64_t>(u.token0) + i;
                         if (p.lse) p.lse[tok * p.heads_q + hr] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
-                        for (int q = 0; q < D / 32; ++q) {
-                            float4 a[8];
+                        for (int q = 0; q < D / 64; ++q) {
+                            float4 a[16];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) a[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            for (int e = 0; e < 16; ++e) a[e] = make_float4(0.f, 0.f, 0.f, 0.f);
                             for (int k = first; k <= last; ++k) {
                                 const float mk = __ldcg(part_of(k) + kChunkRows * D + r);
-                                const float4 *src = reinterpret_cast<const float4 *>(part_of(k)) + 8 * q * kChunkRows + r;
-                                float4 y[8];
+                                const float4 *src = reinterpret_cast<const float4 *>(part_of(k)) + 16 * q * kChunkRows + r;
+                                float4 y[16];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) y[e] = __ldcg(src + e * kChunkRows);
+                                for (int e = 0; e < 16; ++e) y[e] = __ldcg(src + e * kChunkRows);
                                 const float f = (mk == -INFINITY ? 0.f : exp2_fast(mk - M)) * inv;
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) {
+                                for (int e = 0; e < 16; ++e) {
                                     a[e].x += f * y[e].x; a[e].y += f * y[e].y; a[e].z += f * y[e].z; a[e].w += f * y[e].w;
                                 }
                             }
-                            uint4 *dst = reinterpret_cast<uint4 *>(p.out + 2 * (tok * p.out_stride + static_cast<int64_t>(hr) * D + 32 * q));
+                            uint8_t *dst = p.out + 2 * (tok * p.out_stride + static_cast<int64_t>(hr) * D + 64 * q);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                dst[e] = make_uint4(to_bf16x2(a[2 * e].x, a[2 * e].y), to_bf16x2(a[2 * e].z, a[2 * e].w),
-                                                    to_bf16x2(a[2 * e + 1].x, a[2 * e + 1].y), to_bf16x2(a[2 * e + 1].z, a[2 * e + 1].w));
+                            for (int e = 0; e < 4; ++e) {
+                                const uint32_t v[8] = {to_bf16x2(a[4 * e].x, a[4 * e].y), to_bf16x2(a[4 * e].z, a[4 * e].w),
+                                                       to_bf16x2(a[4 * e + 1].x, a[4 * e + 1].y), to_bf16x2(a[4 * e + 1].z, a[4 * e + 1].w),
+                                                       to_bf16x2(a[4 * e + 2].x, a[4 * e + 2].y), to_bf16x2(a[4 * e + 2].z, a[4 * e + 2].w),
+                                                       to_bf16x2(a[4 * e + 3].x, a[4 * e + 3].y), to_bf16x2(a[4 * e + 3].z, a[4 * e + 3].w)};
+                                store_32(dst + 32 * e, v, whole_sectors);
+                            }
                         }
                     }
                 }

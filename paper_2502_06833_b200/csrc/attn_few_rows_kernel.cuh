@@ -184,6 +184,10 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvCacheView &c = p.cache;
 
+    if (tid == 0) {
+        tma_prefetch_desc(&tmK);
+        tma_prefetch_desc(&tmV);
+    }
     if (tid < kFewWarps * S) mbar_init(bars + 8 * tid, 1);
     fence_mbar_init();
 
