@@ -582,14 +582,25 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             const int last = un.last;
             wait_phase(bar_q_empty, (n & 1) ^ 1, p.status, &expired);
             constexpr int kChunks = D / 8;         // 16-byte pieces per row
-            const uint8_t *const q0 = p.q + 2 * (static_cast<int64_t>(un.token0) * p.q_stride + static_cast<int64_t>(un.h) * p.group * D);
-            const int rows = un.rows, row0 = un.row0;
+            // 16 bytes per thread and step, all copies in flight at once, zeros behind the last row; token and head of a row are
+            // carried along (a division per step took longer than the copies: its conversions queue behind the exponentials)
+            constexpr int kStep = 128 / kChunks;   // rows per step
+            const int ch = ft % kChunks, rows = un.rows, step_i = kStep / p.group, step_g = kStep - step_i * p.group;
+            int row = ft / kChunks, i = (un.row0 + row) / p.group, gq = un.row0 + row - i * p.group;
+            const uint8_t *const q0 = p.q + 2 * (static_cast<int64_t>(un.token0) * p.q_stride + static_cast<int64_t>(un.h) * p.group * D + 8 * ch);
+            const uint32_t dst0 = q_smem + (ch >> 3) * (128 * 128);
 #pragma unroll 4
-            for (int y = ft; y < (un.dual ? 256 : 128) * kChunks; y += 128) {        // all copies in flight at once
-                const int row = y / kChunks, ch = y - row * kChunks, i = (row0 + row) / p.group, gq = row0 + row - i * p.group;
-                const uint8_t *src = row < rows ? q0 + 2 * (i * p.q_stride + gq * D + 8 * ch) : p.q;   // zeros behind the last row
-                const uint32_t dst = q_smem + (row >> 7) * L::kQTile + (ch >> 3) * (128 * 128) + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(row < rows ? 16 : 0) : "memory");
+            for (; row < (un.dual ? 256 : 128); row += kStep) {
+                const bool there = row < rows;
+                const uint8_t *src = there ? q0 + 2 * (i * p.q_stride + gq * D) : p.q;
+                const uint32_t dst = dst0 + (row >> 7) * L::kQTile + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+                gq += step_g;
+                i += step_i;
+                if (gq >= p.group) {
+                    gq -= p.group;
+                    ++i;
+                }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             fence_async_shared();
