@@ -1,31 +1,30 @@
 // Attention for units of many packed rows (chunks of new tokens): tcgen05 MMAs with TMEM accumulators.
 //
-// A unit is up to 256 packed rows (new tokens x query heads of one cache head; consecutive rows are the heads of
-// a token), two tiles of 128 rows that share every key tile of 64 keys.  Per key tile and row tile: S = Q K^T (TMEM),
+// A unit is up to two row tiles that share every key tile of 64 keys.  A row tile is as many whole tokens as fit into 128
+// rows, all query heads of one cache head for each (consecutive rows are the heads of a token): one TMA box of the
+// caller's [tokens, heads, head_dim] array.  Per key tile and row tile: S = Q K^T (TMEM),
 // one thread per row turns S into probabilities P, which overwrite S as bf16 in TMEM, O += P V (TMEM).  Every row tile has two
 // S buffers, so the scores of the next key tile are there when the softmax of this one ends: tensor core and softmax do not
 // wait for each other's round trip.  (With 128-key tiles TMEM has room for one S per row tile: 5860 cycles per 256 x 128
-// scores instead of the ~2560 that the operands' reads from shared memory take.)  A unit of at most 128 rows
+// scores instead of the ~2560 that the operands' reads from shared memory take.)  A unit of one row tile
 // gives both turns to the same rows instead: even key tiles go to the first accumulator, odd ones
 // to the second, and the two are joined at the end.
 //
 // Warps: 0-3 softmax and output of the first row tile, 4-7 of the second, 8 and 10 issue their MMAs (the instructions
 // around the MMAs take longer than the MMAs: one warp for both row tiles took twice the time), 9 loads key and value
-// tiles (TMA), 12-15 load the query rows and, for an 8-bit cache, turn codes into bf16 on their way into the MMA's
-// operand tiles (as in the few-rows kernel).  11 walks through the block's units and describes each to the others in shared
-// memory, two ahead at most.  Registers are dealt out by warpgroups, most of them to the softmax, which keeps a row's
+// tiles (TMA).  11 walks through the block's units, describes each to the others in shared memory and loads its query
+// rows (TMA).  For an 8-bit cache, 12-15 turn codes into bf16 on their way into the MMA's operand tiles (as in the
+// few-rows kernel).  Registers are dealt out by warpgroups, most of them to the softmax, which keeps a row's
 // scores in them.
 #pragma once
 #include "attn_common.cuh"
 
 namespace ead {
 
-constexpr int kChunkWarps = 16;
-constexpr int kChunkThreads = 32 * kChunkWarps;
 constexpr int kChunkMmaWarp = 8, kChunkLoadWarp = 9, kChunkUnitWarp = 11, kChunkFeedWarp = 12;
 constexpr int kChunkKeys = 64;                    // keys per tile
 constexpr int kChunkShift = 6;
-constexpr int kChunkRows = 256;                   // packed rows per unit
+constexpr int kChunkRows = 256;                   // rows per unit
 constexpr size_t kChunkPartOffset = 4u << 20;     // the few-rows kernel's parts end below this
 
 // Two bf16 rows of a register's codes, chosen by `pick`, times 2^-120 (see the few-rows kernel).
@@ -48,9 +47,10 @@ struct ChunkLayout {
     static constexpr int kRawBytes = kRaw * (kRawTile + kRawScale);
     static constexpr int kBars = 2 * kStages + 2 * kRaw + 18;
     static constexpr int kSmem = 1024 + 2 * kQTile + kStages * kTileBytes + kRawBytes + 8 * kBars;
-    // registers per thread: two softmax warpgroups, MMA and loads, feeders; together the 4 x 128 of the launch
-    static constexpr int kSoftmaxRegs = FMT == kFmtBf16 ? 168 : 152, kIssueRegs = 88, kFeedRegs = FMT == kFmtBf16 ? 88 : 120;
-    static_assert(2 * kSoftmaxRegs + kIssueRegs + kFeedRegs <= 512, "more than the block was launched with");
+    static constexpr int kWarps = FMT == kFmtBf16 ? 12 : 16, kThreads = 32 * kWarps;
+    // registers per thread: two softmax warpgroups, MMA and loads, converters; together at most what the block is launched with
+    static constexpr int kSoftmaxRegs = FMT == kFmtBf16 ? 200 : 152, kIssueRegs = 88, kFeedRegs = FMT == kFmtBf16 ? 0 : 120;
+    static_assert(2 * kSoftmaxRegs + kIssueRegs + kFeedRegs <= (FMT == kFmtBf16 ? 3 * 168 : 4 * 128), "registers of the launch");
 };
 
 // ---- the string of tiles: units in the order (sequence, cache head, run of rows); a unit costs kChunkUnitCost (query rows
@@ -61,7 +61,7 @@ struct ChunkCursor {
     int b, h, blk;                                // sequence, cache head, run of 256 rows
     int64_t begin;                                // the unit's place in the string
     SeqInfo s;
-    int row0, rows;                               // packed rows of the unit
+    int i0, tokens;                               // first new token of the unit, and how many
     int pa, pb;                                   // positions of its first and last token
     int cost;                                     // per tile
     KeyRange r;
@@ -71,17 +71,17 @@ struct ChunkCursor {
 };
 __device__ __forceinline__ int chunk_blocks(const AttnParams &p, const SeqInfo &s)
 {
-    const int rows = s.n * p.group;               // the host has checked that this fits
-    return rows <= p.few_rows ? 0 : (rows + kChunkRows - 1) / kChunkRows;
+    const int per = 2 * p.tile_tokens;
+    return s.n * p.group <= p.few_rows ? 0 : (s.n + per - 1) / per;   // the host has checked that the product fits
 }
 __device__ __forceinline__ void chunk_unit(const AttnParams &p, const SeqInfo &s, int blk, ChunkCursor *c)
 {
     c->blk = blk;
-    c->row0 = blk * kChunkRows;
-    c->rows = min(kChunkRows, s.n * p.group - c->row0);
-    c->pa = s.p0 + c->row0 / p.group;
-    c->pb = s.p0 + (c->row0 + c->rows - 1) / p.group;
-    c->cost = c->rows > kChunkRows / 2 ? 2 : 1;
+    c->i0 = blk * 2 * p.tile_tokens;
+    c->tokens = min(2 * p.tile_tokens, s.n - c->i0);
+    c->pa = s.p0 + c->i0;
+    c->pb = c->pa + c->tokens - 1;
+    c->cost = c->tokens > p.tile_tokens ? 2 : 1;
     c->r = key_range(c->pa, c->pb, s.len, p.window, p.sinks, kChunkShift);
 }
 // Moves on to the next unit.
@@ -112,7 +112,7 @@ __device__ __forceinline__ void chunk_stretch(const ChunkCursor &c, int64_t g0, 
 // A block's part of a unit, as warp 11 describes it to the others.
 struct ChunkUnit {
     int b, h, token0;                             // sequence, cache head, first row of the sequence in the step
-    int row0, rows;                               // packed rows
+    int i0, tokens;                               // first new token, tokens
     int p0, len;                                  // position of the sequence's first new token, keys in the cache
     int lo, hi, sink_tiles, first_tile;           // keys (KeyRange)
     int ta, nt;                                   // first tile, tiles
@@ -250,12 +250,13 @@ __device__ __forceinline__ void store_32(uint8_t *dst, const uint32_t (&v)[8], b
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 template <int FMT, int D>
-__global__ void __launch_bounds__(kChunkThreads, 1)
-    ead_attn_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, AttnParams p,
+__global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
+    ead_attn_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                          const __grid_constant__ CUtensorMap tmQ, AttnParams p,
                           int box_shift, int min_cost)
 {
     using L = ChunkLayout<FMT, D>;
-    constexpr int S = L::kStages;
+    constexpr int S = L::kStages, kChunkWarps = L::kWarps, kChunkThreads = L::kThreads;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int64_t s_scan[kChunkWarps];
     __shared__ int s_b, s_last;
@@ -278,6 +279,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     if (tid == 32) {
         tma_prefetch_desc(&tmK);
         tma_prefetch_desc(&tmV);
+        tma_prefetch_desc(&tmQ);
     }
     if (tid == 0) {
         for (int i = 0; i < S; ++i) {
@@ -300,7 +302,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             mbar_init(bar_u_full + 8 * i, 1);
             mbar_init(bar_u_empty + 8 * i, kChunkWarps - 1);
         }
-        mbar_init(bar_q_full, 128);
+        mbar_init(bar_q_full, 1);
         mbar_init(bar_q_empty, 2);
         fence_mbar_init();
     }
@@ -397,7 +399,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         // the first unit with a tile that begins at g0 or later
         while (cur.tiles_at() + static_cast<int64_t>(cur.cost) * (cur.r.tiles - 1) < g0) chunk_next(p, &cur);
     }
-    __syncthreads();                               // s_cost is done with; its place takes query rows now
+    fence_async_shared();
+    __syncthreads();                               // s_cost is done with; its place takes query rows now, by TMA
 
     bool expired = false;
     // Every role takes the units one by one: waits for the description, works, releases it (one arrival per warp).
@@ -425,7 +428,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 if (lane == 0) {
                     ChunkUnit &u = s_unit[n & 1];
                     u.b = cur.b; u.h = cur.h; u.token0 = cur.s.token0;
-                    u.row0 = cur.row0; u.rows = cur.rows;
+                    u.i0 = cur.i0; u.tokens = cur.tokens;
                     u.p0 = cur.s.p0; u.len = cur.s.len;
                     u.lo = cur.r.lo; u.hi = cur.r.hi; u.sink_tiles = cur.r.sink_tiles; u.first_tile = cur.r.first_tile;
                     u.ta = ta; u.nt = tb - ta;
@@ -437,6 +440,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                     u.blocks = static_cast<int>(((end - cur.cost + 1) * ctas - 1) / W) - u.first + 1;
                     u.first_part = at <= W * u.first / ctas ? 0 : 1;
                     mbar_arrive(bar_u_full + 8 * (n & 1));
+                }
+                // its query rows, when the unit before has done with theirs (rows of tokens behind the unit's come along)
+                wait_phase(bar_q_empty, (n & 1) ^ 1, p.status, &expired);
+                __syncwarp();
+                if (lane == 0) {
+                    const uint32_t box = p.tile_tokens * p.group * 128;
+                    mbar_arrive_expect_tx(bar_q_full, cur.cost * L::kHalves * box);
+                    for (int x = 0; x < cur.cost * L::kHalves; ++x) {
+                        const int tile = x / L::kHalves, hb = x - tile * L::kHalves;
+                        tma_load_3d(q_smem + tile * L::kQTile + hb * (128 * 128), &tmQ, 64 * hb, cur.h * p.group,
+                                    cur.s.token0 + cur.i0 + tile * p.tile_tokens, bar_q_full);
+                    }
                 }
                 if (end + kChunkUnitCost >= g1) break;
                 chunk_next(p, &cur);
@@ -572,40 +587,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 if (last) break;
             }
         }
-    } else if (warp >= kChunkFeedWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kFeedRegs));
-        // ================================================================ query rows; codes to bf16
+    } else if (FMT == kFmtE4m3 && warp >= kChunkFeedWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(FMT == kFmtE4m3 ? L::kFeedRegs : 24));
+        // ================================================================ codes to bf16
         const int ft = tid - kChunkFeedWarp * 32;  // 0 .. 127
         int t = 0;
         for (int n = 0;; ++n) {
             const ChunkUnit &un = unit_wait(n);
             const int last = un.last;
-            wait_phase(bar_q_empty, (n & 1) ^ 1, p.status, &expired);
-            constexpr int kChunks = D / 8;         // 16-byte pieces per row
-            // 16 bytes per thread and step, all copies in flight at once, zeros behind the last row; token and head of a row are
-            // carried along (a division per step took longer than the copies: its conversions queue behind the exponentials)
-            constexpr int kStep = 128 / kChunks;   // rows per step
-            const int ch = ft % kChunks, rows = un.rows, step_i = kStep / p.group, step_g = kStep - step_i * p.group;
-            int row = ft / kChunks, i = (un.row0 + row) / p.group, gq = un.row0 + row - i * p.group;
-            const uint8_t *const q0 = p.q + 2 * (static_cast<int64_t>(un.token0) * p.q_stride + static_cast<int64_t>(un.h) * p.group * D + 8 * ch);
-            const uint32_t dst0 = q_smem + (ch >> 3) * (128 * 128);
-#pragma unroll 4
-            for (; row < (un.dual ? 256 : 128); row += kStep) {
-                const bool there = row < rows;
-                const uint8_t *src = there ? q0 + 2 * (i * p.q_stride + gq * D) : p.q;
-                const uint32_t dst = dst0 + (row >> 7) * L::kQTile + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-                gq += step_g;
-                i += step_i;
-                if (gq >= p.group) {
-                    gq -= p.group;
-                    ++i;
-                }
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_async_shared();
-            mbar_arrive(bar_q_full);
-            if (FMT == kFmtE4m3) {
+            {
                 for (int k = un.ta, end = un.ta + un.nt; k < end; ++k, ++t)
                     for (int kv = 0; kv < 2; ++kv) {
                         // half a key per thread: threads 0-63 the first half of the dimensions, 64-127 the second
@@ -677,13 +667,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             const ChunkUnit &u = unit_wait(n);
             const bool dual = u.dual != 0;
             const int ta = u.ta, nt = u.nt, rounds = dual ? nt : (nt + 1 - w) >> 1;
-            const int my_row = dual ? w * 128 + row : row;                       // packed row within the unit
-            const int pos = u.p0 + (u.row0 + min(my_row, u.rows - 1)) / p.group;
+            const int my_row = dual ? w * 128 + row : row;                       // row within the unit
+            const int tile0 = dual ? w * p.tile_tokens : 0, tile1 = min(tile0 + p.tile_tokens, u.tokens);   // the row tile's tokens
+            const int my_i = tile0 + row / p.group, gq = row - (my_i - tile0) * p.group;
+            const int first_pos = u.p0 + u.i0, pos = first_pos + min(my_i, u.tokens - 1);
             // A tile needs no mask if its last key is no later than the row tile's first position (and in the cache), and its first
             // key is in the window of the row tile's last one, or all of it are sinks.
-            const int row_a = dual ? w * 128 : 0, row_b = min(row_a + 127, u.rows - 1);
-            const int no_later = min(u.p0 + (u.row0 + row_a) / p.group, u.len - 1) - (kChunkKeys - 1);
-            const int no_sooner = p.window ? u.p0 + (u.row0 + row_b) / p.group - p.window + 1 : -0x40000000;
+            const int no_later = min(first_pos + tile0, u.len - 1) - (kChunkKeys - 1);
+            const int no_sooner = p.window ? first_pos + tile1 - p.window : -0x40000000;
             const int sink_tiles = u.sink_tiles, first_tile = u.first_tile - sink_tiles;
             float m = -INFINITY, l = 0.f;
             for (int i = 0; i < rounds; ++i) {
@@ -807,9 +798,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 }
             }
             const bool holds = dual || w == 0;
-            const bool live = holds && my_row < u.rows;
-            const int pi = (u.row0 + my_row) / p.group, hq = u.h * p.group + (u.row0 + my_row - pi * p.group);
-            const int64_t token = static_cast<int64_t>(u.token0) + pi;
+            const bool live = holds && my_i < tile1;
+            const int hq = u.h * p.group + gq;
+            const int64_t token = static_cast<int64_t>(u.token0) + u.i0 + my_i;
             if (holds) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -868,8 +859,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 if (s_last) {
                     fence_gpu();
                     const int first_slot = u.first_part, last = first + blocks - 1;
-                    if (tid < u.rows) {          // one row per thread, 32 columns at a time
-                        const int r = tid;
+                    const int r = tid, ti = (tid >> 7) * p.tile_tokens + (tid & 127) / p.group;
+                    if (ti < min(((tid >> 7) + 1) * p.tile_tokens, u.tokens)) {    // one row per thread
                         auto part_of = [&](int k) { return parts + (2 * k + (k == first ? first_slot : 0)) * kPart; };
                         float M = -INFINITY, Lsum = 0.f;
 #pragma unroll 4
@@ -880,8 +871,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                             M = top;
                         }
                         const float inv = Lsum == 0.f ? 0.f : 1.f / Lsum;
-                        const int i = (u.row0 + r) / p.group, hr = u.h * p.group + (u.row0 + r - i * p.group);
-                        const int64_t tok = static_cast<int64_t>(u.token0) + i;
+                        const int hr = u.h * p.group + (tid & 127) % p.group;
+                        const int64_t tok = static_cast<int64_t>(u.token0) + u.i0 + ti;
                         if (p.lse) p.lse[tok * p.heads_q + hr] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
                         for (int q = 0; q < D / 64; ++q) {
                             float4 a[16];

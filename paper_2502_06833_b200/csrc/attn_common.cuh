@@ -21,6 +21,7 @@ struct AttnParams {
     int64_t q_stride, out_stride;                 // elements between tokens
     int32_t heads_q, group, window, sinks;
     int32_t few_rows;                             // units of at most this many packed rows go to the few-rows kernel
+    int32_t tile_tokens;                          // chunk kernel: whole tokens in a tile of 128 rows
     float scale_log2;                             // scale * log2(e): logits are kept in units of log 2
     uint32_t *status;
     uint8_t *workspace;

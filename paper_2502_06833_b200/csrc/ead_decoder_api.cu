@@ -67,6 +67,20 @@ bool encode_pool(CUtensorMap *tm, const KvCacheView &c, int format, void *base, 
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The query rows as {dimension, head, token}; a box is 64 dimensions of a cache head's query heads for the tokens of a row tile.
+bool encode_queries(CUtensorMap *tm, const AttnParams &p)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(p.cache.head_dim), static_cast<cuuint64_t>(p.heads_q),
+                                static_cast<cuuint64_t>(p.batch.n_tokens)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(2 * p.cache.head_dim), static_cast<cuuint64_t>(2 * p.q_stride)};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(p.group), static_cast<cuuint32_t>(p.tile_tokens)}, ones[3] = {1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint8_t *>(p.q), dims, strides, box, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int FMT, int D, int NB>
 int launch_few_rows(const AttnParams &p, int sms, cudaStream_t s)
 {
@@ -92,7 +106,9 @@ int launch_chunk(const AttnParams &p, int sms, cudaStream_t s)
     const int keys = std::min(p.cache.page_size, kChunkKeys);
     CUtensorMap tk, tv;
     if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys, 1) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys, 1)) return EAD_ECUDA;
-    ead_attn_chunk_kernel<FMT, D><<<std::min(sms, kAttnMaxCtas), kChunkThreads, L::kSmem, s>>>(tk, tv, p, __builtin_ctz(keys), kChunkMinCost);
+    CUtensorMap tq;
+    if (!encode_queries(&tq, p)) return EAD_ECUDA;
+    ead_attn_chunk_kernel<FMT, D><<<std::min(sms, kAttnMaxCtas), L::kThreads, L::kSmem, s>>>(tk, tv, tq, p, __builtin_ctz(keys), kChunkMinCost);
     return launched();
 }
 
@@ -296,6 +312,7 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
     // Units of up to 16 packed rows have a kernel of their own.  Where longer chunks are there as well, only up to 8:
     // a second group of 8 rows costs every unit, and the other kernel runs anyway.
     const int64_t most = static_cast<int64_t>(p.batch.max_new) * p.group;
+    p.tile_tokens = 128 / p.group;
     p.few_rows = p.group > kDecodeRows ? 0 : most <= 8 || (most > kDecodeRows && p.group <= 8) ? 8 : kDecodeRows;
     if (most > 0x7fffffff) return EAD_EINVALID_ARG;
     const bool bf16 = cache->format == EAD_FMT_BF16, wide = p.cache.head_dim == 128;

@@ -120,6 +120,14 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *tmap, int3
         : "memory");
 }
 
+// 3-D tiled load, as above.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int32_t x0, int32_t x1, int32_t x2, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x0), "r"(x1), "r"(x2), "r"(bar)
+        : "memory");
+}
 // 5-D tiled load, as above.
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const void *tmap, int32_t x0, int32_t x1, int32_t x2, int32_t x3,
                                             int32_t x4, uint32_t bar)
