@@ -915,6 +915,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     tc_fence_before_sync();
     __syncthreads();
     if (warp == kChunkMmaWarp) tmem_dealloc(tmem, 512);
+    griddep_wait();                                // started alongside the few-rows kernel: it ends before this one does
 }
 
 }  // namespace ead

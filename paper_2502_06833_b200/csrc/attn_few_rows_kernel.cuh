@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvCacheView &c = p.cache;
 
+    griddep_launch_dependents();                   // the chunk kernel of the same step needs nothing of this one but its SMs
     if (tid == 0) {
         tma_prefetch_desc(&tmK);
         tma_prefetch_desc(&tmV);

@@ -108,8 +108,22 @@ int launch_chunk(const AttnParams &p, int sms, cudaStream_t s)
     if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys, 1) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys, 1)) return EAD_ECUDA;
     CUtensorMap tq;
     if (!encode_queries(&tq, p)) return EAD_ECUDA;
-    ead_attn_chunk_kernel<FMT, D><<<std::min(sms, kAttnMaxCtas), L::kThreads, L::kSmem, s>>>(tk, tv, tq, p, __builtin_ctz(keys), kChunkMinCost);
-    return launched();
+    // Behind the few-rows kernel of the same call it may start as that one's blocks leave their SMs.
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(std::min(sms, kAttnMaxCtas));
+    cfg.blockDim = dim3(L::kThreads);
+    cfg.dynamicSmemBytes = L::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.few_rows ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, ead_attn_chunk_kernel<FMT, D>, tk, tv, tq, p, static_cast<int>(__builtin_ctz(keys)), kChunkMinCost) != cudaSuccess) {
+        cudaGetLastError();
+        return EAD_ECUDA;
+    }
+    return EAD_OK;
 }
 
 template <int FMT, int D, int NB>
