@@ -225,11 +225,21 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
 // swizzle, 8-row groups 1024 bytes apart.  Tiles are rows of 64 elements.  Query rows and keys are contracted along the row
 // (leading offset unused, 16 bytes).  Values are contracted along the ROW INDEX, their head dimension is the
 // contiguous one: leading offset = next 64 elements of the head dimension, stride offset = next 8 keys.
-__device__ __forceinline__ uint64_t umma_desc_of(uint32_t lo)
-{
-    const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
-    return (static_cast<uint64_t>(hi) << 32) | lo;
-}
+__device__ __forceinline__ uint32_t umma_desc_hi(uint32_t next8) { return (next8 >> 4) | (1u << 14) | (2u << 29); }
+__device__ __forceinline__ uint64_t umma_desc_of(uint32_t lo) { return static_cast<uint64_t>(umma_desc_hi(1024)) << 32 | lo; }
+// A tile of values in shared memory: box after box of 2^shift keys, in each the first 64 dimensions of its keys, then the
+// next 64.  A step of 16 keys lies within one box, or is two boxes of 8.
+template <int D>
+struct ValueTile {
+    int shift;
+    uint32_t line, next8;                         // from 64 dimensions to the next 64, from 8 keys to the next 8
+    __device__ __forceinline__ explicit ValueTile(int box_shift)
+        : shift(box_shift), line(128u << box_shift), next8(box_shift == 3 ? 1024u * (D / 64) : 1024u) {}
+    __device__ __forceinline__ uint32_t at(int key) const
+    {
+        return ((key >> shift) * (D / 64) << shift) * 128u + (key & ((1 << shift) - 1)) * 128u;
+    }
+};
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t p;
@@ -495,9 +505,13 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                             if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D * 2);
                             __syncwarp();
                             if (page >= 0) {
+                                if (kv) {          // all lines of its keys in one box (see the value tiles' descriptor)
+                                    tma_load_5d(dst + (L::kHalves - 1) * lane * box_keys * 128, tm, 0, slot, 0, h, page, bar);
+                                } else {
 #pragma unroll
-                                for (int hb = 0; hb < L::kHalves; ++hb)
-                                    tma_load_5d(dst + hb * L::kLine, tm, 0, slot, hb, h, page, bar);
+                                    for (int hb = 0; hb < L::kHalves; ++hb)
+                                        tma_load_5d(dst + hb * L::kLine, tm, 0, slot, hb, h, page, bar);
+                                }
                             }
                         } else {
                             const int st = x % L::kRaw;
@@ -527,7 +541,9 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             // instead of 663 (measured alone; the tensor core needs 512).
             const int w = __shfl_sync(0xffffffffu, (warp - kChunkMmaWarp) >> 1, 0);  // row tile
             const uint32_t id_qk = umma_idesc_bf16_m128(kChunkKeys), id_pv = umma_idesc_bf16_m128(D) | (1u << 16);
-            const uint32_t q_lo = (q_smem >> 4) | (1u << 16), k_lo = (ring >> 4) | (1u << 16), v_lo = (ring >> 4) | ((L::kLine >> 4) << 16);
+            const uint32_t q_lo = (q_smem >> 4) | (1u << 16), k_lo = (ring >> 4) | (1u << 16);
+            const ValueTile<D> vt(FMT == kFmtBf16 ? box_shift : kChunkShift);
+            const uint32_t v_lo = (ring >> 4) | (vt.line << (16 - 4)), v_hi = umma_desc_hi(vt.next8);
             const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
             int t = 0;
             int ns = 0, np = 0;                    // scores issued and probabilities taken so far
@@ -573,7 +589,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     if (elect_one()) {
 #pragma unroll
                         for (int ks = 0; ks < kChunkKeys / 16; ++ks)
-                            umma_bf16_ts(t_o, pr + ks * 8, umma_desc_of(b + ks * (2048 >> 4)), id_pv, i > 0 || ks > 0);
+                            umma_bf16_ts(t_o, pr + ks * 8, static_cast<uint64_t>(v_hi) << 32 | (b + (vt.at(16 * ks) >> 4)), id_pv, i > 0 || ks > 0);
                         umma_commit(bar_v + 8 * w);
                         umma_commit(bar_empty + 8 * st);
                         if (!dual) umma_commit(bar_empty + 8 * st);
@@ -689,7 +705,8 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                         const int x = 2 * (t + k) + 1, st = x % S;
                         wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
                         if (row < kChunkKeys * L::kHalves && !u.seen(p.sinks, key0 + (row & 63))) {
-                            const uint32_t dst = ring + st * L::kTileBytes + (row >> 6) * L::kLine + (row & 63) * 128;
+                            const ValueTile<D> vt(box_shift);
+                            const uint32_t dst = ring + st * L::kTileBytes + (row >> 6) * vt.line + vt.at(row & 63);
 #pragma unroll
                             for (int ch = 0; ch < 8; ++ch)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + ch * 16), "r"(0) : "memory");

@@ -105,7 +105,8 @@ int launch_chunk(const AttnParams &p, int sms, cudaStream_t s)
     using L = ChunkLayout<FMT, D>;
     const int keys = std::min(p.cache.page_size, kChunkKeys);
     CUtensorMap tk, tv;
-    if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys, 1) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys, 1)) return EAD_ECUDA;
+    if (!encode_pool(&tk, p.cache, FMT, p.cache.k, keys, 1) || !encode_pool(&tv, p.cache, FMT, p.cache.v, keys, FMT == kFmtBf16 ? D / 64 : 1))
+        return EAD_ECUDA;
     CUtensorMap tq;
     if (!encode_queries(&tq, p)) return EAD_ECUDA;
     // Behind the few-rows kernel of the same call it may start as that one's blocks leave their SMs.
