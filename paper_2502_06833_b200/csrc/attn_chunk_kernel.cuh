@@ -257,6 +257,7 @@ __device__ __forceinline__ void store_32(uint8_t *dst, const uint32_t (&v)[8], b
         reinterpret_cast<uint4 *>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
     }
 }
+__device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 template <int FMT, int D>
@@ -693,6 +694,9 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             const int no_sooner = p.window ? first_pos + tile1 - p.window : -0x40000000;
             const int sink_tiles = u.sink_tiles, first_tile = u.first_tile - sink_tiles;
             float m = -INFINITY, l = 0.f;
+            // Two-tile units: the row tiles take turns at the exponentials, so that one's run while the other waits for scores,
+            // loads them and looks for their maximum.
+            if (dual && w == 1) named_arrive(2, 256);
             for (int i = 0; i < rounds; ++i) {
                 const int k = dual ? i : 2 * i + w;
                 const int kt = ta + k, key0 = (kt < sink_tiles ? kt : kt + first_tile) << kChunkShift;
@@ -757,6 +761,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                         }
                     }
                 }
+                if (dual) named_sync(2 + w, 256);  // the other row tile's exponentials are done
                 const float mm = m == -INFINITY ? 0.f : m;
                 const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2), minus2 = pack_f32x2(-mm, -mm);
                 uint64_t sum2[2] = {0, 0};
@@ -775,6 +780,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     }
                     tmem_st16(t_s + 16 * q, pk);   // columns whose scores are in registers
                 }
+                if (dual && (w == 0 || i + 1 < rounds)) named_arrive(3 - w, 256);
                 tmem_wait_st();
                 tc_fence_before_sync();
                 mbar_arrive(done);
