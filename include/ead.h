@@ -423,7 +423,7 @@ typedef struct ead_kv_cache {
  */
 typedef struct ead_kv_batch {
     int32_t B;               /* sequences, 1 .. 4096                                            */
-    int32_t n_tokens;        /* new tokens of the step = new_start[B]; >= 0                     */
+    int32_t n_tokens;        /* new tokens of the step = new_start[B]; 0 .. 2^30                */
     int32_t max_new;         /* >= every n_b                                                    */
     int32_t max_len;         /* >= every kv_len[b], at most 2^30                                */
     const int32_t *new_start;    /* dev [B + 1], ascending, new_start[0] = 0                    */

@@ -45,11 +45,11 @@ struct SeqInfo {
 __device__ __forceinline__ SeqInfo seq_info(const KvBatchView &bt, int b, bool *bad = nullptr)
 {
     SeqInfo s;
-    const int kv = __ldg(bt.kv_len + b), end = __ldg(bt.new_start + b + 1);
+    const int kv = max(__ldg(bt.kv_len + b), 0), end = __ldg(bt.new_start + b + 1);
     s.token0 = __ldg(bt.new_start + b);
     s.n = end - s.token0;
     s.p0 = kv - s.n;
-    s.len = min(max(kv, 0), bt.max_len);
+    s.len = min(kv, bt.max_len);
     const bool wrong = s.n < 0 || s.n > bt.max_new || s.token0 < 0 || end > bt.n_tokens;
     if (wrong) s.n = 0;
     if (bad) *bad = wrong;
@@ -66,7 +66,7 @@ struct KeyRange {
         return (t < sink_tiles ? t : t - sink_tiles + first_tile) << shift;
     }
 };
-// (A negative pb + 1 leaves nothing; positions stay below 2^30 + 2^30.)
+// (A negative pb + 1 leaves nothing.  Positions are at least -2^30 and the window at most 2^30: nothing overflows.)
 __device__ __forceinline__ KeyRange key_range(int pa, int pb, int len, int window, int sinks, int shift)
 {
     KeyRange r;

@@ -205,7 +205,7 @@ int check_batch(const ead_kv_batch *b, const KvCacheView &c, bool needs_len, KvB
     if (!b->new_start || (needs_len && !b->kv_len) || !b->page_table || b->table_stride < 1) return EAD_EINVALID_ARG;
     if (b->n_tokens > static_cast<int64_t>(b->B) * b->max_new) return EAD_EINVALID_ARG;
     if (b->max_len > static_cast<int64_t>(b->table_stride) * c.page_size) return EAD_EINVALID_ARG;
-    if (b->max_len > (1 << 30)) return EAD_EINVALID_ARG;   // positions stay within 32 bits
+    if (b->max_len > (1 << 30) || b->n_tokens > (1 << 30)) return EAD_EINVALID_ARG;   // positions stay within 32 bits
     if (!aligned(b->new_start, 4) || !aligned(b->kv_len, 4) || !aligned(b->page_table, 4)) return EAD_EALIGNMENT;
     v->new_start = b->new_start;
     v->kv_len = b->kv_len;
@@ -318,7 +318,7 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
     p.out_stride = out_stride;
     p.heads_q = heads_q;
     p.group = heads_q / p.cache.heads;
-    p.window = window;
+    p.window = std::min(window, 1 << 30);     // positions lie below
     p.sinks = window ? sinks : 0;
     p.scale_log2 = scale * kLog2e;
     p.workspace = static_cast<uint8_t *>(workspace);

@@ -41,7 +41,8 @@ BAD_BATCH = [(dict(B=0), "I"), (dict(B=4097), "I"), (dict(n_tokens=-1), "I"), (d
              (dict(max_new=1), "I"), (dict(max_len=-1), "I"), (dict(max_len=65), "I"), (dict(new_start=None), "I"),
              (dict(page_table=None), "I"), (dict(table_stride=0), "I"), (dict(reserved=3), "I"),
              (dict(new_start=4098), "A"), (dict(page_table=4097), "A"),
-             (dict(max_len=(1 << 30) + 1, table_stride=1 << 28), "I")]
+             (dict(max_len=(1 << 30) + 1, table_stride=1 << 28), "I"),
+             (dict(n_tokens=(1 << 30) + 1, max_new=1 << 30), "I")]
 
 
 def _code(E, letter):

@@ -128,6 +128,18 @@ def test_attention_rows_that_see_nothing(E, workspace, fmt):
     _check(got, want)
 
 
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 30, 7), (3, 2 ** 31 - 1)])
+def test_attention_extreme_windows_with_rows_that_see_nothing(E, workspace, window, sinks):
+    """The largest windows and sinks next to negative positions and a negative context length."""
+    ctx = Context([4, 40, 1, 200], [1, 13, 700, 150], 2, 128, 16, seed=16)
+    q = _q(ctx, 4)
+    _check(_attend(E, ctx, q, workspace, 0.1, window, sinks), attention(ctx, q, 0.1, min(window, 10 ** 6), min(sinks, 10 ** 6)))
+    ctx.d_len[0] = -5                                   # counts as no context
+    ctx.length[0] = 0
+    out, lse, st = _attend(E, ctx, q, workspace, 0.1, window, sinks, max_len=700)
+    assert st == 0 and (out[:4] == 0).all() and torch.isneginf(lse[:4]).all()
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("layout", ["token", "padded"])
 @pytest.mark.parametrize("dim", [64, 128])
