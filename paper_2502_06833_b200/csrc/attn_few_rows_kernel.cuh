@@ -18,6 +18,8 @@
 // Values: an e4m3 byte placed 4 bits down in a bf16 is 2^-120 of its value, subnormals included; the factor 2^(120 + k)
 // goes to the probabilities (an exact change of exponent), once per key and scale block instead of once per value.
 #pragma once
+#include <type_traits>
+
 #include "attn_common.cuh"
 
 namespace ead {
@@ -52,6 +54,12 @@ __device__ __forceinline__ void mma16816_f16(float (&c)[4], uint32_t a0, uint32_
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same with an accumulator of zeros.
+__device__ __forceinline__ void mma16816_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
@@ -492,13 +500,12 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                     } else {                                    // one scale block: two steps of 16 dimensions
                         float sb[NB][4];
 #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) sb[nb][0] = sb[nb][1] = sb[nb][2] = sb[nb][3] = 0.f;
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)             // matrices 2u (keys 0-7) and 2u + 1 (keys 8-15)
-#pragma unroll
-                            for (int nb = 0; nb < NB; ++nb)
-                                mma16816_f16(sb[nb], codes_to_f16x2_lo(a[2 * u]), codes_to_f16x2_lo(a[2 * u + 1]), codes_to_f16x2_hi(a[2 * u]),
-                                             codes_to_f16x2_hi(a[2 * u + 1]), qf[2 * j + u][nb][0], qf[2 * j + u][nb][1]);
+                        for (int nb = 0; nb < NB; ++nb) {       // matrices 0, 2 (keys 0-7) and 1, 3 (keys 8-15)
+                            mma16816_f16_first(sb[nb], codes_to_f16x2_lo(a[0]), codes_to_f16x2_lo(a[1]), codes_to_f16x2_hi(a[0]),
+                                               codes_to_f16x2_hi(a[1]), qf[2 * j][nb][0], qf[2 * j][nb][1]);
+                            mma16816_f16(sb[nb], codes_to_f16x2_lo(a[2]), codes_to_f16x2_lo(a[3]), codes_to_f16x2_hi(a[2]),
+                                         codes_to_f16x2_hi(a[3]), qf[2 * j + 1][nb][0], qf[2 * j + 1][nb][1]);
+                        }
                         const float f0 = key_scale(ksc[st][0], j), f1 = key_scale(ksc[st][1], j);
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) {
@@ -600,40 +607,48 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
                         pair[i][2] = __byte_perm(e0, e1, 0x7632);
                         pair[i][3] = __byte_perm(o0, o1, 0x7632);
                     }
-                    // the factors: 2^(120 + k), or 2^k where the values themselves are brought to size
-                    const uint32_t bias = far ? 0u : 0x3C003C00u;
+                    if (!whole) {                  // any code is finite: with a finite factor what no query sees counts 0
 #pragma unroll
-                    for (int j = 0; j < D / 32; ++j) {
-                        const uint32_t(&a)[4] = frag[st * PER + j];
-                        uint32_t w[NB][2];
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            uint32_t f = pair[i][j] * 128u + bias;
-                            if (far) {             // byte 255 marks NaNs
-                                if ((f & 0xffffu) == 0x7f80u) f |= 0x40u;
-                                if ((f >> 16) == 0x7f80u) f |= 0x400000u;
-                            }
-#pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) {
-                                w[nb][i] = mul_bf16x2(pf[st][nb][i], f);
-                                if (!whole) w[nb][i] &= keep[i];                // any code is finite so far: its factor decides
-                            }
-                        }
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            uint32_t v[4];
-                            v[0] = codes_to_bf16x2_even(a[2 * u]);
-                            v[1] = codes_to_bf16x2_odd(a[2 * u]);
-                            v[2] = codes_to_bf16x2_even(a[2 * u + 1]);
-                            v[3] = codes_to_bf16x2_odd(a[2 * u + 1]);
-                            if (far) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], 0x7B807B80u);       // 2^120
-                            }
-#pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) mma16816(o[2 * j + u][nb], v[0], v[1], v[2], v[3], w[nb][0], w[nb][1]);
-                        }
+                            for (int j = 0; j < 4; ++j) pair[i][j] &= keep[i];
                     }
+                    auto values = [&](auto is_far) {
+#pragma unroll
+                        for (int j = 0; j < D / 32; ++j) {
+                            const uint32_t(&a)[4] = frag[st * PER + j];
+                            uint32_t w[NB][2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                // the factors: 2^(120 + k), or 2^k where the values themselves are brought to size
+                                uint32_t f = pair[i][j] * 128u + (decltype(is_far)::value ? 0u : 0x3C003C00u);
+                                if (decltype(is_far)::value) {                   // byte 255 marks NaNs
+                                    if ((f & 0xffffu) == 0x7f80u) f |= 0x40u;
+                                    if ((f >> 16) == 0x7f80u) f |= 0x400000u;
+                                }
+#pragma unroll
+                                for (int nb = 0; nb < NB; ++nb) w[nb][i] = mul_bf16x2(pf[st][nb][i], f);
+                            }
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                uint32_t v[4];
+                                v[0] = codes_to_bf16x2_even(a[2 * u]);
+                                v[1] = codes_to_bf16x2_odd(a[2 * u]);
+                                v[2] = codes_to_bf16x2_even(a[2 * u + 1]);
+                                v[3] = codes_to_bf16x2_odd(a[2 * u + 1]);
+                                if (decltype(is_far)::value) {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], 0x7B807B80u);   // 2^120
+                                }
+#pragma unroll
+                                for (int nb = 0; nb < NB; ++nb) mma16816(o[2 * j + u][nb], v[0], v[1], v[2], v[3], w[nb][0], w[nb][1]);
+                            }
+                        }
+                    };
+                    if (far)
+                        values(std::true_type{});
+                    else
+                        values(std::false_type{});
                 }
             }
             }
