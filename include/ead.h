@@ -465,7 +465,11 @@ int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int3
  * with sums and maxima in 32 bits; probabilities are rounded to bf16 (the type of the values
  * they weight) before the product with v.  A query that sees nothing (its position is negative)
  * gets zeros and lse = -infinity.  Keys that no query of a sequence sees are not
- * read, nor are the page table entries of pages that hold only such keys.
+ * read, nor are the page table entries of pages that hold only such keys.  A key that is not finite
+ * touches only the queries that see it; a VALUE that is not finite and is seen by one query can also
+ * reach the sequence's other queries of this call, in its cache head and dimension (a probability of 0 times
+ * NaN is NaN, as in a matrix product with a masked softmax): a caller that has to tell them apart
+ * calls once per token.
  *   q          dev, bf16 [n_tokens, heads_q, head_dim], q_stride elements between tokens
  *   heads_q    a multiple of heads_kv, at most 128 per cache head
  *   scale      of the logits, finite and > 0

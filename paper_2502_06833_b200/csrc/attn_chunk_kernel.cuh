@@ -5,8 +5,8 @@
 // caller's [tokens, heads, head_dim] array.  Per key tile and row tile: S = Q K^T (TMEM),
 // one thread per row turns S into probabilities P, which overwrite S as bf16 in TMEM, O += P V (TMEM).  Every row tile has two
 // S buffers, so the scores of the next key tile are there when the softmax of this one ends: tensor core and softmax do not
-// wait for each other's round trip.  (With 128-key tiles TMEM has room for one S per row tile: 5860 cycles per 256 x 128
-// scores instead of the ~2560 that the operands' reads from shared memory take.)  A unit of one row tile
+// wait for each other's round trip.  (With 128-key tiles TMEM has room for one S per row tile,
+// which exposes that trip: 508 us against 439 on the prompt chunks below, at the time.)  A unit of one row tile
 // gives both turns to the same rows instead: even key tiles go to the first accumulator, odd ones
 // to the second, and the two are joined at the end.
 //
@@ -16,6 +16,13 @@
 // rows (TMA).  For an 8-bit cache, 12-15 turn codes into bf16 on their way into the MMA's operand tiles (as in the
 // few-rows kernel).  Registers are dealt out by warpgroups, most of them to the softmax, which keeps a row's
 // scores in them.
+//
+// What bounds it: at size the tensor core, whose operand reads take 2836 cycles per 256 rows x 128 keys (measured with the
+// MMAs alone), and the exponentials, 2048 cycles of the special function units; together 3560.  Both row tiles'
+// exponentials at once stall each other and then leave the units idle, so the two softmax warpgroups take turns at them
+// (4054 cycles without).  Two chunks of 2041-2048 tokens over 6007-8192 keys, 8 cache heads of 4: 375 us,
+// 1150 TFLOP/s (435 us at the clock the power limit leaves in a long loop).  Short chunks are
+// bound by the units' beginnings and ends (query rows in, output or part out: about 8 500 cycles each).
 #pragma once
 #include "attn_common.cuh"
 
@@ -54,8 +61,8 @@ struct ChunkLayout {
 };
 
 // ---- the string of tiles: units in the order (sequence, cache head, run of rows); a unit costs kChunkUnitCost (query rows
-// in, output out: about 20 000 cycles against 2 100 per key tile of two row tiles), then 2 per tile of a two-tile unit,
-// 1 of a one-tile unit; a tile belongs to the block in whose stretch it begins
+// in, output out: about 8 500 cycles against 1 780 per key tile of two row tiles), then 2 per tile of a two-tile unit,
+// 1 of a one-tile unit; a tile belongs to the block in whose stretch it begins.  9, 12 and 16 differ by 1 % either way.
 constexpr int kChunkUnitCost = 12;
 struct ChunkCursor {
     int b, h, blk;                                // sequence, cache head, run of 256 rows

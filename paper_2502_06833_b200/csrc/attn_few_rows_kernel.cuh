@@ -17,6 +17,10 @@
 // brings its largest element to 1..2, so what an element loses is below 2^-25 of that.
 // Values: an e4m3 byte placed 4 bits down in a bf16 is 2^-120 of its value, subnormals included; the factor 2^(120 + k)
 // goes to the probabilities (an exact change of exponent), once per key and scale block instead of once per value.
+//
+// Measured (head_dim 128, 8 cache heads): bf16, 64 contexts of 1024-8192, 4 query heads each: 195 us, 6.14 TB/s, 0.95 of the
+// device's copy rate.  e4m3, 24 contexts of 4001-32001, 5 query heads each: 190 us, 4.95 TB/s, 0.77; scales applied to every value
+// instead took 234 us with 8 warps, and 12 warps instead of 8 are worth 15 %.
 #pragma once
 #include <type_traits>
 

@@ -3,6 +3,10 @@
 // A warp moves one stretch of 512 of a token's 2 x heads x head_dim values, 16 consecutive ones per lane (one 16-byte
 // store of codes, half a scale block), for a run of consecutive tokens: its lanes look up the places of all of
 // them at once, so the chain new_start -> kv_len -> page table -> data costs its latency once per run.
+//
+// Measured, 8-bit cache, 8 heads of 128: write of 24 k tokens 30-31 us, 5 TB/s, 0.78 of the device's copy rate; read of
+// 107 k tokens 114 us, 5.72 TB/s, 0.89; one step of 64 tokens (bf16) 2.9 us.  The write's bound at size is the chain of
+// look-ups and loads before the first store: with half the instructions for the largest magnitude it took as long.
 #pragma once
 #include "kv_format.cuh"
 #include "ptx_sm100.cuh"

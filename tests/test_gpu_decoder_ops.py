@@ -348,6 +348,36 @@ def test_write_and_read(E, fmt, heads, dim, page, layout):
         torch.testing.assert_close(o.cpu().double(), want_rows[name], rtol=0, atol=0, equal_nan=True)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_large_calls_move_what_small_ones_do(E, fmt):
+    """One call over 2 * 2051 * 32 * 128 values (more than 2^24) writes and reads bit by bit what a call per sequence does."""
+    new, length, heads, dim = [1, 699, 0, 1351], [5, 699, 3, 1400], 32, 128
+    whole, apart = (Context(new, length, heads, dim, 16, fmt, seed=7, stale=3.0) for _ in range(2))
+    n = int(whole.new_start[-1])
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rows = torch.randn(n, 2 * heads, dim, generator=g, device="cuda") * torch.exp(torch.randn(n, 2 * heads, 1, generator=g, device="cuda"))
+    rows = rows.bfloat16()
+    out = torch.empty_like(rows), torch.empty_like(rows)
+    first = torch.tensor([l - m for m, l in zip(new, length)], dtype=torch.int32, device="cuda")
+    st = _status()
+    E.ead_kv_write(whole.cache(E), whole.batch(E), rows[:, :heads], rows[:, heads:], status=st, stream=_stream())
+    E.ead_kv_read(whole.cache(E), whole.batch(E), out[0][:, :heads], out[0][:, heads:], first=first, status=st, stream=_stream())
+    for b, m in enumerate(new):
+        r = slice(int(whole.new_start[b]), int(whole.new_start[b]) + m)
+        if m == 0:
+            continue
+        starts = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+        batch = E.ead_kv_batch(apart.d_table[b:b + 1], starts, apart.d_len[b:b + 1], n_tokens=m, max_new=m, max_len=length[b])
+        E.ead_kv_write(apart.cache(E), batch, rows[r, :heads], rows[r, heads:], status=st, stream=_stream())
+        E.ead_kv_read(apart.cache(E), batch, out[1][r, :heads], out[1][r, heads:], first=first[b:b + 1], status=st, stream=_stream())
+    assert st.item() == 0
+    for name in whole.dev:
+        assert torch.equal(whole.dev[name].view(torch.uint8), apart.dev[name].view(torch.uint8)), name
+    assert torch.equal(out[0].view(torch.int16), out[1].view(torch.int16))
+    if fmt == "bf16":
+        assert torch.equal(out[0], rows)
+
+
 def test_every_code_and_scale_reads_exactly(E):
     """All codes under every scale the library writes: bf16 holds each value exactly."""
     codes = torch.arange(256, dtype=torch.uint8)
