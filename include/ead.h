@@ -492,6 +492,18 @@ int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *batch, const
                      float *lse, void *workspace, uint32_t *status, int32_t device, void *stream);
 
 /*
+ * DIAGNOSTIC.  How ead_kv_attention weighs one sequence for one cache head when it deals a call's chunks out to the SMs (the
+ * rule the kernel applies on the device; pure arithmetic, needs no GPU).  A unit is up to two row tiles of
+ * floor(128 / heads_per_kv) tokens; it costs 12, and per tile of 64 keys that any of its queries sees (at least
+ * one tile) 2, or 1 if it has one row tile.  Sequences of so few rows that the other kernel takes them have no units.
+ *   n_new, kv_len  of the sequence;  max_new, window, sinks  as in the call;  heads_per_kv = heads_q / heads_kv
+ *   out            host, int64 [2]: {units, their cost}
+ * Errors: EAD_EINVALID_ARG.
+ */
+int ead_plan_chunk(int32_t n_new, int32_t kv_len, int32_t max_new, int32_t heads_per_kv, int32_t window, int32_t sinks,
+                   int64_t *out);
+
+/*
  * Residual addition and root-mean-square norm of n_rows hidden rows of H elements:
  *   s = x + residual (32 bits),  residual_out = bf16(s),
  *   y = s / sqrt(mean(s^2) + eps) * weight,  out = y in `format`

@@ -40,7 +40,8 @@ SYMBOLS = ["ead_create", "ead_step", "ead_run", "ead_run_host", "ead_run_timed",
            "ead_launch_info", "ead_destroy", "ead_strerror", "ead_head_entropy_static",
            "ead_plan_split", "ead_plan_units", "ead_usage", "ead_parameter_ratio", "ead_set_done", "ead_get_done",
            "ead_shard_range", "ead_shard_partials", "ead_shard_gate", "ead_shard_connect",
-           "ead_shard_exchange_bytes", "ead_kv_write", "ead_kv_read", "ead_kv_attention", "ead_add_rmsnorm"]
+           "ead_shard_exchange_bytes", "ead_kv_write", "ead_kv_read", "ead_kv_attention", "ead_add_rmsnorm",
+           "ead_plan_chunk"]
 
 
 class EadConfig(C.Structure):
@@ -144,6 +145,8 @@ def lib() -> C.CDLL:
         L.ead_kv_read.argtypes = [vp, vp, vp, vp, vp, i64, vp, i32, vp]
         L.ead_kv_attention.restype = C.c_int
         L.ead_kv_attention.argtypes = [vp, vp, vp, i64, i32, C.c_float, i32, i32, vp, i64, vp, vp, vp, i32, vp]
+        L.ead_plan_chunk.restype = C.c_int
+        L.ead_plan_chunk.argtypes = [i32] * 6 + [C.POINTER(C.c_int64)]
         L.ead_add_rmsnorm.restype = C.c_int
         L.ead_add_rmsnorm.argtypes = [vp, i64, vp, i64, vp, i64, vp, C.c_float, i32, i32, i32, vp, i64, vp, i32, vp]
         L.ead_strerror.restype = C.c_char_p
@@ -450,6 +453,13 @@ def ead_kv_attention(cache: EadKvCache, batch: EadKvBatch, q, out, *, scale, wor
                                 stream)
     if rc:
         _check(rc, "ead_kv_attention")
+
+
+def ead_plan_chunk(n_new, kv_len, *, heads_per_kv, max_new=None, window=0, sinks=0) -> dict:
+    a = (C.c_int64 * 2)()
+    _check(lib().ead_plan_chunk(n_new, kv_len, n_new if max_new is None else max_new, heads_per_kv, window, sinks, a),
+           "ead_plan_chunk")
+    return dict(units=a[0], cost=a[1])
 
 
 def ead_add_rmsnorm(x, weight, out, *, residual=None, residual_out=None, out_scale=None, eps=1e-6, device=0,

@@ -72,16 +72,16 @@ struct ChunkCursor {
     int pa, pb;                                   // positions of its first and last token
     int cost;                                     // per tile
     KeyRange r;
-    __device__ __forceinline__ int length() const { return kChunkUnitCost + cost * r.tiles; }
+    __host__ __device__ __forceinline__ int length() const { return kChunkUnitCost + cost * r.tiles; }
     // where the first tile begins
     __device__ __forceinline__ int64_t tiles_at() const { return begin + kChunkUnitCost; }
 };
-__device__ __forceinline__ int chunk_blocks(const AttnParams &p, const SeqInfo &s)
+__host__ __device__ __forceinline__ int chunk_blocks(const AttnParams &p, const SeqInfo &s)
 {
     const int per = 2 * p.tile_tokens;
     return s.n * p.group <= p.few_rows ? 0 : (s.n + per - 1) / per;   // the host has checked that the product fits
 }
-__device__ __forceinline__ void chunk_unit(const AttnParams &p, const SeqInfo &s, int blk, ChunkCursor *c)
+__host__ __device__ __forceinline__ void chunk_unit(const AttnParams &p, const SeqInfo &s, int blk, ChunkCursor *c)
 {
     c->blk = blk;
     c->i0 = blk * 2 * p.tile_tokens;
@@ -91,7 +91,19 @@ __device__ __forceinline__ void chunk_unit(const AttnParams &p, const SeqInfo &s
     c->cost = c->tokens > p.tile_tokens ? 2 : 1;
     c->r = key_range(c->pa, c->pb, s.len, p.window, p.sinks, kChunkShift);
 }
-// Moves on to the next unit.
+// Cost of a sequence's units `first`, `first + step`, ... for one cache head.  A unit's fits into 32 bits; the sum grows with the
+// square of the prompt (1 M tokens with 32 query heads per cache head: 2^31).
+__host__ __device__ __forceinline__ int64_t chunk_cost(const AttnParams &p, const SeqInfo &s, int first, int step)
+{
+    int64_t sum = 0;
+    ChunkCursor u;
+    for (int k = first, n = chunk_blocks(p, s); k < n; k += step) {
+        chunk_unit(p, s, k, &u);
+        sum += u.length();
+    }
+    return sum;
+}
+// Moves on to the next unit (the search ends with the batch, whatever its arrays hold).
 __device__ __forceinline__ void chunk_next(const AttnParams &p, ChunkCursor *c)
 {
     c->begin += c->length();
@@ -100,10 +112,10 @@ __device__ __forceinline__ void chunk_next(const AttnParams &p, ChunkCursor *c)
         blk = 0;
         if (++c->h >= p.cache.heads) {
             c->h = 0;
-            do {
-                ++c->b;
-                c->s = seq_info(p.batch, c->b);
-            } while (chunk_blocks(p, c->s) == 0);
+            while (c->b + 1 < p.batch.B) {
+                c->s = seq_info(p.batch, ++c->b);
+                if (chunk_blocks(p, c->s)) break;
+            }
         }
     }
     chunk_unit(p, c->s, blk, c);
@@ -330,11 +342,13 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     }
 
     // ---- the string: cost of one cache head of every sequence, and where this block's stretch begins
-    int32_t *const s_cost = reinterpret_cast<int32_t *>(base_ptr);      // [B <= 4096], in the query rows' place for now
+    int64_t *const s_cost = reinterpret_cast<int64_t *>(base_ptr);      // [B], in the query rows' place for now
+    static_assert(kMaxBatch * sizeof(int64_t) <= 2 * L::kQTile, "the costs fit there");
     for (int b0 = warp * 32; b0 < p.batch.B; b0 += kChunkThreads) {
         const int b = b0 + lane;
         SeqInfo s{};
-        int blocks = 0, cost = 0;
+        int blocks = 0;
+        int64_t cost = 0;
         if (b < p.batch.B) {
             bool bad;
             s = seq_info(p.batch, b, &bad);
@@ -343,12 +357,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             if (blockIdx.x == 0 && blocks && s.p0 + s.n > p.batch.max_len) flag_status(p.status, kStatusBadPage);
         }
         unsigned many = __ballot_sync(0xffffffffu, blocks > 2);
-        ChunkCursor u;
-        if (blocks && blocks <= 2)
-            for (int k = 0; k < blocks; ++k) {
-                chunk_unit(p, s, k, &u);
-                cost += u.length();
-            }
+        if (blocks <= 2) cost = chunk_cost(p, s, 0, 1);
         while (many) {                             // long chunks: the warp's lanes share the runs of one sequence
             const int src = __ffs(many) - 1;
             many &= many - 1;
@@ -357,13 +366,9 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             t.p0 = __shfl_sync(0xffffffffu, s.p0, src);
             t.len = __shfl_sync(0xffffffffu, s.len, src);
             t.token0 = 0;
-            const int nb = __shfl_sync(0xffffffffu, blocks, src);
-            int part = 0;
-            for (int k = lane; k < nb; k += 32) {
-                chunk_unit(p, t, k, &u);
-                part += u.length();
-            }
-            part = __reduce_add_sync(0xffffffffu, part);
+            int64_t part = chunk_cost(p, t, lane, 32);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
             if (lane == src) cost = part;
         }
         if (b < p.batch.B) s_cost[b] = cost;
@@ -410,7 +415,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     if (!idle) {
         cur.b = s_b;
         cur.s = seq_info(p.batch, cur.b);
-        const int cost = s_cost[cur.b];
+        const int64_t cost = s_cost[cur.b];
         cur.h = static_cast<int>((g0 - s_before) / cost);
         cur.begin = s_before + static_cast<int64_t>(cur.h) * cost;
         chunk_unit(p, cur.s, 0, &cur);

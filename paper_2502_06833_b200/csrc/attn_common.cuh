@@ -61,13 +61,13 @@ __device__ __forceinline__ SeqInfo seq_info(const KvBatchView &bt, int b, bool *
 struct KeyRange {
     int lo, hi;                                   // window part [lo, hi); sinks are [0, min(sinks, lo))
     int sink_tiles, first_tile, tiles;
-    __device__ __forceinline__ int base(int t, int shift) const
+    __host__ __device__ __forceinline__ int base(int t, int shift) const
     {
         return (t < sink_tiles ? t : t - sink_tiles + first_tile) << shift;
     }
 };
 // (A negative pb + 1 leaves nothing.  Positions are at least -2^30 and the window at most 2^30: nothing overflows.)
-__device__ __forceinline__ KeyRange key_range(int pa, int pb, int len, int window, int sinks, int shift)
+__host__ __device__ __forceinline__ KeyRange key_range(int pa, int pb, int len, int window, int sinks, int shift)
 {
     KeyRange r;
     r.hi = min(max(pb + 1, 0), len);

@@ -127,7 +127,8 @@ __device__ __forceinline__ int few_tiles(const AttnParams &p, const SeqInfo &s, 
     *r = key_range(s.p0, s.p0 + s.n - 1, s.len, p.window, p.sinks, shift);
     return r->tiles;
 }
-// Moves on to the unit that holds tile g of the string (g is in this unit or a later one).
+// Moves on to the unit that holds tile g of the string (g is in this unit or a later one; the search ends with the batch,
+// whatever its arrays hold: the last sequence then counts as one without an end).
 __device__ __forceinline__ void few_seek(const AttnParams &p, int shift, int g, FewCursor *c)
 {
     while (g >= c->begin + c->r.tiles) {
@@ -137,6 +138,10 @@ __device__ __forceinline__ void few_seek(const AttnParams &p, int shift, int g, 
         } else {
             c->h = 0;
             do {
+                if (c->b + 1 >= p.batch.B) {
+                    c->r.tiles = 0x7fffffff - max(c->begin, 0);
+                    return;
+                }
                 ++c->b;
                 c->s = seq_info(p.batch, c->b);
                 c->r.tiles = few_tiles(p, c->s, shift, &c->r);

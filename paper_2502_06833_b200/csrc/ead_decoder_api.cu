@@ -206,7 +206,7 @@ int check_cache(const ead_kv_cache *c, KvCacheView *v)
 
 int check_batch(const ead_kv_batch *b, const KvCacheView &c, bool needs_len, KvBatchView *v)
 {
-    if (!b || b->reserved || b->B < 1 || b->B > 4096 || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0)
+    if (!b || b->reserved || b->B < 1 || b->B > kMaxBatch || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0)
         return EAD_EINVALID_ARG;
     if (!b->new_start || (needs_len && !b->kv_len) || !b->page_table || b->table_stride < 1) return EAD_EINVALID_ARG;
     if (b->n_tokens > static_cast<int64_t>(b->B) * b->max_new) return EAD_EINVALID_ARG;
@@ -249,6 +249,13 @@ int move_setup(const ead_kv_cache *cache, const ead_kv_batch *batch, const void 
     p->row_stride = stride;
     p->status = status;
     return EAD_OK;
+}
+
+// Units of up to 16 packed rows have a kernel of their own.  Where longer chunks are there as well, only up to 8:
+// a second group of 8 rows costs every unit, and the other kernel runs anyway.  `most`: packed rows of the largest unit.
+int few_rows_limit(int group, int64_t most)
+{
+    return group > kDecodeRows ? 0 : most <= 8 || (most > kDecodeRows && group <= 8) ? 8 : kDecodeRows;
 }
 
 // One warp per run of tokens and stretch of a token's values.
@@ -333,11 +340,9 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
     p.workspace = static_cast<uint8_t *>(workspace);
     p.status = status;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    // Units of up to 16 packed rows have a kernel of their own.  Where longer chunks are there as well, only up to 8:
-    // a second group of 8 rows costs every unit, and the other kernel runs anyway.
     const int64_t most = static_cast<int64_t>(p.batch.max_new) * p.group;
     p.tile_tokens = 128 / p.group;
-    p.few_rows = p.group > kDecodeRows ? 0 : most <= 8 || (most > kDecodeRows && p.group <= 8) ? 8 : kDecodeRows;
+    p.few_rows = few_rows_limit(p.group, most);
     if (most > 0x7fffffff) return EAD_EINVALID_ARG;
     const bool bf16 = cache->format == EAD_FMT_BF16, wide = p.cache.head_dim == 128;
     if (p.few_rows) {
@@ -349,6 +354,24 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
         rc = bf16 ? (wide ? launch_chunk<kFmtBf16, 128>(p, d->sms, s) : launch_chunk<kFmtBf16, 64>(p, d->sms, s))
                   : (wide ? launch_chunk<kFmtE4m3, 128>(p, d->sms, s) : launch_chunk<kFmtE4m3, 64>(p, d->sms, s));
     return rc;
+}
+
+extern "C" int ead_plan_chunk(int32_t n_new, int32_t kv_len, int32_t max_new, int32_t heads_per_kv, int32_t window, int32_t sinks,
+                              int64_t *out)
+{
+    if (!out || n_new < 0 || n_new > max_new || max_new > (1 << 30) || kv_len < 0 || kv_len > (1 << 30) || heads_per_kv < 1 ||
+        heads_per_kv > 128 || window < 0 || sinks < 0 || static_cast<int64_t>(max_new) * heads_per_kv > 0x7fffffff)
+        return EAD_EINVALID_ARG;
+    AttnParams p{};
+    p.group = heads_per_kv;
+    p.window = std::min(window, 1 << 30);
+    p.sinks = window ? sinks : 0;
+    p.tile_tokens = 128 / p.group;
+    p.few_rows = few_rows_limit(p.group, static_cast<int64_t>(max_new) * p.group);
+    const SeqInfo s{n_new, kv_len - n_new, kv_len, 0};
+    out[0] = chunk_blocks(p, s);
+    out[1] = chunk_cost(p, s, 0, 1);
+    return EAD_OK;
 }
 
 extern "C" int ead_add_rmsnorm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,

@@ -13,6 +13,7 @@ namespace ead {
 constexpr int kFmtBf16 = 0;
 constexpr int kFmtE4m3 = 1;
 constexpr int kFmtBlock = 32;
+constexpr int kMaxBatch = 4096;                    // sequences of a step
 constexpr uint32_t kStatusBadPage = 0x10u;
 
 struct KvCacheView {

@@ -160,3 +160,41 @@ def test_grid_and_rounding_agree_with_torch():
     amax = np.abs(x.reshape(64, -1, 32)).max(-1).astype(np.float64)
     assert ((amax <= 448 * 2.0 ** (s.astype(float) - 127)) | (s == 246)).all() and (amax > 448 * 2.0 ** (s.astype(float) - 128)).all()
     assert np.abs(values(c, s) - np.clip(x, -448 * 2.0 ** 119, 448 * 2.0 ** 119)).max() <= 2.0 ** -4 * np.abs(x).max()
+
+
+def _chunk_plan(n, kv, group, window=0, sinks=0):
+    """Units of two row tiles of whole tokens, each 12 + (2 | 1) per tile of 64 keys some query of it sees: tiles of the
+    sinks and of the window, none twice, at least one.  Vectorised over the units, in Python integers at the end."""
+    per = 128 // group
+    i0 = np.arange(0, n, 2 * per, dtype=np.int64)
+    tokens = np.minimum(2 * per, n - i0)
+    pa = kv - n + i0
+    hi = np.clip(pa + tokens, 0, kv)
+    lo = np.minimum(np.maximum(pa - window + 1, 0), hi) if window else np.zeros_like(hi)
+    first = lo // 64
+    sink_tiles = np.minimum(-(-np.minimum(sinks, lo) // 64), first)
+    tiles = np.maximum(1, sink_tiles - (-hi // 64) - first)
+    return len(i0), sum((12 + np.where(tokens > per, 2, 1) * tiles).tolist())
+
+
+@pytest.mark.parametrize("n,kv,group", [(525000, 525000, 128), (1050000, 1050000, 32), (2200000, 2200000, 8), (3100000, 3100000, 4),
+                                        (300000, 10300000, 8), (1500000, 1 << 30, 16), (1000000, 1 << 30, 128)])
+def test_chunk_costs_of_the_longest_prompts(E, n, kv, group):
+    """The work string of the chunk kernel passes 32 bits for prompts that the entry point takes."""
+    units, cost = _chunk_plan(n, kv, group)
+    assert cost > 2 ** 31
+    assert E.ead_plan_chunk(n, kv, heads_per_kv=group) == dict(units=units, cost=cost)
+
+
+@pytest.mark.parametrize("group", [1, 4, 5, 16, 71, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (100, 4), (1024, 65), (200, 300), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_chunk_costs_of_ordinary_chunks(E, group, window, sinks):
+    for n, kv in ((17, 17), (40, 900), (200, 150), (2041, 8000), (1, 5)):
+        want = _chunk_plan(n, kv, group, window, sinks if window else 0) if n * group > 16 else (0, 0)
+        assert E.ead_plan_chunk(n, kv, heads_per_kv=group, window=window, sinks=sinks) == dict(units=want[0], cost=want[1]), (n, kv)
+    assert E.ead_plan_chunk(2, 50, heads_per_kv=4, max_new=200)["units"] == 0 and E.ead_plan_chunk(3, 50, heads_per_kv=4, max_new=200)["units"] == 1
+    for bad in (dict(n_new=-1), dict(n_new=9, max_new=8), dict(kv_len=-1), dict(kv_len=(1 << 30) + 1), dict(heads_per_kv=0),
+                dict(heads_per_kv=129), dict(window=-1), dict(sinks=-1), dict(n_new=1 << 24, heads_per_kv=128)):
+        with pytest.raises(E.EadError) as err:
+            E.ead_plan_chunk(**{**dict(n_new=4, kv_len=50, heads_per_kv=4), **bad})
+        assert err.value.code == E.EAD_EINVALID_ARG
