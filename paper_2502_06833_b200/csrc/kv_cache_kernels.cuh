@@ -34,6 +34,9 @@ __device__ __forceinline__ uint4 load_once(const void *p)
     return v;
 }
 
+// First token of this warp's run.  (A thread's index in the grid passes 32 bits from 2^27 tokens on, a warp's does not.)
+__device__ __forceinline__ int first_token(int run) { return static_cast<int>(blockIdx.x * (kKvThreads / 32) + (threadIdx.x >> 5)) * run; }
+
 // Page and slot of token t0 + lane for the lanes below n (page -1: no valid place).
 template <bool WRITE>
 __device__ __forceinline__ void find_places(const KvMoveParams &p, int t0, int n, int lane, int *page, int *slot)
@@ -58,7 +61,7 @@ template <int FMT, int RUN>
 __global__ void __launch_bounds__(kKvThreads) ead_kv_write_kernel(KvMoveParams p)
 {
     const int lane = threadIdx.x & 31;
-    const int t0 = ((blockIdx.x * kKvThreads + threadIdx.x) >> 5) * RUN, n = min(RUN, p.batch.n_tokens - t0);
+    const int t0 = first_token(RUN), n = min(RUN, p.batch.n_tokens - t0);
     if (n <= 0) return;
     const KvCacheView &c = p.cache;
     const int per_half = c.heads * c.head_dim, off = blockIdx.y * kKvPass + lane * kKvLaneValues;
@@ -111,7 +114,7 @@ template <int FMT, int RUN>
 __global__ void __launch_bounds__(kKvThreads) ead_kv_read_kernel(KvMoveParams p)
 {
     const int lane = threadIdx.x & 31;
-    const int t0 = ((blockIdx.x * kKvThreads + threadIdx.x) >> 5) * RUN, n = min(RUN, p.batch.n_tokens - t0);
+    const int t0 = first_token(RUN), n = min(RUN, p.batch.n_tokens - t0);
     if (n <= 0) return;
     const KvCacheView &c = p.cache;
     const int per_half = c.heads * c.head_dim, off = blockIdx.y * kKvPass + lane * kKvLaneValues;

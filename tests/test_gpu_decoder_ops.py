@@ -378,6 +378,33 @@ def test_large_calls_move_what_small_ones_do(E, fmt):
         assert torch.equal(out[0], rows)
 
 
+def test_moves_of_more_than_2_27_tokens(E):
+    """The last tokens of a call that passes 2^32 threads are moved like the first ones.  All but the last three positions are
+    negative (they have no place), so the cache is small and only the rows are large."""
+    n, last = (1 << 27) + 3, 3
+    k, v = (torch.full((2, 1, 8, 64), 3.0, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    cache = E.ead_kv_cache(k, v)
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    lens, first = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (last, last - n))
+    batch = E.ead_kv_batch(table, starts, lens, n_tokens=n, max_new=n, max_len=16)
+    rows = torch.zeros(n, 1, 64, dtype=torch.bfloat16, device="cuda")
+    marks = torch.arange(1, 65, dtype=torch.bfloat16, device="cuda") * torch.tensor([1.0, 2.0, -1.0], device="cuda").bfloat16()[:, None]
+    rows[-last:, 0] = marks
+    st = _status()
+    E.ead_kv_write(cache, batch, rows, rows, status=st, stream=_stream())
+    assert st.item() == E.EAD_STATUS_BAD_PAGE                          # of the tokens without a place
+    for pool in (k, v):
+        assert torch.equal(pool[1, 0, :last], marks) and (pool[1, 0, last:] == 3.0).all() and (pool[0] == 3.0).all()
+    rows.fill_(9.0)
+    E.ead_kv_read(cache, batch, rows, rows, first=first, status=st, stream=_stream())
+    assert torch.equal(rows[-last:, 0], marks)
+    for at in range(0, n - last, 1 << 24):
+        assert not rows[at:min(at + (1 << 24), n - last)].any()
+    del rows
+    torch.cuda.empty_cache()
+
+
 def test_every_code_and_scale_reads_exactly(E):
     """All codes under every scale the library writes: bf16 holds each value exactly."""
     codes = torch.arange(256, dtype=torch.uint8)
