@@ -51,7 +51,7 @@ extern "C" {
 /* Bits of the device status word (ead_status). */
 #define EAD_STATUS_NONFINITE   0x1u /* some row saw a NaN / infinite logit (row gets H = NaN) */
 #define EAD_STATUS_WAIT_EXPIRED 0x2u /* a bounded wait inside a kernel ran out                 */
-#define EAD_STATUS_BAD_COUNT   0x4u /* internal row counts inconsistent                       */
+#define EAD_STATUS_BAD_COUNT   0x4u /* row counts inconsistent (internal ones, or a step's new_start) */
 #define EAD_STATUS_SHARD_MISMATCH 0x8u /* vocabulary shards disagree on the step or on a row's model */
 #define EAD_STATUS_BAD_PAGE    0x10u /* paged cache: page index out of range, or position not below max_len */
 
@@ -439,7 +439,9 @@ typedef struct ead_kv_batch {
  *                 (heads of a token are contiguous), so both may be slices of one projection
  *   status        dev uint32 or NULL; EAD_STATUS_BAD_PAGE is OR-ed in when a token has no valid
  *                 place (its page index is out of range, its position negative or not below
- *                 max_len); such a token is not written
+ *                 max_len), EAD_STATUS_BAD_COUNT when new_start contradicts n_tokens or max_new (a token
+ *                 at or behind new_start[B], or of a sequence that brings more than max_new or ends behind
+ *                 n_tokens); such a token is not written
  * Two tokens of a step must not share a slot.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT,
  * EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
  */
@@ -451,7 +453,7 @@ int ead_kv_write(const ead_kv_cache *cache, const ead_kv_batch *batch, const voi
  * sequence b (first NULL: 0), for i < n_b; batch->kv_len is not used and may be NULL.
  *   k_out, v_out  dev, bf16 [n_tokens, heads_kv, head_dim], out_stride elements between tokens
  *   first         dev int32 [B] or NULL
- * A token without a valid place reads as zeros and sets EAD_STATUS_BAD_PAGE in status.
+ * A token without a valid place reads as zeros and sets EAD_STATUS_BAD_PAGE or EAD_STATUS_BAD_COUNT as above.
  * Errors as ead_kv_write.
  */
 int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int32_t *first, void *k_out, void *v_out,

@@ -47,11 +47,13 @@ __device__ __forceinline__ void find_places(const KvMoveParams &p, int t0, int n
     *slot = 0;
     if (lane < n) {
         while (b + 1 < p.batch.B && __ldg(p.batch.new_start + b + 1) <= t) ++b;
-        const int pos = WRITE ? __ldg(p.batch.kv_len + b) - (__ldg(p.batch.new_start + b + 1) - t)
-                              : (p.first ? __ldg(p.first + b) : 0) + t - __ldg(p.batch.new_start + b);
-        *page = find_page(p.cache, p.batch, b, pos);
+        const int begin = __ldg(p.batch.new_start + b), end = __ldg(p.batch.new_start + b + 1);
+        const int pos = WRITE ? __ldg(p.batch.kv_len + b) - (end - t) : (p.first ? __ldg(p.first + b) : 0) + t - begin;
+        // a token of no sequence, or of one that contradicts the host's bounds, has no place whatever the page table says
+        const bool bad = begin < 0 || t < begin || t >= end || end > p.batch.n_tokens || end - begin > p.batch.max_new;
+        *page = bad ? -1 : find_page(p.cache, p.batch, b, pos);
         *slot = pos & (p.cache.page_size - 1);
-        if (*page < 0) flag_status(p.status, kStatusBadPage);
+        if (*page < 0) flag_status(p.status, bad ? kStatusBadCount : kStatusBadPage);
     }
     __syncwarp();
 }

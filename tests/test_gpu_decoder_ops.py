@@ -447,6 +447,80 @@ def test_tokens_without_a_place(E, fmt):
     assert zero == [True, True, True, True, False, False, True]
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("large", [False, True])
+@pytest.mark.parametrize("case", ["behind", "ahead", "many", "beyond"])
+def test_moves_with_counts_that_contradict_each_other(E, fmt, large, case):
+    """Tokens behind new_start[B] or before new_start[0], sequences of more than max_new tokens and ones that end behind
+    n_tokens: not written, read as zeros, reported, and the other sequences are served.  All of the page table is in range (a
+    captured step replays with old entries behind the contexts), so a token that got a place would be seen."""
+    heads, dim, page, n = (32, 128, 16, 2100) if large else (2, 64, 16, 12)    # large: more than 2^24 values
+    unit = 350 if large else 2
+    starts = dict(behind=[0, unit, 2 * unit, 4 * unit], ahead=[unit, 2 * unit, 3 * unit, 6 * unit],
+                  many=[0, unit, 5 * unit, 6 * unit], beyond=[0, unit, 3 * unit, 6 * unit + 1])[case]
+    served = dict(behind=[0, 1, 2], ahead=[0, 1, 2], many=[0, 2], beyond=[0, 1])[case]
+    max_new = 3 * unit + 1
+    per = -(-4 * unit // page) + 2
+    g = torch.Generator().manual_seed(6)
+    table = torch.randperm(3 * per + 4, generator=g)[:3 * per].int().view(3, per)
+    lens = torch.tensor([starts[i + 1] - starts[i] + 3 for i in range(3)], dtype=torch.int32)
+    shape = (3 * per + 4, heads, page, dim)
+    dtype = torch.bfloat16 if fmt == "bf16" else torch.uint8
+    k, v = (torch.full(shape, 3, dtype=dtype, device="cuda") for _ in "kv")
+    scales = [torch.full((*shape[:3], dim // 32), 120, dtype=torch.uint8, device="cuda") for _ in "kv"] if fmt == "e4m3" else []
+    cache = E.ead_kv_cache(k, v, *scales)
+    batch = E.ead_kv_batch(table.cuda(), torch.tensor(starts, dtype=torch.int32, device="cuda"), lens.cuda(), n_tokens=n, max_new=max_new,
+                           max_len=per * page)
+    rows = torch.ones(n, heads, dim, dtype=torch.bfloat16, device="cuda")
+    st = _status()
+    E.ead_kv_write(cache, batch, rows, rows, status=st, stream=_stream())
+    assert st.item() == E.EAD_STATUS_BAD_COUNT
+    want = torch.zeros(shape[0], page, dtype=torch.bool)
+    for b in served:
+        for p in range(3, int(lens[b])):
+            want[table[b, p // page], p % page] = True
+    for pool, old in ((k, 3), (v, 3), *((s, 120) for s in scales)):
+        changed = pool != old
+        assert torch.equal(changed.any(3).any(1).cpu(), want) and torch.equal(changed.all(3).all(1).cpu(), want)
+    out = torch.full((n, 2 * heads, dim), 9.0, dtype=torch.bfloat16, device="cuda")
+    st.zero_()
+    E.ead_kv_read(cache, batch, out[:, :heads], out[:, heads:], first=torch.full((3,), 3, dtype=torch.int32, device="cuda"), status=st,
+                  stream=_stream())
+    assert st.item() == E.EAD_STATUS_BAD_COUNT
+    ones = torch.zeros(n, dtype=torch.bool)
+    for b in served:
+        ones[starts[b]:starts[b + 1]] = True
+    assert torch.equal((out == 1).flatten(1).all(1).cpu(), ones) and torch.equal((out == 0).flatten(1).all(1).cpu(), ~ones)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new,group", [([1, 2, 1], 4), ([40, 70, 30], 4), ([1, 70, 30], 4), ([3, 5, 4], 20)])
+def test_attention_reports_counts_that_contradict_each_other(E, workspace, fmt, new, group):
+    """Few-rows kernel, chunk kernel and both: sequences of more than max_new tokens or that end behind n_tokens are reported and
+    their rows not written; rows behind new_start[B] are not written; the other sequences are as before."""
+    ctx = Context(new, [150, 260, 90], 2, 64, 16, fmt, seed=17)
+    q = _q(ctx, group)
+    good = _attend(E, ctx, q, workspace, 0.1)
+    want = attention(ctx, q, 0.1, 0, 0)
+    _check(good, want)
+    untouched = lambda x, r: bool((x[0][r] == -7.0).all() and (x[1][r] == -7.0).all())          # noqa: E731
+    served = lambda x, *rows: [_check((x[0][r], x[1][r], 0), [w[r] for w in want]) for r in rows if len(x[0][r])]   # noqa: E731
+    a, b, n = int(ctx.new_start[1]), int(ctx.new_start[2]), int(ctx.new_start[3])
+    got = _attend(E, ctx, q, workspace, 0.1, max_new=new[1] - 1) if new[1] * 3 > n + 2 else None
+    if got:
+        assert got[2] == E.EAD_STATUS_BAD_COUNT and untouched(got, slice(a, b))
+        served(got, slice(0, a), slice(b, n))
+    got = _attend(E, ctx, q[:n - 1], workspace, 0.1, n_tokens=n - 1)
+    assert got[2] == E.EAD_STATUS_BAD_COUNT and untouched(got, slice(b, n - 1))
+    served(got, slice(0, b))
+    wide = torch.cat([q, q[:1].expand(5, -1, -1)])
+    got = _attend(E, ctx, wide, workspace, 0.1, n_tokens=n + 5, max_new=max(new) + 5)
+    assert got[2] == 0 and untouched(got, slice(n, n + 5))
+    served(got, slice(0, n))
+    again = _attend(E, ctx, q, workspace, 0.1)
+    assert again[2] == 0 and torch.equal(again[0], good[0]) and torch.equal(again[1], good[1])
+
+
 @pytest.mark.parametrize("H", [8, 40, 64, 1536, 4096, 5120, 8200, 16384])
 @pytest.mark.parametrize("rows,pad,with_residual", [(1, 0, True), (7, 8, True), (300, 0, False)])
 def test_norm_bf16(E, H, rows, pad, with_residual):
