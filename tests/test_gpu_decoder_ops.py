@@ -169,6 +169,39 @@ def test_attention_long_context_split_over_many_blocks(E, workspace, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new,length,heads,group,dim,page,window,sinks", [
+    ([1], [30011], 1, 4, 128, 32, 0, 0), ([1], [20011], 1, 8, 64, 16, 0, 0), ([3], [20011], 1, 4, 128, 64, 0, 0),
+    ([100], [9000], 1, 4, 128, 32, 0, 0), ([20], [9003], 2, 4, 64, 16, 0, 0), ([150, 1], [6000, 9000], 1, 5, 128, 16, 0, 0),
+    ([1, 70], [12000, 9000], 1, 4, 128, 16, 5000, 300), ([40], [5000], 1, 20, 64, 128, 0, 0)])
+def test_every_value_tile_counts_once(E, workspace, fmt, new, length, heads, group, dim, page, window, sinks):
+    """Work split over many blocks: keys 16 i .. 16 i + 15 have value 1 in dimension i % head_dim and 0 elsewhere, and logits are
+    nearly flat, so a run of 16 values that is lost or counted twice moves its dimension by far more than the tolerance.
+    That it does is checked on the 64-bit result."""
+    def fill(name, b, x):
+        if name == "v":
+            x = torch.zeros_like(x)
+            key = torch.arange(len(x))
+            x[key, :, key // 16 % dim] = 1.0
+        return x
+    ctx = Context(new, length, heads, dim, page, fmt, seed=18, fill=fill)
+    q = _q(ctx, group, size=0.3)
+    scale = dim ** -0.5
+    want = attention(ctx, q, scale, window, sinks)
+    t = 0
+    for b, (m, l) in enumerate(zip(new, length)):
+        pos = l - 1                                            # the sequence's last query, all of whose heads are looked at
+        seen = torch.arange(l)
+        seen = (seen > pos - window) | (seen < sinks) if window else seen <= pos
+        for hq in range(heads * group):
+            z = scale * (ctx.host["k"][b][:, hq // group] @ q[t + m - 1, hq].double())
+            w = torch.softmax(torch.where(seen, z, torch.full((), -np.inf, dtype=torch.float64)), 0)[:l // 16 * 16].view(-1, 16)
+            whole = seen[:l // 16 * 16].view(-1, 16).all(1)
+            assert (w.sum(1) > 2 * want[2][t + m - 1, hq][torch.arange(l // 16) % dim])[whole].all()
+        t += m
+    _check(_attend(E, ctx, q, workspace, scale, window, sinks), want)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("size,trend", [(8.0, 0.0), (3.0, 1.0), (3.0, -1.0), (60.0, 0.0)])
 @pytest.mark.parametrize("new", [1, 140])
 def test_attention_wide_logits(E, workspace, fmt, size, trend, new):
@@ -568,6 +601,39 @@ def test_norm_e4m3(E, H, rows, pad):
     step = np.repeat(2.0 ** (got_by.astype(float) - 127), 32, -1)
     # nearest code: half a step of 2^-3 relative (2^-4), or of the subnormal spacing 2^-9 of the scale
     assert (np.abs(got - y) <= np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * step) * (1 + 2.0 ** -12)).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H,rows", [(64, 30011), (1536, 8111), (4096, 1793), (5120, 2501), (8224, 1903), (16384, 1207)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_norm_of_more_rows_than_blocks(E, fmt, H, rows, in_place):
+    """Blocks that walk over several rows, the last turn with some of them: every row against the 64-bit result; in place means
+    the residual's own buffer for the sum and, for bf16, the input's own for the output."""
+    g = torch.Generator(device="cuda").manual_seed(H)
+    x, r = ((torch.randn(rows, H, generator=g, device="cuda") * torch.exp(torch.randn(rows, 1, generator=g, device="cuda"))).bfloat16()
+            for _ in range(2))
+    w = (1 + 0.3 * torch.randn(H, generator=g, device="cuda")).bfloat16()
+    dx, dr = x.clone(), r.clone()
+    res = dr if in_place else torch.empty_like(dr)
+    if fmt == "bf16":
+        out, scale = dx if in_place else torch.empty_like(dx), None
+    else:
+        out, scale = (torch.empty(rows, n, dtype=torch.uint8, device="cuda") for n in (H, H // 32))
+    E.ead_add_rmsnorm(dx, w, out, residual=dr, residual_out=res, out_scale=scale, eps=1e-5, stream=_stream())
+    for at in range(0, rows, 1024):
+        rows_ = slice(at, at + 1024)
+        s = x[rows_].double() + r[rows_].double()
+        y = s / torch.sqrt(s.square().mean(-1, keepdim=True) + 1e-5) * w.double()
+        assert torch.equal(res[rows_], s.float().bfloat16())
+        if fmt == "bf16":                          # tolerance as for few rows above
+            assert ((out[rows_].double() - y).abs() <= (2.0 ** -8 + 2.0 ** -16) * y.abs() + 1e-30).all()
+        else:                                      # the smallest power that holds the block, give or take 32-bit rounding; then the nearest code
+            power = torch.exp2(scale[rows_].double() - 127)[..., None]
+            amax = y.abs().view(len(y), -1, 32).amax(-1, keepdim=True)
+            assert (amax <= 448 * power * (1 + 2.0 ** -16)).all() and (amax > 224 * power * (1 - 2.0 ** -16)).all()
+            got = (out[rows_].view(torch.float8_e4m3fn).double().view(len(y), -1, 32) * power).view_as(y)
+            step = power.expand(-1, -1, 32).reshape(y.shape)
+            assert ((got - y).abs() <= torch.maximum(2.0 ** -4 * y.abs(), 2.0 ** -10 * step) * (1 + 2.0 ** -12)).all()
 
 
 def test_norm_of_zeros_and_non_finite_rows(E):
