@@ -484,7 +484,8 @@ int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int3
  *   status     dev uint32 or NULL.  EAD_STATUS_BAD_PAGE: a page index was out of range (its
  *              tokens count as zeros) or a context is longer than max_len (the rest is not
  *              seen); EAD_STATUS_BAD_COUNT: new_start contradicts max_new or n_tokens (the rows
- *              of such a sequence are not written); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out
+ *              of such a sequence are not written); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out (the
+ *              outputs are not valid, and the workspace has to be zero-filled again)
  * The result does not depend on the order in which blocks run: partial results are joined in a
  * fixed order.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
  */
@@ -492,6 +493,12 @@ int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int3
 int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *batch, const void *q, int64_t q_stride,
                      int32_t heads_q, float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride,
                      float *lse, void *workspace, uint32_t *status, int32_t device, void *stream);
+
+/*
+ * DIAGNOSTIC.  The limit of the bounded waits in ead_kv_attention's kernels, in nanoseconds, for calls of this process from now
+ * on; negative: the default (2 s).  With a limit that is too short waits run out in sound calls: for tests of what then happens.
+ */
+int ead_kv_wait_limit(int32_t ns);
 
 /*
  * DIAGNOSTIC.  How ead_kv_attention weighs one sequence for one cache head when it deals a call's chunks out to the SMs (the

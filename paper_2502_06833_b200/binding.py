@@ -41,7 +41,7 @@ SYMBOLS = ["ead_create", "ead_step", "ead_run", "ead_run_host", "ead_run_timed",
            "ead_plan_split", "ead_plan_units", "ead_usage", "ead_parameter_ratio", "ead_set_done", "ead_get_done",
            "ead_shard_range", "ead_shard_partials", "ead_shard_gate", "ead_shard_connect",
            "ead_shard_exchange_bytes", "ead_kv_write", "ead_kv_read", "ead_kv_attention", "ead_add_rmsnorm",
-           "ead_plan_chunk"]
+           "ead_plan_chunk", "ead_kv_wait_limit"]
 
 
 class EadConfig(C.Structure):
@@ -145,6 +145,8 @@ def lib() -> C.CDLL:
         L.ead_kv_read.argtypes = [vp, vp, vp, vp, vp, i64, vp, i32, vp]
         L.ead_kv_attention.restype = C.c_int
         L.ead_kv_attention.argtypes = [vp, vp, vp, i64, i32, C.c_float, i32, i32, vp, i64, vp, vp, vp, i32, vp]
+        L.ead_kv_wait_limit.restype = C.c_int
+        L.ead_kv_wait_limit.argtypes = [i32]
         L.ead_plan_chunk.restype = C.c_int
         L.ead_plan_chunk.argtypes = [i32] * 6 + [C.POINTER(C.c_int64)]
         L.ead_add_rmsnorm.restype = C.c_int
@@ -453,6 +455,11 @@ def ead_kv_attention(cache: EadKvCache, batch: EadKvBatch, q, out, *, scale, wor
                                 stream)
     if rc:
         _check(rc, "ead_kv_attention")
+
+
+def ead_kv_wait_limit(ns: int) -> None:
+    """Limit of the attention kernels' bounded waits; negative: the default."""
+    _check(lib().ead_kv_wait_limit(ns), "ead_kv_wait_limit")
 
 
 def ead_plan_chunk(n_new, kv_len, *, heads_per_kv, max_new=None, window=0, sinks=0) -> dict:

@@ -52,7 +52,7 @@ struct ChunkLayout {
     static constexpr int kRawScale = FMT == kFmtE4m3 ? kChunkKeys * (D / kFmtBlock) : 0;
     static constexpr int kRaw = 3;                                       // stages of codes
     static constexpr int kRawBytes = kRaw * (kRawTile + kRawScale);
-    static constexpr int kBars = 2 * kStages + 2 * kRaw + 18;
+    static constexpr int kBars = 2 * kStages + 2 * kRaw + 20;
     static constexpr int kSmem = 1024 + 2 * kQTile + kStages * kTileBytes + kRawBytes + 8 * kBars;
     static constexpr int kWarps = FMT == kFmtBf16 ? 12 : 16, kThreads = 32 * kWarps;
     // registers per thread: two softmax warpgroups, MMA and loads, converters; together at most what the block is launched with
@@ -278,6 +278,14 @@ __device__ __forceinline__ void store_32(uint8_t *dst, const uint32_t (&v)[8], b
 }
 __device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+// The same, and whether `ok` held for all of the barrier's threads.
+__device__ __forceinline__ bool named_all(int id, int threads, bool ok)
+{
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"(id), "r"(threads), "r"(static_cast<uint32_t>(ok)) : "memory");
+    return all != 0;
+}
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
@@ -293,7 +301,8 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     __shared__ ChunkUnit s_unit[2];
     __shared__ float s_stat[2][128];               // maxima and sums of a one-tile unit's second accumulator
     __shared__ int64_t s_before;
-    __shared__ uint32_t s_tmem;
+    __shared__ uint32_t s_tmem, s_gave_up;
+    __shared__ int s_units, s_tiles;               // units whose query rows, tiles that have been asked for (written when a role stops)
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - raw);
     const uint32_t q_smem = base, ring = base + 2 * L::kQTile, rawk = ring + S * L::kTileBytes;
@@ -302,7 +311,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     const uint32_t bar_full = bars, bar_empty = bars + 8 * S, bar_raw_full = bar_empty + 8 * S, bar_raw_empty = bar_raw_full + 8 * L::kRaw;
     // scores and probabilities: one barrier per row tile (16 bytes apart) and buffer
     const uint32_t bar_s = bar_raw_empty + 8 * L::kRaw, bar_p = bar_s + 32, bar_o = bar_p + 32, bar_v = bar_o + 16, bar_q_full = bar_v + 16, bar_q_empty = bar_q_full + 8;
-    const uint32_t bar_u_full = bar_q_empty + 8, bar_u_empty = bar_u_full + 16;
+    const uint32_t bar_u_full = bar_q_empty + 8, bar_u_empty = bar_u_full + 16, bar_last = bar_u_empty + 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvCacheView &c = p.cache;
 
@@ -331,7 +340,9 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_u_full + 8 * i, 1);
             mbar_init(bar_u_empty + 8 * i, kChunkWarps - 1);
+            mbar_init(bar_last + 8 * i, 1);
         }
+        s_gave_up = 0;
         mbar_init(bar_q_full, 1);
         mbar_init(bar_q_empty, 2);
         fence_mbar_init();
@@ -425,13 +436,14 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     fence_async_shared();
     __syncthreads();                               // s_cost is done with; its place takes query rows now, by TMA
 
-    bool expired = false;
     // Every role takes the units one by one: waits for the description, works, releases it (one arrival per warp).
-    auto unit_wait = [&](int n) -> const ChunkUnit & {
-        wait_phase(bar_u_full + 8 * (n & 1), (n >> 1) & 1, p.status, &expired);
-        __syncwarp();
-        return s_unit[n & 1];
-    };
+    // When a wait runs out, a warp that loads stops at its next wait that does, every other role walks through the unit
+    // whose description it holds and stops (the softmax warps, which meet at barriers, all at the same one): nobody
+    // reads a description that is not there.  What is under way then comes in before the block ends.  (A look at the block's
+    // `gave_up` before every tile's load would end the loads sooner; it made the hand-over step 2 to 5 % slower.)
+    auto wait = [&](uint32_t bar, uint32_t parity) { return wait_phase(bar, parity, p, &s_gave_up); };
+    auto warp_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+    auto unit_wait = [&](int n) { return warp_wait(bar_u_full + 8 * (n & 1), (n >> 1) & 1); };
     auto unit_done = [&](int n) {
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_u_empty + 8 * (n & 1));
@@ -442,12 +454,12 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kIssueRegs));
         if (warp == kChunkUnitWarp) {
             // ============================================================ units
-            for (int n = 0;; ++n) {
+            int n = 0;
+            for (;; ++n) {
                 int ta, tb;
                 chunk_stretch(cur, g0, g1, &ta, &tb);
                 const int64_t at = cur.tiles_at(), end = at + static_cast<int64_t>(cur.cost) * cur.r.tiles;
-                wait_phase(bar_u_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, p.status, &expired);
-                __syncwarp();
+                if (!warp_wait(bar_u_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1)) break;
                 if (lane == 0) {
                     ChunkUnit &u = s_unit[n & 1];
                     u.b = cur.b; u.h = cur.h; u.token0 = cur.s.token0;
@@ -465,8 +477,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     mbar_arrive(bar_u_full + 8 * (n & 1));
                 }
                 // its query rows, when the unit before has done with theirs (rows of tokens behind the unit's come along)
-                wait_phase(bar_q_empty, (n & 1) ^ 1, p.status, &expired);
-                __syncwarp();
+                if (!warp_wait(bar_q_empty, (n & 1) ^ 1)) break;
                 if (lane == 0) {
                     const uint32_t box = p.tile_tokens * p.group * 128;
                     mbar_arrive_expect_tx(bar_q_full, cur.cost * L::kHalves * box);
@@ -476,15 +487,21 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                                     cur.s.token0 + cur.i0 + tile * p.tile_tokens, bar_q_full);
                     }
                 }
-                if (end + kChunkUnitCost >= g1) break;
+                if (end + kChunkUnitCost >= g1) {
+                    ++n;
+                    break;
+                }
                 chunk_next(p, &cur);
             }
+            if (lane == 0) s_units = n;
         } else if (warp == kChunkLoadWarp) {
             // ============================================================ key and value tiles
             const int boxes = kChunkKeys >> box_shift, box_keys = 1 << box_shift;     // at most 8
-            int t = 0;                             // tiles so far
-            for (int n = 0;; ++n) {
-                const ChunkUnit &u = unit_wait(n);
+            int x = 0;                             // tiles asked for
+            bool go = true;
+            for (int n = 0; go; ++n) {
+                if (!unit_wait(n)) break;
+                const ChunkUnit &u = s_unit[n & 1];
                 const int ta = u.ta, nt = u.nt, last = u.last, b = u.b, h = u.h;
                 KeyRange r;
                 r.lo = u.lo; r.hi = u.hi; r.sink_tiles = u.sink_tiles; r.first_tile = u.first_tile; r.tiles = 0;
@@ -496,7 +513,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     return any ? max(__ldg(p.batch.page_table + static_cast<int64_t>(b) * p.batch.table_stride + (at >> c.page_shift)), -1) : -2;
                 };
                 int entry = look_up(ta);
-                for (int k = ta; k < ta + nt; ++k, ++t) {
+                for (int k = ta; go && k < ta + nt; ++k) {
                     const int slot = (r.base(k, kChunkShift) + lane * box_keys) & (c.page_size - 1);
                     const int next = k + 1 < ta + nt ? look_up(k + 1) : -2;       // its latency runs under this tile's waits
                     int page = entry;
@@ -509,12 +526,12 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     const int good = __popc(__ballot_sync(0xffffffffu, page >= 0 && page < c.n_pages));
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
-                        const int x = 2 * t + kv;
+                        if (!go) break;
                         const CUtensorMap *tm = kv ? &tmV : &tmK;
                         if (FMT == kFmtBf16) {
                             const int st = x % S;
                             const uint32_t bar = bar_full + 8 * st, dst = ring + st * L::kTileBytes + lane * box_keys * 128;
-                            wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
+                            if (!(go = warp_wait(bar_empty + 8 * st, ((x / S) & 1) ^ 1))) break;
                             if (lane == 0) mbar_arrive_expect_tx(bar, live * box_keys * D * 2);
                             __syncwarp();
                             if (page >= 0) {
@@ -531,7 +548,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                             const uint32_t bar = bar_raw_full + 8 * st;
                             const uint32_t sc = raw_scale + st * L::kRawScale + lane * box_keys * (D / kFmtBlock);
                             const uint32_t sc_bytes = box_keys * (D / kFmtBlock);
-                            wait_phase(bar_raw_empty + 8 * st, ((x / L::kRaw) & 1) ^ 1, p.status, &expired);
+                            if (!(go = warp_wait(bar_raw_empty + 8 * st, ((x / L::kRaw) & 1) ^ 1))) break;
                             if (page == c.n_pages)
                                 for (uint32_t y = 0; y < sc_bytes; y += 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc + y), "r"(0) : "memory");
                             __syncwarp();
@@ -543,10 +560,12 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                                     bulk_load(sc, (kv ? c.v_scale : c.k_scale) + scale_offset(c, page, h, slot), sc_bytes, bar);
                             }
                         }
+                        ++x;
                     }
                 }
                 if (last) break;
             }
+            if (lane == 0) s_tiles = x;
         } else {
             // ============================================================ MMAs
             // The whole warp walks through the loop, one lane issues.  It is chosen by elect.sync, not by its number: only then
@@ -561,16 +580,17 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             int t = 0;
             int ns = 0, np = 0;                    // scores issued and probabilities taken so far
             for (int n = 0;; ++n) {
-                const ChunkUnit &u = unit_wait(n);
+                if (!unit_wait(n)) break;
+                const ChunkUnit &u = s_unit[n & 1];
                 const bool dual = __shfl_sync(0xffffffffu, u.dual, 0) != 0;
                 const int nt = __shfl_sync(0xffffffffu, u.nt, 0), last = __shfl_sync(0xffffffffu, u.last, 0);
                 unit_done(n);
                 const int rounds = dual ? nt : (nt + 1 - w) >> 1;
-                wait_phase(bar_q_full, n & 1, p.status, &expired);
+                wait(bar_q_full, n & 1);
                 const uint32_t a = q_lo + (dual ? w * (L::kQTile >> 4) : 0);
                 auto scores = [&](int i) {         // S = Q K^T of the i-th tile
                     const int x = 2 * (t + (dual ? i : 2 * i + w)), st = x % S;
-                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                    wait(bar_full + 8 * st, (x / S) & 1);
                     __syncwarp();
                     tc_fence_after_sync();
                     const uint32_t d = t_s + (ns & 1) * 64, b = k_lo + st * (L::kTileBytes >> 4);
@@ -595,8 +615,8 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                 for (int i = 0; i < rounds; ++i) {
                     const int x = 2 * (t + (dual ? i : 2 * i + w)) + 1, st = x % S;
                     const uint32_t pr = t_s + (np & 1) * 64, b = v_lo + st * (L::kTileBytes >> 4);
-                    wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
-                    wait_phase(bar_p + 16 * w + 8 * (np & 1), (np >> 1) & 1, p.status, &expired);
+                    wait(bar_full + 8 * st, (x / S) & 1);
+                    wait(bar_p + 16 * w + 8 * (np & 1), (np >> 1) & 1);
                     __syncwarp();
                     tc_fence_after_sync();
                     if (elect_one()) {
@@ -622,14 +642,15 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
         const int ft = tid - kChunkFeedWarp * 32;  // 0 .. 127
         int t = 0;
         for (int n = 0;; ++n) {
-            const ChunkUnit &un = unit_wait(n);
+            if (!unit_wait(n)) break;
+            const ChunkUnit &un = s_unit[n & 1];
             const int last = un.last;
             {
                 for (int k = un.ta, end = un.ta + un.nt; k < end; ++k, ++t)
                     for (int kv = 0; kv < 2; ++kv) {
                         // half a key per thread: threads 0-63 the first half of the dimensions, 64-127 the second
                         const int x = 2 * t + kv, st = x % S, rs = x % L::kRaw, key = ft & 63, part = ft >> 6;
-                        wait_phase(bar_raw_full + 8 * rs, (x / L::kRaw) & 1, p.status, &expired);
+                        wait(bar_raw_full + 8 * rs, (x / L::kRaw) & 1);
                         uint32_t w[D / 8], sc;
                         const uint32_t src = rawk + rs * L::kRawTile + key * D;
 #pragma unroll
@@ -646,7 +667,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                             asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(sa) : "memory");
                         // a key no query of the unit sees was perhaps not even loaded: zeros
                         const bool keep = un.seen(p.sinks, un.base(k) + key);
-                        wait_phase(bar_empty + 8 * st, ((x / S) & 1) ^ 1, p.status, &expired);
+                        wait(bar_empty + 8 * st, ((x / S) & 1) ^ 1);
                         const uint32_t dst = ring + st * L::kTileBytes + key * 128;
 #pragma unroll
                         for (int g = 0; g < D / 64; ++g) {
@@ -693,7 +714,8 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
         // a thread writes a row: 32 bytes at a time, a whole sector each, if every row begins at one
         const bool whole_sectors = ((reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(2 * p.out_stride)) & 31) == 0;
         for (int n = 0;; ++n) {
-            const ChunkUnit &u = unit_wait(n);
+            if (!named_all(1, 256, unit_wait(n))) break;
+            const ChunkUnit &u = s_unit[n & 1];
             const bool dual = u.dual != 0;
             const int ta = u.ta, nt = u.nt, rounds = dual ? nt : (nt + 1 - w) >> 1;
             const int my_row = dual ? w * 128 + row : row;                       // row within the unit
@@ -719,7 +741,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     const bool clean = key0 + kChunkKeys <= u.hi && (key0 >= u.lo || key0 + kChunkKeys <= p.sinks);
                     if (!clean) {
                         const int x = 2 * (t + k) + 1, st = x % S;
-                        wait_phase(bar_full + 8 * st, (x / S) & 1, p.status, &expired);
+                        wait(bar_full + 8 * st, (x / S) & 1);
                         if (row < kChunkKeys * L::kHalves && !u.seen(p.sinks, key0 + (row & 63))) {
                             const ValueTile<D> vt(box_shift);
                             const uint32_t dst = ring + st * L::kTileBytes + (row >> 6) * vt.line + vt.at(row & 63);
@@ -731,7 +753,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     }
                 }
                 const uint32_t t_s = tmem + lanes + w * 128 + (ns & 1) * 64, done = bar_p + 16 * w + 8 * (ns & 1);
-                wait_phase(bar_s + 16 * w + 8 * (ns & 1), (ns >> 1) & 1, p.status, &expired);
+                wait(bar_s + 16 * w + 8 * (ns & 1), (ns >> 1) & 1);
                 ++ns;
                 __syncwarp();
                 tc_fence_after_sync();
@@ -759,7 +781,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     l *= f;
                     if (i > 0) {
                         // the product of the tile before may still be running (the one before that is not: S came behind it)
-                        wait_phase(bar_v + 8 * w, (ns - 2) & 1, p.status, &expired);
+                        wait(bar_v + 8 * w, (ns - 2) & 1);
                         __syncwarp();
                         tc_fence_after_sync();
 #pragma unroll
@@ -804,7 +826,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             // ---- output: this thread's row
             const bool alone = u.part < 0;
             if (rounds > 0) {
-                wait_phase(bar_o + 8 * w, outputs[w] & 1, p.status, &expired);
+                wait(bar_o + 8 * w, outputs[w] & 1);
                 __syncwarp();
                 tc_fence_after_sync();
             }
@@ -826,7 +848,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     l = l * f0 + l1 * f1;
                     m = M;
                     if (nt > 1) {                  // the second accumulator's products are complete, too
-                        wait_phase(bar_o + 8, outputs[1] & 1, p.status, &expired);
+                        wait(bar_o + 8, outputs[1] & 1);
                         __syncwarp();
                         tc_fence_after_sync();
                     }
@@ -949,6 +971,19 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     }
     tc_fence_before_sync();
     __syncthreads();
+    if (s_gave_up) {                               // nobody sets it any more
+        constexpr int R = FMT == kFmtBf16 ? S : L::kRaw;
+        if (warp == kChunkUnitWarp && s_units) wait_own(bar_q_full, (s_units - 1) & 1);
+        if (warp == kChunkLoadWarp)
+            for (int x = max(0, s_tiles - R); x < s_tiles; ++x) wait_own((FMT == kFmtBf16 ? bar_full : bar_raw_full) + 8 * (x % R), (x / R) & 1);
+        if (warp == kChunkMmaWarp || warp == kChunkMmaWarp + 2) {
+            const uint32_t bar = bar_last + 4 * (warp - kChunkMmaWarp);
+            if (elect_one()) umma_commit(bar);
+            __syncwarp();
+            wait_own(bar, 0);
+        }
+        __syncthreads();
+    }
     if (warp == kChunkMmaWarp) tmem_dealloc(tmem, 512);
     griddep_wait();                                // started alongside the few-rows kernel: it ends before this one does
 }

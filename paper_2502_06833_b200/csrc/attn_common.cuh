@@ -25,6 +25,7 @@ struct AttnParams {
     float scale_log2;                             // scale * log2(e): logits are kept in units of log 2
     uint32_t *status;
     uint8_t *workspace;
+    uint32_t wait_ns, wait_hint;                  // when a wait has run out, and how long one look at a barrier may last
 };
 
 constexpr float kLn2 = 0.6931471805599453f;
@@ -113,18 +114,27 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
-// Waits for a phase of an mbarrier; gives up after kWaitLimitNs and from then on does not wait again.
-__device__ __forceinline__ void wait_phase(uint32_t bar, uint32_t parity, uint32_t *status, bool *expired)
+// Waits for a phase of an mbarrier.  False if the wait has run out (recorded in the status) or another one of the block has
+// (recorded in `gave_up`, shared memory, for warps that wait for one another; NULL for one that waits for its own loads alone).
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, const AttnParams &p, uint32_t *gave_up)
 {
-    if (*expired || mbar_try_wait(bar, parity)) return;
+    if (mbar_try_wait(bar, parity)) return true;
     const uint64_t t0 = globaltimer_ns();
-    while (!mbar_try_wait_hint(bar, parity, 20000)) {
-        if (globaltimer_ns() - t0 > kWaitLimitNs) {
-            *expired = true;
-            flag_status(status, kStatusWaitExpired);
-            return;
+    while (!mbar_try_wait_hint(bar, parity, p.wait_hint)) {
+        if (gave_up && *reinterpret_cast<volatile uint32_t *>(gave_up)) return false;
+        if (globaltimer_ns() - t0 >= p.wait_ns) {
+            if (gave_up) *reinterpret_cast<volatile uint32_t *>(gave_up) = 1u;
+            flag_status(p.status, kStatusWaitExpired);
+            return false;
         }
     }
+    return true;
+}
+// After that: waits for a copy or product of one's own that is under way, so that none outlives the block.
+__device__ __forceinline__ void wait_own(uint32_t bar, uint32_t parity)
+{
+    const uint64_t t0 = globaltimer_ns();
+    while (!mbar_try_wait_hint(bar, parity, 20000u) && globaltimer_ns() - t0 < kWaitLimitNs) { }
 }
 
 // Orders the block's partial results in the workspace before an arrival, and the other blocks' before a read.

@@ -399,7 +399,6 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     int stage = 0;
     uint32_t phase = 0;
     int g = warp, unit_lo = 0;
-    bool expired = false;
     while (unit_lo < n_tiles) {
         const int unit_end = cur.begin + cur.r.tiles, unit_hi = min(unit_end, n_tiles);
         const int rows = cur.s.n * p.group;
@@ -465,7 +464,12 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             const bool whole = base + TT - 1 <= cur.s.p0 && base + TT <= cur.s.len &&
                                (p.window == 0 || base > pb - p.window || base + TT <= p.sinks);
             uint32_t kb = my_ring + stage * 2 * kFewHalf, vb = kb + kFewHalf;
-            wait_phase(my_bars + 8 * stage, phase, p.status, &expired);
+            if (!wait_phase(my_bars + 8 * stage, phase, p, nullptr)) {
+                // the status says that the result is not valid; this warp's loads come in, then it leaves (barriers do not wait for it)
+                for (int x = (g - warp) / kFewWarps, end = min(x + S, (n_tiles - warp + kFewWarps - 1) / kFewWarps); x < end; ++x)
+                    wait_own(my_bars + 8 * (x % S), (x / S) & 1);
+                return;
+            }
             __syncwarp();
             // Steps of 16 keys, NS of them side by side: the fragment loads for the keys, all score products, the loads
             // for the values (their latency runs under the softmax), then the products with them.

@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <mutex>
 
@@ -47,6 +48,8 @@ struct DeviceInfo {
 };
 
 std::mutex g_mu;
+std::atomic<uint32_t> g_wait_ns{static_cast<uint32_t>(kWaitLimitNs)};   // of the attention kernels' bounded waits
+static_assert(kWaitLimitNs <= 0x7fffffffu, "held in 32 bits");
 DeviceInfo g_dev[kMaxDevices];
 
 int launched() { return cudaGetLastError() == cudaSuccess ? EAD_OK : EAD_ECUDA; }
@@ -339,6 +342,8 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
     p.scale_log2 = scale * kLog2e;
     p.workspace = static_cast<uint8_t *>(workspace);
     p.status = status;
+    p.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+    p.wait_hint = std::min(p.wait_ns, 20000u);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int64_t most = static_cast<int64_t>(p.batch.max_new) * p.group;
     p.tile_tokens = 128 / p.group;
@@ -354,6 +359,12 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
         rc = bf16 ? (wide ? launch_chunk<kFmtBf16, 128>(p, d->sms, s) : launch_chunk<kFmtBf16, 64>(p, d->sms, s))
                   : (wide ? launch_chunk<kFmtE4m3, 128>(p, d->sms, s) : launch_chunk<kFmtE4m3, 64>(p, d->sms, s));
     return rc;
+}
+
+extern "C" int ead_kv_wait_limit(int32_t ns)
+{
+    g_wait_ns.store(ns < 0 ? static_cast<uint32_t>(kWaitLimitNs) : static_cast<uint32_t>(ns), std::memory_order_relaxed);
+    return EAD_OK;
 }
 
 extern "C" int ead_plan_chunk(int32_t n_new, int32_t kv_len, int32_t max_new, int32_t heads_per_kv, int32_t window, int32_t sinks,

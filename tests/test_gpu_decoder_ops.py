@@ -305,6 +305,63 @@ def test_attention_on_another_stream_and_in_a_graph(E, workspace):
     _check((out.cpu(), lse.cpu(), st.item()), want)
 
 
+@pytest.mark.parametrize("fmt,new,length,heads,dim,runs_out", [
+    ("bf16", [1] * 64, [1024 + 113 * b for b in range(64)], 8, 128, False), ("e4m3", [1] * 64, [1024 + 113 * b for b in range(64)], 8, 128, False),
+    ("bf16", [300], [30000], 8, 128, True), ("e4m3", [300], [30000], 8, 128, True), ("bf16", [300, 1], [30000, 9000], 8, 64, True),
+    ("e4m3", [1, 40, 300, 17], [20000, 5000, 30000, 17], 4, 64, True)])
+def test_attention_waits_that_run_out(E, fmt, new, length, heads, dim, runs_out):
+    """With limits far below what loads under full load and whole units take, waits run out in the middle of everything: the call
+    ends, says so and writes nowhere but into its rows, and with a cleared workspace the next call is sound.  (A single
+    look at a barrier lasts several microseconds, about what a copy takes under full load: the few-rows kernel's waits, all of
+    them for copies, may or may not run out.)"""
+    g = torch.Generator(device="cuda").manual_seed(20)
+    page, group = 16, 4
+    pages = [-(-n // page) for n in length]
+    table = torch.zeros(len(new), max(pages), dtype=torch.int32)
+    order, at = torch.randperm(sum(pages), generator=torch.Generator().manual_seed(20)).int(), 0
+    for b, n in enumerate(pages):
+        table[b, :n] = order[at:at + n]
+        at += n
+    shape = (sum(pages), heads, page, dim)
+    if fmt == "bf16":
+        pools = [torch.randn(shape, generator=g, device="cuda").bfloat16() for _ in "kv"]
+    else:
+        pools = [torch.randint(0, 0x7F, shape, generator=g, device="cuda", dtype=torch.uint8) for _ in "kv"]
+        pools += [torch.randint(112, 119, (*shape[:3], dim // 32), generator=g, device="cuda", dtype=torch.uint8) for _ in "kv"]
+    before = [x.clone() for x in pools]
+    n = sum(new)
+    starts = torch.tensor([0] + new).cumsum(0).int().cuda()
+    batch = E.ead_kv_batch(table.cuda(), starts, torch.tensor(length, dtype=torch.int32, device="cuda"), n_tokens=n, max_new=max(new),
+                           max_len=max(length))
+    cache = E.ead_kv_cache(*pools)
+    q = torch.randn(n, heads * group, dim, generator=g, device="cuda").bfloat16()
+    ws = torch.zeros(E.EAD_KV_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+
+    def call(limit):
+        out = torch.full((n, heads * group + 1, dim), -7.0, dtype=torch.bfloat16, device="cuda")
+        lse, st = torch.full((n, heads * group), -7.0, device="cuda"), _status()
+        E.ead_kv_wait_limit(limit)
+        try:
+            E.ead_kv_attention(cache, batch, q, out[:, :-1], scale=0.1, lse=lse, workspace=ws, status=st, stream=_stream())
+        finally:
+            E.ead_kv_wait_limit(-1)
+        assert (out[:, -1] == -7.0).all()
+        if st.item():
+            assert st.item() == E.EAD_STATUS_WAIT_EXPIRED
+            ws.zero_()
+        return out, lse, st.item()
+    sound = call(-1)
+    assert sound[2] == 0
+    seen = set()
+    for limit in (20000, 8000, 4000, 2000, 1000, 500, 100, 0, 0, 0, -1):
+        got = call(limit)
+        seen.add(got[2])
+        if got[2] == 0:
+            assert torch.equal(got[0], sound[0]) and torch.equal(got[1], sound[1])
+    assert got[2] == 0 and (len(seen) == 2 or not runs_out)
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(pools, before))
+
+
 def test_attention_many_sequences(E, workspace):
     rng = np.random.default_rng(12)
     for B, hi in ((700, 40), (4096, 9)):
