@@ -487,7 +487,8 @@ int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int3
  *              of such a sequence are not written); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out (the
  *              outputs are not valid, and the workspace has to be zero-filled again)
  * The result does not depend on the order in which blocks run: partial results are joined in a
- * fixed order.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ * fixed order.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (B * heads_kv * max_len above 2^34 per SM), EAD_EUNSUPPORTED_ARCH,
+ * EAD_ECUDA.
  */
 #define EAD_KV_WORKSPACE_BYTES (64u << 20)
 int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *batch, const void *q, int64_t q_stride,

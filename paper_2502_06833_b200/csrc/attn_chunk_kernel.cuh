@@ -128,6 +128,11 @@ __device__ __forceinline__ void chunk_stretch(const ChunkCursor &c, int64_t g0, 
     *tb = b < c.r.tiles ? static_cast<int>(b) : c.r.tiles;
 }
 
+// Tiles so far only matter modulo the rings: a count that has grown past two periods goes on from the one before, so that it
+// stays within 32 bits however long a block works.
+constexpr int kChunkRingPeriod = 240;
+__device__ __forceinline__ int ring_count(int tiles) { return tiles < 2 * kChunkRingPeriod ? tiles : kChunkRingPeriod + tiles % kChunkRingPeriod; }
+
 // A block's part of a unit, as warp 11 describes it to the others.
 struct ChunkUnit {
     int b, h, token0;                             // sequence, cache head, first row of the sequence in the step
@@ -295,6 +300,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
 {
     using L = ChunkLayout<FMT, D>;
     constexpr int S = L::kStages, kChunkWarps = L::kWarps, kChunkThreads = L::kThreads;
+    static_assert(kChunkRingPeriod % S == 0 && kChunkRingPeriod % L::kRaw == 0, "a period brings stages and phases back");
     extern __shared__ uint8_t smem_raw[];
     __shared__ int64_t s_scan[kChunkWarps];
     __shared__ int s_b, s_last;
@@ -499,7 +505,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             const int boxes = kChunkKeys >> box_shift, box_keys = 1 << box_shift;     // at most 8
             int x = 0;                             // tiles asked for
             bool go = true;
-            for (int n = 0; go; ++n) {
+            for (int n = 0;; ++n) {
                 if (!unit_wait(n)) break;
                 const ChunkUnit &u = s_unit[n & 1];
                 const int ta = u.ta, nt = u.nt, last = u.last, b = u.b, h = u.h;
@@ -563,7 +569,8 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                         ++x;
                     }
                 }
-                if (last) break;
+                if (last || !go) break;
+                x = 2 * ring_count(x / 2);
             }
             if (lane == 0) s_tiles = x;
         } else {
@@ -578,7 +585,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             const uint32_t v_lo = (ring >> 4) | (vt.line << (16 - 4)), v_hi = umma_desc_hi(vt.next8);
             const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
             int t = 0;
-            int ns = 0, np = 0;                    // scores issued and probabilities taken so far
+            uint32_t ns = 0, np = 0;               // scores issued and probabilities taken so far
             for (int n = 0;; ++n) {
                 if (!unit_wait(n)) break;
                 const ChunkUnit &u = s_unit[n & 1];
@@ -632,7 +639,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                     ++np;
                     if (i + 2 < rounds) scores(i + 2);
                 }
-                t += nt;
+                t = ring_count(t + nt);
                 if (last) break;
             }
         }
@@ -702,6 +709,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
             }
             unit_done(n);
             if (last) break;
+            t = ring_count(t);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kSoftmaxRegs));
@@ -709,8 +717,9 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
         const int w = warp >> 2, row = tid & 127;
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;            // this warp's 32 lanes of tensor memory
         const uint32_t t_o = tmem + lanes + 256 + w * 128;
-        int t = 0, ns = 0;
-        int outputs[2] = {0, 0};                   // finished outputs per accumulator
+        int t = 0;
+        uint32_t ns = 0;
+        uint32_t outputs[2] = {0, 0};                  // finished outputs per accumulator
         // a thread writes a row: 32 bytes at a time, a whole sector each, if every row begins at one
         const bool whole_sectors = ((reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(2 * p.out_stride)) & 31) == 0;
         for (int n = 0;; ++n) {
@@ -961,7 +970,7 @@ __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
                 }
                 named_sync(1, 256);                // s_last may be written again
             }
-            t += nt;
+            t = ring_count(t + nt);
             outputs[0] += 1;                       // the first accumulator has a tile in every unit
             outputs[1] += dual || nt > 1;
             const int last = u.last;

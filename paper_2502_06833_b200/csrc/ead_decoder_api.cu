@@ -349,6 +349,9 @@ extern "C" int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *b
     p.tile_tokens = 128 / p.group;
     p.few_rows = few_rows_limit(p.group, most);
     if (most > 0x7fffffff) return EAD_EINVALID_ARG;
+    // the few-rows kernel counts a block's tiles, of at least 16 keys, in 32 bits (a block takes minutes for so many)
+    if (p.few_rows && static_cast<int64_t>(p.batch.B) * p.cache.heads * (p.batch.max_len / 16 + 2) / std::min(d->sms, kAttnMaxCtas) > (1 << 30))
+        return EAD_ELIMIT;
     const bool bf16 = cache->format == EAD_FMT_BF16, wide = p.cache.head_dim == 128;
     if (p.few_rows) {
         rc = bf16 ? (wide ? launch_few_rows<kFmtBf16, 128>(p, d->sms, s) : launch_few_rows<kFmtBf16, 64>(p, d->sms, s))

@@ -362,6 +362,20 @@ def test_attention_waits_that_run_out(E, fmt, new, length, heads, dim, runs_out)
     assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(pools, before))
 
 
+def test_attention_of_more_tiles_than_a_block_counts_is_refused(E, workspace):
+    """4096 sequences of up to 2^30 keys with 128 cache heads; nothing is launched, so nothing of it exists."""
+    import ctypes as C
+    k = torch.zeros(1, 128, 256, 64, dtype=torch.bfloat16, device="cuda")
+    cache = E.ead_kv_cache(k, k)
+    table = torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = torch.zeros(1, 128, 64, dtype=torch.bfloat16, device="cuda")
+    call = lambda B, max_len: E.lib().ead_kv_attention(                                              # noqa: E731
+        C.byref(cache), C.byref(E.EadKvBatch(B, 1, 1, max_len, table.data_ptr(), table.data_ptr(), table.data_ptr(), 1 << 22, 0)), q.data_ptr(),
+        128 * 64, 128, 0.1, 0, 0, q.data_ptr(), 128 * 64, None, workspace.data_ptr(), None, 0, _stream())
+    assert call(4096, 1 << 30) == E.EAD_ELIMIT
+    assert call(4096, 1 << 24) == E.EAD_ELIMIT
+
+
 def test_attention_many_sequences(E, workspace):
     rng = np.random.default_rng(12)
     for B, hi in ((700, 40), (4096, 9)):
