@@ -375,10 +375,11 @@ def ead_kv_cache(k, v, k_scale=None, v_scale=None) -> EadKvCache:
     ``transpose(1, 2)`` of its tensor), the same for both."""
     T = _t()
     e4m3 = k_scale is not None
+    strides = lambda t: [s if n > 1 else t.shape[3] for s, n in zip(t.stride()[:3], t.shape)]   # noqa: E731  (of one element: any)
     for t, name in ((k, "k"), (v, "v")):
         if t.dtype not in ((T.float8_e4m3fn, T.uint8) if e4m3 else (T.bfloat16,)):
             raise ValueError(f"{name}: {t.dtype} does not fit a cache {'with' if e4m3 else 'without'} scales")
-        if t.dim() != 4 or t.stride(3) != 1 or t.shape != k.shape or t.stride() != k.stride():
+        if t.dim() != 4 or t.stride(3) != 1 or t.shape != k.shape or strides(t) != strides(k):
             raise ValueError(f"{name}: want [n_pages, heads_kv, page_size, head_dim], contiguous in the last "
                              "dimension, k and v alike")
     for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
@@ -387,7 +388,7 @@ def ead_kv_cache(k, v, k_scale=None, v_scale=None) -> EadKvCache:
         if e4m3:
             _dense(t, (*k.shape[:3], k.shape[3] // EAD_FMT_BLOCK), T.uint8, name)
     c = EadKvCache(EAD_FMT_E4M3 if e4m3 else EAD_FMT_BF16, k.shape[1], k.shape[3], k.shape[2], k.shape[0], 0,
-                   *k.stride()[:3], _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+                   *strides(k), _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
     c.held = (k, v, k_scale, v_scale)
     c.ref = C.byref(c)
     return c
@@ -399,13 +400,13 @@ def ead_kv_batch(page_table, new_start, kv_len=None, *, n_tokens, max_new, max_l
     of them.  ``kv_len`` may be omitted for reading."""
     i32 = _t().int32
     B = page_table.shape[0]
-    if page_table.dtype is not i32 or page_table.dim() != 2 or page_table.stride(1) != 1:
+    if page_table.dtype is not i32 or page_table.dim() != 2 or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
         raise ValueError("page_table: want int32 [B, entries] with contiguous rows")
     _dense(new_start, (B + 1,), i32, "new_start")
     if kv_len is not None:
         _dense(kv_len, (B,), i32, "kv_len")
     c = EadKvBatch(B, int(n_tokens), int(max_new), int(max_len), _ptr(new_start), _ptr(kv_len), _ptr(page_table),
-                   page_table.stride(0) if B > 1 else page_table.shape[1], 0)
+                   max(page_table.stride(0) if B > 1 else page_table.shape[1], 1), 0)
     c.held = (page_table, new_start, kv_len)
     c.ref = C.byref(c)
     return c

@@ -146,6 +146,25 @@ def test_binding_refuses_wrong_types_and_shapes(E):
             bad()
 
 
+def test_strides_of_dimensions_of_one_element_do_not_matter(E):
+    """torch gives a dimension of one element any stride; it addresses nothing."""
+    pools = torch.zeros(4, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 16, 64, dtype=torch.bfloat16)
+    odd = [x.as_strided((4, 1, 16, 64), (1024, s, 64, 1)) for x, s in zip(pools, (3, 1024))]
+    cache = E.ead_kv_cache(*odd)
+    assert (cache.page_stride, cache.slot_stride) == (1024, 64) and cache.head_stride % 8 == 0 and cache.heads_kv == 1
+    one = torch.zeros(2, 16, 64, dtype=torch.bfloat16)
+    odd = [one.as_strided((1, 2, 16, 64), (s, 1024, 64, 1)) for s in (5, 2048)]
+    cache = E.ead_kv_cache(*odd)
+    assert cache.page_stride % 8 == 0 and (cache.head_stride, cache.n_pages) == (1024, 1)
+    with pytest.raises(ValueError):                # others do matter
+        E.ead_kv_cache(torch.zeros(4, 2, 16, 64).bfloat16(), torch.zeros(4, 16, 2, 64).bfloat16().transpose(1, 2))
+    starts, lens = torch.tensor([0, 1, 2], dtype=torch.int32), torch.tensor([9, 9], dtype=torch.int32)
+    batch = E.ead_kv_batch(torch.zeros(1, 2, dtype=torch.int32).t(), starts, lens, n_tokens=2, max_new=1, max_len=16)
+    assert batch.table_stride == 1
+    batch = E.ead_kv_batch(torch.zeros(1, 0, dtype=torch.int32), starts[:2], lens[:1], n_tokens=1, max_new=1, max_len=0)
+    assert batch.table_stride == 1                 # contexts that have no page yet
+
+
 def test_grid_and_rounding_agree_with_torch():
     g = e4m3_grid()
     assert len(g) == 127 and g[-1] == 448 and (np.diff(g) > 0).all()

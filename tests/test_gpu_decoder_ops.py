@@ -149,6 +149,22 @@ def test_attention_strides(E, workspace, fmt, layout, dim):
     _check(_attend(E, ctx, q, workspace, 0.1, pad=3), attention(ctx, q, 0.1, 0, 0))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new", [1, 60])
+def test_attention_with_meaningless_strides(E, workspace, dim, new):
+    """One cache head, one page: the strides of those dimensions may be anything."""
+    ctx = Context([new], [200], 1, dim, 256, seed=21)
+    q = _q(ctx, 4)
+    want = attention(ctx, q, 0.1, 0, 0)
+    page = int(ctx.table[0, 0])
+    for name in "kv":
+        ctx.dev[name] = ctx.dev[name][page:page + 1].as_strided((1, 1, 256, dim), (7 if name == "k" else 8, 3, dim, 1),
+                                                                ctx.dev[name][page].storage_offset())
+    ctx.table[:] = 0
+    ctx.d_table = torch.zeros(1, 1, dtype=torch.int32, device="cuda").as_strided((1, 1), (1, 5))
+    _check(_attend(E, ctx, q, workspace, 0.1), want)
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 def test_attention_long_context_split_over_many_blocks(E, workspace, fmt):
     """One sequence over all the GPU's blocks; repeated calls agree bit for bit and reuse the workspace."""
