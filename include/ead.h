@@ -145,7 +145,8 @@ int ead_run_host(ead_ctx *ctx, int32_t T, const void *h_small_seq, const void *h
 
 /*
  * DIAGNOSTIC (measurement aid, not part of the gate step's interface; so are
- * ead_kernel_launches, ead_launch_info, ead_plan_split and ead_plan_units below).
+ * ead_kernel_launches, ead_launch_info, ead_plan_split, ead_plan_units, ead_plan_chunk and
+ * ead_kv_wait_limit below).
  * The same T steps as ead_run, launched kernel by kernel (no graph replay) with
  * CUDA events around every kernel on cfg.stream, to attribute device time.
  *   kernel_ms  host, float [3]: summed device time in milliseconds of the
@@ -465,7 +466,11 @@ int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int3
  * at position p sees key j iff j <= p and (window == 0 or j > p - window or j < sinks):
  *   z_j = scale * q . k_j,  out = sum_j exp(z_j) v_j / sum_j exp(z_j),  lse = ln sum_j exp(z_j)
  * with sums and maxima in 32 bits; probabilities are rounded to bf16 (the type of the values
- * they weight) before the product with v.  A query that sees nothing (its position is negative)
+ * they weight) before the product with v.  That product is divided by the sum at the end, and probabilities relative
+ * to the running maximum reach 2^8: values above 2^120 / (number of keys seen) can overflow on the way.  Sequences
+ * of at most 16 rows (new tokens x query heads per cache head) over an 8-bit cache take q as f16 after a power of two
+ * has brought the row's largest element to 1 .. 2: elements below 2^-17 of it are rounded to multiples of
+ * 2^-24.  A query that sees nothing (its position is negative)
  * gets zeros and lse = -infinity.  Keys that no query of a sequence sees are not
  * read, nor are the page table entries of pages that hold only such keys.  A key that is not finite
  * touches only the queries that see it; a VALUE that is not finite and is seen by one query can also
@@ -521,7 +526,7 @@ int ead_plan_chunk(int32_t n_new, int32_t kv_len, int32_t max_new, int32_t heads
  * ead_step takes as h_small / h_large.
  *   x             dev, bf16 rows, x_stride elements apart
  *   residual      dev, bf16 rows, residual_stride apart, or NULL (s = x)
- *   residual_out  dev, bf16 rows, residual_out_stride apart, or NULL; may be residual itself
+ *   residual_out  dev, bf16 rows, residual_out_stride apart, or NULL; may be residual or x itself
  *   weight        dev, bf16 [H]
  *   out           dev, bf16 or e4m3 rows, out_stride apart; may be x itself for EAD_FMT_BF16
  *   out_scale     dev, uint8 [n_rows, H / 32], EAD_FMT_E4M3 only, else NULL

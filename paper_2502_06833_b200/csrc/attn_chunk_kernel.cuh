@@ -20,8 +20,9 @@
 // What bounds it: at size the tensor core, whose operand reads take 2836 cycles per 256 rows x 128 keys (measured with the
 // MMAs alone), and the exponentials, 2048 cycles of the special function units; together 3560.  Both row tiles'
 // exponentials at once stall each other and then leave the units idle, so the two softmax warpgroups take turns at them
-// (4054 cycles without).  Two chunks of 2041-2048 tokens over 6007-8192 keys, 8 cache heads of 4: 375 us,
-// 1150 TFLOP/s (435 us at the clock the power limit leaves in a long loop).  Short chunks are
+// (4054 cycles without).  Two chunks of 2041-2048 tokens over 6007-8192 keys, 8 cache heads of 4: 420-440 us,
+// 980-1030 TFLOP/s, at the clock the power limit leaves in a long loop; 371-375 us, 1160 TFLOP/s, at full clock.  The same over an
+// 8-bit cache: 475 us at full clock.  Short chunks are
 // bound by the units' beginnings and ends (query rows in, output or part out: about 8 500 cycles each).
 #pragma once
 #include "attn_common.cuh"

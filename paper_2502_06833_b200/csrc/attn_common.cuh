@@ -30,9 +30,11 @@ struct AttnParams {
 
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Workspace: arrival counters of both kernels (zero between calls), then the partial results.
-constexpr size_t kAttnCounterBytes = 4096;        // 256 counters of 32 bits per kernel, 4 kernels at most
+// Workspace: arrival counters, one of 32 bits per block (zero between calls), of the few-rows kernel, then of the chunk kernel,
+// then the partial results of each.
+constexpr size_t kAttnCounterBytes = 4096;        // per kernel
 constexpr int kAttnMaxCtas = 160;
+static_assert(kAttnMaxCtas * sizeof(uint32_t) <= kAttnCounterBytes, "a counter per block");
 constexpr int kDecodeRows = 16;                   // most packed rows of a unit of the few-rows kernel
 constexpr size_t kDecodePartFloats = kDecodeRows * (128 + 2);
 constexpr size_t kDecodePartOffset = 2 * kAttnCounterBytes;

@@ -2,10 +2,10 @@
 // decoding and very short chunks.
 //
 // Every key and value is read from HBM once and used for 8 or 16 rows only, so HBM bounds it; the
-// kernel is built to keep many bytes in flight and little else.  Eight warps per SM work independently:
-// each has its own ring of 8 KiB stages (4 KiB of keys, 4 KiB of values) filled by TMA boxes of
-// one page each and takes every eighth tile of the block's stretch, so no barrier stands between the loads of
-// consecutive tiles or units.  Products are mma.sync with the keys (values) as the 16-row
+// kernel is built to keep many bytes in flight and little else.  The block's kWarps warps (8; 12 for an 8-bit cache
+// and at most 8 rows) work independently: each has its own ring of 8 KiB stages (4 KiB of keys, 4 KiB of values) filled by
+// TMA boxes of one page each and takes every kWarps-th tile of the block's stretch, so no barrier stands between the loads
+// of consecutive tiles or units.  Products are mma.sync with the keys (values) as the 16-row
 // operand and the packed query rows as the 8-column operand: a tensor-memory accumulator has 128 rows, of which
 // 8 would carry anything.  S^T = K Q^T has the layout that, transposed 8 x 8, is the second
 // operand of O^T = V^T P^T.
@@ -14,13 +14,15 @@
 // bytes, are what an 8-bit cache is short of, so the scales are applied where there is least to apply them to.
 // Keys: codes are exact in f16; the products of one scale block are summed apart and the four sums of a key are
 // scaled in 32 bits.  The query rows are f16 then, too: each row is first divided by a power of two that
-// brings its largest element to 1..2, so what an element loses is below 2^-25 of that.
+// brings its largest element to 1..2.  Elements down to 2^-17 of that are exact, smaller ones lose at most 2^-25 (the
+// chunk kernel takes them as the bf16 they are).
 // Values: an e4m3 byte placed 4 bits down in a bf16 is 2^-120 of its value, subnormals included; the factor 2^(120 + k)
 // goes to the probabilities (an exact change of exponent), once per key and scale block instead of once per value.
 //
-// Measured (head_dim 128, 8 cache heads): bf16, 64 contexts of 1024-8192, 4 query heads each: 195 us, 6.14 TB/s, 0.95 of the
-// device's copy rate.  e4m3, 24 contexts of 4001-32001, 5 query heads each: 190 us, 4.95 TB/s, 0.77; scales applied to every value
-// instead took 234 us with 8 warps, and 12 warps instead of 8 are worth 15 %.
+// Measured (head_dim 128, 8 cache heads), in graph replay: bf16, 64 contexts of 1024-8192, 4 query heads each: 191-197 us, 6.2 TB/s,
+// 0.95 of the device's copy rate.  e4m3, 24 contexts of 4001-32001, 5 query heads each: 188-190 us, 5.0 TB/s, 0.77; scales applied to
+// every value instead took 234 us with 8 warps, and 12 warps instead of 8 are worth 15 %.  As calls: 198 and 199 us.  With 3-4 new
+// tokens per sequence (two groups of 8 rows), 32 contexts of 1000-8000, 4 query heads each: bf16 114-116 us, e4m3 117-119.
 #pragma once
 #include <type_traits>
 
@@ -150,7 +152,10 @@ __device__ __forceinline__ void few_seek(const AttnParams &p, int shift, int g, 
     }
 }
 
-// Units of at most so many tiles are not divided among blocks (joining parts costs more than the imbalance).
+// Units of at most so many tiles are not divided among blocks: joining parts costs more than the imbalance where contexts are
+// short.  Measured, 48 against 0 (always divided), us: 4 contexts of 300 keys, 2 heads of 128, bf16 8.2 / 12.8; 64 of 300, 8 heads
+// of 128, bf16 20.9 / 25.2, e4m3 23.9 / 30.0; 16 of 1500, 8 heads of 64, e4m3 14.0 / 19.5; one of 777, 8 heads of 64, bf16 9.9 / 13.9;
+// one of 1500, 2 heads of 128, bf16 16.7 / 15.6 (the largest loss).  Longer units, divided either way, differ by up to 6 %.
 constexpr int kFewWholeTiles = 48;
 
 // NB: packed rows in groups of 8 (1 or 2).
@@ -282,7 +287,7 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
     const int n_tiles = static_cast<int>(g1 - g0);  // from here on tiles are counted from g0
     if (next_unit) few_seek(p, L::kShift, 0, &cur);
 
-    // ---- loads: this warp's tiles are warp, warp + 8, ...
+    // ---- loads: this warp's tiles are warp, warp + kFewWarps, ...
     const uint32_t my_ring = ring0 + warp * S * 2 * kFewHalf;
     const uint32_t my_scales = smem_u32(scales_ptr) + warp * S * kFewScaleBytes;
     const uint32_t my_bars = bars + warp * S * 8;
@@ -679,7 +684,8 @@ __global__ void __launch_bounds__(FewLayout<FMT, D, NB>::kThreads, 1)
             few_seek(p, L::kShift, unit_hi, &after);
             if (NB == 1) query_rows(after);
         }
-        // ---- the warps' parts of the unit come together: warps 4-7 hand theirs to 0-3 lane by lane, those lay them out by rows
+        // ---- the warps' parts of the unit come together: the upper half of the warps hand theirs to the lower half lane by lane,
+        // those lay them out by rows
         constexpr int kHalf = kFewWarps / 2;
         if (warp >= kHalf) {
             float *mw = merge + (warp - kHalf) * L::kMergeWarp + lane;

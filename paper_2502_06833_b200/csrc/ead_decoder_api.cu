@@ -36,10 +36,14 @@ constexpr int kNormThreadsPerSm = 2048;   // what an SM holds; further rows are 
 // never gains (2^24 values 12.5 against 13.7, 2^26 47.6 against 48.6): twice the stores keep the memory busy by themselves.
 constexpr int kKvRun = 4;
 constexpr int64_t kKvLongRunValues = 1 << 24;
-constexpr int kChunkMinCost = 24;         // cost per block (a tile of 128 rows x 64 keys: 1), likewise
+// Least work per block of the chunk kernel (a tile of 128 rows x 64 keys: 1), so that a short call does not cut every unit into
+// parts.  16, 24 and 48 did not differ beyond noise.
+constexpr int kChunkMinCost = 24;
 static_assert(kChunkMinCost >= kChunkUnitCost + 2, "every block's stretch has to hold the beginning of a tile");
-// Tiles of 8 KiB per block before another block is worth its part in the join: one context of 777 keys takes 9.9 us with 16,
-// 9.8 with 8, 15.3 with 32; large calls have more tiles per SM than that anyway.
+// Tiles of 8 KiB per block before another block is worth its part in the join; it decides calls with less than that per SM.
+// Measured, 8 / 16 / 32 tiles, us: one context of 777 keys, 8 heads of 64, bf16 9.7 / 9.9 / 15.2; 4 of 777, 2 heads of 128, bf16
+// 16.0 / 13.2 / 14.4; 4 of 300, 8 heads of 64, bf16 7.6 / 10.5 / 17.3, e4m3 13.4 / 23.0 / 37.1; 16 of 777, 8 heads of 128, e4m3
+// 14.1 / 14.2 / 23.6.
 constexpr int kFewMinTiles = 16;
 
 struct DeviceInfo {

@@ -4,8 +4,9 @@
 // store of codes, half a scale block), for a run of consecutive tokens: its lanes look up the places of all of
 // them at once, so the chain new_start -> kv_len -> page table -> data costs its latency once per run.
 //
-// Measured, 8-bit cache, 8 heads of 128: write of 24 k tokens 30-31 us, 5 TB/s, 0.78 of the device's copy rate; read of
-// 107 k tokens 114 us, 5.72 TB/s, 0.89; one step of 64 tokens (bf16) 2.9 us.  The write's bound at size is the chain of
+// Measured, 8-bit cache, 8 heads of 128: write of 24 k tokens 31 us from a cold cache, 4.9 TB/s, 0.76 of the device's copy rate; read
+// of 107 k tokens 115 us, 5.7 TB/s, 0.88; one step of 64 tokens (bf16) 2.9 us.  bf16, 8 heads of 128: write of 23 k tokens 33 us
+// with the rows in L2, read of 55 k 78 us, 5.8 TB/s.  The write's bound at size is the chain of
 // look-ups and loads before the first store: with half the instructions for the largest magnitude it took as long.
 #pragma once
 #include "kv_format.cuh"

@@ -723,6 +723,20 @@ def test_norm_of_more_rows_than_blocks(E, fmt, H, rows, in_place):
             assert ((got - y).abs() <= torch.maximum(2.0 ** -4 * y.abs(), 2.0 ** -10 * step) * (1 + 2.0 ** -12)).all()
 
 
+@pytest.mark.parametrize("H,rows", [(64, 20000), (5120, 1500)])
+def test_norm_writes_the_sum_over_its_input(E, H, rows):
+    """residual_out may be x: without a residual that is a copy onto itself, with one the stream's new value."""
+    g = torch.Generator(device="cuda").manual_seed(22)
+    x, r = (torch.randn(rows, H, generator=g, device="cuda").bfloat16() for _ in range(2))
+    w = torch.ones(H, dtype=torch.bfloat16, device="cuda")
+    for residual in (None, r):
+        dx, ref, out, res = x.clone(), torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+        E.ead_add_rmsnorm(x, w, ref, residual=residual, residual_out=res, stream=_stream())
+        E.ead_add_rmsnorm(dx, w, out, residual=residual, residual_out=dx, stream=_stream())
+        assert torch.equal(out, ref) and torch.equal(dx, res)
+        assert torch.equal(res, x if residual is None else (x.float() + r.float()).bfloat16())
+
+
 def test_norm_of_zeros_and_non_finite_rows(E):
     x = torch.zeros(3, 64, dtype=torch.bfloat16)
     x[1, 5], x[2, 7] = float("inf"), float("nan")
