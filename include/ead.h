@@ -489,7 +489,8 @@ int ead_kv_read(const ead_kv_cache *cache, const ead_kv_batch *batch, const int3
  *   status     dev uint32 or NULL.  EAD_STATUS_BAD_PAGE: a page index was out of range (its
  *              tokens count as zeros) or a context is longer than max_len (the rest is not
  *              seen); EAD_STATUS_BAD_COUNT: new_start contradicts max_new or n_tokens (the rows
- *              of such a sequence are not written); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out (the
+ *              of such a sequence are not written; rows of no sequence, behind new_start[B], are not written
+ *              either and not reported); EAD_STATUS_WAIT_EXPIRED: a bounded wait in a kernel ran out (the
  *              outputs are not valid, and the workspace has to be zero-filled again)
  * The result does not depend on the order in which blocks run: partial results are joined in a
  * fixed order.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (B * heads_kv * max_len above 2^34 per SM), EAD_EUNSUPPORTED_ARCH,
