@@ -54,6 +54,7 @@ extern "C" {
 #define EAD_STATUS_BAD_COUNT   0x4u /* row counts inconsistent (internal ones, or a step's new_start) */
 #define EAD_STATUS_SHARD_MISMATCH 0x8u /* vocabulary shards disagree on the step or on a row's model */
 #define EAD_STATUS_BAD_PAGE    0x10u /* paged cache: page index out of range, or position not below max_len */
+#define EAD_STATUS_BAD_TOKEN   0x20u /* ead_token_logprobs: a given token is not below the vocabulary size */
 
 typedef struct ead_ctx ead_ctx; /* opaque */
 
@@ -393,6 +394,8 @@ int ead_head_entropy_static(const void *W, const void *h, int32_t B, int32_t V, 
  */
 #define EAD_FMT_BF16 0
 #define EAD_FMT_E4M3 1
+#define EAD_FMT_F32 2                  /* outputs of ead_linear, logits of ead_token_logprobs    */
+#define EAD_FMT_F16 3                  /* logits of ead_token_logprobs                           */
 #define EAD_FMT_BLOCK 32               /* values per scale byte */
 
 /*
@@ -502,7 +505,7 @@ int ead_kv_attention(const ead_kv_cache *cache, const ead_kv_batch *batch, const
                      float *lse, void *workspace, uint32_t *status, int32_t device, void *stream);
 
 /*
- * DIAGNOSTIC.  The limit of the bounded waits in ead_kv_attention's kernels, in nanoseconds, for calls of this process from now
+ * DIAGNOSTIC.  The limit of the bounded waits in the kernels of ead_kv_attention and ead_linear, in nanoseconds, for calls of this process from now
  * on; negative: the default (2 s).  With a limit that is too short waits run out in sound calls: for tests of what then happens.
  */
 int ead_kv_wait_limit(int32_t ns);
@@ -539,6 +542,121 @@ int ead_add_rmsnorm(const void *x, int64_t x_stride, const void *residual, int64
                     void *residual_out, int64_t residual_out_stride, const void *weight, float eps, int32_t n_rows,
                     int32_t H, int32_t format, void *out, int64_t out_stride, uint8_t *out_scale, int32_t device,
                     void *stream);
+
+/*
+ * The 8-bit pass of a decoder: products of 8-bit activations with 8-bit weights, the quantisation around them, the norm and rotation
+ * of query and key heads between the projection and the cache, and, behind the head, what logits say of given tokens.  (The
+ * paper defines none of them.)  The conventions of the decoder-side operators above hold: work is only enqueued on
+ * `stream` of `device`, nothing is allocated, every buffer is the caller's.
+ *
+ * A matrix of e4m3 codes [rows, cols] with one scale byte (as above) per block of block_rows x block_cols; blocks at the
+ * end of a row or column may be cut short.  1 x 32 is what ead_add_rmsnorm writes; 1 x 128 suits activations, 128 x 128 weights.
+ */
+typedef struct ead_e4m3_matrix {
+    int32_t rows;            /* 0 .. 2^30                                                        */
+    int32_t cols;            /* multiple of 32, at most 2^30                                     */
+    int32_t block_rows;      /* 1 or 128                                                         */
+    int32_t block_cols;      /* 32 (with block_rows = 1) or 128                                  */
+    int64_t row_stride;      /* bytes between rows, a multiple of 16                             */
+    void *codes;             /* dev, 16-byte aligned                                             */
+    uint8_t *scale;          /* dev [ceil(rows / block_rows), ceil(cols / block_cols)], contiguous;
+                                4-byte aligned for blocks of 32                                  */
+    int32_t reserved;        /* 0                                                                */
+} ead_e4m3_matrix;
+
+/*
+ * y = x, or y = x * gate / (1 + e^-gate) with a gate (the activations of a gated MLP), into 8-bit blocks: scales and codes as
+ * defined above, for blocks of any of the three shapes.  A block with an x or gate that is not finite reads as NaNs.
+ *   x, gate   dev, bf16 [rows, cols], x_stride and gate_stride elements apart; gate NULL: none (and none with 128 x 128 blocks)
+ *   out       what is written; its codes' rows are block_cols wide stretches of y
+ * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (more than 2^31 - 1 blocks of threads: rows x cols above 2^42 or so),
+ * EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ */
+int ead_quantise(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, const ead_e4m3_matrix *out, int32_t device,
+                 void *stream);
+
+/*
+ * out = x w^T (+ bias): tokens x [T, K] with weights w [N, K], products and sums in 32 bits, rounded once.
+ *   x          1 x 32 or 1 x 128 blocks;  w  128 x 128 blocks;  the same number of columns
+ *   bias       dev, bf16 [N] or NULL
+ *   format     of out: EAD_FMT_BF16 or EAD_FMT_F32
+ *   out        dev [T, N], out_stride elements apart (rows keep 16-byte alignment; N need not be a multiple of anything)
+ *   workspace  dev, EAD_LINEAR_WORKSPACE_BYTES bytes, 256-byte aligned, zero-filled ONCE by the caller; every call leaves it ready
+ *              for the next one.  Calls that may overlap on the device need a workspace each (and it is not ead_kv_attention's)
+ *   status     dev uint32 or NULL.  EAD_STATUS_WAIT_EXPIRED: a bounded wait ran out (the output is not valid, the workspace has
+ *              to be zero-filled again)
+ * A NaN in a row of x or w makes that row or column of the output NaN and no other.  The result does not depend on the order in
+ * which blocks run.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (more than 2^30 tiles of 128 x 240 outputs),
+ * EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ */
+#define EAD_LINEAR_WORKSPACE_BYTES (40u << 20)
+int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, const void *bias, int32_t format, void *out, int64_t out_stride,
+               void *workspace, uint32_t *status, int32_t device, void *stream);
+
+/*
+ * Norm and rotation of query and key heads.  Every head x of head_dim elements, where it has a weight:
+ *   y = x / sqrt(mean(x^2) + eps) * weight
+ * (without one y = x), then its first rot_dim elements in pairs (a, b), pair j turned by position * inv_freq[j]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin)
+ * Pair j is elements j and j + rot_dim / 2, or 2j and 2j + 1 (interleaved).  The angle is exact to 32 bits of a turn at any
+ * position; arithmetic is in 32 bits, rounded once at the end.
+ */
+typedef struct ead_rope {
+    int32_t head_dim;        /* 64 or 128                                                        */
+    int32_t rot_dim;         /* multiple of 16, 0 .. head_dim                                    */
+    int32_t interleaved;     /* 0 or 1                                                           */
+    float eps;
+    const float *inv_freq;   /* dev [rot_dim / 2], radians per position                          */
+    const void *q_weight;    /* dev bf16 [head_dim] or NULL: queries are not normalised          */
+    const void *k_weight;    /* the same for keys                                                */
+    int32_t reserved;        /* 0                                                                */
+} ead_rope;
+
+/*
+ * The heads of n_tokens tokens from tensors into tensors.
+ *   positions     dev int32 [n_tokens]
+ *   q, q_out      dev, bf16 [n_tokens, heads_q, head_dim], strides in elements between tokens (heads of a token are contiguous);
+ *                 q_out may be q.  k, k_out the same with heads_kv.  heads_q (0 .. 16384) or heads_kv (0 .. 128) may be 0
+ * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ */
+int ead_qk_norm_rope(const ead_rope *rope, const int32_t *positions, int32_t n_tokens, const void *q, int64_t q_stride, int32_t heads_q,
+                     const void *k, int64_t k_stride, int32_t heads_kv, void *q_out, int64_t q_out_stride, void *k_out,
+                     int64_t k_out_stride, int32_t device, void *stream);
+
+/*
+ * The same in front of ead_kv_attention: queries into a tensor, keys (normalised and rotated) and values (as they are) into the paged cache, quantised
+ * where its format says so (from the unrounded 32-bit keys).  Tokens go to the places that ead_kv_write gives them.
+ *   positions     dev int32 [n_tokens] or NULL: a token's place in its context (kv_len[b] - n_b + i)
+ *   q, q_out      as above;  k, v  dev, bf16 [n_tokens, heads_kv, head_dim], kv_stride apart
+ *   status        as in ead_kv_write; of a token that has no valid place nothing is written, its queries neither
+ * Errors as above.
+ */
+int ead_kv_rotate_write(const ead_rope *rope, const ead_kv_cache *cache, const ead_kv_batch *batch, const int32_t *positions,
+                        const void *q, int64_t q_stride, int32_t heads_q, const void *k, const void *v, int64_t kv_stride, void *q_out,
+                        int64_t q_out_stride, uint32_t *status, int32_t device, void *stream);
+
+/*
+ * What rows of logits z say: with p = softmax(z),
+ *   logprob = ln p[token],   entropy = -sum p ln p (nats),   rank = number of tokens that come before the given one,
+ *   top[j], top_logprob[j] = the token at place j of the order and ln p of it, j < k
+ * in the order of falling logits, the lower token first among equal ones.  -infinity masks a token (p = 0; it takes part in the
+ * order).  Where k exceeds V, places from V on get token -1 and -infinity.  A row with a NaN or +infinity, or with
+ * nothing but -infinity, gets NaNs, rank -1 and tokens -1, and sets EAD_STATUS_NONFINITE.
+ *   logits       dev, `format` (EAD_FMT_BF16, EAD_FMT_F16 or EAD_FMT_F32) [n_rows, V], stride elements apart; no alignment beyond
+ *                the element's
+ *   tokens       dev int32 [n_rows], or NULL (then logprob and rank are NULL); one below 0 means none: logprob NaN,
+ *                rank -1; so does one from V on, which sets EAD_STATUS_BAD_TOKEN
+ *   logprob, entropy  dev float [n_rows], each or NULL;  rank  dev int32 [n_rows] or NULL
+ *   k            0 .. 64;  top  dev int32 [n_rows, k] or NULL;  top_logprob  dev float [n_rows, k] or NULL
+ *   workspace    dev, EAD_LOGPROB_WORKSPACE_BYTES bytes, 256-byte aligned, zero-filled ONCE by the caller; every call leaves it
+ *                ready for the next one.  Calls that may overlap on the device need a workspace each
+ *   status       dev uint32 or NULL
+ * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (k), EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
+ */
+#define EAD_LOGPROB_WORKSPACE_BYTES (1u << 20)
+int ead_token_logprobs(const void *logits, int32_t format, int64_t stride, int32_t n_rows, int32_t V, const int32_t *tokens,
+                       float *logprob, float *entropy, int32_t *rank, int32_t k, int32_t *top, float *top_logprob, void *workspace,
+                       uint32_t *status, int32_t device, void *stream);
 
 /* Static, NUL-terminated description of an EAD_E* code. */
 const char *ead_strerror(int code);

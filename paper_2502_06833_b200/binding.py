@@ -29,11 +29,16 @@ EAD_STATUS_SHARD_MISMATCH = 0x8
 EAD_SHARD_RECORD_BYTES = 32
 EAD_SHARD_MAX = 16
 EAD_STATUS_BAD_PAGE = 0x10
+EAD_STATUS_BAD_TOKEN = 0x20
 EAD_FMT_BF16 = 0
 EAD_FMT_E4M3 = 1
+EAD_FMT_F32 = 2
+EAD_FMT_F16 = 3
 EAD_FMT_BLOCK = 32
 EAD_KV_WORKSPACE_BYTES = 64 << 20
 EAD_NORM_MAX_H = 16384
+EAD_LINEAR_WORKSPACE_BYTES = 40 << 20
+EAD_LOGPROB_WORKSPACE_BYTES = 1 << 20
 
 SYMBOLS = ["ead_create", "ead_step", "ead_run", "ead_run_host", "ead_run_timed", "ead_reset", "ead_status",
            "ead_state_size", "ead_get_state", "ead_set_state", "ead_kernel_launches",
@@ -41,7 +46,8 @@ SYMBOLS = ["ead_create", "ead_step", "ead_run", "ead_run_host", "ead_run_timed",
            "ead_plan_split", "ead_plan_units", "ead_usage", "ead_parameter_ratio", "ead_set_done", "ead_get_done",
            "ead_shard_range", "ead_shard_partials", "ead_shard_gate", "ead_shard_connect",
            "ead_shard_exchange_bytes", "ead_kv_write", "ead_kv_read", "ead_kv_attention", "ead_add_rmsnorm",
-           "ead_plan_chunk", "ead_kv_wait_limit"]
+           "ead_plan_chunk", "ead_kv_wait_limit", "ead_quantise", "ead_linear", "ead_qk_norm_rope", "ead_kv_rotate_write",
+           "ead_token_logprobs"]
 
 
 class EadConfig(C.Structure):
@@ -66,6 +72,18 @@ class EadKvBatch(C.Structure):
     _fields_ = [("B", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32),
                 ("new_start", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p),
                 ("table_stride", C.c_int32), ("reserved", C.c_int32)]
+
+
+class EadE4m3Matrix(C.Structure):
+    """``struct ead_e4m3_matrix``; made by ``ead_e4m3_matrix``."""
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("block_rows", C.c_int32), ("block_cols", C.c_int32),
+                ("row_stride", C.c_int64), ("codes", C.c_void_p), ("scale", C.c_void_p), ("reserved", C.c_int32)]
+
+
+class EadRope(C.Structure):
+    """``struct ead_rope``; made by ``ead_rope``."""
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float),
+                ("inv_freq", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("reserved", C.c_int32)]
 
 
 class EadError(RuntimeError):
@@ -151,6 +169,16 @@ def lib() -> C.CDLL:
         L.ead_plan_chunk.argtypes = [i32] * 6 + [C.POINTER(C.c_int64)]
         L.ead_add_rmsnorm.restype = C.c_int
         L.ead_add_rmsnorm.argtypes = [vp, i64, vp, i64, vp, i64, vp, C.c_float, i32, i32, i32, vp, i64, vp, i32, vp]
+        L.ead_quantise.restype = C.c_int
+        L.ead_quantise.argtypes = [vp, i64, vp, i64, vp, i32, vp]
+        L.ead_linear.restype = C.c_int
+        L.ead_linear.argtypes = [vp, vp, vp, i32, vp, i64, vp, vp, i32, vp]
+        L.ead_qk_norm_rope.restype = C.c_int
+        L.ead_qk_norm_rope.argtypes = [vp, vp, i32, vp, i64, i32, vp, i64, i32, vp, i64, vp, i64, i32, vp]
+        L.ead_kv_rotate_write.restype = C.c_int
+        L.ead_kv_rotate_write.argtypes = [vp, vp, vp, vp, vp, i64, i32, vp, vp, i64, vp, i64, vp, i32, vp]
+        L.ead_token_logprobs.restype = C.c_int
+        L.ead_token_logprobs.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp]
         L.ead_strerror.restype = C.c_char_p
         L.ead_strerror.argtypes = [C.c_int]
         _lib = L
@@ -492,6 +520,135 @@ def ead_add_rmsnorm(x, weight, out, *, residual=None, residual_out=None, out_sca
                                out.data_ptr(), out_stride, _ptr(out_scale), device, stream)
     if rc:
         _check(rc, "ead_add_rmsnorm")
+
+
+def current_stream() -> int:
+    """Handle of torch's current stream on its current device (what ``torch.cuda.current_stream().cuda_stream`` gives,
+    without the object around it, which takes a few microseconds to make)."""
+    T = _t()
+    return T._C._cuda_getCurrentRawStream(T.cuda.current_device())
+
+
+def ead_e4m3_matrix(codes, scale, *, block) -> EadE4m3Matrix:
+    """Describes 8-bit values ``codes`` ``[rows, cols]`` (``torch.float8_e4m3fn`` or ``torch.uint8``, contiguous rows) with a
+    scale byte per ``block = (rows, cols)``: ``scale`` uint8 ``[ceil(rows / block[0]), ceil(cols / block[1])]``.  The tensors
+    are borrowed (the description keeps them alive)."""
+    T = _t()
+    rows, cols = codes.shape
+    stride = _rows2(codes, codes.shape, "codes", (T.float8_e4m3fn, T.uint8))
+    if tuple(block) not in ((1, 32), (1, 128), (128, 128)):
+        raise ValueError(f"block {tuple(block)}: want (1, 32), (1, 128) or (128, 128)")
+    _dense(scale, (-(-rows // block[0]), -(-cols // block[1])), T.uint8, "scale")
+    m = EadE4m3Matrix(rows, cols, block[0], block[1], stride, _ptr(codes), _ptr(scale), 0)
+    m.held = (codes, scale)
+    m.ref = C.byref(m)
+    return m
+
+
+def ead_quantise(x, out: EadE4m3Matrix, *, gate=None, device=0, stream=0) -> None:
+    """bf16 ``x`` (or ``x * silu(gate)``) ``[rows, cols]`` into the 8-bit blocks that ``out`` describes."""
+    T = _t()
+    shape, bf16 = (out.rows, out.cols), (T.bfloat16,)
+    stride = _rows2(x, shape, "x", bf16)
+    rc = lib().ead_quantise(x.data_ptr(), stride, _ptr(gate), 0 if gate is None else _rows2(gate, shape, "gate", bf16), out.ref, device, stream)
+    if rc:
+        _check(rc, "ead_quantise")
+
+
+def ead_linear(x: EadE4m3Matrix, w: EadE4m3Matrix, out, *, workspace, bias=None, status=None, device=0, stream=0) -> None:
+    """``out = x w^T + bias``, ``out`` bf16 or float ``[x.rows, w.rows]``, ``bias`` bf16 ``[w.rows]``; ``workspace`` is a
+    zero-filled buffer of ``EAD_LINEAR_WORKSPACE_BYTES`` that calls which may overlap must not share."""
+    T = _t()
+    stride = _rows2(out, (x.rows, w.rows), "out", (T.bfloat16, T.float32))
+    if bias is not None:
+        _dense(bias, (w.rows,), T.bfloat16, "bias")
+    if workspace.nbytes < EAD_LINEAR_WORKSPACE_BYTES:
+        raise ValueError("workspace: want EAD_LINEAR_WORKSPACE_BYTES bytes")
+    rc = lib().ead_linear(x.ref, w.ref, _ptr(bias), EAD_FMT_F32 if out.dtype is T.float32 else EAD_FMT_BF16, out.data_ptr(), stride,
+                          workspace.data_ptr(), _ptr(status), device, stream)
+    if rc:
+        _check(rc, "ead_linear")
+
+
+def ead_rope(inv_freq, head_dim, *, interleaved=False, q_weight=None, k_weight=None, eps=1e-6) -> EadRope:
+    """Describes the norm and rotation of query and key heads: ``inv_freq`` float ``[rot_dim / 2]``, weights bf16 ``[head_dim]``
+    or None (no norm).  The tensors are borrowed (the description keeps them alive)."""
+    T = _t()
+    _dense(inv_freq, (inv_freq.numel(),), T.float32, "inv_freq")
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None:
+            _dense(t, (head_dim,), T.bfloat16, name)
+    r = EadRope(head_dim, 2 * inv_freq.numel(), int(bool(interleaved)), float(eps), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), 0)
+    r.held = (inv_freq, q_weight, k_weight)
+    r.ref = C.byref(r)
+    return r
+
+
+def _heads(t, n, dim, what: str):
+    """Heads and row stride of a bf16 tensor ``[n, heads, dim]``; of None: none."""
+    if t is None:
+        return 0, 0
+    shape = (n, t.shape[1] if t.dim() == 3 else -1, dim)
+    return shape[1], _rows3(t, shape, what)
+
+
+def ead_qk_norm_rope(rope: EadRope, positions, q, k, q_out, k_out, *, device=0, stream=0) -> None:
+    """Norm and rotation of ``q`` ``[n, heads_q, head_dim]`` and ``k`` (either may be None) into ``q_out`` and ``k_out`` (which may
+    be the same tensors); ``positions`` int32 ``[n]``."""
+    n, dim = positions.shape[0], rope.head_dim
+    _dense(positions, (n,), _t().int32, "positions")
+    heads_q, q_stride = _heads(q, n, dim, "q")
+    heads_kv, k_stride = _heads(k, n, dim, "k")
+    qo_stride = _rows3(q_out, (n, heads_q, dim), "q_out") if heads_q else 0
+    ko_stride = _rows3(k_out, (n, heads_kv, dim), "k_out") if heads_kv else 0
+    rc = lib().ead_qk_norm_rope(rope.ref, positions.data_ptr(), n, _ptr(q), q_stride, heads_q, _ptr(k), k_stride, heads_kv, _ptr(q_out),
+                                qo_stride, _ptr(k_out), ko_stride, device, stream)
+    if rc:
+        _check(rc, "ead_qk_norm_rope")
+
+
+def ead_kv_rotate_write(rope: EadRope, cache: EadKvCache, batch: EadKvBatch, q, k, v, q_out, *, positions=None, status=None, device=0,
+                        stream=0) -> None:
+    """Norm and rotation of the step's queries into ``q_out``, of its keys, with the values, into the cache; ``positions`` int32
+    ``[n_tokens]``, by default the tokens' places in their contexts."""
+    n, dim = batch.n_tokens, cache.head_dim
+    heads_q, q_stride = _heads(q, n, dim, "q")
+    qo_stride = _rows3(q_out, (n, heads_q, dim), "q_out") if heads_q else 0
+    kv_stride = _rows3(k, (n, cache.heads_kv, dim), "k")
+    if _rows3(v, (n, cache.heads_kv, dim), "v") != kv_stride:
+        raise ValueError("k and v: want the same row stride")
+    if positions is not None:
+        _dense(positions, (n,), _t().int32, "positions")
+    rc = lib().ead_kv_rotate_write(rope.ref, cache.ref, batch.ref, _ptr(positions), _ptr(q), q_stride, heads_q, k.data_ptr(), v.data_ptr(),
+                                   kv_stride, _ptr(q_out), qo_stride, _ptr(status), device, stream)
+    if rc:
+        _check(rc, "ead_kv_rotate_write")
+
+
+def ead_token_logprobs(logits, tokens, *, workspace, logprob=None, entropy=None, rank=None, top=None, top_logprob=None, status=None,
+                       device=0, stream=0) -> None:
+    """Of rows of ``logits`` ``[n, V]`` (bf16, half or float, contiguous rows): log probability and rank of the given ``tokens``
+    (int32 ``[n]`` or None), entropy, and the most likely tokens ``top`` (int32 ``[n, k]``) with ``top_logprob`` (float ``[n, k]``).
+    Results go into the tensors that are given; ``workspace`` is a zero-filled buffer of ``EAD_LOGPROB_WORKSPACE_BYTES`` that
+    calls which may overlap must not share."""
+    T = _t()
+    formats = {T.bfloat16: EAD_FMT_BF16, T.float16: EAD_FMT_F16, T.float32: EAD_FMT_F32}
+    n, V = logits.shape
+    stride = _rows2(logits, logits.shape, "logits", formats)
+    k = 0
+    for t, dtype, name in ((tokens, T.int32, "tokens"), (logprob, T.float32, "logprob"), (entropy, T.float32, "entropy"), (rank, T.int32, "rank")):
+        if t is not None:
+            _dense(t, (n,), dtype, name)
+    for t, dtype, name in ((top, T.int32, "top"), (top_logprob, T.float32, "top_logprob")):
+        if t is not None:
+            k = t.shape[-1] if top is None else top.shape[-1]
+            _dense(t, (n, k), dtype, name)
+    if workspace.nbytes < EAD_LOGPROB_WORKSPACE_BYTES:
+        raise ValueError("workspace: want EAD_LOGPROB_WORKSPACE_BYTES bytes")
+    rc = lib().ead_token_logprobs(logits.data_ptr(), formats[logits.dtype], stride, n, V, _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(rank),
+                                  k, _ptr(top), _ptr(top_logprob), workspace.data_ptr(), _ptr(status), device, stream)
+    if rc:
+        _check(rc, "ead_token_logprobs")
 
 
 def ead_destroy(ctx) -> None:

@@ -11,35 +11,55 @@ import sys
 
 _DIR = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_DIR, "csrc")
+_OBJ = os.path.join(_DIR, "build")
 LIB_PATH = os.path.join(_DIR, "libead_b200.so")
-SOURCES = [os.path.join(_CSRC, f) for f in ("ead_api.cu", "ead_decoder_api.cu")]
+SOURCES = [os.path.join(_CSRC, f) for f in ("ead_api.cu", "ead_decoder_api.cu", "ead_pass_api.cu")]
+_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a", "-Xcompiler", "-fPIC,-O2,-Wall"]
 
 
-def _deps():
-    inc = os.path.join(os.path.dirname(_DIR), "include", "ead.h")
-    return [inc] + [os.path.join(_CSRC, f) for f in sorted(os.listdir(_CSRC))]
+def _nvcc() -> str:
+    return os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
-def nvcc_command(verbose: bool = False):
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-std=c++17", "-O3", "-lineinfo",
-           "-gencode", "arch=compute_100a,code=sm_100a",
-           "-Xcompiler", "-fPIC,-O2,-Wall", "-shared", "-cudart", "static",
-           "-o", LIB_PATH] + SOURCES
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    return cmd
+def _object(source: str) -> str:
+    return os.path.join(_OBJ, os.path.splitext(os.path.basename(source))[0] + ".o")
+
+
+def _stale(target: str, deps) -> bool:
+    return not os.path.exists(target) or any(not os.path.exists(d) or os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
+
+
+def _deps(source: str):
+    """The source and this repository's headers that it was last compiled with; all headers before the first time."""
+    try:
+        with open(_object(source) + ".d") as f:
+            words = f.read().replace("\\\n", " ").split()[1:]
+    except OSError:
+        return [source] + [os.path.join(_CSRC, f) for f in os.listdir(_CSRC)]
+    root = os.path.dirname(_DIR)
+    return [source] + [w for w in map(os.path.abspath, words) if w.startswith(root + os.sep)]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    stale = (not os.path.exists(LIB_PATH)
-             or any(os.path.getmtime(d) > os.path.getmtime(LIB_PATH) for d in _deps()))
-    if force or stale:
-        res = subprocess.run(nvcc_command(verbose), capture_output=True, text=True)
-        if verbose or res.returncode != 0:
+    os.makedirs(_OBJ, exist_ok=True)
+    jobs = []
+    for s in SOURCES:
+        if force or _stale(_object(s), _deps(s)):
+            cmd = [_nvcc(), *_FLAGS, "-MD", "-MF", _object(s) + ".d", "-c", s, "-o", _object(s)]
+            jobs.append(subprocess.Popen(cmd[:1] + (["-Xptxas=-v"] if verbose else []) + cmd[1:], cwd=_DIR, text=True,
+                                         stdout=subprocess.PIPE, stderr=subprocess.STDOUT))
+    said = [j.communicate()[0] for j in jobs]
+    if verbose or any(j.returncode for j in jobs):
+        sys.stderr.write("".join(said))
+    if any(j.returncode for j in jobs):
+        raise RuntimeError("nvcc failed building libead_b200.so")
+    objects = [_object(s) for s in SOURCES]
+    if jobs or _stale(LIB_PATH, objects):
+        res = subprocess.run([_nvcc(), "-shared", "-cudart", "static", "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB_PATH, *objects],
+                             capture_output=True, text=True)
+        if res.returncode:
             sys.stderr.write(res.stdout + res.stderr)
-        if res.returncode != 0:
-            raise RuntimeError("nvcc failed building libead_b200.so")
+            raise RuntimeError("nvcc failed linking libead_b200.so")
     return LIB_PATH
 
 

@@ -234,8 +234,6 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Shared-memory writes of this thread become visible to the tensor core and to TMA.
-__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // D[tmem] (+)= A[tmem] * B[smem], A packed bf16.
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
@@ -265,12 +263,6 @@ struct ValueTile {
         return ((key >> shift) * (D / 64) << shift) * 128u + (key & ((1 << shift) - 1)) * 128u;
     }
 };
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(p));
-    return p != 0;
-}
 // 32 bytes to global memory, in one store if `wide` (the address is a multiple of 32 then).
 __device__ __forceinline__ void store_32(uint8_t *dst, const uint32_t (&v)[8], bool wide)
 {
@@ -282,17 +274,6 @@ __device__ __forceinline__ void store_32(uint8_t *dst, const uint32_t (&v)[8], b
         reinterpret_cast<uint4 *>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
     }
 }
-__device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-// The same, and whether `ok` held for all of the barrier's threads.
-__device__ __forceinline__ bool named_all(int id, int threads, bool ok)
-{
-    uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(all) : "r"(id), "r"(threads), "r"(static_cast<uint32_t>(ok)) : "memory");
-    return all != 0;
-}
-
 template <int FMT, int D>
 __global__ void __launch_bounds__(ChunkLayout<FMT, D>::kThreads, 1)
     ead_attn_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,

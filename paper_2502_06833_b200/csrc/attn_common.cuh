@@ -118,11 +118,14 @@ __device__ __forceinline__ float exp2_fast(float x)
 
 // Waits for a phase of an mbarrier.  False if the wait has run out (recorded in the status) or another one of the block has
 // (recorded in `gave_up`, shared memory, for warps that wait for one another; NULL for one that waits for its own loads alone).
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, const AttnParams &p, uint32_t *gave_up)
+// BRIEF: the first look takes no time (a plain try_wait may be held up for as long as the hardware likes), and with a limit of 0 there is
+// no other.
+template <bool BRIEF = false, typename Params>
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, const Params &p, uint32_t *gave_up)
 {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (BRIEF ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
     const uint64_t t0 = globaltimer_ns();
-    while (!mbar_try_wait_hint(bar, parity, p.wait_hint)) {
+    while ((BRIEF && p.wait_ns == 0) || !mbar_try_wait_hint(bar, parity, p.wait_hint)) {
         if (gave_up && *reinterpret_cast<volatile uint32_t *>(gave_up)) return false;
         if (globaltimer_ns() - t0 >= p.wait_ns) {
             if (gave_up) *reinterpret_cast<volatile uint32_t *>(gave_up) = 1u;

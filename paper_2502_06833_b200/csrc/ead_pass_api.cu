@@ -1,0 +1,303 @@
+// Host side of the operators of a decoder's 8-bit pass declared in include/ead.h: product with block scales, quantisation,
+// norm and rotation of query and key heads, log probabilities of given tokens.  Stateless: arguments are checked, kernels are enqueued.
+#include "../../include/ead.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "decoder_host.h"
+#include "linear_kernel.cuh"
+#include "logprob_kernel.cuh"
+#include "quantise_kernel.cuh"
+#include "rope_kernel.cuh"
+#include "tma_host.h"
+
+using namespace ead;
+
+namespace {
+
+// Least stretch of K, in stages, of a block that shares a tile: the parts' way through the workspace costs about as much as these.
+constexpr int kLinMinStretch = 4;
+// Blocks of a call that scores few rows, per SM, and the least 16-byte vectors of a part.
+constexpr int kScoreBlocksPerSm = 2;
+constexpr int kScoreMinVectors = 256;
+
+DeviceTable g_devices;
+
+template <int BLOCK, bool F32>
+bool allow_smem()
+{
+    return cudaFuncSetAttribute(ead_linear_kernel<BLOCK, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmem) == cudaSuccess;
+}
+
+int use_device(int device, DeviceInfo **out)
+{
+    return g_devices.use(device, out, [] { return allow_smem<32, false>() && allow_smem<32, true>() && allow_smem<128, false>() && allow_smem<128, true>(); });
+}
+
+// 8-bit rows as boxes of 128 bytes x `rows`, with the 128-byte swizzle.
+bool encode_codes(CUtensorMap *tm, const ead_e4m3_matrix &m, int rows)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(m.row_stride)};
+    const cuuint32_t box[2] = {kLinK, static_cast<cuuint32_t>(rows)}, ones[2] = {1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, m.codes, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int check_matrix(const ead_e4m3_matrix *m, int block_rows)
+{
+    if (!m || m->reserved || m->rows < 0 || m->cols < kFmtBlock || m->cols > (1 << 30) || m->rows > (1 << 30)) return EAD_EINVALID_ARG;
+    if (m->block_rows != block_rows) return EAD_EINVALID_ARG;
+    if (m->block_cols != 128 && (m->block_cols != kFmtBlock || block_rows != 1)) return EAD_EINVALID_ARG;
+    if (m->rows == 0) return EAD_OK;              // nothing there: it may have no address
+    if (!m->codes || !m->scale || m->row_stride < m->cols || m->row_stride > (int64_t{1} << 39)) return EAD_EINVALID_ARG;
+    if (m->cols % kFmtBlock || !aligned(m->codes, 16) || m->row_stride % 16) return EAD_EALIGNMENT;
+    if (m->block_cols == kFmtBlock && !aligned(m->scale, 4)) return EAD_EALIGNMENT;
+    return EAD_OK;
+}
+
+int check_rope(const ead_rope *r, RopeParams *p)
+{
+    if (!r || r->reserved || (r->head_dim != 64 && r->head_dim != 128) || r->rot_dim < 0 || r->rot_dim > r->head_dim || r->rot_dim % 16)
+        return EAD_EINVALID_ARG;
+    if ((r->interleaved != 0 && r->interleaved != 1) || !std::isfinite(r->eps) || r->eps < 0.f) return EAD_EINVALID_ARG;
+    if (r->rot_dim && !r->inv_freq) return EAD_EINVALID_ARG;
+    if (!aligned(r->inv_freq, 4) || !aligned(r->q_weight, 16) || !aligned(r->k_weight, 16)) return EAD_EALIGNMENT;
+    p->inv_freq = r->inv_freq;
+    p->q_weight = static_cast<const uint8_t *>(r->q_weight);
+    p->k_weight = static_cast<const uint8_t *>(r->k_weight);
+    p->dim = r->head_dim;
+    p->rot = r->rot_dim;
+    p->interleaved = r->interleaved;
+    p->eps = r->eps;
+    return EAD_OK;
+}
+
+dim3 rope_grid(int n_tokens, int64_t values)
+{
+    return dim3(n_tokens, static_cast<unsigned>((values + kRopeBlockValues - 1) / kRopeBlockValues));
+}
+
+template <int BLOCK, bool F32>
+int launch_linear(const CUtensorMap &tw, const CUtensorMap &tx, const LinearParams &p, int grid, int smem, cudaStream_t s)
+{
+    ead_linear_kernel<BLOCK, F32><<<grid, kLinThreads, smem, s>>>(tw, tx, p);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, const void *bias, int32_t format, void *out, int64_t out_stride,
+                          void *workspace, uint32_t *status, int32_t device, void *stream)
+{
+    int rc = check_matrix(x, 1);
+    if (rc == EAD_OK) rc = check_matrix(w, 128);
+    if (rc != EAD_OK) return rc;
+    const bool f32 = format == EAD_FMT_F32;
+    if ((format != EAD_FMT_BF16 && !f32) || x->cols != w->cols || !workspace) return EAD_EINVALID_ARG;
+    if (x->rows == 0 || w->rows == 0) return EAD_OK;
+    if (!out || out_stride < w->rows) return EAD_EINVALID_ARG;
+    if (!aligned(out, 16) || out_stride % (f32 ? 4 : 8) || !aligned(bias, 2) || !aligned(workspace, 256) || !aligned(status, 4)) return EAD_EALIGNMENT;
+    LinearParams p{};
+    p.x_scale = x->scale;
+    p.w_scale = w->scale;
+    p.bias = static_cast<const uint8_t *>(bias);
+    p.out = static_cast<uint8_t *>(out);
+    p.workspace = static_cast<uint8_t *>(workspace);
+    p.out_stride = out_stride;
+    p.T = x->rows;
+    p.N = w->rows;
+    p.kblocks = (x->cols + kLinK - 1) / kLinK;
+    p.x_scale_cols = (x->cols + x->block_cols - 1) / x->block_cols;
+    p.w_scale_cols = p.kblocks;
+    p.token_tiles = (p.T + kLinMaxTokens - 1) / kLinMaxTokens;
+    p.tile_tokens = ((p.T + p.token_tiles - 1) / p.token_tiles + 15) / 16 * 16;
+    p.token_tiles = (p.T + p.tile_tokens - 1) / p.tile_tokens;
+    const int64_t tiles = static_cast<int64_t>((p.N + kLinM - 1) / kLinM) * p.token_tiles;
+    if (tiles > (1 << 30)) return EAD_ELIMIT;
+    DeviceInfo *d = nullptr;
+    rc = use_device(device, &d);
+    if (rc != EAD_OK) return rc;
+    p.tiles = static_cast<int>(tiles);
+    const int sms = std::min(d->sms, kLinMaxCtas);
+    p.whole = p.tiles / sms * sms;
+    const int rest = p.tiles - p.whole;
+    p.rest_ctas = std::min<int64_t>(sms, std::max<int64_t>(rest, static_cast<int64_t>(rest) * p.kblocks / kLinMinStretch));
+    const int stage = kLinM * kLinK + p.tile_tokens * kLinK + kLinScaleStage, room = kLinSmem - 1024 - 4 * kLinOutBytes;
+    p.stages = std::min(kLinMaxStages, room / stage);
+    p.status = status;
+    p.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+    p.wait_hint = std::min(p.wait_ns, 20000u);
+    CUtensorMap tw, tx;
+    if (!encode_codes(&tw, *w, kLinM) || !encode_codes(&tx, *x, p.tile_tokens)) return EAD_ECUDA;
+    const int grid = p.whole ? sms : p.rest_ctas, smem = 1024 + p.stages * stage + 4 * kLinOutBytes;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return x->block_cols == 128 ? (f32 ? launch_linear<128, true>(tw, tx, p, grid, smem, s) : launch_linear<128, false>(tw, tx, p, grid, smem, s))
+                                : (f32 ? launch_linear<32, true>(tw, tx, p, grid, smem, s) : launch_linear<32, false>(tw, tx, p, grid, smem, s));
+}
+
+extern "C" int ead_quantise(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, const ead_e4m3_matrix *out, int32_t device,
+                            void *stream)
+{
+    if (!out) return EAD_EINVALID_ARG;
+    const bool tiles = out->block_rows == 128;
+    int rc = check_matrix(out, tiles ? 128 : 1);
+    if (rc != EAD_OK) return rc;
+    if (tiles && gate) return EAD_EINVALID_ARG;
+    if (out->rows == 0) return EAD_OK;
+    rc = check_rows(x, x_stride, out->cols);
+    if (rc == EAD_OK && gate) rc = check_rows(gate, gate_stride, out->cols);
+    DeviceInfo *d = nullptr;
+    if (rc == EAD_OK) rc = use_device(device, &d);
+    if (rc != EAD_OK) return rc;
+    QuantParams p{};
+    p.x = static_cast<const uint8_t *>(x);
+    p.gate = static_cast<const uint8_t *>(gate);
+    p.out = static_cast<uint8_t *>(out->codes);
+    p.out_scale = out->scale;
+    p.x_stride = x_stride;
+    p.gate_stride = gate_stride;
+    p.out_stride = out->row_stride;
+    p.rows = out->rows;
+    p.cols = out->cols;
+    p.scale_cols = (p.cols + out->block_cols - 1) / out->block_cols;
+    p.passes = (p.cols + kQuantPass - 1) / kQuantPass;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int64_t blocks = tiles ? static_cast<int64_t>((p.rows + int64_t{127}) / 128) * p.scale_cols
+                                 : (static_cast<int64_t>(p.rows) * p.passes + kQuantThreads / 32 - 1) / (kQuantThreads / 32);
+    if (blocks > 0x7fffffff) return EAD_ELIMIT;
+    const unsigned grid = static_cast<unsigned>(blocks);
+    if (tiles)
+        ead_quantise_tiles_kernel<<<grid, kQuantThreads, 0, s>>>(p);
+    else if (out->block_cols == 128)
+        gate ? ead_quantise_rows_kernel<128, true><<<grid, kQuantThreads, 0, s>>>(p) : ead_quantise_rows_kernel<128, false><<<grid, kQuantThreads, 0, s>>>(p);
+    else
+        gate ? ead_quantise_rows_kernel<32, true><<<grid, kQuantThreads, 0, s>>>(p) : ead_quantise_rows_kernel<32, false><<<grid, kQuantThreads, 0, s>>>(p);
+    return launched();
+}
+
+extern "C" int ead_qk_norm_rope(const ead_rope *rope, const int32_t *positions, int32_t n_tokens, const void *q, int64_t q_stride, int32_t heads_q,
+                                const void *k, int64_t k_stride, int32_t heads_kv, void *q_out, int64_t q_out_stride, void *k_out,
+                                int64_t k_out_stride, int32_t device, void *stream)
+{
+    RopeParams p{};
+    int rc = check_rope(rope, &p);
+    if (rc != EAD_OK) return rc;
+    if (n_tokens < 0 || n_tokens > (1 << 30) || heads_q < 0 || heads_q > 16384 || heads_kv < 0 || heads_kv > 128) return EAD_EINVALID_ARG;
+    if (n_tokens == 0 || heads_q + heads_kv == 0) return EAD_OK;
+    if (!positions) return EAD_EINVALID_ARG;
+    if (heads_q) rc = check_rows(q, q_stride, static_cast<int64_t>(heads_q) * p.dim);
+    if (rc == EAD_OK && heads_q) rc = check_rows(q_out, q_out_stride, static_cast<int64_t>(heads_q) * p.dim);
+    if (rc == EAD_OK && heads_kv) rc = check_rows(k, k_stride, static_cast<int64_t>(heads_kv) * p.dim);
+    if (rc == EAD_OK && heads_kv) rc = check_rows(k_out, k_out_stride, static_cast<int64_t>(heads_kv) * p.dim);
+    if (rc == EAD_OK && !aligned(positions, 4)) rc = EAD_EALIGNMENT;
+    DeviceInfo *d = nullptr;
+    if (rc == EAD_OK) rc = use_device(device, &d);
+    if (rc != EAD_OK) return rc;
+    p.positions = positions;
+    p.q = static_cast<const uint8_t *>(q);
+    p.k = static_cast<const uint8_t *>(k);
+    p.q_out = static_cast<uint8_t *>(q_out);
+    p.k_out = static_cast<uint8_t *>(k_out);
+    p.q_stride = q_stride;
+    p.kv_stride = k_stride;
+    p.q_out_stride = q_out_stride;
+    p.k_out_stride = k_out_stride;
+    p.heads_q = heads_q;
+    p.heads_kv = heads_kv;
+    const dim3 grid = rope_grid(n_tokens, (static_cast<int64_t>(heads_q) + heads_kv) * p.dim);
+    ead_rotate_kernel<kFmtBf16, true><<<grid, kRopeThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
+    return launched();
+}
+
+extern "C" int ead_kv_rotate_write(const ead_rope *rope, const ead_kv_cache *cache, const ead_kv_batch *batch, const int32_t *positions,
+                                   const void *q, int64_t q_stride, int32_t heads_q, const void *k, const void *v, int64_t kv_stride, void *q_out,
+                                   int64_t q_out_stride, uint32_t *status, int32_t device, void *stream)
+{
+    RopeParams p{};
+    int rc = check_rope(rope, &p);
+    if (rc == EAD_OK) rc = check_cache(cache, &p.cache);
+    if (rc == EAD_OK) rc = check_batch(batch, p.cache, true, &p.batch);
+    if (rc != EAD_OK) return rc;
+    if (rope->head_dim != cache->head_dim || heads_q < 0 || heads_q > 16384) return EAD_EINVALID_ARG;
+    if (p.batch.n_tokens == 0) return EAD_OK;
+    const int64_t q_row = static_cast<int64_t>(heads_q) * p.dim, kv_row = static_cast<int64_t>(p.cache.heads) * p.dim;
+    if (heads_q) rc = check_rows(q, q_stride, q_row);
+    if (rc == EAD_OK && heads_q) rc = check_rows(q_out, q_out_stride, q_row);
+    if (rc == EAD_OK) rc = check_rows(k, kv_stride, kv_row);
+    if (rc == EAD_OK) rc = check_rows(v, kv_stride, kv_row);
+    if (rc == EAD_OK && (!aligned(positions, 4) || !aligned(status, 4))) rc = EAD_EALIGNMENT;
+    DeviceInfo *d = nullptr;
+    if (rc == EAD_OK) rc = use_device(device, &d);
+    if (rc != EAD_OK) return rc;
+    p.positions = positions;
+    p.q = static_cast<const uint8_t *>(q);
+    p.k = static_cast<const uint8_t *>(k);
+    p.v = static_cast<const uint8_t *>(v);
+    p.q_out = static_cast<uint8_t *>(q_out);
+    p.q_stride = q_stride;
+    p.kv_stride = kv_stride;
+    p.q_out_stride = q_out_stride;
+    p.heads_q = heads_q;
+    p.heads_kv = p.cache.heads;
+    p.status = status;
+    const dim3 grid = rope_grid(p.batch.n_tokens, q_row + 2 * kv_row);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (cache->format == EAD_FMT_BF16)
+        ead_rotate_kernel<kFmtBf16, false><<<grid, kRopeThreads, 0, s>>>(p);
+    else
+        ead_rotate_kernel<kFmtE4m3, false><<<grid, kRopeThreads, 0, s>>>(p);
+    return launched();
+}
+
+extern "C" int ead_token_logprobs(const void *logits, int32_t format, int64_t stride, int32_t n_rows, int32_t V, const int32_t *tokens,
+                                  float *logprob, float *entropy, int32_t *rank, int32_t k, int32_t *top, float *top_logprob, void *workspace,
+                                  uint32_t *status, int32_t device, void *stream)
+{
+    if ((format != EAD_FMT_BF16 && format != EAD_FMT_F16 && format != EAD_FMT_F32) || n_rows < 0 || V < 1 || V > (1 << 30) || k < 0 || !workspace)
+        return EAD_EINVALID_ARG;
+    if (k > kScoreMaxTop) return EAD_ELIMIT;
+    if (!tokens && (logprob || rank)) return EAD_EINVALID_ARG;
+    if (n_rows == 0) return EAD_OK;
+    if (!logits || stride < V) return EAD_EINVALID_ARG;
+    if (!aligned(logits, format == EAD_FMT_F32 ? 4 : 2) || !aligned(workspace, 256) || !aligned(tokens, 4) || !aligned(logprob, 4) ||
+        !aligned(entropy, 4) || !aligned(rank, 4) || !aligned(top, 4) || !aligned(top_logprob, 4) || !aligned(status, 4))
+        return EAD_EALIGNMENT;
+    DeviceInfo *d = nullptr;
+    const int rc = use_device(device, &d);
+    if (rc != EAD_OK) return rc;
+    ScoreParams p{};
+    p.logits = static_cast<const uint8_t *>(logits);
+    p.stride = stride;
+    p.tokens = tokens;
+    p.logprob = logprob;
+    p.entropy = entropy;
+    p.rank = rank;
+    p.k = top || top_logprob ? k : 0;
+    p.top = top;
+    p.top_logprob = top_logprob;
+    p.n_rows = n_rows;
+    p.V = V;
+    p.workspace = static_cast<uint8_t *>(workspace);
+    p.status = status;
+    const int per = format == EAD_FMT_F32 ? 4 : 8, blocks = kScoreBlocksPerSm * d->sms;
+    const int64_t vectors = (static_cast<int64_t>(V) + per - 1) / per;
+    int64_t parts = std::min<int64_t>(blocks / n_rows, vectors / kScoreMinVectors);
+    parts = std::min<int64_t>(parts, kScoreMaxParts);
+    if (p.k) parts = std::min<int64_t>(parts, kScoreMaxJoin / p.k);
+    p.parts = static_cast<int>(std::max<int64_t>(parts, 1));
+    const dim3 grid(p.parts, std::min(n_rows, 65535));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (format == EAD_FMT_BF16)
+        ead_token_logprobs_kernel<kFmtBf16><<<grid, kScoreThreads, 0, s>>>(p);
+    else if (format == EAD_FMT_F16)
+        ead_token_logprobs_kernel<kFmtF16><<<grid, kScoreThreads, 0, s>>>(p);
+    else
+        ead_token_logprobs_kernel<kFmtF32><<<grid, kScoreThreads, 0, s>>>(p);
+    return launched();
+}

@@ -12,9 +12,12 @@ namespace ead {
 
 constexpr int kFmtBf16 = 0;
 constexpr int kFmtE4m3 = 1;
+constexpr int kFmtF32 = 2;
+constexpr int kFmtF16 = 3;
 constexpr int kFmtBlock = 32;
 constexpr int kMaxBatch = 4096;                    // sequences of a step
 constexpr uint32_t kStatusBadPage = 0x10u;
+constexpr uint32_t kStatusBadToken = 0x20u;
 
 struct KvCacheView {
     uint8_t *k, *v;                               // pools

@@ -1,0 +1,127 @@
+// bf16 values into 8-bit blocks: rows with a scale per 32 or 128 consecutive values (activations; of a gated MLP
+// y = silu(gate) * x is taken on the way), and matrices with a scale per 128 x 128 (weights).
+// Every value is read once and every code written once, so HBM bounds both at size and the launch at one step.
+#pragma once
+#include "kv_format.cuh"
+#include "rmsnorm_kernel.cuh"
+
+namespace ead {
+
+constexpr int kQuantThreads = 256;
+constexpr int kQuantPass = 512;                    // values of a row that a warp takes at a time
+
+struct QuantParams {
+    const uint8_t *x, *gate;
+    uint8_t *out, *out_scale;
+    int64_t x_stride, gate_stride, out_stride;     // elements
+    int32_t rows, cols, scale_cols;
+    int32_t passes;                                // ceil(cols / kQuantPass)
+};
+
+__device__ __forceinline__ uint2 to_e4m3x8(const float (&y)[8], float inv)
+{
+    return make_uint2(to_e4m3x2(y[0] * inv, y[1] * inv) | to_e4m3x2(y[2] * inv, y[3] * inv) << 16,
+                      to_e4m3x2(y[4] * inv, y[5] * inv) | to_e4m3x2(y[6] * inv, y[7] * inv) << 16);
+}
+
+__device__ __forceinline__ uint4 load_stream(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// g / (1 + e^-g): the exponential and the quotient by the special function unit, a few units of the last 32-bit place off.
+__device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.f + __expf(-g)); }
+
+// A warp takes kQuantPass values of a row, a lane 8 consecutive ones of each half: BLOCK / 8 neighbouring lanes share a scale.
+template <int BLOCK, bool GATED>
+__global__ void __launch_bounds__(kQuantThreads) ead_quantise_rows_kernel(QuantParams p)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    const int row = static_cast<int>(unit / p.passes);
+    if (row >= p.rows) return;
+    const int col0 = static_cast<int>(unit - static_cast<int64_t>(row) * p.passes) * kQuantPass + lane * 8;
+    uint4 x[2], g[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int col = col0 + h * (kQuantPass / 2);
+        x[h] = g[h] = make_uint4(0, 0, 0, 0);
+        if (col < p.cols) {
+            x[h] = load_stream(p.x + 2 * (row * p.x_stride + col));
+            if (GATED) g[h] = load_stream(p.gate + 2 * (row * p.gate_stride + col));
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int col = col0 + h * (kQuantPass / 2);
+        float y[8];
+        unpack8(x[h], y);
+        if (GATED) {
+            float a[8];
+            unpack8(g[h], a);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] *= silu(a[k]);
+        }
+        uint32_t amax = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) amax = max(amax, abs_bits(y[k]));
+        if (GATED && amax >= 0x7f800000u) {        // a product of finite values that passes 32 bits saturates like any other large value
+            float u[8], a[8];
+            unpack8(x[h], u);
+            unpack8(g[h], a);
+            amax = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (abs_bits(y[k]) == 0x7f800000u && isfinite(u[k]) && isfinite(a[k])) y[k] = copysignf(3.402823466e38f, y[k]);
+                amax = max(amax, abs_bits(y[k]));
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < BLOCK / 8; o <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        const int byte = scale_byte(amax);
+        if (col < p.cols) {
+            *reinterpret_cast<uint2 *>(p.out + row * p.out_stride + col) = to_e4m3x8(y, inverse_scale(byte));
+            if ((lane & (BLOCK / 8 - 1)) == 0) p.out_scale[static_cast<int64_t>(row) * p.scale_cols + col / BLOCK] = static_cast<uint8_t>(byte);
+        }
+    }
+}
+
+// A block takes 128 x 128 values: thread t columns 8 (t mod 16) .. + 7 of rows t / 16 + 16 i.
+__global__ void __launch_bounds__(kQuantThreads) ead_quantise_tiles_kernel(QuantParams p)
+{
+    __shared__ uint32_t part[kQuantThreads / 32];
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x / p.scale_cols) * 128 + threadIdx.x / 16;
+    const int col = static_cast<int>(blockIdx.x % p.scale_cols) * 128 + (threadIdx.x & 15) * 8;
+    uint4 x[8];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (col < p.cols && row0 + 16 * i < p.rows) x[i] = load_stream(p.x + 2 * ((row0 + 16 * i) * p.x_stride + col));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float y[8];
+        unpack8(x[i], y);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) amax = max(amax, abs_bits(y[k]));
+    }
+    amax = __reduce_max_sync(0xffffffffu, amax);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kQuantThreads / 32; ++i) amax = max(amax, part[i]);
+    const int byte = scale_byte(amax);
+    const float inv = inverse_scale(byte);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float y[8];
+        unpack8(x[i], y);
+        if (col < p.cols && row0 + 16 * i < p.rows) *reinterpret_cast<uint2 *>(p.out + (row0 + 16 * i) * p.out_stride + col) = to_e4m3x8(y, inv);
+    }
+    if (threadIdx.x == 0) p.out_scale[blockIdx.x] = static_cast<uint8_t>(byte);
+}
+
+}  // namespace ead
