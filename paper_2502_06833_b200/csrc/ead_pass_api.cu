@@ -18,23 +18,100 @@ using namespace ead;
 
 namespace {
 
-// Least stretch of K, in stages, of a block that shares a tile: the parts' way through the workspace costs about as much as these.
-constexpr int kLinMinStretch = 4;
+// What the join of a tile's parts costs, in stages of 128 values along K.
+constexpr double kLinJoinStages = 4;
 // Blocks of a call that scores few rows, per SM, and the least 16-byte vectors of a part.
 constexpr int kScoreBlocksPerSm = 2;
 constexpr int kScoreMinVectors = 256;
 
 DeviceTable g_devices;
+int g_clusters[kMaxDevices][kLinMaxSplit + 1];    // clusters of ead_linear's blocks that a device holds at a time, by their size
 
-template <int BLOCK, bool F32>
-bool allow_smem()
+template <int BLOCK, bool F32, bool PAIR>
+bool prepare_linear()
 {
-    return cudaFuncSetAttribute(ead_linear_kernel<BLOCK, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmem) == cudaSuccess;
+    return cudaFuncSetAttribute(ead_linear_kernel<BLOCK, F32, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmem) == cudaSuccess;
+}
+
+cudaLaunchConfig_t linear_config(int blocks, int cluster, int smem, cudaStream_t s, cudaLaunchAttribute *attr)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(kLinThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
 }
 
 int use_device(int device, DeviceInfo **out)
 {
-    return g_devices.use(device, out, [] { return allow_smem<32, false>() && allow_smem<32, true>() && allow_smem<128, false>() && allow_smem<128, true>(); });
+    return g_devices.use(device, out, [device] {
+        if (!prepare_linear<32, false, false>() || !prepare_linear<32, true, false>() || !prepare_linear<128, false, false>() ||
+            !prepare_linear<128, true, false>() || !prepare_linear<32, false, true>() || !prepare_linear<32, true, true>() ||
+            !prepare_linear<128, false, true>() || !prepare_linear<128, true, true>())
+            return false;
+        for (int c = 1; c <= kLinMaxSplit; ++c) {
+            cudaLaunchAttribute attr[1];
+            const cudaLaunchConfig_t cfg = linear_config(c, c, kLinSmem, nullptr, attr);
+            if (cudaOccupancyMaxActiveClusters(&g_clusters[device][c], ead_linear_kernel<128, false, false>, &cfg) != cudaSuccess) return false;
+        }
+        return true;
+    });
+}
+
+// How a product is divided (what the comments of linear_kernel.cuh describe).
+struct LinearPlan {
+    bool pair;
+    int tile_tokens, token_tiles, split, whole, rest, blocks;
+};
+
+// Costs are in cycles per 128 values along K.
+LinearPlan plan_linear(int T, int N, int kblocks, int block, const int *clusters)
+{
+    const int most = block == 128 ? LinLayout<128>::kMaxTokens : LinLayout<32>::kMaxTokens;
+    const int64_t features = (N + int64_t{kLinM} - 1) / kLinM;
+    LinearPlan best{};
+    if (T <= most) {
+        best.tile_tokens = (T + 15) / 16 * 16;
+        best.token_tiles = 1;
+        double cost = 1e300;
+        for (int c = 1; c <= std::min(kLinMaxSplit, kblocks); ++c) {
+            const int64_t held = clusters[c], blocks = held * c;
+            if (held < 1) continue;
+            int64_t whole = features / blocks * blocks, rest = features - whole;
+            if (c == 1 || rest > held) {
+                whole = features;
+                rest = 0;
+            }
+            const double t = static_cast<double>((whole + blocks - 1) / blocks) * kblocks + (rest ? (kblocks + c - 1) / c + kLinJoinStages : 0);
+            if (t < cost) {
+                cost = t;
+                best.split = c;
+                best.whole = static_cast<int>(whole);
+                best.rest = static_cast<int>(rest);
+                best.blocks = static_cast<int>(whole ? std::min(blocks, (whole + c - 1) / c * c) : rest * c);
+            }
+        }
+        return best;
+    }
+    const int64_t pairs = clusters[2], feature_pairs = (features + 1) / 2, least = (T + int64_t{most} - 1) / most;
+    int64_t cost = INT64_MAX;
+    for (int64_t n = least; n <= least + pairs; ++n) {
+        const int tile = static_cast<int>((T + n - 1) / n + 15) / 16 * 16;
+        const int64_t tiles = feature_pairs * ((T + int64_t{tile} - 1) / tile), rounds = (tiles + pairs - 1) / pairs;
+        const int64_t t = rounds * std::max(200 * tile, 16400 + 64 * tile);
+        if (t < cost) {
+            cost = t;
+            best = LinearPlan{true, tile, static_cast<int>((T + int64_t{tile} - 1) / tile), 2, static_cast<int>(tiles), 0, static_cast<int>(2 * std::min(pairs, tiles))};
+        }
+        if (tile == 16) break;
+    }
+    return best;
 }
 
 // 8-bit rows as boxes of 128 bytes x `rows`, with the 128-byte swizzle.
@@ -83,11 +160,25 @@ dim3 rope_grid(int n_tokens, int64_t values)
     return dim3(n_tokens, static_cast<unsigned>((values + kRopeBlockValues - 1) / kRopeBlockValues));
 }
 
-template <int BLOCK, bool F32>
-int launch_linear(const CUtensorMap &tw, const CUtensorMap &tx, const LinearParams &p, int grid, int smem, cudaStream_t s)
+template <int BLOCK, bool F32, bool PAIR>
+int launch_linear(const CUtensorMap &tw, const CUtensorMap &tx, LinearParams p, int blocks, cudaStream_t s)
 {
-    ead_linear_kernel<BLOCK, F32><<<grid, kLinThreads, smem, s>>>(tw, tx, p);
-    return launched();
+    using L = LinLayout<BLOCK>;
+    const int stage = L::stage_bytes(p.tile_tokens, PAIR);
+    p.stages = std::min(kLinMaxStages, (kLinSmem - L::fixed_bytes()) / stage);
+    cudaLaunchAttribute attr[1];
+    const cudaLaunchConfig_t cfg = linear_config(blocks, p.split, L::fixed_bytes() + p.stages * stage, s, attr);
+    if (cudaLaunchKernelEx(&cfg, ead_linear_kernel<BLOCK, F32, PAIR>, tw, tx, p) != cudaSuccess) {
+        cudaGetLastError();
+        return EAD_ECUDA;
+    }
+    return EAD_OK;
+}
+
+template <int BLOCK, bool F32>
+int launch_linear(const CUtensorMap &tw, const CUtensorMap &tx, const LinearParams &p, const LinearPlan &plan, cudaStream_t s)
+{
+    return plan.pair ? launch_linear<BLOCK, F32, true>(tw, tx, p, plan.blocks, s) : launch_linear<BLOCK, F32, false>(tw, tx, p, plan.blocks, s);
 }
 
 }  // namespace
@@ -108,37 +199,32 @@ extern "C" int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, co
     p.w_scale = w->scale;
     p.bias = static_cast<const uint8_t *>(bias);
     p.out = static_cast<uint8_t *>(out);
-    p.workspace = static_cast<uint8_t *>(workspace);
     p.out_stride = out_stride;
     p.T = x->rows;
     p.N = w->rows;
     p.kblocks = (x->cols + kLinK - 1) / kLinK;
     p.x_scale_cols = (x->cols + x->block_cols - 1) / x->block_cols;
     p.w_scale_cols = p.kblocks;
-    p.token_tiles = (p.T + kLinMaxTokens - 1) / kLinMaxTokens;
-    p.tile_tokens = ((p.T + p.token_tiles - 1) / p.token_tiles + 15) / 16 * 16;
-    p.token_tiles = (p.T + p.tile_tokens - 1) / p.tile_tokens;
-    const int64_t tiles = static_cast<int64_t>((p.N + kLinM - 1) / kLinM) * p.token_tiles;
-    if (tiles > (1 << 30)) return EAD_ELIMIT;
+    // every tile has an index of 32 bits, whatever the plan
+    if ((p.N / kLinM + int64_t{1}) * (p.T / 16 + int64_t{1}) > (1 << 30)) return EAD_ELIMIT;
     DeviceInfo *d = nullptr;
     rc = use_device(device, &d);
     if (rc != EAD_OK) return rc;
-    p.tiles = static_cast<int>(tiles);
-    const int sms = std::min(d->sms, kLinMaxCtas);
-    p.whole = p.tiles / sms * sms;
-    const int rest = p.tiles - p.whole;
-    p.rest_ctas = std::min<int64_t>(sms, std::max<int64_t>(rest, static_cast<int64_t>(rest) * p.kblocks / kLinMinStretch));
-    const int stage = kLinM * kLinK + p.tile_tokens * kLinK + kLinScaleStage, room = kLinSmem - 1024 - 4 * kLinOutBytes;
-    p.stages = std::min(kLinMaxStages, room / stage);
+    const LinearPlan plan = plan_linear(p.T, p.N, p.kblocks, x->block_cols, g_clusters[device]);
+    if (!plan.blocks) return EAD_ECUDA;
+    p.tile_tokens = plan.tile_tokens;
+    p.token_tiles = plan.token_tiles;
+    p.whole = plan.whole;
+    p.rest = plan.rest;
+    p.split = plan.split;
     p.status = status;
     p.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     p.wait_hint = std::min(p.wait_ns, 20000u);
     CUtensorMap tw, tx;
-    if (!encode_codes(&tw, *w, kLinM) || !encode_codes(&tx, *x, p.tile_tokens)) return EAD_ECUDA;
-    const int grid = p.whole ? sms : p.rest_ctas, smem = 1024 + p.stages * stage + 4 * kLinOutBytes;
+    if (!encode_codes(&tw, *w, kLinM) || !encode_codes(&tx, *x, plan.pair ? p.tile_tokens / 2 : p.tile_tokens)) return EAD_ECUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return x->block_cols == 128 ? (f32 ? launch_linear<128, true>(tw, tx, p, grid, smem, s) : launch_linear<128, false>(tw, tx, p, grid, smem, s))
-                                : (f32 ? launch_linear<32, true>(tw, tx, p, grid, smem, s) : launch_linear<32, false>(tw, tx, p, grid, smem, s));
+    return x->block_cols == 128 ? (f32 ? launch_linear<128, true>(tw, tx, p, plan, s) : launch_linear<128, false>(tw, tx, p, plan, s))
+                                : (f32 ? launch_linear<32, true>(tw, tx, p, plan, s) : launch_linear<32, false>(tw, tx, p, plan, s));
 }
 
 extern "C" int ead_quantise(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, const ead_e4m3_matrix *out, int32_t device,

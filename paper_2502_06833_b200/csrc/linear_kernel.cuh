@@ -1,14 +1,16 @@
 // Product of 8-bit activations with 8-bit weights, both with power-of-two scales:
 //   out[t, n] = sum_k x[t, k] 2^(sx[t, k / block] - 127) w[n, k] 2^(sw[n / 128, k / 128] - 127) + bias[n]
 // The tensor core takes the scales itself: tcgen05.mma kind::mxf8f6f4 multiplies every 32 values along K by one power of two
-// per row of each operand, read from TMEM, at the rate of the plain 8-bit product; a coarser block repeats its byte.
+// per row of each operand, read from TMEM, at the rate of the plain 8-bit product.
 //
 // The weights are the M operand (128 features: exactly one row of scale blocks), the tokens the N operand, so one token costs an
-// MMA of 16 columns and not of 128 rows.  A tile is 128 features x up to 240 tokens; two accumulators of 240 columns leave TMEM 32
-// columns for two sets of scales, so the next tile's products run under this one's output.
+// MMA of 16 columns and not of 128 rows.  Two accumulators leave room in TMEM for the scales of two groups of 4 x 128 values of K:
+// the next tile's products run under this one's output, the next group's scales come in under this one's products.
 //
-// Whole rounds of tiles go to the SMs one each; what is left over is cut along K, every SM an equal stretch, and the
-// last block of a tile to finish adds the parts in the order of K: the result does not depend on who comes last.
+// Few tokens (PAIR = false): a tile is 128 features of one block.  Whole rounds of tiles go to the blocks one each; what is left over is
+// cut along K among the blocks of a cluster, which add their parts up in the order of K through distributed shared memory.
+// Many tokens (PAIR = true): two blocks share a tile of 256 features (cta_group::2), each holds its features' weights and half of the
+// tokens: per product a third less passes through L2, which bounds the other form at size.
 #pragma once
 #include "attn_common.cuh"
 
@@ -16,28 +18,35 @@ namespace ead {
 
 constexpr int kLinThreads = 256;                  // a loading warp, an MMA warp, two warps for scales, four for the output
 constexpr int kLinM = 128, kLinK = 128;           // features and values along K of a stage
-constexpr int kLinMaxTokens = 240;                // of a tile
 constexpr int kLinMaxStages = 12;
-constexpr int kLinScaleBytes = 512;               // scales of 128 rows x 4 blocks of 32
-constexpr int kLinScaleStage = 3 * kLinScaleBytes;   // weights, then up to 256 tokens
-constexpr int kLinScaleColumns = 12;              // the same in TMEM
+constexpr int kLinGroups = 3;                     // groups of scales in shared memory, each for 4 stages
+constexpr int kLinScaleBytes = 512;               // scales of 128 rows x 4 blocks along K
 constexpr int kLinOutBytes = 4096;                // 32 x 32 outputs of a warp
 constexpr int kLinSmem = 232448 - 2048;           // beside it: static shared memory and what the system takes
-constexpr int kLinMaxCtas = 160;
-constexpr size_t kLinCounterBytes = 4096;
-constexpr size_t kLinPartFloats = kLinM * kLinMaxTokens;
-static_assert(2 * kLinMaxTokens + 2 * kLinScaleColumns <= 512, "TMEM");
-static_assert(kLinMaxCtas * sizeof(uint32_t) <= kLinCounterBytes, "fewer tiles than blocks are cut");
+constexpr int kLinMaxSplit = 8;                   // blocks of a cluster
+
+// BLOCK: values of a token that share a scale.  With 128 the four bytes of a TMEM column serve four stages, with 32 one.
+template <int BLOCK>
+struct LinLayout {
+    static constexpr int kTokenSets = BLOCK == 128 ? 1 : 4;                          // sets of token scales in a group
+    static constexpr int kMaxTokens = BLOCK == 128 ? 240 : 208;                      // of a tile
+    static constexpr int kGroupBytes = kLinScaleBytes * (1 + 2 * kTokenSets);        // weights, then up to 256 tokens per set
+    static constexpr int kGroupColumns = 4 + 8 * kTokenSets;
+    static_assert(2 * kMaxTokens + 2 * kGroupColumns <= 512, "TMEM");
+    __host__ __device__ static constexpr int stage_bytes(int tile_tokens, bool pair) { return kLinM * kLinK + (pair ? tile_tokens / 2 : tile_tokens) * kLinK; }
+    __host__ __device__ static constexpr int fixed_bytes() { return 1024 + kLinGroups * kGroupBytes + 4 * kLinOutBytes; }
+};
 
 struct LinearParams {
     const uint8_t *x_scale, *w_scale, *bias;
-    uint8_t *out, *workspace;
+    uint8_t *out;
     int64_t out_stride;
     int32_t T, N, kblocks;                        // kblocks: of 128
     int32_t x_scale_cols, w_scale_cols;
-    int32_t tile_tokens, token_tiles, tiles;
-    int32_t whole;                                // tiles in whole rounds
-    int32_t rest_ctas;                            // blocks among which the others are cut
+    int32_t tile_tokens, token_tiles;
+    int32_t whole;                                // tiles that are served by one block (PAIR: by one pair) each
+    int32_t rest;                                 // tiles behind them, one cluster each
+    int32_t split;                                // blocks of a cluster (PAIR: 2)
     int32_t stages;
     uint32_t *status;
     uint32_t wait_ns, wait_hint;
@@ -47,80 +56,217 @@ struct LinearParams {
 struct LinSegment {
     int tile, k0, k1;
 };
+template <bool PAIR>
 struct LinWork {
-    int next, stride, whole;                      // whole tiles
-    int64_t u, u1;                                // then units (tile, 128 values of K) of the rest
-    __device__ __forceinline__ LinWork(const LinearParams &p) : next(blockIdx.x), stride(gridDim.x), whole(p.whole), u(0), u1(0)
-    {
-        if (static_cast<int>(blockIdx.x) < p.rest_ctas) {
-            u = first_unit(p, blockIdx.x);
-            u1 = first_unit(p, blockIdx.x + 1);
-        }
-    }
-    static __device__ __forceinline__ int64_t rest_units(const LinearParams &p) { return static_cast<int64_t>(p.tiles - p.whole) * p.kblocks; }
-    static __device__ __forceinline__ int64_t first_unit(const LinearParams &p, int cta) { return rest_units(p) * cta / p.rest_ctas; }
-    static __device__ __forceinline__ int cta_of(const LinearParams &p, int64_t unit)
-    {
-        return static_cast<int>(((unit + 1) * p.rest_ctas - 1) / rest_units(p));
-    }
+    int next;
+    __device__ __forceinline__ LinWork() : next(PAIR ? blockIdx.x / 2 : blockIdx.x) {}
     __device__ __forceinline__ bool get(const LinearParams &p, LinSegment &s)
     {
-        if (next < whole) {
+        if (next < 0) return false;
+        if (next < p.whole) {
             s = LinSegment{next, 0, p.kblocks};
-            next += stride;
+            next += PAIR ? gridDim.x / 2 : gridDim.x;
             return true;
         }
-        if (u >= u1) return false;
-        const int tile = static_cast<int>(u / p.kblocks), k0 = static_cast<int>(u - static_cast<int64_t>(tile) * p.kblocks);
-        const int n = static_cast<int>(min(u1 - u, static_cast<int64_t>(p.kblocks - k0)));
-        s = LinSegment{whole + tile, k0, k0 + n};
-        u += n;
+        next = -1;
+        if (PAIR) return false;
+        const int cluster = blockIdx.x / p.split, rank = blockIdx.x - cluster * p.split;
+        if (cluster >= p.rest) return false;
+        s = LinSegment{p.whole + cluster, static_cast<int>(static_cast<int64_t>(p.kblocks) * rank / p.split),
+                       static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split)};
         return true;
     }
 };
 
-// Shared-memory descriptor of an operand tile of 128-byte rows with the 128-byte swizzle (as for bf16: it counts bytes), and of a block of
-// scales: 32 rows of 16 bytes, no swizzle, groups of 8 rows 128 bytes apart.
+// Place in a ring of n barriers, and the parity of the phase that ends there next.  (Counted on: divisions by n in every stage were
+// a third of the time of the warp that issues the products.)
+struct LinRing {
+    uint32_t i = 0, phase = 0;
+    __device__ __forceinline__ void next(uint32_t n)
+    {
+        if (++i == n) {
+            i = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+// Shared-memory descriptor of a block of scales: 32 rows of 16 bytes, no swizzle, groups of 8 rows 128 bytes apart.  (An operand tile of
+// 128-byte rows with the 128-byte swizzle has the descriptor of a bf16 one, which counts bytes.)
 __device__ __forceinline__ uint64_t scale_smem_desc(uint32_t saddr)
 {
     const uint32_t lo = ((saddr >> 4) & 0x3FFFu) | (1u << 16);
     const uint32_t hi = (128u >> 4) | (1u << 14);
     return (static_cast<uint64_t>(hi) << 32) | lo;
 }
-// Scales of 128 rows from shared memory to 4 columns of TMEM (all four quadrants of lanes get them).
+// Scales of 128 rows from shared memory to 4 columns of TMEM (all four quadrants of lanes get them); of a pair, each block from its own
+// shared memory to its own TMEM.
+template <bool PAIR>
 __device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t saddr)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(scale_smem_desc(saddr)) : "memory");
+    if (PAIR)
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(scale_smem_desc(saddr)) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(scale_smem_desc(saddr)) : "memory");
 }
-// Instruction descriptor of kind::mxf8f6f4: e4m3 operands (both K-major), scales of type ue8m0, M = 128, N a multiple of 16; `k`: which of
-// the four scales of a row this instruction takes.
-__device__ __forceinline__ uint32_t umma_idesc_mxf8(uint32_t n, uint32_t k)
+// Instruction descriptor of kind::mxf8f6f4: e4m3 operands (both K-major), scales of type ue8m0, M = 128 (of a pair 256), N a multiple of 16;
+// ka, kb: which of the four scales of a row of A and B this instruction takes.
+template <bool PAIR>
+__device__ __forceinline__ uint32_t umma_idesc_mxf8(uint32_t n, uint32_t ka, uint32_t kb)
 {
-    return (k << 4) | ((n >> 3) << 17) | (1u << 23) | ((128u >> 7) << 27) | (k << 29);
+    return (kb << 4) | ((n >> 3) << 17) | (1u << 23) | ((PAIR ? 2u : 1u) << 27) | (ka << 29);
 }
+template <bool PAIR>
 __device__ __forceinline__ void umma_mxf8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scale, uint32_t b_scale,
                                           uint32_t accumulate)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
-        : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+            : "memory");
+}
+// Arrives on the barrier (of a pair: on the one at this place in both blocks) when everything issued so far by this thread has completed.
+template <bool PAIR>
+__device__ __forceinline__ void lin_commit(uint32_t bar)
+{
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                     "h"(static_cast<uint16_t>(3)) : "memory");
+    else
+        umma_commit(bar);
+}
+// The same on this block's barrier alone.
+template <bool PAIR>
+__device__ __forceinline__ void umma_commit_own(uint32_t bar)
+{
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else
+        umma_commit(bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void lin_tmem_alloc(uint32_t result)
+{
+    if (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(result) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        tmem_alloc(result, 512);
+        tmem_relinquish();
+    }
+}
+template <bool PAIR>
+__device__ __forceinline__ void lin_tmem_dealloc(uint32_t tmem)
+{
+    if (PAIR)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    else
+        tmem_dealloc(tmem, 512);
 }
 
-// The scale bytes of the four blocks of 32 in 128 values of one row; of blocks behind the last one 0 (their values are zeros).
-template <int BLOCK>
-__device__ __forceinline__ uint32_t row_scales(const uint8_t *scale, int cols, int kb)
+// A tiled load of one block of a pair, counted on the leading block's barrier (bar: its address in this block's own window; the bit that
+// tells the two blocks apart is cleared).
+__device__ __forceinline__ void pair_load_2d(uint32_t dst, const void *tmap, int32_t x, int32_t y, uint32_t bar)
 {
-    if (BLOCK == 128) return __ldg(scale + kb) * 0x01010101u;
-    if ((cols & 3) == 0) return __ldg(reinterpret_cast<const uint32_t *>(scale) + kb);
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(bar & 0xFEFFFFFFu)
+        : "memory");
+}
+// Counts bytes that nobody will bring.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+// ----------------------------------------------------------------- clusters
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Address in the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void cluster_mbar_arrive(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_ld_u32(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float cluster_ld(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// The scales of a row's blocks behind 128 values: of four stages one byte each (BLOCK = 128: kb = the first stage, n of them count), or
+// of the four blocks of 32 of stage kb; what lies behind the row's end is 0 (its values are zeros).
+template <int BLOCK>
+__device__ __forceinline__ uint32_t row_scales(const uint8_t *scale, int cols, int kb, int n)
+{
     uint32_t v = 0;
+    if (BLOCK == 128) {
+        if (((cols | kb) & 3) == 0 && (reinterpret_cast<uintptr_t>(scale) & 3) == 0) return __ldg(reinterpret_cast<const uint32_t *>(scale + kb));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) v |= static_cast<uint32_t>(__ldg(scale + kb + i)) << (8 * i);
+        return v;
+    }
+    if ((cols & 3) == 0) return __ldg(reinterpret_cast<const uint32_t *>(scale) + kb);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (4 * kb + i < cols) v |= static_cast<uint32_t>(__ldg(scale + 4 * kb + i)) << (8 * i);
     return v;
 }
+
+// A group of scales on its way from global to shared memory: of 4 x 32 tokens for up to four stages, and of the weights.
+template <int BLOCK, bool PAIR>
+struct LinScales {
+    static constexpr int kSets = LinLayout<BLOCK>::kTokenSets;
+    uint32_t v[kSets][4], w;
+    // c: which 128 tokens of the tile
+    __device__ __forceinline__ void load(const LinearParams &p, const LinSegment &g, int kb, int c, int lane, int rank)
+    {
+        const int feature_tile = g.tile / p.token_tiles * (PAIR ? 2 : 1) + rank, token_tile = g.tile % p.token_tiles;
+        const int token0 = token_tile * p.tile_tokens + c * 128 + lane, end = min(p.T, (token_tile + 1) * p.tile_tokens), n = min(4, g.k1 - kb);
+        w = 0;
+        if (feature_tile * kLinM < p.N)
+            w = row_scales<128>(p.w_scale + static_cast<int64_t>(feature_tile) * p.w_scale_cols, p.w_scale_cols, kb, n);
+#pragma unroll
+        for (int i = 0; i < kSets; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = token0 + 32 * j;
+                v[i][j] = t < end && i < n ? row_scales<BLOCK>(p.x_scale + static_cast<int64_t>(t) * p.x_scale_cols, p.x_scale_cols, kb + i, n) : 0;
+            }
+    }
+    __device__ __forceinline__ void store(uint32_t group, int c, int chunks, int lane) const
+    {
+        const uint32_t to = group + 16 * lane;
+        if (c < chunks)
+#pragma unroll
+            for (int i = 0; i < kSets; ++i) st_shared_16(to + (1 + 2 * i + c) * kLinScaleBytes, v[i][0], v[i][1], v[i][2], v[i][3]);
+        if (c == 1) st_shared_16(to, w, w, w, w);
+    }
+};
 
 // One warp's 32 features x up to 32 tokens, transposed through its own shared memory: rows of 32 features leave in 16-byte stores.
 template <bool F32>
@@ -159,30 +305,38 @@ __device__ __forceinline__ void store_outputs(const LinearParams &p, uint8_t *bu
     }
 }
 
-template <int BLOCK, bool F32>
+template <int BLOCK, bool F32, bool PAIR>
 __global__ void __launch_bounds__(kLinThreads, 1)
-    ead_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, LinearParams p)
+    ead_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinearParams p)
 {
+    using L = LinLayout<BLOCK>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t s_bars[3 * kLinMaxStages + 5];
+    __shared__ alignas(8) uint64_t s_bars[2 * kLinMaxStages + 2 * kLinGroups + 5];
     __shared__ uint32_t s_tmem, s_gave_up;
-    __shared__ int s_last, s_loads;
+    __shared__ int s_loads;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    const int S = p.stages, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t x_bytes = p.tile_tokens * kLinK, stage_bytes = kLinM * kLinK + x_bytes;
-    const uint32_t scales = base + S * stage_bytes, out_smem = scales + S * kLinScaleStage;
-    const uint32_t bar_tile = smem_u32(s_bars), bar_scale = bar_tile + 8 * kLinMaxStages, bar_empty = bar_scale + 8 * kLinMaxStages;
-    const uint32_t bar_acc_full = bar_empty + 8 * kLinMaxStages, bar_acc_empty = bar_acc_full + 16, bar_last = bar_acc_empty + 16;
+    const uint32_t S = p.stages;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(blockIdx.x % p.split);
+    const int pair_rank = PAIR ? rank : 0;
+    const uint32_t stage_bytes = L::stage_bytes(p.tile_tokens, PAIR);
+    const uint32_t groups = base + S * stage_bytes, out_smem = groups + kLinGroups * L::kGroupBytes;
+    // tile and empty per stage, scales and empty per group (of a pair, what comes in is counted in the leading block for both)
+    const uint32_t bar_tile = smem_u32(s_bars), bar_empty = bar_tile + 8 * kLinMaxStages;
+    const uint32_t bar_scale = bar_empty + 8 * kLinMaxStages, bar_scale_empty = bar_scale + 8 * kLinGroups;
+    const uint32_t bar_acc_full = bar_scale_empty + 8 * kLinGroups, bar_acc_empty = bar_acc_full + 16, bar_last = bar_acc_empty + 16;
     const int chunks = (p.tile_tokens + 127) >> 7;
     if (tid == 0) {
-        for (int i = 0; i < S; ++i) {
+        for (uint32_t i = 0; i < S; ++i) {
             mbar_init(bar_tile + 8 * i, 1);
-            mbar_init(bar_scale + 8 * i, 2);
             mbar_init(bar_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kLinGroups; ++i) {
+            mbar_init(bar_scale + 8 * i, PAIR ? 4 : 2);
+            mbar_init(bar_scale_empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_acc_full + 8 * i, 1);
-            mbar_init(bar_acc_empty + 8 * i, 4);
+            mbar_init(bar_acc_empty + 8 * i, PAIR ? 8 : 4);
         }
         mbar_init(bar_last, 1);
         s_gave_up = 0;
@@ -193,122 +347,153 @@ __global__ void __launch_bounds__(kLinThreads, 1)
         tma_prefetch_desc(&tmW);
         tma_prefetch_desc(&tmX);
     }
-    if (warp == 1) {
-        tmem_alloc(smem_u32(&s_tmem), 512);
-        tmem_relinquish();
-    }
+    if (warp == 1) lin_tmem_alloc<PAIR>(smem_u32(&s_tmem));
     tc_fence_before_sync();
     __syncthreads();
+    if (PAIR) {                                   // the other block's barriers are there
+        cluster_arrive();
+        cluster_wait();
+    }
     tc_fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&s_tmem);
-    // A wait that runs out makes every other role stop at its next one that does.
+    // A wait that runs out makes every other role of the block stop at its next one that does.
     auto wait = [&](uint32_t bar, uint32_t parity) { return wait_phase<true>(bar, parity, p, &s_gave_up); };
     auto warp_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-    LinWork work(p);
+    LinWork<PAIR> work;
     LinSegment g;
-    uint32_t it = 0;                              // stages so far
+    LinRing stage, group;
 
     if (warp == 0) {
         // ------------------------------------------------------------- operand tiles
-        bool go = true;
-        while (go && work.get(p, g)) {
-            const int feature0 = (g.tile / p.token_tiles) * kLinM, token0 = (g.tile % p.token_tiles) * p.tile_tokens;
-            for (int kb = g.k0; kb < g.k1; ++kb, ++it) {
-                const int st = it % S;
-                if (!(go = warp_wait(bar_empty + 8 * st, ((it / S) & 1) ^ 1))) break;
-                if (elect_one()) {
-                    const uint32_t a = base + st * stage_bytes;
-                    mbar_arrive_expect_tx(bar_tile + 8 * st, stage_bytes);
-                    tma_load_2d(a, &tmW, kb * kLinK, feature0, bar_tile + 8 * st);
-                    tma_load_2d(a + kLinM * kLinK, &tmX, kb * kLinK, token0, bar_tile + 8 * st);
+        if (elect_one()) {
+            const int x_rows = PAIR ? p.tile_tokens / 2 : p.tile_tokens;
+            int loads = 0;
+            bool go = true;
+            while (go && work.get(p, g)) {
+                const int feature0 = (g.tile / p.token_tiles * (PAIR ? 2 : 1) + pair_rank) * kLinM;
+                const int token0 = (g.tile % p.token_tiles) * p.tile_tokens + pair_rank * x_rows;
+                for (int kb = g.k0; kb < g.k1; ++kb) {
+                    if (!(go = wait(bar_empty + 8 * stage.i, stage.phase ^ 1))) break;
+                    const uint32_t a = base + stage.i * stage_bytes, bar = bar_tile + 8 * stage.i;
+                    if (PAIR) {
+                        if (pair_rank == 0) mbar_arrive_expect_tx(bar, 2 * stage_bytes);
+                        pair_load_2d(a, &tmW, kb * kLinK, feature0, bar);
+                        pair_load_2d(a + kLinM * kLinK, &tmX, kb * kLinK, token0, bar);
+                    } else {
+                        mbar_arrive_expect_tx(bar, stage_bytes);
+                        tma_load_2d(a, &tmW, kb * kLinK, feature0, bar);
+                        tma_load_2d(a + kLinM * kLinK, &tmX, kb * kLinK, token0, bar);
+                    }
+                    stage.next(S);
+                    ++loads;
                 }
-                __syncwarp();
             }
+            s_loads = loads;
         }
-        if (lane == 0) s_loads = it;
     } else if (warp == 1) {
-        // ------------------------------------------------------------- products
-        bool go = true;
-        for (uint32_t n = 0; go && work.get(p, g); ++n) {
-            const uint32_t acc = tmem + (n & 1) * kLinMaxTokens;
-            if (!(go = warp_wait(bar_acc_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1))) break;
-            for (int kb = g.k0; kb < g.k1; ++kb, ++it) {
-                const int st = it % S;
-                // the set of scales was used two stages ago
-                if (it >= 2 && !(go = warp_wait(bar_empty + 8 * ((it - 2) % S), ((it - 2) / S) & 1))) break;
-                if (!(go = warp_wait(bar_tile + 8 * st, (it / S) & 1) && warp_wait(bar_scale + 8 * st, (it / S) & 1))) break;
-                tc_fence_after_sync();
-                if (elect_one()) {
-                    const uint32_t a = base + st * stage_bytes, sc = scales + st * kLinScaleStage;
-                    const uint32_t ta = tmem + 2 * kLinMaxTokens + (it & 1) * kLinScaleColumns, tb = ta + 4;
-                    copy_scales(ta, sc);
-                    for (int c = 0; c < chunks; ++c) copy_scales(tb + 4 * c, sc + (1 + c) * kLinScaleBytes);
+        // ------------------------------------------------------------- products (of a pair: by the leading block)
+        if (pair_rank == 0 && elect_one()) {
+            const uint32_t a0 = static_cast<uint32_t>(umma_smem_desc(base)), a_step = stage_bytes >> 4;
+            const uint64_t desc_hi = umma_smem_desc(0) & 0xffffffff00000000ull;
+            const uint32_t idesc = umma_idesc_mxf8<PAIR>(p.tile_tokens, 0, 0);
+            uint32_t n_groups = 0;
+            bool go = true;
+            for (uint32_t n = 0; go && work.get(p, g); ++n) {
+                const uint32_t acc = tmem + (n & 1) * L::kMaxTokens;
+                if (!(go = wait(bar_acc_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1))) break;
+                int in_group = 0;
+                for (int kb = g.k0; kb < g.k1; ++kb) {
+                    const uint32_t ta = tmem + 2 * L::kMaxTokens + (n_groups & 1) * L::kGroupColumns, tb = ta + 4;
+                    if (in_group == 0) {
+                        // the columns were used two groups ago: one place further in the ring of three
+                        if (n_groups >= 2 && !(go = wait(bar_scale_empty + 8 * (group.i == 2 ? 0 : group.i + 1), group.i == 2 ? group.phase : group.phase ^ 1))) break;
+                        if (!(go = wait(bar_scale + 8 * group.i, group.phase))) break;
+                    }
+                    if (!(go = wait(bar_tile + 8 * stage.i, stage.phase))) break;
+                    const bool group_ends = in_group == 3 || kb + 1 == g.k1;
+                    tc_fence_after_sync();
+                    const uint32_t a = a0 + stage.i * a_step, b = a + (kLinM * kLinK >> 4);
+                    if (in_group == 0) {
+                        const uint32_t sc = groups + group.i * L::kGroupBytes;
+                        copy_scales<PAIR>(ta, sc);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        umma_mxf8(acc, umma_smem_desc(a + 32 * k), umma_smem_desc(a + kLinM * kLinK + 32 * k), umma_idesc_mxf8(p.tile_tokens, k), ta, tb,
-                                  kb > g.k0 || k > 0);
-                    umma_commit(bar_empty + 8 * st);
-                    if (kb + 1 == g.k1) umma_commit(bar_acc_full + 8 * (n & 1));
+                        for (int i = 0; i < L::kTokenSets; ++i) {
+                            copy_scales<PAIR>(tb + 8 * i, sc + (1 + 2 * i) * kLinScaleBytes);
+                            if (chunks > 1) copy_scales<PAIR>(tb + 8 * i + 4, sc + (2 + 2 * i) * kLinScaleBytes);
+                        }
+                    }
+                    const uint32_t b_scale = BLOCK == 128 ? tb : tb + 8 * in_group, id = idesc + (in_group << 29) + (BLOCK == 128 ? in_group << 4 : 0);
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k)
+                        umma_mxf8<PAIR>(acc, desc_hi | (a + 2 * k), desc_hi | (b + 2 * k), BLOCK == 128 ? id : id + (k << 4), ta, b_scale, kb > g.k0 || k > 0);
+                    lin_commit<PAIR>(bar_empty + 8 * stage.i);
+                    if (group_ends) lin_commit<PAIR>(bar_scale_empty + 8 * group.i);
+                    if (kb + 1 == g.k1) lin_commit<PAIR>(bar_acc_full + 8 * (n & 1));
+                    stage.next(S);
+                    ++in_group;
+                    if (group_ends) {
+                        in_group = 0;
+                        group.next(kLinGroups);
+                        ++n_groups;
+                    }
                 }
-                __syncwarp();
             }
         }
     } else if (warp < 4) {
         // ------------------------------------------------------------- scales: 128 tokens a warp, the second warp the weights' too
         const int c = warp - 2;
-        bool go = true;
-        while (go && work.get(p, g)) {
-            const int feature_tile = g.tile / p.token_tiles, token0 = (g.tile % p.token_tiles) * p.tile_tokens + c * 128 + lane;
-            const int end = min(p.T, (g.tile % p.token_tiles + 1) * p.tile_tokens);
-            for (int kb0 = g.k0; go && kb0 < g.k1; kb0 += 4) {
-                uint32_t v[4][4], w[4];           // four stages' loads before the first wait
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = c == 1 && kb0 + i < g.k1 ? __ldg(p.w_scale + static_cast<int64_t>(feature_tile) * p.w_scale_cols + kb0 + i) * 0x01010101u : 0;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int t = token0 + 32 * j;
-                        v[i][j] = t < end && kb0 + i < g.k1 ? row_scales<BLOCK>(p.x_scale + static_cast<int64_t>(t) * p.x_scale_cols, p.x_scale_cols, kb0 + i) : 0;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (kb0 + i >= g.k1) break;
-                    const int st = it % S;
-                    if (!(go = warp_wait(bar_empty + 8 * st, ((it / S) & 1) ^ 1))) break;
-                    const uint32_t to = scales + st * kLinScaleStage + 16 * lane;
-                    if (c < chunks) st_shared_16(to + (1 + c) * kLinScaleBytes, v[i][0], v[i][1], v[i][2], v[i][3]);
-                    if (c == 1) st_shared_16(to, w[i], w[i], w[i], w[i]);
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar_scale + 8 * st);
-                    ++it;
-                }
+        const uint32_t leader_scale = PAIR ? cluster_addr(bar_scale, 0) : 0;
+        LinScales<BLOCK, PAIR> now, later;
+        bool more = work.get(p, g);
+        int kb = g.k0, later_loads = 0;
+        if (more) now.load(p, g, kb, c, lane, pair_rank);
+        while (more) {                            // the next group's loads are in flight while this one waits for its place
+            kb += 4;
+            if (kb >= g.k1) {
+                more = work.get(p, g);
+                kb = g.k0;
             }
+            const bool first = later_loads == 0;  // (the first group's place is free: it goes there before the second one's loads)
+            if (!first && more) later.load(p, g, kb, c, lane, pair_rank);
+            if (!warp_wait(bar_scale_empty + 8 * group.i, group.phase ^ 1)) break;
+            now.store(groups + group.i * L::kGroupBytes, c, chunks, lane);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR)
+                    cluster_mbar_arrive(leader_scale + 8 * group.i);
+                else
+                    mbar_arrive(bar_scale + 8 * group.i);
+            }
+            group.next(kLinGroups);
+            if (first && more) later.load(p, g, kb, c, lane, pair_rank);
+            later_loads = 1;
+            now = later;
         }
     } else {
         // ------------------------------------------------------------- output
         const int quadrant = warp - 4, row = quadrant * 32 + lane;
         uint8_t *const buf = smem_raw + (out_smem - raw) + quadrant * kLinOutBytes;
-        float *const parts = reinterpret_cast<float *>(p.workspace + kLinCounterBytes);
+        const uint32_t leader_acc_empty = PAIR ? cluster_addr(bar_acc_empty, 0) : 0;
+        bool joins = false;
+        int feature0 = 0, token0 = 0, tokens = 0;
+        float bias = 0.f;
         for (uint32_t n = 0; work.get(p, g); ++n) {
-            const int feature0 = (g.tile / p.token_tiles) * kLinM + quadrant * 32, token0 = (g.tile % p.token_tiles) * p.tile_tokens;
-            const int tokens = min(p.tile_tokens, p.T - token0);
-            const bool part = g.k1 - g.k0 < p.kblocks;
-            if (!named_all(1, 128, warp_wait(bar_acc_full + 8 * (n & 1), (n >> 1) & 1))) break;
+            feature0 = (g.tile / p.token_tiles * (PAIR ? 2 : 1) + pair_rank) * kLinM + quadrant * 32;
+            token0 = (g.tile % p.token_tiles) * p.tile_tokens;
+            tokens = min(p.tile_tokens, p.T - token0);
+            joins = !PAIR && p.split > 1 && g.tile >= p.whole;
+            bias = p.bias && feature0 + lane < p.N ? __uint_as_float(static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(p.bias) + feature0 + lane)) << 16) : 0.f;
+            if (!warp_wait(bar_acc_full + 8 * (n & 1), (n >> 1) & 1)) break;
             tc_fence_after_sync();
-            const uint32_t acc = tmem + (n & 1) * kLinMaxTokens + (static_cast<uint32_t>(quadrant) << 21);
-            const float bias = p.bias && feature0 + lane < p.N ? __uint_as_float(static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(p.bias) + feature0 + lane)) << 16) : 0.f;
-            // a block has at most two parts: of the tile that began in an earlier block (or with its stretch), and of the next one
-            const int64_t tile_unit = static_cast<int64_t>(g.tile - p.whole) * p.kblocks;
-            float *const mine = parts + (2 * blockIdx.x + (LinWork::first_unit(p, blockIdx.x) < tile_unit)) * kLinPartFloats + row;
+            const uint32_t acc = tmem + (n & 1) * L::kMaxTokens + (static_cast<uint32_t>(quadrant) << 21);
             for (int c = 0; c < tokens; c += 32) {
                 float v[32];
                 tmem_ld_32cols(acc + c, v);
-                if (part) {
+                if (joins) {                      // the last stretch of the block: the stages' place is free for it
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
-                        if (c + j < tokens) __stcg(mine + (c + j) * kLinM, v[j]);
+                        if (c + j < tokens) asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + 4 * ((c + j) * kLinM + row)), "f"(v[j]) : "memory");
                 } else {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] += bias;
@@ -317,48 +502,71 @@ __global__ void __launch_bounds__(kLinThreads, 1)
             }
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar_acc_empty + 8 * (n & 1));
-            if (!part) continue;
-            fence_gpu();
-            named_sync(1, 128);
-            const int first = LinWork::cta_of(p, tile_unit), last = LinWork::cta_of(p, tile_unit + p.kblocks - 1);
-            uint32_t *const counter = reinterpret_cast<uint32_t *>(p.workspace) + (g.tile - p.whole);
-            if (tid == 128) s_last = atomicAdd(counter, 1u) == static_cast<uint32_t>(last - first);
-            named_sync(1, 128);
-            if (s_last) {
-                fence_gpu();
-                for (int c = 0; c < tokens; c += 32) {
+            if (lane == 0) {
+                if (PAIR)
+                    cluster_mbar_arrive(leader_acc_empty + 8 * (n & 1));
+                else
+                    mbar_arrive(bar_acc_empty + 8 * (n & 1));
+            }
+        }
+        if (!PAIR && p.split > 1 && p.rest) {
+            __syncwarp();
+            cluster_arrive();                     // (the other warps: below)
+            cluster_wait();
+            if (joins) {                          // every block adds up and stores its share of the tokens
+                const int c0 = tokens * rank / p.split, c1 = tokens * (rank + 1) / p.split;
+                for (int c = c0; c < c1; c += 32) {
                     float v[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                    for (int i = first; i <= last; ++i) {
-                        const float *const from = parts + (2 * i + (LinWork::first_unit(p, i) < tile_unit)) * kLinPartFloats + row;
+                    for (int r = 0; r < p.split; ++r) {
+                        const uint32_t from = cluster_addr(base, r) + 4 * (c * kLinM + row);
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            if (c + j < tokens) v[j] += __ldcg(from + (c + j) * kLinM);
+                            if (c + j < c1) v[j] += cluster_ld(from + 4 * j * kLinM);
                     }
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] += bias;
-                    store_outputs<F32>(p, buf, v, lane, feature0, token0 + c, tokens - c);
+                    store_outputs<F32>(p, buf, v, lane, feature0, token0 + c, c1 - c);
                 }
-                if (tid == 128) *counter = 0;     // ready for the next call
             }
-            named_sync(1, 128);                   // s_last may be written again
         }
+    }
+    __syncwarp();
+    if (!PAIR && p.split > 1 && p.rest && warp < 4) {
+        cluster_arrive();
+        cluster_wait();
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (s_gave_up) {                              // nobody sets it any more: wait for loads and products under way
-        if (warp == 0)
-            for (int i = max(0, s_loads - S); i < s_loads; ++i) wait_own(bar_tile + 8 * (i % S), (i / S) & 1);
-        if (warp == 1) {
-            if (elect_one()) umma_commit(bar_last);
+    if (PAIR) {                                   // (of a pair, both end in this way if one does)
+        cluster_arrive();
+        cluster_wait();
+    }
+    const bool gave_up = s_gave_up || (PAIR && cluster_ld_u32(cluster_addr(smem_u32(&s_gave_up), pair_rank ^ 1)));
+    if (gave_up) {                                // nobody sets it any more: wait for loads and products under way
+        if (warp == 0 && lane == 0 && pair_rank == 0) {
+            const int n = static_cast<int>(S), other = PAIR ? static_cast<int>(cluster_ld_u32(cluster_addr(smem_u32(&s_loads), 1))) : s_loads;
+            for (int i = min(s_loads, other); i < max(s_loads, other); ++i) {      // stages that only one block of the pair has asked for
+                if (i < s_loads)
+                    mbar_complete_tx(bar_tile + 8 * (i % n), stage_bytes);
+                else
+                    mbar_arrive_expect_tx(bar_tile + 8 * (i % n), stage_bytes);
+            }
+            for (int i = max(0, max(s_loads, other) - n); i < max(s_loads, other); ++i) wait_own(bar_tile + 8 * (i % n), (i / n) & 1);
+        }
+        if (warp == 1 && pair_rank == 0) {
+            if (elect_one()) umma_commit_own<PAIR>(bar_last);      // (the lane that issued the products)
             __syncwarp();
             wait_own(bar_last, 0);
         }
         __syncthreads();
     }
-    if (warp == 1) tmem_dealloc(tmem, 512);
+    if (p.split > 1) {                            // nobody leaves while the others may read or signal its shared memory
+        cluster_arrive_relaxed();
+        cluster_wait();
+    }
+    if (warp == 1) lin_tmem_dealloc<PAIR>(tmem);
 }
 
 }  // namespace ead
