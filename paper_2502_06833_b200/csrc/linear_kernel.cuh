@@ -16,7 +16,7 @@
 
 namespace ead {
 
-constexpr int kLinThreads = 256;                  // a loading warp, an MMA warp, two warps for scales, four for the output
+constexpr int kLinThreads = 320;                  // a loading warp, an MMA warp, four warps for scales, four for the output
 constexpr int kLinM = 128, kLinK = 128;           // features and values along K of a stage
 constexpr int kLinMaxStages = 12;
 constexpr int kLinGroups = 3;                     // groups of scales in shared memory, each for 4 stages
@@ -52,6 +52,46 @@ struct LinearParams {
     uint32_t wait_ns, wait_hint;
 };
 
+// ----------------------------------------------------------------- clusters
+__device__ __forceinline__ int cluster_id()
+{
+    int i;
+    asm("mov.u32 %0, %%clusterid.x;" : "=r"(i));
+    return i;
+}
+__device__ __forceinline__ int cluster_rank()
+{
+    int i;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(i));
+    return i;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Address in the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void cluster_mbar_arrive(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_ld_u32(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float cluster_ld(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 // The stretches of work of one block, in order.
 struct LinSegment {
     int tile, k0, k1;
@@ -59,6 +99,9 @@ struct LinSegment {
 template <bool PAIR>
 struct LinWork {
     int next;
+    // Row block of the weights and tile of tokens.  (With few tokens there is one tile of them.)
+    static __device__ __forceinline__ int feature_tile(const LinearParams &p, const LinSegment &s, int rank) { return PAIR ? s.tile / p.token_tiles * 2 + rank : s.tile; }
+    static __device__ __forceinline__ int token0(const LinearParams &p, const LinSegment &s) { return PAIR ? s.tile % p.token_tiles * p.tile_tokens : 0; }
     __device__ __forceinline__ LinWork() : next(PAIR ? blockIdx.x / 2 : blockIdx.x) {}
     __device__ __forceinline__ bool get(const LinearParams &p, LinSegment &s)
     {
@@ -70,10 +113,9 @@ struct LinWork {
         }
         next = -1;
         if (PAIR) return false;
-        const int cluster = blockIdx.x / p.split, rank = blockIdx.x - cluster * p.split;
+        const int cluster = cluster_id(), rank = cluster_rank();
         if (cluster >= p.rest) return false;
-        s = LinSegment{p.whole + cluster, static_cast<int>(static_cast<int64_t>(p.kblocks) * rank / p.split),
-                       static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split)};
+        s = LinSegment{p.whole + cluster, p.kblocks * rank / p.split, p.kblocks * (rank + 1) / p.split};     // (at most 2^23 x 8)
         return true;
     }
 };
@@ -189,34 +231,6 @@ __device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// ----------------------------------------------------------------- clusters
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// Address in the shared memory of block `rank` of the cluster.
-__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ void cluster_mbar_arrive(uint32_t cluster_bar)
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ uint32_t cluster_ld_u32(uint32_t addr)
-{
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float cluster_ld(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
 // The scales of a row's blocks behind 128 values: of four stages one byte each (BLOCK = 128: kb = the first stage, n of them count), or
 // of the four blocks of 32 of stage kb; what lies behind the row's end is 0 (its values are zeros).
 template <int BLOCK>
@@ -245,8 +259,8 @@ struct LinScales {
     // c: which 128 tokens of the tile
     __device__ __forceinline__ void load(const LinearParams &p, const LinSegment &g, int kb, int c, int lane, int rank)
     {
-        const int feature_tile = g.tile / p.token_tiles * (PAIR ? 2 : 1) + rank, token_tile = g.tile % p.token_tiles;
-        const int token0 = token_tile * p.tile_tokens + c * 128 + lane, end = min(p.T, (token_tile + 1) * p.tile_tokens), n = min(4, g.k1 - kb);
+        const int feature_tile = LinWork<PAIR>::feature_tile(p, g, rank), first = LinWork<PAIR>::token0(p, g);
+        const int token0 = first + c * 128 + lane, end = min(p.T, first + p.tile_tokens), n = min(4, g.k1 - kb);
         w = 0;
         if (feature_tile * kLinM < p.N)
             w = row_scales<128>(p.w_scale + static_cast<int64_t>(feature_tile) * p.w_scale_cols, p.w_scale_cols, kb, n);
@@ -305,6 +319,32 @@ __device__ __forceinline__ void store_outputs(const LinearParams &p, uint8_t *bu
     }
 }
 
+// Sums of the cluster's parts of one feature and up to 32 tokens, in the order of the blocks; `at`: the first one's place in each block's shared
+// memory.  32 loads are on their way at a time.
+template <int R>
+__device__ __forceinline__ void add_parts(float (&v)[32], uint32_t at, int split, int tokens)
+{
+    constexpr int J = 32 / R;
+    uint32_t from[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) from[r] = cluster_addr(at, min(r, split - 1));
+#pragma unroll
+    for (int j0 = 0; j0 < 32; j0 += J) {
+        if (j0 >= tokens) break;
+        float part[R][J];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < J; ++j) part[r][j] = r < split && j0 + j < tokens ? cluster_ld(from[r] + 4 * (j0 + j) * kLinM) : 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            v[j0 + j] = part[0][j];
+#pragma unroll
+            for (int r = 1; r < R; ++r) v[j0 + j] += part[r][j];
+        }
+    }
+}
+
 template <int BLOCK, bool F32, bool PAIR>
 __global__ void __launch_bounds__(kLinThreads, 1)
     ead_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinearParams p)
@@ -316,7 +356,7 @@ __global__ void __launch_bounds__(kLinThreads, 1)
     __shared__ int s_loads;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const uint32_t S = p.stages;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(blockIdx.x % p.split);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
     const int pair_rank = PAIR ? rank : 0;
     const uint32_t stage_bytes = L::stage_bytes(p.tile_tokens, PAIR);
     const uint32_t groups = base + S * stage_bytes, out_smem = groups + kLinGroups * L::kGroupBytes;
@@ -370,8 +410,7 @@ __global__ void __launch_bounds__(kLinThreads, 1)
             int loads = 0;
             bool go = true;
             while (go && work.get(p, g)) {
-                const int feature0 = (g.tile / p.token_tiles * (PAIR ? 2 : 1) + pair_rank) * kLinM;
-                const int token0 = (g.tile % p.token_tiles) * p.tile_tokens + pair_rank * x_rows;
+                const int feature0 = LinWork<PAIR>::feature_tile(p, g, pair_rank) * kLinM, token0 = LinWork<PAIR>::token0(p, g) + pair_rank * x_rows;
                 for (int kb = g.k0; kb < g.k1; ++kb) {
                     if (!(go = wait(bar_empty + 8 * stage.i, stage.phase ^ 1))) break;
                     const uint32_t a = base + stage.i * stage_bytes, bar = bar_tile + 8 * stage.i;
@@ -400,87 +439,76 @@ __global__ void __launch_bounds__(kLinThreads, 1)
             bool go = true;
             for (uint32_t n = 0; go && work.get(p, g); ++n) {
                 const uint32_t acc = tmem + (n & 1) * L::kMaxTokens;
-                if (!(go = wait(bar_acc_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1))) break;
-                int in_group = 0;
-                for (int kb = g.k0; kb < g.k1; ++kb) {
+                go = wait(bar_acc_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1);
+                for (int kb = g.k0; go && kb < g.k1; kb += 4) {
                     const uint32_t ta = tmem + 2 * L::kMaxTokens + (n_groups & 1) * L::kGroupColumns, tb = ta + 4;
-                    if (in_group == 0) {
-                        // the columns were used two groups ago: one place further in the ring of three
-                        if (n_groups >= 2 && !(go = wait(bar_scale_empty + 8 * (group.i == 2 ? 0 : group.i + 1), group.i == 2 ? group.phase : group.phase ^ 1))) break;
-                        if (!(go = wait(bar_scale + 8 * group.i, group.phase))) break;
-                    }
-                    if (!(go = wait(bar_tile + 8 * stage.i, stage.phase))) break;
-                    const bool group_ends = in_group == 3 || kb + 1 == g.k1;
+                    // the columns were used two groups ago: one place further in the ring of three
+                    if (n_groups >= 2) go = wait(bar_scale_empty + 8 * (group.i == 2 ? 0 : group.i + 1), group.i == 2 ? group.phase : group.phase ^ 1);
+                    go = go && wait(bar_scale + 8 * group.i, group.phase);
+                    if (!go) break;
                     tc_fence_after_sync();
-                    const uint32_t a = a0 + stage.i * a_step, b = a + (kLinM * kLinK >> 4);
-                    if (in_group == 0) {
-                        const uint32_t sc = groups + group.i * L::kGroupBytes;
-                        copy_scales<PAIR>(ta, sc);
+                    const uint32_t sc = groups + group.i * L::kGroupBytes;
+                    copy_scales<PAIR>(ta, sc);
 #pragma unroll
-                        for (int i = 0; i < L::kTokenSets; ++i) {
-                            copy_scales<PAIR>(tb + 8 * i, sc + (1 + 2 * i) * kLinScaleBytes);
-                            if (chunks > 1) copy_scales<PAIR>(tb + 8 * i + 4, sc + (2 + 2 * i) * kLinScaleBytes);
-                        }
+                    for (int i = 0; i < L::kTokenSets; ++i) {
+                        copy_scales<PAIR>(tb + 8 * i, sc + (1 + 2 * i) * kLinScaleBytes);
+                        if (chunks > 1) copy_scales<PAIR>(tb + 8 * i + 4, sc + (2 + 2 * i) * kLinScaleBytes);
                     }
-                    const uint32_t b_scale = BLOCK == 128 ? tb : tb + 8 * in_group, id = idesc + (in_group << 29) + (BLOCK == 128 ? in_group << 4 : 0);
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k)
-                        umma_mxf8<PAIR>(acc, desc_hi | (a + 2 * k), desc_hi | (b + 2 * k), BLOCK == 128 ? id : id + (k << 4), ta, b_scale, kb > g.k0 || k > 0);
-                    lin_commit<PAIR>(bar_empty + 8 * stage.i);
-                    if (group_ends) lin_commit<PAIR>(bar_scale_empty + 8 * group.i);
-                    if (kb + 1 == g.k1) lin_commit<PAIR>(bar_acc_full + 8 * (n & 1));
-                    stage.next(S);
-                    ++in_group;
-                    if (group_ends) {
-                        in_group = 0;
-                        group.next(kLinGroups);
-                        ++n_groups;
+                    for (uint32_t j = 0; j < 4; ++j) {    // unrolled: the way round a loop costs this thread 170 cycles
+                        if (kb + static_cast<int>(j) >= g.k1) break;
+                        go = go && wait(bar_tile + 8 * stage.i, stage.phase);
+                        if (!go) break;
+                        tc_fence_after_sync();
+                        const uint32_t a = a0 + stage.i * a_step, b = a + (kLinM * kLinK >> 4);
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k)
+                            umma_mxf8<PAIR>(acc, desc_hi | (a + 2 * k), desc_hi | (b + 2 * k), idesc + (j << 29) + ((BLOCK == 128 ? j : k) << 4), ta,
+                                            BLOCK == 128 ? tb : tb + 8 * j, kb > g.k0 || j > 0 || k > 0);
+                        lin_commit<PAIR>(bar_empty + 8 * stage.i);
+                        stage.next(S);
                     }
+                    lin_commit<PAIR>(bar_scale_empty + 8 * group.i);
+                    group.next(kLinGroups);
+                    ++n_groups;
+                }
+                if (go) lin_commit<PAIR>(bar_acc_full + 8 * (n & 1));
+            }
+        }
+    } else if (warp < 6) {
+        // ------------------------------------------------------------- scales: 128 tokens a warp, the second warp of two the weights' too; two
+        // warps take every other group (a group's way through one warp is about as long as its products take)
+        const int c = warp & 1, turn = (warp - 2) >> 1;
+        uint32_t n_groups = 0;
+        const uint32_t leader_scale = PAIR ? cluster_addr(bar_scale, 0) : 0;
+        bool go = true;
+        while (go && work.get(p, g))
+            for (int kb = g.k0; kb < g.k1; kb += 4, group.next(kLinGroups), ++n_groups) {
+                if ((n_groups & 1) != turn) continue;
+                LinScales<BLOCK, PAIR> sc;        // (loads of the next group before this one's arrival would hold it up: it waits for them)
+                sc.load(p, g, kb, c, lane, pair_rank);
+                if (!(go = warp_wait(bar_scale_empty + 8 * group.i, group.phase ^ 1))) break;
+                sc.store(groups + group.i * L::kGroupBytes, c, chunks, lane);
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR)
+                        cluster_mbar_arrive(leader_scale + 8 * group.i);
+                    else
+                        mbar_arrive(bar_scale + 8 * group.i);
                 }
             }
-        }
-    } else if (warp < 4) {
-        // ------------------------------------------------------------- scales: 128 tokens a warp, the second warp the weights' too
-        const int c = warp - 2;
-        const uint32_t leader_scale = PAIR ? cluster_addr(bar_scale, 0) : 0;
-        LinScales<BLOCK, PAIR> now, later;
-        bool more = work.get(p, g);
-        int kb = g.k0, later_loads = 0;
-        if (more) now.load(p, g, kb, c, lane, pair_rank);
-        while (more) {                            // the next group's loads are in flight while this one waits for its place
-            kb += 4;
-            if (kb >= g.k1) {
-                more = work.get(p, g);
-                kb = g.k0;
-            }
-            const bool first = later_loads == 0;  // (the first group's place is free: it goes there before the second one's loads)
-            if (!first && more) later.load(p, g, kb, c, lane, pair_rank);
-            if (!warp_wait(bar_scale_empty + 8 * group.i, group.phase ^ 1)) break;
-            now.store(groups + group.i * L::kGroupBytes, c, chunks, lane);
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) {
-                if (PAIR)
-                    cluster_mbar_arrive(leader_scale + 8 * group.i);
-                else
-                    mbar_arrive(bar_scale + 8 * group.i);
-            }
-            group.next(kLinGroups);
-            if (first && more) later.load(p, g, kb, c, lane, pair_rank);
-            later_loads = 1;
-            now = later;
-        }
     } else {
         // ------------------------------------------------------------- output
-        const int quadrant = warp - 4, row = quadrant * 32 + lane;
+        const int quadrant = warp & 3, row = quadrant * 32 + lane;      // a warp reads the TMEM lanes of its place in four
         uint8_t *const buf = smem_raw + (out_smem - raw) + quadrant * kLinOutBytes;
         const uint32_t leader_acc_empty = PAIR ? cluster_addr(bar_acc_empty, 0) : 0;
         bool joins = false;
         int feature0 = 0, token0 = 0, tokens = 0;
         float bias = 0.f;
         for (uint32_t n = 0; work.get(p, g); ++n) {
-            feature0 = (g.tile / p.token_tiles * (PAIR ? 2 : 1) + pair_rank) * kLinM + quadrant * 32;
-            token0 = (g.tile % p.token_tiles) * p.tile_tokens;
+            feature0 = LinWork<PAIR>::feature_tile(p, g, pair_rank) * kLinM + quadrant * 32;
+            token0 = LinWork<PAIR>::token0(p, g);
             tokens = min(p.tile_tokens, p.T - token0);
             joins = !PAIR && p.split > 1 && g.tile >= p.whole;
             bias = p.bias && feature0 + lane < p.N ? __uint_as_float(static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(p.bias) + feature0 + lane)) << 16) : 0.f;
@@ -517,14 +545,13 @@ __global__ void __launch_bounds__(kLinThreads, 1)
                 const int c0 = tokens * rank / p.split, c1 = tokens * (rank + 1) / p.split;
                 for (int c = c0; c < c1; c += 32) {
                     float v[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                    for (int r = 0; r < p.split; ++r) {
-                        const uint32_t from = cluster_addr(base, r) + 4 * (c * kLinM + row);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (c + j < c1) v[j] += cluster_ld(from + 4 * j * kLinM);
-                    }
+                    const uint32_t at = base + 4 * (c * kLinM + row);
+                    if (p.split <= 2)
+                        add_parts<2>(v, at, p.split, c1 - c);
+                    else if (p.split <= 4)
+                        add_parts<4>(v, at, p.split, c1 - c);
+                    else
+                        add_parts<8>(v, at, p.split, c1 - c);
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] += bias;
                     store_outputs<F32>(p, buf, v, lane, feature0, token0 + c, c1 - c);
@@ -533,7 +560,7 @@ __global__ void __launch_bounds__(kLinThreads, 1)
         }
     }
     __syncwarp();
-    if (!PAIR && p.split > 1 && p.rest && warp < 4) {
+    if (!PAIR && p.split > 1 && p.rest && warp < 6) {
         cluster_arrive();
         cluster_wait();
     }
