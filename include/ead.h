@@ -581,17 +581,13 @@ int ead_quantise(const void *x, int64_t x_stride, const void *gate, int64_t gate
  *   bias       dev, bf16 [N] or NULL
  *   format     of out: EAD_FMT_BF16 or EAD_FMT_F32
  *   out        dev [T, N], out_stride elements apart (rows keep 16-byte alignment; N need not be a multiple of anything)
- *   workspace  dev, EAD_LINEAR_WORKSPACE_BYTES bytes, 256-byte aligned, zero-filled ONCE by the caller; every call leaves it ready
- *              for the next one.  Calls that may overlap on the device need a workspace each (and it is not ead_kv_attention's)
- *   status     dev uint32 or NULL.  EAD_STATUS_WAIT_EXPIRED: a bounded wait ran out (the output is not valid, the workspace has
- *              to be zero-filled again)
+ *   status     dev uint32 or NULL.  EAD_STATUS_WAIT_EXPIRED: a bounded wait ran out (the output is not valid)
  * A NaN in a row of x or w makes that row or column of the output NaN and no other.  The result does not depend on the order in
- * which blocks run.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (more than 2^30 tiles of 128 x 240 outputs),
+ * which blocks run.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (N / 128 x T / 16 above 2^30),
  * EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
  */
-#define EAD_LINEAR_WORKSPACE_BYTES (40u << 20)
 int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, const void *bias, int32_t format, void *out, int64_t out_stride,
-               void *workspace, uint32_t *status, int32_t device, void *stream);
+               uint32_t *status, int32_t device, void *stream);
 
 /*
  * Norm and rotation of query and key heads.  Every head x of head_dim elements, where it has a weight:

@@ -37,7 +37,6 @@ EAD_FMT_F16 = 3
 EAD_FMT_BLOCK = 32
 EAD_KV_WORKSPACE_BYTES = 64 << 20
 EAD_NORM_MAX_H = 16384
-EAD_LINEAR_WORKSPACE_BYTES = 40 << 20
 EAD_LOGPROB_WORKSPACE_BYTES = 1 << 20
 
 SYMBOLS = ["ead_create", "ead_step", "ead_run", "ead_run_host", "ead_run_timed", "ead_reset", "ead_status",
@@ -172,7 +171,7 @@ def lib() -> C.CDLL:
         L.ead_quantise.restype = C.c_int
         L.ead_quantise.argtypes = [vp, i64, vp, i64, vp, i32, vp]
         L.ead_linear.restype = C.c_int
-        L.ead_linear.argtypes = [vp, vp, vp, i32, vp, i64, vp, vp, i32, vp]
+        L.ead_linear.argtypes = [vp, vp, vp, i32, vp, i64, vp, i32, vp]
         L.ead_qk_norm_rope.restype = C.c_int
         L.ead_qk_norm_rope.argtypes = [vp, vp, i32, vp, i64, i32, vp, i64, i32, vp, i64, vp, i64, i32, vp]
         L.ead_kv_rotate_write.restype = C.c_int
@@ -555,17 +554,14 @@ def ead_quantise(x, out: EadE4m3Matrix, *, gate=None, device=0, stream=0) -> Non
         _check(rc, "ead_quantise")
 
 
-def ead_linear(x: EadE4m3Matrix, w: EadE4m3Matrix, out, *, workspace, bias=None, status=None, device=0, stream=0) -> None:
-    """``out = x w^T + bias``, ``out`` bf16 or float ``[x.rows, w.rows]``, ``bias`` bf16 ``[w.rows]``; ``workspace`` is a
-    zero-filled buffer of ``EAD_LINEAR_WORKSPACE_BYTES`` that calls which may overlap must not share."""
+def ead_linear(x: EadE4m3Matrix, w: EadE4m3Matrix, out, *, bias=None, status=None, device=0, stream=0) -> None:
+    """``out = x w^T + bias``, ``out`` bf16 or float ``[x.rows, w.rows]``, ``bias`` bf16 ``[w.rows]``."""
     T = _t()
     stride = _rows2(out, (x.rows, w.rows), "out", (T.bfloat16, T.float32))
     if bias is not None:
         _dense(bias, (w.rows,), T.bfloat16, "bias")
-    if workspace.nbytes < EAD_LINEAR_WORKSPACE_BYTES:
-        raise ValueError("workspace: want EAD_LINEAR_WORKSPACE_BYTES bytes")
     rc = lib().ead_linear(x.ref, w.ref, _ptr(bias), EAD_FMT_F32 if out.dtype is T.float32 else EAD_FMT_BF16, out.data_ptr(), stride,
-                          workspace.data_ptr(), _ptr(status), device, stream)
+                          _ptr(status), device, stream)
     if rc:
         _check(rc, "ead_linear")
 

@@ -43,8 +43,10 @@ cudaLaunchConfig_t linear_config(int blocks, int cluster, int smem, cudaStream_t
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cfg;
 }
 
@@ -56,7 +58,7 @@ int use_device(int device, DeviceInfo **out)
             !prepare_linear<128, false, true>() || !prepare_linear<128, true, true>())
             return false;
         for (int c = 1; c <= kLinMaxSplit; ++c) {
-            cudaLaunchAttribute attr[1];
+            cudaLaunchAttribute attr[2];
             const cudaLaunchConfig_t cfg = linear_config(c, c, kLinSmem, nullptr, attr);
             if (cudaOccupancyMaxActiveClusters(&g_clusters[device][c], ead_linear_kernel<128, false, false>, &cfg) != cudaSuccess) return false;
         }
@@ -166,7 +168,7 @@ int launch_linear(const CUtensorMap &tw, const CUtensorMap &tx, LinearParams p, 
     using L = LinLayout<BLOCK>;
     const int stage = L::stage_bytes(p.tile_tokens, PAIR);
     p.stages = std::min(kLinMaxStages, (kLinSmem - L::fixed_bytes()) / stage);
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     const cudaLaunchConfig_t cfg = linear_config(blocks, p.split, L::fixed_bytes() + p.stages * stage, s, attr);
     if (cudaLaunchKernelEx(&cfg, ead_linear_kernel<BLOCK, F32, PAIR>, tw, tx, p) != cudaSuccess) {
         cudaGetLastError();
@@ -184,16 +186,16 @@ int launch_linear(const CUtensorMap &tw, const CUtensorMap &tx, const LinearPara
 }  // namespace
 
 extern "C" int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, const void *bias, int32_t format, void *out, int64_t out_stride,
-                          void *workspace, uint32_t *status, int32_t device, void *stream)
+                          uint32_t *status, int32_t device, void *stream)
 {
     int rc = check_matrix(x, 1);
     if (rc == EAD_OK) rc = check_matrix(w, 128);
     if (rc != EAD_OK) return rc;
     const bool f32 = format == EAD_FMT_F32;
-    if ((format != EAD_FMT_BF16 && !f32) || x->cols != w->cols || !workspace) return EAD_EINVALID_ARG;
+    if ((format != EAD_FMT_BF16 && !f32) || x->cols != w->cols) return EAD_EINVALID_ARG;
     if (x->rows == 0 || w->rows == 0) return EAD_OK;
     if (!out || out_stride < w->rows) return EAD_EINVALID_ARG;
-    if (!aligned(out, 16) || out_stride % (f32 ? 4 : 8) || !aligned(bias, 2) || !aligned(workspace, 256) || !aligned(status, 4)) return EAD_EALIGNMENT;
+    if (!aligned(out, 16) || out_stride % (f32 ? 4 : 8) || !aligned(bias, 2) || !aligned(status, 4)) return EAD_EALIGNMENT;
     LinearParams p{};
     p.x_scale = x->scale;
     p.w_scale = w->scale;

@@ -395,6 +395,8 @@ __global__ void __launch_bounds__(kLinThreads, 1)
         cluster_wait();
     }
     tc_fence_after_sync();
+    griddep_wait();                               // nothing above touches global memory: it runs under the end of the kernel before
+    griddep_launch_dependents();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&s_tmem);
     // A wait that runs out makes every other role of the block stop at its next one that does.
     auto wait = [&](uint32_t bar, uint32_t parity) { return wait_phase<true>(bar, parity, p, &s_gave_up); };

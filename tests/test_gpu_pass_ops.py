@@ -15,11 +15,6 @@ def E():
 
 
 @pytest.fixture(scope="module")
-def workspace(E):
-    return torch.zeros(E.EAD_LINEAR_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
-
-
-@pytest.fixture(scope="module")
 def score_space(E):
     return torch.zeros(E.EAD_LOGPROB_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
 
@@ -53,11 +48,11 @@ class Product:
         self.mw = E.ead_e4m3_matrix(_padded(dev[2], pad), dev[3].cuda(), block=(128, 128))
         self.bias = torch.from_numpy(rng.normal(0, 4, N)).bfloat16().cuda()
 
-    def run(self, E, workspace, dtype, bias=True, pad=0, **kw):
+    def run(self, E, dtype, bias=True, pad=0, **kw):
         T, N = len(self.xv), len(self.wv)
         out = torch.full((T, -(-N // 8) * 8 + pad), -7.0, dtype=dtype, device="cuda")
         st = _status()
-        E.ead_linear(self.mx, self.mw, out[:, :N], bias=self.bias if bias else None, workspace=workspace, status=st, **kw)
+        E.ead_linear(self.mx, self.mw, out[:, :N], bias=self.bias if bias else None, status=st, **kw)
         assert (out[:, N:] == -7.0).all() and st.item() == 0
         return out[:, :N].cpu()
 
@@ -80,31 +75,31 @@ class Product:
 @pytest.mark.parametrize("block", [32, 128])
 @pytest.mark.parametrize("T,N,K", [(1, 128, 128), (1, 40, 32), (2, 129, 96), (15, 256, 1536), (16, 300, 160), (17, 1000, 512), (64, 7168, 640),
                                    (129, 257, 4128), (240, 384, 256), (241, 130, 1024), (500, 5000, 288), (1000, 1030, 2048)])
-def test_linear(E, workspace, dtype, block, T, N, K):
+def test_linear(E, dtype, block, T, N, K):
     p = Product(E, T, N, K, block, seed=T + N + K)
-    p.check(p.run(E, workspace, dtype))
+    p.check(p.run(E, dtype))
 
 
 @pytest.mark.parametrize("block", [32, 128])
-def test_linear_rows_of_wider_buffers(E, workspace, block):
+def test_linear_rows_of_wider_buffers(E, block):
     p = Product(E, 37, 203, 416, block, pad=48)
     for bias in (False, True):
-        p.check(p.run(E, workspace, torch.bfloat16, bias, pad=24), bias)
-        p.check(p.run(E, workspace, torch.float32, bias, pad=16), bias)
+        p.check(p.run(E, torch.bfloat16, bias, pad=24), bias)
+        p.check(p.run(E, torch.float32, bias, pad=16), bias)
 
 
 @pytest.mark.parametrize("T,N,K", [(1, 2048, 1536), (3, 128, 8192), (64, 1280, 5120), (300, 1300, 4096)])
-def test_linear_is_the_same_every_time(E, workspace, T, N, K):
-    """Tiles cut along K are joined in the order of K, whoever comes last; and the workspace is left ready."""
+def test_linear_is_the_same_every_time(E, T, N, K):
+    """Tiles cut along K are joined in the order of K, whichever block is slow."""
     p = Product(E, T, N, K, 128)
-    first = p.run(E, workspace, torch.float32)
+    first = p.run(E, torch.float32)
     p.check(first)
     for _ in range(20):
-        assert torch.equal(p.run(E, workspace, torch.float32), first)
+        assert torch.equal(p.run(E, torch.float32), first)
 
 
 @pytest.mark.parametrize("block", [32, 128])
-def test_linear_every_scale_reaches_its_block(E, workspace, block):
+def test_linear_every_scale_reaches_its_block(E, block):
     """Codes of 1 and scales that name their place: the sums are exact in 32 bits."""
     T, N, K = 140, 260, 1152
 
@@ -114,25 +109,25 @@ def test_linear_every_scale_reaches_its_block(E, workspace, block):
         p.x[1][:] = 127 + rng.integers(-3, 4, p.x[1].shape)
         p.w[1][:] = 127 + rng.integers(-3, 4, p.w[1].shape)
     p = Product(E, T, N, K, block, edit=edit)
-    got = p.run(E, workspace, torch.float32, bias=False)
+    got = p.run(E, torch.float32, bias=False)
     assert np.array_equal(got.double().numpy(), p.xv @ p.wv.T)
 
 
-def test_linear_far_scales(E, workspace):
+def test_linear_far_scales(E):
     """The ends of the scales' range: products that vanish, that stay, and that overflow to infinity."""
     def edit(p):
         p.x[0][:], p.w[0][:] = 0x38, 0x38
         p.x[1][:] = np.array([[7], [127], [246], [246]])
         p.w[1][:] = np.array([[7], [246]])
     p = Product(E, 4, 256, 128, 128, edit=edit)
-    got = p.run(E, workspace, torch.float32, bias=False).double().numpy()
+    got = p.run(E, torch.float32, bias=False).double().numpy()
     want = p.xv @ p.wv.T                                                 # 128 * 2^(a + b)
     want = np.where(want > 3.4e38, np.inf, np.where(want < 2.0 ** -126, 0.0, want))
     assert np.array_equal(np.where(got < 2.0 ** -126, 0.0, got), want)   # below the smallest normal number either 0 or the number
 
 
 @pytest.mark.parametrize("block", [32, 128])
-def test_linear_nan_stays_in_its_row_and_column(E, workspace, block):
+def test_linear_nan_stays_in_its_row_and_column(E, block):
     def edit(p):
         p.x[0][3, 200] = 0x7F
         p.x[1][70, 1] = 255
@@ -140,22 +135,22 @@ def test_linear_nan_stays_in_its_row_and_column(E, workspace, block):
         p.w[0][130, 5] = 0xFF
         p.w[1][0, 2] = 255
     p = Product(E, 90, 300, 384, block, edit=edit)
-    got = p.run(E, workspace, torch.bfloat16)
+    got = p.run(E, torch.bfloat16)
     want = torch.from_numpy(p.xv @ p.wv.T).isnan()
     assert want[3].all() and want[70].all() and want[:, 130].all() and want[:, :128].all() and not want[0, 128:130].any()
     assert torch.equal(got.isnan(), want)
 
 
-def test_linear_captured_and_replayed(E, workspace):
+def test_linear_captured_and_replayed(E):
     a, b = Product(E, 9, 700, 1536, 128, seed=1), Product(E, 9, 700, 1536, 128, seed=2)
     out = torch.zeros(9, 704, device="cuda")[:, :700]
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
-        E.ead_linear(a.mx, a.mw, out, workspace=workspace, stream=side.cuda_stream)
+        E.ead_linear(a.mx, a.mw, out, stream=side.cuda_stream)
     torch.cuda.synchronize()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g, stream=side):
-        E.ead_linear(a.mx, a.mw, out, workspace=workspace, stream=side.cuda_stream)
+        E.ead_linear(a.mx, a.mw, out, stream=side.cuda_stream)
     g.replay()
     torch.cuda.synchronize()
     a.check(out.cpu(), bias=False)
@@ -168,7 +163,7 @@ def test_linear_captured_and_replayed(E, workspace):
     b.check(out.cpu(), bias=False)
 
 
-def test_linear_offsets_beyond_32_bits(E, workspace):
+def test_linear_offsets_beyond_32_bits(E):
     """More than 2^31 outputs: the last rows are checked, and that nothing is written behind them."""
     T, N, K = 16500, 131072, 32
     codes, scale = torch.full((T, K), 0x38, dtype=torch.uint8, device="cuda"), torch.full((T, 1), 127, dtype=torch.uint8, device="cuda")
@@ -176,27 +171,26 @@ def test_linear_offsets_beyond_32_bits(E, workspace):
     w, ws = torch.full((N, K), 0x38, dtype=torch.uint8, device="cuda"), torch.full((N // 128, 1), 127, dtype=torch.uint8, device="cuda")
     ws[-1] = 128
     out = torch.full((T + 1, N), -1.0, dtype=torch.bfloat16, device="cuda")
-    E.ead_linear(E.ead_e4m3_matrix(codes, scale, block=(1, 32)), E.ead_e4m3_matrix(w, ws, block=(128, 128)), out[:T], workspace=workspace)
+    E.ead_linear(E.ead_e4m3_matrix(codes, scale, block=(1, 32)), E.ead_e4m3_matrix(w, ws, block=(128, 128)), out[:T])
     assert (out[T] == -1).all() and (out[0, :-128] == 32).all() and (out[T - 2, :-128] == 32).all()
     assert (out[T - 1, :-128] == 256).all() and (out[T - 1, -128:] == 512).all() and (out[T - 2, -128:] == 64).all()
 
 
-def test_linear_waits_that_run_out(E):
-    """With a limit of no time waits run out in the middle of sound calls: the kernel ends in order and says so, and after the
-    workspace is cleared the next call is right."""
-    space = torch.zeros(E.EAD_LINEAR_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
-    p = Product(E, 300, 1300, 4096, 128)
-    out, st = torch.zeros(300, 1304, device="cuda"), _status()
+@pytest.mark.parametrize("T,N,K,block", [(300, 1300, 4096, 128), (500, 1300, 4096, 32), (40, 512, 8192, 32), (5, 5000, 2048, 128), (64, 40000, 512, 128)])
+def test_linear_waits_that_run_out(E, T, N, K, block):
+    """With a limit of no time waits run out in the middle of sound calls: the kernel ends in order and says so, and the next
+    call is right."""
+    p = Product(E, T, N, K, block)
+    out, st = torch.zeros(T, -(-N // 8) * 8, device="cuda"), _status()
     try:
         for ns in (0, 300, 1000, 3000, 10000):
             E.ead_kv_wait_limit(ns)
-            E.ead_linear(p.mx, p.mw, out[:, :1300], workspace=space, status=st)
+            E.ead_linear(p.mx, p.mw, out[:, :N], status=st)
             torch.cuda.synchronize()
         assert st.item() == E.EAD_STATUS_WAIT_EXPIRED
     finally:
         E.ead_kv_wait_limit(-1)
-    space.zero_()
-    p.check(p.run(E, space, torch.float32))
+    p.check(p.run(E, torch.float32))
 
 
 # ----------------------------------------------------------------------------- quantisation

@@ -25,11 +25,11 @@ def _matrix(E, rows=4, cols=64, block_rows=1, block_cols=32, row_stride=64, code
     return E.EadE4m3Matrix(rows, cols, block_rows, block_cols, row_stride, codes, scale, reserved)
 
 
-def _linear(E, x=None, w=None, bias=None, format=0, out=8192, out_stride=128, workspace=4096, status=None):
+def _linear(E, x=None, w=None, bias=None, format=0, out=8192, out_stride=128, status=None):
     x = _matrix(E) if x is None else x
     w = _matrix(E, rows=128, block_rows=128, block_cols=128) if w is None else w
     ref = lambda m: None if m == 0 else C.byref(m)                       # noqa: E731
-    return E.lib().ead_linear(ref(x), ref(w), bias, format, out, out_stride, workspace, status, 0, None)
+    return E.lib().ead_linear(ref(x), ref(w), bias, format, out, out_stride, status, 0, None)
 
 
 BAD_MATRIX = [(dict(rows=-1), "I"), (dict(rows=(1 << 30) + 1), "I"), (dict(cols=0), "I"), (dict(cols=16), "I"), (dict(cols=72, row_stride=80), "A"),
@@ -49,8 +49,7 @@ def test_bad_matrices_are_refused(E, bad, letter):
 
 @pytest.mark.parametrize("bad,letter", [
     (dict(x=0), "I"), (dict(w=0), "I"), (dict(format=1), "I"), (dict(format=3), "I"), (dict(out=None), "I"), (dict(out=8200), "A"),
-    (dict(out_stride=127), "I"), (dict(out_stride=132), "A"), (dict(out_stride=130, format=2), "A"), (dict(workspace=None), "I"),
-    (dict(workspace=4096 + 128), "A"), (dict(status=4098), "A"), (dict(bias=4097), "A")])
+    (dict(out_stride=127), "I"), (dict(out_stride=132), "A"), (dict(out_stride=130, format=2), "A"), (dict(status=4098), "A"), (dict(bias=4097), "A")])
 def test_bad_products_are_refused(E, bad, letter):
     assert _linear(E, **bad) == _code(E, letter)
 
@@ -160,7 +159,7 @@ def test_binding_refuses_wrong_types_and_shapes(E):
     x, w = E.ead_e4m3_matrix(b8(3, 160), b8(3, 5), block=(1, 32)), E.ead_e4m3_matrix(b8(130, 160), b8(2, 2), block=(128, 128))
     assert (x.row_stride, w.rows, w.block_cols) == (160, 130, 128)
     assert E.ead_e4m3_matrix(b8(3, 192)[:, :160].view(torch.float8_e4m3fn), b8(3, 2), block=(1, 128)).row_stride == 192
-    space, small = torch.zeros(E.EAD_LINEAR_WORKSPACE_BYTES, dtype=u8), torch.zeros(16, dtype=u8)
+    space, small = torch.zeros(E.EAD_LOGPROB_WORKSPACE_BYTES, dtype=u8), torch.zeros(16, dtype=u8)
     rope = E.ead_rope(torch.zeros(32), 64, q_weight=bf(64))
     assert (rope.rot_dim, rope.head_dim) == (64, 64)
     cache = E.ead_kv_cache(bf(4, 2, 16, 64), bf(4, 2, 16, 64))
@@ -172,9 +171,8 @@ def test_binding_refuses_wrong_types_and_shapes(E):
                 lambda: E.ead_e4m3_matrix(b8(3, 160), b8(3, 5).int(), block=(1, 32)), lambda: E.ead_e4m3_matrix(b8(160, 3).t(), b8(3, 5), block=(1, 32)),
                 lambda: E.ead_e4m3_matrix(bf(3, 160), b8(3, 5), block=(1, 32)),
                 lambda: E.ead_quantise(bf(3, 128), x), lambda: E.ead_quantise(bf(3, 160).float(), x), lambda: E.ead_quantise(bf(3, 160), x, gate=bf(2, 160)),
-                lambda: E.ead_linear(x, w, bf(3, 128), workspace=space), lambda: E.ead_linear(x, w, bf(3, 130).half(), workspace=space),
-                lambda: E.ead_linear(x, w, bf(3, 136)[:, :130], workspace=small), lambda: E.ead_linear(x, w, bf(3, 136)[:, :130], bias=bf(128), workspace=space),
-                lambda: E.ead_linear(x, w, bf(3, 136)[:, :130], bias=torch.zeros(130), workspace=space),
+                lambda: E.ead_linear(x, w, bf(3, 128)), lambda: E.ead_linear(x, w, bf(3, 130).half()),
+                lambda: E.ead_linear(x, w, bf(3, 136)[:, :130], bias=bf(128)), lambda: E.ead_linear(x, w, bf(3, 136)[:, :130], bias=torch.zeros(130)),
                 lambda: E.ead_rope(torch.zeros(32).double(), 64), lambda: E.ead_rope(torch.zeros(32), 64, q_weight=bf(32)),
                 lambda: E.ead_rope(torch.zeros(32), 64, k_weight=torch.zeros(64)),
                 lambda: E.ead_qk_norm_rope(rope, place.long(), q, k, q, k), lambda: E.ead_qk_norm_rope(rope, place, q[:1], k, q, k),
