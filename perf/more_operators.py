@@ -275,7 +275,7 @@ def _own(s):
         if "x_matrix" not in s:                                          # a program describes its weights and buffers once
             s["x_matrix"] = E.ead_e4m3_matrix(s["x"], s["x_scale"], block=(1, case["block"]))
             s["w_matrix"] = E.ead_e4m3_matrix(s["w"], s["w_scale"], block=(128, 128))
-        E.ead_linear(s["x_matrix"], s["w_matrix"], s["out"], bias=s["bias"], workspace=s["workspace"], stream=stream)
+        E.ead_linear(s["x_matrix"], s["w_matrix"], s["out"], bias=s["bias"], stream=stream)
         return s["out"]
     if case["op"] == "quantise":
         if "matrix" not in s:
