@@ -13,10 +13,13 @@
 
 namespace ead {
 
-constexpr int kScoreThreads = 512;
+constexpr int kScoreThreads = 256;
+constexpr int kScoreSettle = 1024;                // runs between settlements of a thread's counts
+constexpr int kScoreUnroll = 4;                   // vectors of a run: a thread has them on their way together
 constexpr int kScoreMaxTop = 64;                  // alternatives
-constexpr int kScoreMaxParts = 512;               // parts of a row, at most this many
+constexpr int kScoreMaxParts = kScoreThreads;     // of a row, at most
 constexpr int kScoreMaxJoin = 2048;               // parts x alternatives, at most
+constexpr int kScoreSlack = 8;                    // threads beyond k that may be looked at again
 constexpr int kScoreCandidates = 2048;            // logits that reach the bound; beyond, a slower way
 constexpr int kScoreMaxCutRows = 1024;            // rows of a call that cuts its rows
 constexpr size_t kScoreCounterBytes = kScoreMaxCutRows * sizeof(uint32_t);
@@ -36,7 +39,7 @@ struct ScoreParams {
 
 // A part's (or a thread's) share of a row.
 struct ScoreSums {
-    float m, s, t;                                // largest logit; sums relative to max(m, lowest finite value)
+    float m, s, t;                                // largest logit; sums
     int before;                                   // logits that come before the given token
 };
 
@@ -52,9 +55,12 @@ __device__ __forceinline__ unsigned long long order_key(float z, int index)
     return static_cast<unsigned long long>(order_bits(z)) << 32 | (0xffffffffu - static_cast<uint32_t>(index));
 }
 
+// kFloor: logits below it count as this much (its product with log2 e is exact, or small); kLow .. kHigh: where the largest logit of a part lies
+// for the quick sums to be right: what is at the floor or below adds nothing then, and rounded products with log2 e are not far off.
 template <int FMT>
 struct LogitVec {
     static constexpr int kSize = FMT == kFmtF32 ? 4 : 2, kN = 16 / kSize;
+    static constexpr float kFloor = FMT == kFmtF16 ? -65504.f : -1048576.f, kLow = FMT == kFmtF16 ? -60000.f : -524288.f, kHigh = 1048576.f;
 };
 
 __device__ __forceinline__ uint4 load_logits(const uint8_t *p)
@@ -103,20 +109,27 @@ struct RowVectors {
     }
     __device__ __forceinline__ int column(int g) const { return g * LogitVec<FMT>::kN - shift; }
     __device__ __forceinline__ bool whole(int g) const { return (g > 0 || shift == 0) && column(g) + LogitVec<FMT>::kN <= V; }
-    // Columns outside the row read as -infinity.
-    __device__ __forceinline__ void load(int g, float (&z)[LogitVec<FMT>::kN]) const
+    // The vector as it lies in memory; columns outside the row are -infinity.
+    __device__ __forceinline__ uint4 raw(int g) const
     {
         constexpr int N = LogitVec<FMT>::kN;
-        if (whole(g)) {
-            unpack_logits<FMT>(load_logits(base + 16 * static_cast<int64_t>(g)), z);
-        } else {
+        if (whole(g)) return load_logits(base + 16 * static_cast<int64_t>(g));
+        uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int c = column(g) + i;
-                z[i] = c >= 0 && c < V ? logit_at<FMT>(base, static_cast<int64_t>(g) * N + i) : -INFINITY;
+        for (int i = 0; i < N; ++i) {
+            const int c = column(g) + i;
+            const bool in = c >= 0 && c < V;
+            const int64_t at = static_cast<int64_t>(g) * N + i;
+            if (FMT == kFmtF32) {
+                w[i] = in ? __ldg(reinterpret_cast<const uint32_t *>(base) + at) : 0xff800000u;
+            } else {
+                const uint32_t h = in ? __ldg(reinterpret_cast<const uint16_t *>(base) + at) : FMT == kFmtF16 ? 0xfc00u : 0xff80u;
+                w[i / 2] = (i & 1) ? w[i / 2] | h << 16 : h;
             }
         }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ __forceinline__ void load(int g, float (&z)[LogitVec<FMT>::kN]) const { unpack_logits<FMT>(raw(g), z); }
 };
 
 __device__ __forceinline__ float exp2_of(float x)
@@ -134,11 +147,12 @@ __device__ __forceinline__ float below_max(float z, float m)
 }
 
 // Sums of two disjoint sets of logits.  With s = NaN or infinite (a logit that is NaN or +infinity) the result has it too.
-__device__ __forceinline__ ScoreSums join_sums(const ScoreSums &a, const ScoreSums &b)
+// `low`: sums are relative to max(m, low).
+__device__ __forceinline__ ScoreSums join_sums(const ScoreSums &a, const ScoreSums &b, float low)
 {
     ScoreSums r;
     r.m = fmaxf(a.m, b.m);
-    const float m = fmaxf(r.m, kLowest), da = below_max(fmaxf(a.m, kLowest), m), db = below_max(fmaxf(b.m, kLowest), m);
+    const float m = fmaxf(r.m, low), da = below_max(fmaxf(a.m, low), m), db = below_max(fmaxf(b.m, low), m);
     const float ea = exp2_of(da), eb = exp2_of(db);
     r.s = a.s * ea + b.s * eb;
     r.t = fmaf(a.s, da, a.t) * ea + fmaf(b.s, db, b.t) * eb;
@@ -157,33 +171,48 @@ struct ScoreShared {
     unsigned long long cand[kScoreCandidates];
     unsigned long long best[kScoreMaxTop];        // the k largest keys, descending; 0: none
     unsigned long long warp_key[kScoreThreads / 32];
-    int chosen[kScoreThreads];                    // threads whose maximum reaches the bound
-    int n_chosen, n_cand, last;
+    uint2 warp_range[kScoreThreads / 32];
+    int run[kScoreThreads], strip[kScoreThreads]; // of threads whose maximum reaches the bound: its run's first vector, or the thread
+    int n_runs, n_strips, n_cand, last;
 };
 
 // Sums over the block, in every thread.  (The tree is the same whatever the timing.)
-__device__ __forceinline__ ScoreSums block_sums(ScoreShared &sh, ScoreSums a)
+__device__ __forceinline__ ScoreSums block_sums(ScoreShared &sh, ScoreSums a, float low)
 {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) a = join_sums(a, shuffle_xor(a, o));
+    for (int o = 1; o < 32; o <<= 1) a = join_sums(a, shuffle_xor(a, o), low);
     if ((threadIdx.x & 31) == 0) sh.warp_sums[threadIdx.x >> 5] = a;
     __syncthreads();
     a = sh.warp_sums[threadIdx.x & (kScoreThreads / 32 - 1)];
+    __syncthreads();                              // it may be written again
 #pragma unroll
-    for (int o = 1; o < kScoreThreads / 32; o <<= 1) a = join_sums(a, shuffle_xor(a, o));
+    for (int o = 1; o < kScoreThreads / 32; o <<= 1) a = join_sums(a, shuffle_xor(a, o), low);
     return a;
 }
 
-// A lower bound of the k-th largest of the threads' keys (32 bits, 0: none), as large as possible; 0 if fewer than k threads have one.
-__device__ __forceinline__ uint32_t bound_of(uint32_t key, int k)
+// A lower bound of the k-th largest of the threads' keys (32 bits, 0: none) that few more than k of them reach; 0 if fewer than k
+// threads have one.
+__device__ __forceinline__ uint32_t bound_of(ScoreShared &sh, uint32_t key, int k)
 {
-    uint32_t bound = 0;
-    for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-        const int n = __syncthreads_count(key >= (bound | bit));
-        if (n >= k) bound |= bit;
-        if (n == k) break;
+    const uint32_t low = __reduce_min_sync(0xffffffffu, key ? key : 0xffffffffu), high = __reduce_max_sync(0xffffffffu, key);
+    if ((threadIdx.x & 31) == 0) sh.warp_range[threadIdx.x >> 5] = make_uint2(low, high);
+    if (__syncthreads_count(key != 0) < k) return 0;
+    uint32_t lo = 0xffffffffu, hi = 0;            // at least k keys reach lo, none passes hi
+#pragma unroll
+    for (int w = 0; w < kScoreThreads / 32; ++w) {
+        lo = min(lo, sh.warp_range[w].x);
+        hi = max(hi, sh.warp_range[w].y);
     }
-    return bound;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo + 1) / 2;
+        const int n = __syncthreads_count(key >= mid);
+        if (n >= k)
+            lo = mid;
+        else
+            hi = mid - 1;
+        if (n >= k && n <= k + kScoreSlack) break;
+    }
+    return lo;
 }
 
 // The k largest of the n keys in sh.cand, all different, into sh.best (filled up with 0).
@@ -200,29 +229,66 @@ __device__ __forceinline__ void sort_candidates(ScoreShared &sh, int n, int k)
     __syncthreads();
 }
 
-// The k largest keys of the row's vectors [g0, g1).  `thread_max`: of the vectors g0 + threadIdx.x, + kScoreThreads, ...
+// Largest of a vector's logits; a NaN is passed over.
 template <int FMT>
-__device__ __forceinline__ void find_top(ScoreShared &sh, const RowVectors<FMT> &row, int g0, int g1, float thread_max, int k)
+__device__ __forceinline__ float largest(const uint4 &v)
+{
+    if constexpr (FMT == kFmtF32) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    } else if constexpr (FMT == kFmtBf16) {
+        const __nv_bfloat162 *const h = reinterpret_cast<const __nv_bfloat162 *>(&v);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    } else {
+        const __half2 *const h = reinterpret_cast<const __half2 *>(&v);
+        const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+}
+// Puts a vector's logits that reach the bound among the candidates.
+template <int FMT>
+__device__ __forceinline__ void add_candidates(ScoreShared &sh, const RowVectors<FMT> &row, const uint4 &v, int g, uint32_t bound)
+{
+    constexpr int N = LogitVec<FMT>::kN;
+    if (bound && order_bits(largest<FMT>(v)) < bound) return;
+    float z[N];
+    unpack_logits<FMT>(v, z);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int col = row.column(g) + i;
+        if (col >= 0 && col < row.V && order_bits(z[i]) >= bound) {
+            const int n = atomicAdd(&sh.n_cand, 1);
+            if (n < kScoreCandidates) sh.cand[n] = order_key(z[i], col);
+        }
+    }
+}
+
+// The k largest keys of the row's vectors [g0, g1).  Of the vectors g0 + threadIdx.x, + kScoreThreads, ... that this thread saw: the largest logit, the
+// first vector of its run, the largest logit of the other runs.  A thread whose other runs stay below the bound has only that run looked at again.
+template <int FMT>
+__device__ __forceinline__ void find_top(ScoreShared &sh, const RowVectors<FMT> &row, int g0, int g1, float thread_max, int run, float second, int k)
 {
     constexpr int N = LogitVec<FMT>::kN;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) sh.n_chosen = sh.n_cand = 0;
+    if (threadIdx.x == 0) sh.n_runs = sh.n_strips = sh.n_cand = 0;
     const uint32_t key = g0 + static_cast<int>(threadIdx.x) < g1 ? order_bits(thread_max) : 0;
-    const uint32_t bound = bound_of(key, k);      // (its barriers also publish the zeros above)
-    if (key && key >= bound) sh.chosen[atomicAdd(&sh.n_chosen, 1)] = threadIdx.x;
+    const uint32_t bound = bound_of(sh, key, k);  // (its barriers also publish the zeros above)
+    if (key && key >= bound) {
+        if (bound && order_bits(second) < bound)
+            sh.run[atomicAdd(&sh.n_runs, 1)] = run;
+        else
+            sh.strip[atomicAdd(&sh.n_strips, 1)] = threadIdx.x;
+    }
     __syncthreads();
-    for (int c = warp; c < sh.n_chosen; c += kScoreThreads / 32)
-        for (int64_t g = g0 + sh.chosen[c] + static_cast<int64_t>(lane) * kScoreThreads; g < g1; g += 32 * kScoreThreads) {
-            float z[N];
-            row.load(static_cast<int>(g), z);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int col = row.column(static_cast<int>(g)) + i;
-                if (col >= 0 && col < row.V && order_bits(z[i]) >= bound) {
-                    const int at = atomicAdd(&sh.n_cand, 1);
-                    if (at < kScoreCandidates) sh.cand[at] = order_key(z[i], col);
-                }
-            }
+    for (int i = threadIdx.x; i < sh.n_runs * kScoreUnroll; i += kScoreThreads) {
+        const int64_t g = sh.run[i / kScoreUnroll] + static_cast<int64_t>(i % kScoreUnroll) * kScoreThreads;
+        if (g < g1) add_candidates<FMT>(sh, row, row.raw(static_cast<int>(g)), static_cast<int>(g), bound);
+    }
+    const int per_thread = (g1 - g0 + kScoreThreads - 1) / kScoreThreads;
+    for (int c = 0; c < sh.n_strips; ++c)
+        for (int i = threadIdx.x; i < per_thread; i += kScoreThreads) {
+            const int64_t g = g0 + sh.strip[c] + static_cast<int64_t>(i) * kScoreThreads;
+            if (g < g1) add_candidates<FMT>(sh, row, row.raw(static_cast<int>(g)), static_cast<int>(g), bound);
         }
     __syncthreads();
     if (sh.n_cand <= kScoreCandidates) {
@@ -289,9 +355,168 @@ __device__ __forceinline__ void write_scores(const ScoreParams &p, const ScoreSh
     }
 }
 
+// The vector with nothing below the floor; a NaN stays one.
+template <int FMT>
+__device__ __forceinline__ uint4 floored(uint4 v)
+{
+    if constexpr (FMT == kFmtF32) {
+        uint32_t *const w = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+r"(w[i]) : "f"(LogitVec<FMT>::kFloor));
+    } else if constexpr (FMT == kFmtBf16) {
+        __nv_bfloat162 *const h = reinterpret_cast<__nv_bfloat162 *>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __hmax2_nan(h[i], __float2bfloat162_rn(LogitVec<FMT>::kFloor));
+    } else {
+        __half2 *const h = reinterpret_cast<__half2 *>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __hmax2_nan(h[i], __float2half2_rn(LogitVec<FMT>::kFloor));
+    }
+    return v;
+}
+
+// Two 32-bit values in one register pair, for the instructions that take two at a time.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 r, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// A threshold that a 16-bit vector's logits are compared with, twice in a word.  strict: themselves; else the next lower number, so that
+// "above" it is "not below" z.  (z is neither NaN nor infinite.)
+template <int FMT>
+__device__ __forceinline__ uint32_t threshold(float z, bool strict)
+{
+    if (FMT == kFmtF32) {
+        const uint32_t b = __float_as_uint(z + 0.f);
+        return strict ? b : b == 0 ? 0x80000001u : (b & 0x80000000u) ? b + 1 : b - 1;
+    }
+    const uint32_t b = FMT == kFmtBf16 ? __float_as_uint(z + 0.f) >> 16 : __half_as_ushort(__float2half_rn(z + 0.f));
+    const uint32_t t = strict ? b : b == 0 ? 0x8001u : (b & 0x8000u) ? b + 1 : b - 1;
+    return t << 16 | t;
+}
+// Counts of logits above a threshold.  16-bit logits are compared two at a time; a comparison gives 0xffff in its half, and a 32-bit sum
+// of such words holds both halves' counts, which come apart as long as neither passes 65535.
+template <int FMT>
+struct CountAbove {
+    uint32_t sum = 0;
+    int total = 0;
+    __device__ __forceinline__ void add(const uint4 &v, uint32_t t)
+    {
+        if constexpr (FMT == kFmtF32) {
+            const float x = __uint_as_float(t);
+            total += (__uint_as_float(v.x) > x) + (__uint_as_float(v.y) > x) + (__uint_as_float(v.z) > x) + (__uint_as_float(v.w) > x);
+        } else if constexpr (FMT == kFmtBf16) {
+            const __nv_bfloat162 *const h = reinterpret_cast<const __nv_bfloat162 *>(&v), x = *reinterpret_cast<const __nv_bfloat162 *>(&t);
+            sum += __hgt2_mask(h[0], x) + __hgt2_mask(h[1], x);
+            sum += __hgt2_mask(h[2], x) + __hgt2_mask(h[3], x);
+        } else {
+            const __half2 *const h = reinterpret_cast<const __half2 *>(&v), x = *reinterpret_cast<const __half2 *>(&t);
+            sum += __hgt2_mask(h[0], x) + __hgt2_mask(h[1], x);
+            sum += __hgt2_mask(h[2], x) + __hgt2_mask(h[3], x);
+        }
+    }
+    // After at most 16383 vectors.
+    __device__ __forceinline__ void settle()
+    {
+        if (FMT == kFmtF32) return;
+        const uint32_t low = (0u - sum) & 0xffffu;                    // sum = (low - high) 2^16 - low
+        total += static_cast<int>(low + ((low - ((sum + low) >> 16)) & 0xffffu));
+        sum = 0;
+    }
+};
+
+// One thread's running maximum and sums.
+template <int FMT>
+struct ScoreThread {
+    static constexpr int N = LogitVec<FMT>::kN;
+    float m, second;                              // largest logit; largest of the runs that it is not in
+    int at;                                       // first vector of its run
+    float m_log2;                                 // s, t (even and odd places) are relative to max(m, floor) = m_log2 / log2 e
+    f32x2 s, t;
+    CountAbove<FMT> above;
+    int before;
+    __device__ __forceinline__ ScoreThread() : m(-INFINITY), second(-INFINITY), at(0), m_log2(LogitVec<FMT>::kFloor * kLog2e), s(0), t(0), before(0) {}
+    // U vectors from g on, kScoreThreads apart; EDGE: some of their columns may lie outside the row.  g_given: the given token's vector.
+    template <int U, bool EDGE>
+    __device__ __forceinline__ void take(const RowVectors<FMT> &row, const uint4 (&v)[U], int g, bool given, float z_given, uint32_t t_or_equal, uint32_t t_above, int token, int g_given)
+    {
+        float top = largest<FMT>(v[0]);
+#pragma unroll
+        for (int u = 1; u < U; ++u) top = fmaxf(top, largest<FMT>(v[u]));
+        if (top <= m) {
+            second = fmaxf(second, top);
+        } else if (top > m) {
+            second = m;
+            m = top;
+            at = g;
+            const float m1 = fmaxf(top, LogitVec<FMT>::kFloor) * kLog2e, d = fmaxf(m_log2 - m1, -1000.f), e = exp2_of(d);
+            const f32x2 ee = pack2(e, e);
+            t = fma2(fma2(s, pack2(d, d), t), ee, 0);
+            s = fma2(s, ee, 0);
+            m_log2 = m1;
+        }
+        const f32x2 scale = pack2(kLog2e, kLog2e), minus_m = pack2(-m_log2, -m_log2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float z[N];
+            unpack_logits<FMT>(floored<FMT>(v[u]), z);
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                const f32x2 y = fma2(pack2(z[i], z[i + 1]), scale, minus_m);
+                float y0, y1;
+                unpack2(y, y0, y1);
+                const f32x2 e = pack2(exp2_of(y0), exp2_of(y1));
+                s = add2(s, e);
+                t = fma2(e, y, t);
+            }
+        }
+        if (given && top >= z_given) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int gu = g + u * kScoreThreads;
+                if (EDGE || gu == g_given || z_given == -INFINITY) {
+                    float z[N];
+                    unpack_logits<FMT>(v[u], z);
+                    const int col = row.column(gu);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) before += z[i] > z_given || (z[i] == z_given && col + i < token && col + i >= 0);
+                } else {
+                    above.add(v[u], gu < g_given ? t_or_equal : t_above);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ ScoreSums sums() const
+    {
+        float s0, s1, t0, t1;
+        unpack2(s, s0, s1);
+        unpack2(t, t0, t1);
+        const float ss = s0 + s1, tt = t0 + t1;
+        if (m == -INFINITY && ss == ss) return ScoreSums{m, 0.f, 0.f, before};             // nothing but -infinity
+        const float c = fmaf(-fmaxf(m, LogitVec<FMT>::kFloor), kLog2e, m_log2), e = exp2_of(c);     // what the rounding of m_log2 added to every distance
+        return ScoreSums{m, ss * e, fmaf(ss, c, tt) * e, before};
+    }
+};
+
 // Block (x, y): part x of row y, y + gridDim.y, ...
 template <int FMT>
-__global__ void __launch_bounds__(kScoreThreads) ead_token_logprobs_kernel(ScoreParams p)
+__global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(ScoreParams p)
 {
     __shared__ ScoreShared sh;
     constexpr int N = LogitVec<FMT>::kN;
@@ -303,37 +528,54 @@ __global__ void __launch_bounds__(kScoreThreads) ead_token_logprobs_kernel(Score
         const int token = p.tokens ? __ldg(p.tokens + row) : -1;
         const bool given = p.rank && token >= 0 && token < p.V;
         const float z_given = given ? logit_at<FMT>(logits, token) : INFINITY;
-        ScoreSums a{-INFINITY, 0.f, 0.f, 0};
-        float m = kLowest;                        // max(a.m, kLowest)
-        for (int64_t g64 = g0 + threadIdx.x; g64 < g1; g64 += kScoreThreads) {
-            const int g = static_cast<int>(g64);
-            float z[N];
-            vec.load(g, z);
-            float top = z[0];
-#pragma unroll
-            for (int i = 1; i < N; ++i) top = fmaxf(top, z[i]);
-            if (top > a.m) {
-                a.m = top;
-                const float m1 = fmaxf(top, kLowest), d = below_max(m, m1), e = exp2_of(d);
-                a.t = fmaf(a.s, d, a.t) * e;
-                a.s *= e;
-                m = m1;
+        const int g_given = given ? static_cast<int>((static_cast<int64_t>(token) + vec.shift) / N) : 0;
+        const uint32_t t_or_equal = threshold<FMT>(z_given, false), t_above = threshold<FMT>(z_given, true);
+        ScoreThread<FMT> th;
+        const int n = g1 - g0, whole_end = vec.whole(g1 - 1) ? n : n - 1;                // vectors of this part
+        int i = 0;
+        auto one = [&] {
+            const int g = g0 + i + threadIdx.x;
+            if (g < g1) {
+                const uint4 v[1] = {vec.raw(g)};
+                th.template take<1, true>(vec, v, g, given, z_given, t_or_equal, t_above, token, g_given);
             }
+            i += kScoreThreads;
+        };
+        if (!vec.whole(g0)) one();                // (whole_end may then be wrong for a row of one vector: no quick run fits)
+        constexpr int kRun = kScoreUnroll * kScoreThreads;
+        while (i + kRun <= whole_end) {
+            const int stop = min(whole_end, i + kScoreSettle * kRun);
+            for (; i + kRun <= stop; i += kRun) {
+                const int g = g0 + i + threadIdx.x;
+                const uint8_t *const from = vec.base + 16 * static_cast<int64_t>(g);
+                uint4 v[kScoreUnroll];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float y = below_max(z[i], m), e = exp2_of(y);
-                a.s += e;
-                a.t = fmaf(e, y, a.t);
+                for (int u = 0; u < kScoreUnroll; ++u) v[u] = load_logits(from + 16 * u * kScoreThreads);
+                th.template take<kScoreUnroll, false>(vec, v, g, given, z_given, t_or_equal, t_above, token, g_given);
             }
-            if (given && top >= z_given) {
-                const int col = vec.column(g);
-#pragma unroll
-                for (int i = 0; i < N; ++i) a.before += z[i] > z_given || (z[i] == z_given && col + i < token && col + i >= 0);
-            }
+            th.above.settle();
         }
-        const float thread_max = a.m;
-        if (p.k) find_top<FMT>(sh, vec, g0, g1, thread_max, p.k);
-        a = block_sums(sh, a);
+        while (i < n) one();
+        th.before += th.above.total;
+        if (p.k) find_top<FMT>(sh, vec, g0, g1, th.m, th.at, th.second, p.k);
+        ScoreSums a = block_sums(sh, th.sums(), LogitVec<FMT>::kFloor);
+        if (a.m > -INFINITY && a.m < INFINITY && !(a.m >= LogitVec<FMT>::kLow && a.m <= LogitVec<FMT>::kHigh)) {
+            // logits at the ends of the type's range: once more, relative to the part's maximum
+            ScoreSums x{a.m, 0.f, 0.f, 0};
+            for (int64_t g = g0 + threadIdx.x; g < g1; g += kScoreThreads) {
+                float z[N];
+                vec.load(static_cast<int>(g), z);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float y = below_max(z[e], a.m), w = exp2_of(y);
+                    x.s += w;
+                    x.t = fmaf(w, y, x.t);
+                }
+            }
+            const int before = a.before;
+            a = block_sums(sh, x, kLowest);
+            a.before = before;
+        }
         if (p.parts == 1) {
             write_scores<FMT>(p, sh, row, logits, a);
             __syncthreads();
@@ -357,14 +599,13 @@ __global__ void __launch_bounds__(kScoreThreads) ead_token_logprobs_kernel(Score
             const float4 v = __ldcg(reinterpret_cast<const float4 *>(sums + threadIdx.x));
             all = ScoreSums{v.x, v.y, v.z, __float_as_int(v.w)};
         }
-        __syncthreads();                          // warp_sums is used again
-        all = block_sums(sh, all);
+        all = block_sums(sh, all, kLowest);
         if (p.k) {
             const int n = p.parts * p.k;
             uint32_t mine = 0;
             for (int i = threadIdx.x; i < n; i += kScoreThreads) mine = max(mine, static_cast<uint32_t>(__ldcg(keys + i) >> 32));
             if (threadIdx.x == 0) sh.n_cand = 0;
-            const uint32_t bound = bound_of(mine, p.k);
+            const uint32_t bound = bound_of(sh, mine, p.k);
             for (int i = threadIdx.x; i < n; i += kScoreThreads) {
                 const unsigned long long key = __ldcg(keys + i);
                 if (key && static_cast<uint32_t>(key >> 32) >= bound) sh.cand[atomicAdd(&sh.n_cand, 1)] = key;
