@@ -24,6 +24,9 @@ constexpr double kLinJoinStages = 4;
 constexpr int kScoreBlocksPerSm = 2;
 constexpr int kScoreMinVectors = 256;
 
+// Warps per SM that a call with few tokens is divided into, for the rotation.
+constexpr int kRopeWarpsPerSm = 32;
+
 DeviceTable g_devices;
 int g_clusters[kMaxDevices][kLinMaxSplit + 1];    // clusters of ead_linear's blocks that a device holds at a time, by their size
 
@@ -157,9 +160,35 @@ int check_rope(const ead_rope *r, RopeParams *p)
     return EAD_OK;
 }
 
-dim3 rope_grid(int n_tokens, int64_t values)
+// A kernel whose setup runs under the end of the one before it in the stream.
+template <typename Params>
+int launch_early(void (*kernel)(Params), unsigned grid, int threads, const Params &p, cudaStream_t s)
 {
-    return dim3(n_tokens, static_cast<unsigned>((values + kRopeBlockValues - 1) / kRopeBlockValues));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) {
+        cudaGetLastError();
+        return EAD_ECUDA;
+    }
+    return EAD_OK;
+}
+
+template <int FMT, bool DENSE>
+int launch_rotate(RopeParams &p, int n_tokens, int sms, cudaStream_t s)
+{
+    const int64_t values = (static_cast<int64_t>(p.heads_q) + (DENSE ? 1 : 2) * p.heads_kv) * p.dim;
+    const int runs = static_cast<int>((values + kRopeRun - 1) / kRopeRun);
+    p.n_tokens = n_tokens;
+    p.split = static_cast<int>(std::min<int64_t>(runs, std::max<int64_t>(1, int64_t{kRopeWarpsPerSm} * sms / n_tokens)));
+    const int64_t blocks = (static_cast<int64_t>(n_tokens) * p.split + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
+    return launch_early(ead_rotate_kernel<FMT, DENSE>, static_cast<unsigned>(blocks), kRopeThreads, p, s);
 }
 
 template <int BLOCK, bool F32, bool PAIR>
@@ -298,9 +327,7 @@ extern "C" int ead_qk_norm_rope(const ead_rope *rope, const int32_t *positions, 
     p.k_out_stride = k_out_stride;
     p.heads_q = heads_q;
     p.heads_kv = heads_kv;
-    const dim3 grid = rope_grid(n_tokens, (static_cast<int64_t>(heads_q) + heads_kv) * p.dim);
-    ead_rotate_kernel<kFmtBf16, true><<<grid, kRopeThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return launched();
+    return launch_rotate<kFmtBf16, true>(p, n_tokens, d->sms, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int ead_kv_rotate_write(const ead_rope *rope, const ead_kv_cache *cache, const ead_kv_batch *batch, const int32_t *positions,
@@ -334,13 +361,9 @@ extern "C" int ead_kv_rotate_write(const ead_rope *rope, const ead_kv_cache *cac
     p.heads_q = heads_q;
     p.heads_kv = p.cache.heads;
     p.status = status;
-    const dim3 grid = rope_grid(p.batch.n_tokens, q_row + 2 * kv_row);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cache->format == EAD_FMT_BF16)
-        ead_rotate_kernel<kFmtBf16, false><<<grid, kRopeThreads, 0, s>>>(p);
-    else
-        ead_rotate_kernel<kFmtE4m3, false><<<grid, kRopeThreads, 0, s>>>(p);
-    return launched();
+    return cache->format == EAD_FMT_BF16 ? launch_rotate<kFmtBf16, false>(p, p.batch.n_tokens, d->sms, s)
+                                         : launch_rotate<kFmtE4m3, false>(p, p.batch.n_tokens, d->sms, s);
 }
 
 extern "C" int ead_token_logprobs(const void *logits, int32_t format, int64_t stride, int32_t n_rows, int32_t V, const int32_t *tokens,
