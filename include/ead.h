@@ -569,7 +569,7 @@ typedef struct ead_e4m3_matrix {
  * defined above, for blocks of any of the three shapes.  A block with an x or gate that is not finite reads as NaNs.
  *   x, gate   dev, bf16 [rows, cols], x_stride and gate_stride elements apart; gate NULL: none (and none with 128 x 128 blocks)
  *   out       what is written; its codes' rows are block_cols wide stretches of y
- * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (more than 2^31 - 1 blocks of threads: rows x cols above 2^42 or so),
+ * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (rows x cols / 2048 above 2^32),
  * EAD_EUNSUPPORTED_ARCH, EAD_ECUDA.
  */
 int ead_quantise(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, const ead_e4m3_matrix *out, int32_t device,
@@ -580,7 +580,8 @@ int ead_quantise(const void *x, int64_t x_stride, const void *gate, int64_t gate
  *   x          1 x 32 or 1 x 128 blocks;  w  128 x 128 blocks;  the same number of columns
  *   bias       dev, bf16 [N] or NULL
  *   format     of out: EAD_FMT_BF16 or EAD_FMT_F32
- *   out        dev [T, N], out_stride elements apart (rows keep 16-byte alignment; N need not be a multiple of anything)
+ *   out        dev [T, N], out_stride elements apart; N need not be a multiple of anything, and no alignment is asked for beyond the
+ *              element's (rows that are 16-byte aligned are stored faster)
  *   status     dev uint32 or NULL.  EAD_STATUS_WAIT_EXPIRED: a bounded wait ran out (the output is not valid)
  * A NaN in a row of x or w makes that row or column of the output NaN and no other.  The result does not depend on the order in
  * which blocks run.  Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (N / 128 x T / 16 above 2^30),

@@ -24,6 +24,9 @@ constexpr double kLinJoinStages = 4;
 constexpr int kScoreBlocksPerSm = 2;
 constexpr int kScoreMinVectors = 256;
 
+// Passes of 512 values of a warp that quantises, and the warps per SM below which it has fewer.
+constexpr int kQuantMinPasses = 14;
+constexpr int kQuantWarpsPerSm = 64;
 // Warps per SM that a call with few tokens is divided into, for the rotation.
 constexpr int kRopeWarpsPerSm = 32;
 
@@ -162,10 +165,10 @@ int check_rope(const ead_rope *r, RopeParams *p)
 
 // A kernel whose setup runs under the end of the one before it in the stream.
 template <typename Params>
-int launch_early(void (*kernel)(Params), unsigned grid, int threads, const Params &p, cudaStream_t s)
+int launch_early(void (*kernel)(Params), dim3 grid, int threads, const Params &p, cudaStream_t s)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -224,7 +227,7 @@ extern "C" int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, co
     if ((format != EAD_FMT_BF16 && !f32) || x->cols != w->cols) return EAD_EINVALID_ARG;
     if (x->rows == 0 || w->rows == 0) return EAD_OK;
     if (!out || out_stride < w->rows) return EAD_EINVALID_ARG;
-    if (!aligned(out, 16) || out_stride % (f32 ? 4 : 8) || !aligned(bias, 2) || !aligned(status, 4)) return EAD_EALIGNMENT;
+    if (!aligned(out, f32 ? 4 : 2) || !aligned(bias, 2) || !aligned(status, 4)) return EAD_EALIGNMENT;
     LinearParams p{};
     p.x_scale = x->scale;
     p.w_scale = w->scale;
@@ -248,6 +251,7 @@ extern "C" int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, co
     p.whole = plan.whole;
     p.rest = plan.rest;
     p.split = plan.split;
+    p.wide = aligned(out, 16) && out_stride % (f32 ? 4 : 8) == 0;
     p.status = status;
     p.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     p.wait_hint = std::min(p.wait_ns, 20000u);
@@ -285,17 +289,17 @@ extern "C" int ead_quantise(const void *x, int64_t x_stride, const void *gate, i
     p.scale_cols = (p.cols + out->block_cols - 1) / out->block_cols;
     p.passes = (p.cols + kQuantPass - 1) / kQuantPass;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int64_t most = static_cast<int64_t>(kQuantWarpsPerSm) * d->sms;          // with few rows a warp has one pass, with many kQuantMinPasses
+    const int passes = static_cast<int>(std::min<int64_t>(kQuantMinPasses, std::max<int64_t>(1, static_cast<int64_t>(p.rows) * p.passes / most)));
+    p.split = (p.passes + passes - 1) / passes;
     const int64_t blocks = tiles ? static_cast<int64_t>((p.rows + int64_t{127}) / 128) * p.scale_cols
-                                 : (static_cast<int64_t>(p.rows) * p.passes + kQuantThreads / 32 - 1) / (kQuantThreads / 32);
-    if (blocks > 0x7fffffff) return EAD_ELIMIT;
+                                 : (static_cast<int64_t>(p.rows) * p.split + kQuantThreads / 32 - 1) / (kQuantThreads / 32);
+    if (blocks > 0x1fffffff) return EAD_ELIMIT;   // warps are counted in 32 bits
     const unsigned grid = static_cast<unsigned>(blocks);
-    if (tiles)
-        ead_quantise_tiles_kernel<<<grid, kQuantThreads, 0, s>>>(p);
-    else if (out->block_cols == 128)
-        gate ? ead_quantise_rows_kernel<128, true><<<grid, kQuantThreads, 0, s>>>(p) : ead_quantise_rows_kernel<128, false><<<grid, kQuantThreads, 0, s>>>(p);
-    else
-        gate ? ead_quantise_rows_kernel<32, true><<<grid, kQuantThreads, 0, s>>>(p) : ead_quantise_rows_kernel<32, false><<<grid, kQuantThreads, 0, s>>>(p);
-    return launched();
+    if (tiles) return launch_early(ead_quantise_tiles_kernel, grid, kQuantThreads, p, s);
+    if (out->block_cols == 128)
+        return gate ? launch_early(ead_quantise_rows_kernel<128, true>, grid, kQuantThreads, p, s) : launch_early(ead_quantise_rows_kernel<128, false>, grid, kQuantThreads, p, s);
+    return gate ? launch_early(ead_quantise_rows_kernel<32, true>, grid, kQuantThreads, p, s) : launch_early(ead_quantise_rows_kernel<32, false>, grid, kQuantThreads, p, s);
 }
 
 extern "C" int ead_qk_norm_rope(const ead_rope *rope, const int32_t *positions, int32_t n_tokens, const void *q, int64_t q_stride, int32_t heads_q,
@@ -404,11 +408,7 @@ extern "C" int ead_token_logprobs(const void *logits, int32_t format, int64_t st
     p.parts = static_cast<int>(std::max<int64_t>(parts, 1));
     const dim3 grid(p.parts, std::min(n_rows, 65535));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (format == EAD_FMT_BF16)
-        ead_token_logprobs_kernel<kFmtBf16><<<grid, kScoreThreads, 0, s>>>(p);
-    else if (format == EAD_FMT_F16)
-        ead_token_logprobs_kernel<kFmtF16><<<grid, kScoreThreads, 0, s>>>(p);
-    else
-        ead_token_logprobs_kernel<kFmtF32><<<grid, kScoreThreads, 0, s>>>(p);
-    return launched();
+    return format == EAD_FMT_BF16 ? launch_early(ead_token_logprobs_kernel<kFmtBf16>, grid, kScoreThreads, p, s)
+           : format == EAD_FMT_F16 ? launch_early(ead_token_logprobs_kernel<kFmtF16>, grid, kScoreThreads, p, s)
+                                   : launch_early(ead_token_logprobs_kernel<kFmtF32>, grid, kScoreThreads, p, s);
 }

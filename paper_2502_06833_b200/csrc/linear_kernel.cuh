@@ -48,6 +48,7 @@ struct LinearParams {
     int32_t rest;                                 // tiles behind them, one cluster each
     int32_t split;                                // blocks of a cluster (PAIR: 2)
     int32_t stages;
+    int32_t wide;                                 // the output's rows are 16-byte aligned
     uint32_t *status;
     uint32_t wait_ns, wait_hint;
 };
@@ -282,11 +283,25 @@ struct LinScales {
     }
 };
 
-// One warp's 32 features x up to 32 tokens, transposed through its own shared memory: rows of 32 features leave in 16-byte stores.
+// One warp's 32 features x up to 32 tokens, transposed through its own shared memory: rows of 32 features leave in 16-byte stores.  (Where the
+// output's rows are not aligned for that, an element per lane.)
 template <bool F32>
 __device__ __forceinline__ void store_outputs(const LinearParams &p, uint8_t *buf, const float (&v)[32], int lane, int feature0, int64_t token0, int tokens)
 {
     constexpr int kSize = F32 ? 4 : 2, kPer = 16 / kSize, kLanes = 32 / kPer;     // lanes of a row
+    if (!p.wide) {
+        uint8_t *const to = p.out + kSize * (token0 * p.out_stride + feature0 + lane);
+        if (feature0 + lane < p.N)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                if (j >= tokens) break;
+                if (F32)
+                    *reinterpret_cast<float *>(to + kSize * j * p.out_stride) = v[j];
+                else
+                    *reinterpret_cast<__nv_bfloat16 *>(to + kSize * j * p.out_stride) = __float2bfloat16_rn(v[j]);
+            }
+        return;
+    }
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < 32; ++j) {

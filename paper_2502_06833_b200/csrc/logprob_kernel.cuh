@@ -9,6 +9,7 @@
 #include <cuda_fp16.h>
 
 #include "kv_format.cuh"
+#include "ptx_sm100.cuh"
 #include "rmsnorm_kernel.cuh"
 
 namespace ead {
@@ -498,6 +499,8 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
 {
     __shared__ ScoreShared sh;
     constexpr int N = LogitVec<FMT>::kN;
+    griddep_wait();
+    griddep_launch_dependents();
     for (int row = blockIdx.y; row < p.n_rows; row += gridDim.y) {
         const uint8_t *const logits = p.logits + LogitVec<FMT>::kSize * (row * p.stride);
         const RowVectors<FMT> vec(logits, p.V);

@@ -16,6 +16,7 @@ struct QuantParams {
     int64_t x_stride, gate_stride, out_stride;     // elements
     int32_t rows, cols, scale_cols;
     int32_t passes;                                // ceil(cols / kQuantPass)
+    int32_t split;                                 // warps that share a row
 };
 
 __device__ __forceinline__ uint2 to_e4m3x8(const float (&y)[8], float inv)
@@ -34,56 +35,73 @@ __device__ __forceinline__ uint4 load_stream(const void *p)
 // g / (1 + e^-g): the exponential and the quotient by the special function unit, a few units of the last 32-bit place off.
 __device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.f + __expf(-g)); }
 
-// A warp takes kQuantPass values of a row, a lane 8 consecutive ones of each half: BLOCK / 8 neighbouring lanes share a scale.
+// A warp takes a stretch of a row, kQuantPass values at a time, a lane 8 consecutive ones of each half of them: BLOCK / 8 neighbouring lanes share a
+// scale.  The next values' loads are on their way under the arithmetic.
 template <int BLOCK, bool GATED>
 __global__ void __launch_bounds__(kQuantThreads) ead_quantise_rows_kernel(QuantParams p)
 {
+    griddep_wait();
+    griddep_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kQuantThreads / 32) + (threadIdx.x >> 5);
-    const int row = static_cast<int>(unit / p.passes);
+    const uint32_t unit = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);      // (the host sees to it that these fit)
+    const int row = static_cast<int>(unit / static_cast<uint32_t>(p.split)), share = static_cast<int>(unit - static_cast<uint32_t>(row) * p.split);
     if (row >= p.rows) return;
-    const int col0 = static_cast<int>(unit - static_cast<int64_t>(row) * p.passes) * kQuantPass + lane * 8;
+    const int pass0 = static_cast<int>(static_cast<int64_t>(p.passes) * share / p.split), pass1 = static_cast<int>(static_cast<int64_t>(p.passes) * (share + 1) / p.split);
+    const uint8_t *const x_row = p.x + 2 * row * p.x_stride, *const g_row = GATED ? p.gate + 2 * row * p.gate_stride : nullptr;
+    uint8_t *const out_row = p.out + row * p.out_stride, *const scale_row = p.out_scale + static_cast<int64_t>(row) * p.scale_cols;
     uint4 x[2], g[2];
+    auto load = [&](int pass) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int col = col0 + h * (kQuantPass / 2);
-        x[h] = g[h] = make_uint4(0, 0, 0, 0);
-        if (col < p.cols) {
-            x[h] = load_stream(p.x + 2 * (row * p.x_stride + col));
-            if (GATED) g[h] = load_stream(p.gate + 2 * (row * p.gate_stride + col));
-        }
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int col = col0 + h * (kQuantPass / 2);
-        float y[8];
-        unpack8(x[h], y);
-        if (GATED) {
-            float a[8];
-            unpack8(g[h], a);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] *= silu(a[k]);
-        }
-        uint32_t amax = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) amax = max(amax, abs_bits(y[k]));
-        if (GATED && amax >= 0x7f800000u) {        // a product of finite values that passes 32 bits saturates like any other large value
-            float u[8], a[8];
-            unpack8(x[h], u);
-            unpack8(g[h], a);
-            amax = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (abs_bits(y[k]) == 0x7f800000u && isfinite(u[k]) && isfinite(a[k])) y[k] = copysignf(3.402823466e38f, y[k]);
-                amax = max(amax, abs_bits(y[k]));
+        for (int h = 0; h < 2; ++h) {
+            const int col = pass * kQuantPass + h * (kQuantPass / 2) + lane * 8;
+            x[h] = g[h] = make_uint4(0, 0, 0, 0);
+            if (col < p.cols) {
+                x[h] = load_stream(x_row + 2 * static_cast<int64_t>(col));
+                if (GATED) g[h] = load_stream(g_row + 2 * static_cast<int64_t>(col));
             }
         }
+    };
+    load(pass0);
+    for (int pass = pass0; pass < pass1; ++pass) {
+        uint4 xn[2], gn[2];
 #pragma unroll
-        for (int o = 1; o < BLOCK / 8; o <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        const int byte = scale_byte(amax);
-        if (col < p.cols) {
-            *reinterpret_cast<uint2 *>(p.out + row * p.out_stride + col) = to_e4m3x8(y, inverse_scale(byte));
-            if ((lane & (BLOCK / 8 - 1)) == 0) p.out_scale[static_cast<int64_t>(row) * p.scale_cols + col / BLOCK] = static_cast<uint8_t>(byte);
+        for (int h = 0; h < 2; ++h) {
+            xn[h] = x[h];
+            gn[h] = g[h];
+        }
+        if (pass + 1 < pass1) load(pass + 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int col = pass * kQuantPass + h * (kQuantPass / 2) + lane * 8;
+            float y[8];
+            unpack8(xn[h], y);
+            if (GATED) {
+                float a[8];
+                unpack8(gn[h], a);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] *= silu(a[k]);
+            }
+            uint32_t amax = 0;
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) amax = __vimax3_u32(amax, abs_bits(y[k]), abs_bits(y[k + 1]));
+            if (GATED && amax >= 0x7f800000u) {    // a product of finite values that passes 32 bits saturates like any other large value
+                float u[8], a[8];
+                unpack8(xn[h], u);
+                unpack8(gn[h], a);
+                amax = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (abs_bits(y[k]) == 0x7f800000u && isfinite(u[k]) && isfinite(a[k])) y[k] = copysignf(3.402823466e38f, y[k]);
+                    amax = max(amax, abs_bits(y[k]));
+                }
+            }
+#pragma unroll
+            for (int o = 1; o < BLOCK / 8; o <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            const int byte = scale_byte(amax);
+            if (col < p.cols) {
+                *reinterpret_cast<uint2 *>(out_row + col) = to_e4m3x8(y, inverse_scale(byte));
+                if ((lane & (BLOCK / 8 - 1)) == 0) scale_row[col / BLOCK] = static_cast<uint8_t>(byte);
+            }
         }
     }
 }
@@ -92,6 +110,8 @@ __global__ void __launch_bounds__(kQuantThreads) ead_quantise_rows_kernel(QuantP
 __global__ void __launch_bounds__(kQuantThreads) ead_quantise_tiles_kernel(QuantParams p)
 {
     __shared__ uint32_t part[kQuantThreads / 32];
+    griddep_wait();
+    griddep_launch_dependents();
     const int64_t row0 = static_cast<int64_t>(blockIdx.x / p.scale_cols) * 128 + threadIdx.x / 16;
     const int col = static_cast<int>(blockIdx.x % p.scale_cols) * 128 + (threadIdx.x & 15) * 8;
     uint4 x[8];

@@ -88,6 +88,20 @@ def test_linear_rows_of_wider_buffers(E, block):
         p.check(p.run(E, torch.float32, bias, pad=16), bias)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,N,K", [(1, 203, 416), (40, 129, 2048), (241, 301, 128)])
+def test_linear_output_rows_anywhere(E, dtype, T, N, K):
+    """Rows that begin at any element; what lies before, between and behind them stays."""
+    p = Product(E, T, N, K, 128)
+    for offset, stride in ((0, N), (1, N + 2), (3, N + 5)):
+        flat = torch.full((offset + T * stride + 7,), -7.0, dtype=dtype, device="cuda")
+        out = flat[offset:offset + T * stride].view(T, stride)[:, :N]
+        E.ead_linear(p.mx, p.mw, out, bias=p.bias)
+        p.check(out.cpu())
+        out.fill_(-7.0)
+        assert (flat == -7.0).all()
+
+
 @pytest.mark.parametrize("T,N,K", [(1, 2048, 1536), (3, 128, 8192), (64, 1280, 5120), (300, 1300, 4096)])
 def test_linear_is_the_same_every_time(E, T, N, K):
     """Tiles cut along K are joined in the order of K, whichever block is slow."""

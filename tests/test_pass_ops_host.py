@@ -48,8 +48,8 @@ def test_bad_matrices_are_refused(E, bad, letter):
 
 
 @pytest.mark.parametrize("bad,letter", [
-    (dict(x=0), "I"), (dict(w=0), "I"), (dict(format=1), "I"), (dict(format=3), "I"), (dict(out=None), "I"), (dict(out=8200), "A"),
-    (dict(out_stride=127), "I"), (dict(out_stride=132), "A"), (dict(out_stride=130, format=2), "A"), (dict(status=4098), "A"), (dict(bias=4097), "A")])
+    (dict(x=0), "I"), (dict(w=0), "I"), (dict(format=1), "I"), (dict(format=3), "I"), (dict(out=None), "I"), (dict(out=8193), "A"),
+    (dict(out_stride=127), "I"), (dict(out=8194, format=2), "A"), (dict(status=4098), "A"), (dict(bias=4097), "A")])
 def test_bad_products_are_refused(E, bad, letter):
     assert _linear(E, **bad) == _code(E, letter)
 
