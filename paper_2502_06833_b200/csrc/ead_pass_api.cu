@@ -18,6 +18,9 @@ using namespace ead;
 
 namespace {
 
+// What a pair's tile costs beside its tokens, in tokens.  Measured, 4099 x 7168 x 5120, us per round of tiles: 9.8 for 96 tokens, 10.8 for 128, 12.4 for
+// 160, 13.3 for 192, 14.3 for 208, 16.0 for 240.
+constexpr int kLinPairFixed = 130;
 // What the join of a tile's parts costs, in stages of 128 values along K.
 constexpr double kLinJoinStages = 4;
 // Blocks of a call that scores few rows, per SM, and the least 16-byte vectors of a part.
@@ -78,7 +81,6 @@ struct LinearPlan {
     int tile_tokens, token_tiles, split, whole, rest, blocks;
 };
 
-// Costs are in cycles per 128 values along K.
 LinearPlan plan_linear(int T, int N, int kblocks, int block, const int *clusters)
 {
     const int most = block == 128 ? LinLayout<128>::kMaxTokens : LinLayout<32>::kMaxTokens;
@@ -112,7 +114,7 @@ LinearPlan plan_linear(int T, int N, int kblocks, int block, const int *clusters
     for (int64_t n = least; n <= least + pairs; ++n) {
         const int tile = static_cast<int>((T + n - 1) / n + 15) / 16 * 16;
         const int64_t tiles = feature_pairs * ((T + int64_t{tile} - 1) / tile), rounds = (tiles + pairs - 1) / pairs;
-        const int64_t t = rounds * std::max(200 * tile, 16400 + 64 * tile);
+        const int64_t t = rounds * (tile + kLinPairFixed);
         if (t < cost) {
             cost = t;
             best = LinearPlan{true, tile, static_cast<int>((T + int64_t{tile} - 1) / tile), 2, static_cast<int>(tiles), 0, static_cast<int>(2 * std::min(pairs, tiles))};

@@ -232,24 +232,14 @@ __device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// The scales of a row's blocks behind 128 values: of four stages one byte each (BLOCK = 128: kb = the first stage, n of them count), or
-// of the four blocks of 32 of stage kb; what lies behind the row's end is 0 (its values are zeros).
-template <int BLOCK>
-__device__ __forceinline__ uint32_t row_scales(const uint8_t *scale, int cols, int kb, int n)
+// n (at most 4) consecutive bytes from any address, 0 behind them, by one or two aligned loads.  (A word is only read if one of the n lies in it.)
+__device__ __forceinline__ uint32_t load_bytes(const uint8_t *p, int n)
 {
-    uint32_t v = 0;
-    if (BLOCK == 128) {
-        if (((cols | kb) & 3) == 0 && (reinterpret_cast<uintptr_t>(scale) & 3) == 0) return __ldg(reinterpret_cast<const uint32_t *>(scale + kb));
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) v |= static_cast<uint32_t>(__ldg(scale + kb + i)) << (8 * i);
-        return v;
-    }
-    if ((cols & 3) == 0) return __ldg(reinterpret_cast<const uint32_t *>(scale) + kb);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (4 * kb + i < cols) v |= static_cast<uint32_t>(__ldg(scale + 4 * kb + i)) << (8 * i);
-    return v;
+    if (n <= 0) return 0;
+    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 3u;
+    const uint32_t *const word = reinterpret_cast<const uint32_t *>(p - off);
+    const uint32_t lo = __ldg(word), hi = static_cast<int>(off) + n > 4 ? __ldg(word + 1) : 0;
+    return __funnelshift_r(lo, hi, 8 * off) & (n < 4 ? (1u << (8 * n)) - 1 : 0xffffffffu);
 }
 
 // A group of scales on its way from global to shared memory: of 4 x 32 tokens for up to four stages, and of the weights.
@@ -264,14 +254,22 @@ struct LinScales {
         const int token0 = first + c * 128 + lane, end = min(p.T, first + p.tile_tokens), n = min(4, g.k1 - kb);
         w = 0;
         if (feature_tile * kLinM < p.N)
-            w = row_scales<128>(p.w_scale + static_cast<int64_t>(feature_tile) * p.w_scale_cols, p.w_scale_cols, kb, n);
+            w = load_bytes(p.w_scale + static_cast<int64_t>(feature_tile) * p.w_scale_cols + kb, n);
+        const uint8_t *const row0 = p.x_scale + static_cast<int64_t>(token0) * p.x_scale_cols;
+        // of four stages one byte each, or of the four blocks of 32 of one stage: a word where rows are made of whole ones
+        const bool words = (p.x_scale_cols & 3) == 0 && (BLOCK == 32 || (kb & 3) == 0) && (reinterpret_cast<uintptr_t>(p.x_scale) & 3) == 0 && (BLOCK == 32 || n == 4);
 #pragma unroll
-        for (int i = 0; i < kSets; ++i)
+        for (int i = 0; i < kSets; ++i) {
+            const int at = BLOCK == 128 ? kb : 4 * (kb + i), count = BLOCK == 128 ? n : i < n ? min(4, p.x_scale_cols - at) : 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int t = token0 + 32 * j;
-                v[i][j] = t < end && i < n ? row_scales<BLOCK>(p.x_scale + static_cast<int64_t>(t) * p.x_scale_cols, p.x_scale_cols, kb + i, n) : 0;
+                const uint8_t *const from = row0 + 32 * j * p.x_scale_cols + at;
+                if (words)
+                    v[i][j] = token0 + 32 * j < end && i < n ? __ldg(reinterpret_cast<const uint32_t *>(from)) : 0;
+                else
+                    v[i][j] = token0 + 32 * j < end ? load_bytes(from, count) : 0;
             }
+        }
     }
     __device__ __forceinline__ void store(uint32_t group, int c, int chunks, int lane) const
     {
