@@ -18,9 +18,12 @@ using namespace ead;
 
 namespace {
 
-// What a pair's tile costs beside its tokens, in tokens.  Measured, 4099 x 7168 x 5120, us per round of tiles: 9.8 for 96 tokens, 10.8 for 128, 12.4 for
-// 160, 13.3 for 192, 14.3 for 208, 16.0 for 240.
-constexpr int kLinPairFixed = 130;
+// Most tokens of a product that single blocks serve.  Measured, 7168 x 5120, us, single blocks against pairs: 128 tokens 12.8 / 13.4, 160 tokens 14.2 / 14.0,
+// 200 tokens 17.2 / 14.2; 2048 x 5120: 160 tokens 10.5 / 11.5, 200 tokens 12.0 / 11.5; 14336 x 5120: 18.0 / 19.4, 21.7 / 20.3.
+constexpr int kLinFewTokens = 160;
+// What a pair's tile costs beside its tokens, in tokens.  Measured, us per round of tiles, 4099 x 7168 x 5120: 8.1 for 64 tokens, 9.5 for 96, 10.6 for 128, 11.8
+// for 160, 13.1 for 192, 14.3 for 208, 15.7 for 240; 1024 x 7168 x 5120: 7.2, 8.4, 9.1, 11.5, 12.0, 15.3, 16.5.
+constexpr int kLinPairFixed = 100;
 // What the join of a tile's parts costs, in stages of 128 values along K.
 constexpr double kLinJoinStages = 4;
 // Blocks of a call that scores few rows, per SM, and the least 16-byte vectors of a part.
@@ -42,11 +45,11 @@ bool prepare_linear()
     return cudaFuncSetAttribute(ead_linear_kernel<BLOCK, F32, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmem) == cudaSuccess;
 }
 
-cudaLaunchConfig_t linear_config(int blocks, int cluster, int smem, cudaStream_t s, cudaLaunchAttribute *attr)
+cudaLaunchConfig_t linear_config(int blocks, int threads, int cluster, int smem, cudaStream_t s, cudaLaunchAttribute *attr)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(kLinThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -68,7 +71,7 @@ int use_device(int device, DeviceInfo **out)
             return false;
         for (int c = 1; c <= kLinMaxSplit; ++c) {
             cudaLaunchAttribute attr[2];
-            const cudaLaunchConfig_t cfg = linear_config(c, c, kLinSmem, nullptr, attr);
+            const cudaLaunchConfig_t cfg = linear_config(c, LinLayout<128, false>::kThreads, c, kLinSmem, nullptr, attr);
             if (cudaOccupancyMaxActiveClusters(&g_clusters[device][c], ead_linear_kernel<128, false, false>, &cfg) != cudaSuccess) return false;
         }
         return true;
@@ -83,10 +86,10 @@ struct LinearPlan {
 
 LinearPlan plan_linear(int T, int N, int kblocks, int block, const int *clusters)
 {
-    const int most = block == 128 ? LinLayout<128>::kMaxTokens : LinLayout<32>::kMaxTokens;
+    const int most = block == 128 ? LinLayout<128, true>::kMaxTokens : LinLayout<32, true>::kMaxTokens;
     const int64_t features = (N + int64_t{kLinM} - 1) / kLinM;
     LinearPlan best{};
-    if (T <= most) {
+    if (T <= kLinFewTokens) {
         best.tile_tokens = (T + 15) / 16 * 16;
         best.token_tiles = 1;
         double cost = 1e300;
@@ -199,11 +202,11 @@ int launch_rotate(RopeParams &p, int n_tokens, int sms, cudaStream_t s)
 template <int BLOCK, bool F32, bool PAIR>
 int launch_linear(const CUtensorMap &tw, const CUtensorMap &tx, LinearParams p, int blocks, cudaStream_t s)
 {
-    using L = LinLayout<BLOCK>;
-    const int stage = L::stage_bytes(p.tile_tokens, PAIR);
+    using L = LinLayout<BLOCK, PAIR>;
+    const int stage = L::stage_bytes(p.tile_tokens);
     p.stages = std::min(kLinMaxStages, (kLinSmem - L::fixed_bytes()) / stage);
     cudaLaunchAttribute attr[2];
-    const cudaLaunchConfig_t cfg = linear_config(blocks, p.split, L::fixed_bytes() + p.stages * stage, s, attr);
+    const cudaLaunchConfig_t cfg = linear_config(blocks, L::kThreads, p.split, L::fixed_bytes() + p.stages * stage, s, attr);
     if (cudaLaunchKernelEx(&cfg, ead_linear_kernel<BLOCK, F32, PAIR>, tw, tx, p) != cudaSuccess) {
         cudaGetLastError();
         return EAD_ECUDA;

@@ -16,25 +16,30 @@
 
 namespace ead {
 
-constexpr int kLinThreads = 320;                  // a loading warp, an MMA warp, four warps for scales, four for the output
 constexpr int kLinM = 128, kLinK = 128;           // features and values along K of a stage
 constexpr int kLinMaxStages = 12;
-constexpr int kLinGroups = 3;                     // groups of scales in shared memory, each for 4 stages
+constexpr int kLinMaxGroups = 4;
 constexpr int kLinScaleBytes = 512;               // scales of 128 rows x 4 blocks along K
 constexpr int kLinOutBytes = 4096;                // 32 x 32 outputs of a warp
 constexpr int kLinSmem = 232448 - 2048;           // beside it: static shared memory and what the system takes
 constexpr int kLinMaxSplit = 8;                   // blocks of a cluster
 
 // BLOCK: values of a token that share a scale.  With 128 the four bytes of a TMEM column serve four stages, with 32 one.
-template <int BLOCK>
+template <int BLOCK, bool PAIR>
 struct LinLayout {
+    // Pairs of warps that bring groups of scales in turns, and groups in shared memory.  A pair's group takes longest on its way (its arrival
+    // crosses to the other block): four against two turns, 4099 x 7168 x 5120: 112 against 115 us, blocks of 32 124 against 153; a single block's
+    // first group comes later the more of them load at a time: 64 tokens 10.9 us with two, 11.2 with four, 200 tokens 22.4 and 28.5.
+    static constexpr int kTurns = PAIR ? 4 : 2, kGroups = PAIR ? 4 : 3;
+    static constexpr int kThreads = 32 * (6 + 2 * kTurns);       // a loading warp, an MMA warp, the warps for scales, four for the output
+    static_assert(kGroups <= kLinMaxGroups, "barriers");
     static constexpr int kTokenSets = BLOCK == 128 ? 1 : 4;                          // sets of token scales in a group
     static constexpr int kMaxTokens = BLOCK == 128 ? 240 : 208;                      // of a tile
     static constexpr int kGroupBytes = kLinScaleBytes * (1 + 2 * kTokenSets);        // weights, then up to 256 tokens per set
     static constexpr int kGroupColumns = 4 + 8 * kTokenSets;
     static_assert(2 * kMaxTokens + 2 * kGroupColumns <= 512, "TMEM");
-    __host__ __device__ static constexpr int stage_bytes(int tile_tokens, bool pair) { return kLinM * kLinK + (pair ? tile_tokens / 2 : tile_tokens) * kLinK; }
-    __host__ __device__ static constexpr int fixed_bytes() { return 1024 + kLinGroups * kGroupBytes + 4 * kLinOutBytes; }
+    __host__ __device__ static constexpr int stage_bytes(int tile_tokens) { return kLinM * kLinK + (PAIR ? tile_tokens / 2 : tile_tokens) * kLinK; }
+    __host__ __device__ static constexpr int fixed_bytes() { return 1024 + kGroups * kGroupBytes + 4 * kLinOutBytes; }
 };
 
 struct LinearParams {
@@ -245,7 +250,7 @@ __device__ __forceinline__ uint32_t load_bytes(const uint8_t *p, int n)
 // A group of scales on its way from global to shared memory: of 4 x 32 tokens for up to four stages, and of the weights.
 template <int BLOCK, bool PAIR>
 struct LinScales {
-    static constexpr int kSets = LinLayout<BLOCK>::kTokenSets;
+    static constexpr int kSets = LinLayout<BLOCK, PAIR>::kTokenSets;
     uint32_t v[kSets][4], w;
     // c: which 128 tokens of the tile
     __device__ __forceinline__ void load(const LinearParams &p, const LinSegment &g, int kb, int c, int lane, int rank)
@@ -359,31 +364,31 @@ __device__ __forceinline__ void add_parts(float (&v)[32], uint32_t at, int split
 }
 
 template <int BLOCK, bool F32, bool PAIR>
-__global__ void __launch_bounds__(kLinThreads, 1)
+__global__ void __launch_bounds__(LinLayout<BLOCK, PAIR>::kThreads, 1)
     ead_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinearParams p)
 {
-    using L = LinLayout<BLOCK>;
+    using L = LinLayout<BLOCK, PAIR>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t s_bars[2 * kLinMaxStages + 2 * kLinGroups + 5];
+    __shared__ alignas(8) uint64_t s_bars[2 * kLinMaxStages + 2 * kLinMaxGroups + 5];
     __shared__ uint32_t s_tmem, s_gave_up;
     __shared__ int s_loads;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const uint32_t S = p.stages;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
     const int pair_rank = PAIR ? rank : 0;
-    const uint32_t stage_bytes = L::stage_bytes(p.tile_tokens, PAIR);
-    const uint32_t groups = base + S * stage_bytes, out_smem = groups + kLinGroups * L::kGroupBytes;
+    const uint32_t stage_bytes = L::stage_bytes(p.tile_tokens);
+    const uint32_t groups = base + S * stage_bytes, out_smem = groups + L::kGroups * L::kGroupBytes;
     // tile and empty per stage, scales and empty per group (of a pair, what comes in is counted in the leading block for both)
     const uint32_t bar_tile = smem_u32(s_bars), bar_empty = bar_tile + 8 * kLinMaxStages;
-    const uint32_t bar_scale = bar_empty + 8 * kLinMaxStages, bar_scale_empty = bar_scale + 8 * kLinGroups;
-    const uint32_t bar_acc_full = bar_scale_empty + 8 * kLinGroups, bar_acc_empty = bar_acc_full + 16, bar_last = bar_acc_empty + 16;
+    const uint32_t bar_scale = bar_empty + 8 * kLinMaxStages, bar_scale_empty = bar_scale + 8 * kLinMaxGroups;
+    const uint32_t bar_acc_full = bar_scale_empty + 8 * kLinMaxGroups, bar_acc_empty = bar_acc_full + 16, bar_last = bar_acc_empty + 16;
     const int chunks = (p.tile_tokens + 127) >> 7;
     if (tid == 0) {
         for (uint32_t i = 0; i < S; ++i) {
             mbar_init(bar_tile + 8 * i, 1);
             mbar_init(bar_empty + 8 * i, 1);
         }
-        for (int i = 0; i < kLinGroups; ++i) {
+        for (int i = 0; i < L::kGroups; ++i) {
             mbar_init(bar_scale + 8 * i, PAIR ? 4 : 2);
             mbar_init(bar_scale_empty + 8 * i, 1);
         }
@@ -457,8 +462,9 @@ __global__ void __launch_bounds__(kLinThreads, 1)
                 go = wait(bar_acc_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1);
                 for (int kb = g.k0; go && kb < g.k1; kb += 4) {
                     const uint32_t ta = tmem + 2 * L::kMaxTokens + (n_groups & 1) * L::kGroupColumns, tb = ta + 4;
-                    // the columns were used two groups ago: one place further in the ring of three
-                    if (n_groups >= 2) go = wait(bar_scale_empty + 8 * (group.i == 2 ? 0 : group.i + 1), group.i == 2 ? group.phase : group.phase ^ 1);
+                    // the columns were used two groups ago
+                    if (n_groups >= 2)
+                        go = group.i >= 2 ? wait(bar_scale_empty + 8 * (group.i - 2), group.phase) : wait(bar_scale_empty + 8 * (group.i + L::kGroups - 2), group.phase ^ 1);
                     go = go && wait(bar_scale + 8 * group.i, group.phase);
                     if (!go) break;
                     tc_fence_after_sync();
@@ -484,22 +490,22 @@ __global__ void __launch_bounds__(kLinThreads, 1)
                         stage.next(S);
                     }
                     lin_commit<PAIR>(bar_scale_empty + 8 * group.i);
-                    group.next(kLinGroups);
+                    group.next(L::kGroups);
                     ++n_groups;
                 }
                 if (go) lin_commit<PAIR>(bar_acc_full + 8 * (n & 1));
             }
         }
-    } else if (warp < 6) {
+    } else if (warp < 2 + 2 * L::kTurns) {
         // ------------------------------------------------------------- scales: 128 tokens a warp, the second warp of two the weights' too; two
-        // warps take every other group (a group's way through one warp is about as long as its products take)
+        // of these warps take every L::kTurns-th group (a group's way through one warp is longer than its products take)
         const int c = warp & 1, turn = (warp - 2) >> 1;
         uint32_t n_groups = 0;
         const uint32_t leader_scale = PAIR ? cluster_addr(bar_scale, 0) : 0;
         bool go = true;
         while (go && work.get(p, g))
-            for (int kb = g.k0; kb < g.k1; kb += 4, group.next(kLinGroups), ++n_groups) {
-                if ((n_groups & 1) != turn) continue;
+            for (int kb = g.k0; kb < g.k1; kb += 4, group.next(L::kGroups), ++n_groups) {
+                if (n_groups % L::kTurns != turn) continue;
                 LinScales<BLOCK, PAIR> sc;        // (loads of the next group before this one's arrival would hold it up: it waits for them)
                 sc.load(p, g, kb, c, lane, pair_rank);
                 if (!(go = warp_wait(bar_scale_empty + 8 * group.i, group.phase ^ 1))) break;
@@ -575,7 +581,7 @@ __global__ void __launch_bounds__(kLinThreads, 1)
         }
     }
     __syncwarp();
-    if (!PAIR && p.split > 1 && p.rest && warp < 6) {
+    if (!PAIR && p.split > 1 && p.rest && warp < 2 + 2 * L::kTurns) {
         cluster_arrive();
         cluster_wait();
     }
