@@ -237,14 +237,14 @@ __device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// n (at most 4) consecutive bytes from any address, 0 behind them, by one or two aligned loads.  (A word is only read if one of the n lies in it.)
+// n (at most 4) consecutive bytes from any address, 0 behind them, by two aligned loads without a branch (a branch around a load keeps the next
+// one from being issued under it).  p is the address of a byte that is there; a word is only read if it has one.
 __device__ __forceinline__ uint32_t load_bytes(const uint8_t *p, int n)
 {
-    if (n <= 0) return 0;
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 3u;
     const uint32_t *const word = reinterpret_cast<const uint32_t *>(p - off);
-    const uint32_t lo = __ldg(word), hi = static_cast<int>(off) + n > 4 ? __ldg(word + 1) : 0;
-    return __funnelshift_r(lo, hi, 8 * off) & (n < 4 ? (1u << (8 * n)) - 1 : 0xffffffffu);
+    const uint32_t lo = __ldg(word), hi = __ldg(word + (static_cast<int>(off) + n > 4));
+    return __funnelshift_r(lo, hi, 8 * off) & (n >= 4 ? 0xffffffffu : (1u << (8 * max(n, 0))) - 1);
 }
 
 // A group of scales on its way from global to shared memory: of 4 x 32 tokens for up to four stages, and of the weights.
@@ -252,29 +252,44 @@ template <int BLOCK, bool PAIR>
 struct LinScales {
     static constexpr int kSets = LinLayout<BLOCK, PAIR>::kTokenSets;
     uint32_t v[kSets][4], w;
-    // c: which 128 tokens of the tile
+    // c: which 128 tokens of the tile.  What belongs to no token or stage may be anything: such rows and columns are not stored, and values behind a
+    // row's end are zeros (their scales are not NaN: 0).
     __device__ __forceinline__ void load(const LinearParams &p, const LinSegment &g, int kb, int c, int lane, int rank)
     {
-        const int feature_tile = LinWork<PAIR>::feature_tile(p, g, rank), first = LinWork<PAIR>::token0(p, g);
-        const int token0 = first + c * 128 + lane, end = min(p.T, first + p.tile_tokens), n = min(4, g.k1 - kb);
-        w = 0;
-        if (feature_tile * kLinM < p.N)
-            w = load_bytes(p.w_scale + static_cast<int64_t>(feature_tile) * p.w_scale_cols + kb, n);
-        const uint8_t *const row0 = p.x_scale + static_cast<int64_t>(token0) * p.x_scale_cols;
-        // of four stages one byte each, or of the four blocks of 32 of one stage: a word where rows are made of whole ones
-        const bool words = (p.x_scale_cols & 3) == 0 && (BLOCK == 32 || (kb & 3) == 0) && (reinterpret_cast<uintptr_t>(p.x_scale) & 3) == 0 && (BLOCK == 32 || n == 4);
+        const int first = LinWork<PAIR>::token0(p, g), last = min(p.T, first + p.tile_tokens) - 1, n = min(4, g.k1 - kb), cols = p.x_scale_cols;
+        const int at = BLOCK == 128 ? kb : 4 * kb;
+        const uint8_t *row[4];
 #pragma unroll
-        for (int i = 0; i < kSets; ++i) {
-            const int at = BLOCK == 128 ? kb : 4 * (kb + i), count = BLOCK == 128 ? n : i < n ? min(4, p.x_scale_cols - at) : 0;
+        for (int j = 0; j < 4; ++j) row[j] = p.x_scale + static_cast<int64_t>(min(first + c * 128 + 32 * j + lane, last)) * cols + at;
+        const uint32_t odd = cols | at | static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p.x_scale));      // alignment of all rows' pieces
+        if (BLOCK == 128) {                       // of four stages one byte each
+            if ((odd & 3) == 0 && n == 4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[0][j] = __ldg(reinterpret_cast<const uint32_t *>(row[j]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[0][j] = load_bytes(row[j], n);
+            }
+        } else if ((odd & 15) == 0) {             // of four stages four bytes each
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint8_t *const from = row0 + 32 * j * p.x_scale_cols + at;
-                if (words)
-                    v[i][j] = token0 + 32 * j < end && i < n ? __ldg(reinterpret_cast<const uint32_t *>(from)) : 0;
-                else
-                    v[i][j] = token0 + 32 * j < end ? load_bytes(from, count) : 0;
+                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(row[j]));
+                v[0][j] = x.x;
+                v[kSets - 3][j] = x.y;
+                v[kSets - 2][j] = x.z;
+                v[kSets - 1][j] = x.w;
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSets; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int count = i < n ? min(4, cols - at - 4 * i) : 0;
+                    v[i][j] = load_bytes(count > 0 ? row[j] + 4 * i : p.x_scale, count);
+                }
         }
+        const int feature_tile = min(LinWork<PAIR>::feature_tile(p, g, rank), (p.N - 1) / kLinM);
+        w = c == 1 ? load_bytes(p.w_scale + static_cast<int64_t>(feature_tile) * p.w_scale_cols + kb, n) : 0;
     }
     __device__ __forceinline__ void store(uint32_t group, int c, int chunks, int lane) const
     {
