@@ -91,6 +91,7 @@ __device__ __forceinline__ uint32_t cluster_ld_u32(uint32_t addr)
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void cluster_st(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ float cluster_ld(uint32_t addr)
 {
     float v;
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(LinLayout<BLOCK, PAIR>::kThreads, 1)
     using L = LinLayout<BLOCK, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ alignas(8) uint64_t s_bars[2 * kLinMaxStages + 2 * kLinMaxGroups + 5];
-    __shared__ uint32_t s_tmem, s_gave_up;
+    __shared__ uint32_t s_tmem, s_gave_up, s_peer_gave_up;
     __shared__ int s_loads;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const uint32_t S = p.stages;
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(LinLayout<BLOCK, PAIR>::kThreads, 1)
             mbar_init(bar_acc_empty + 8 * i, PAIR ? 8 : 4);
         }
         mbar_init(bar_last, 1);
-        s_gave_up = 0;
+        s_gave_up = s_peer_gave_up = 0;
         s_loads = 0;
         fence_mbar_init();
     }
@@ -602,12 +603,13 @@ __global__ void __launch_bounds__(LinLayout<BLOCK, PAIR>::kThreads, 1)
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (PAIR) {                                   // (of a pair, both end in this way if one does)
+    if (PAIR) {                                   // neither block leaves, or ends the other way below, before the other one is done
+        if (tid == 0 && s_gave_up) cluster_st(cluster_addr(smem_u32(&s_peer_gave_up), pair_rank ^ 1), 1u);
+        __syncwarp();
         cluster_arrive();
         cluster_wait();
     }
-    const bool gave_up = s_gave_up || (PAIR && cluster_ld_u32(cluster_addr(smem_u32(&s_gave_up), pair_rank ^ 1)));
-    if (gave_up) {                                // nobody sets it any more: wait for loads and products under way
+    if (s_gave_up || s_peer_gave_up) {            // nobody sets it any more: wait for loads and products under way
         if (warp == 0 && lane == 0 && pair_rank == 0) {
             const int n = static_cast<int>(S), other = PAIR ? static_cast<int>(cluster_ld_u32(cluster_addr(smem_u32(&s_loads), 1))) : s_loads;
             for (int i = min(s_loads, other); i < max(s_loads, other); ++i) {      // stages that only one block of the pair has asked for
@@ -624,8 +626,12 @@ __global__ void __launch_bounds__(LinLayout<BLOCK, PAIR>::kThreads, 1)
             wait_own(bar_last, 0);
         }
         __syncthreads();
+        if (PAIR) {
+            cluster_arrive();
+            cluster_wait();
+        }
     }
-    if (p.split > 1) {                            // nobody leaves while the others may read or signal its shared memory
+    if (!PAIR && p.split > 1) {                   // nobody leaves while the others may read its shared memory
         cluster_arrive_relaxed();
         cluster_wait();
     }
