@@ -581,11 +581,13 @@ def ead_rope(inv_freq, head_dim, *, interleaved=False, q_weight=None, k_weight=N
 
 
 def _heads(t, n, dim, what: str):
-    """Heads and row stride of a bf16 tensor ``[n, heads, dim]``; of None: none."""
+    """Address, heads and row stride of a bf16 tensor ``[n, heads, dim]``; of None: none."""
     if t is None:
-        return 0, 0
-    shape = (n, t.shape[1] if t.dim() == 3 else -1, dim)
-    return shape[1], _rows3(t, shape, what)
+        return None, 0, 0
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != n or shape[2] != dim:
+        raise ValueError(f"{what}: {tuple(shape)}, want {(n, 'heads', dim)}")
+    return t.data_ptr(), shape[1], _rows3(t, shape, what)
 
 
 def ead_qk_norm_rope(rope: EadRope, positions, q, k, q_out, k_out, *, device=0, stream=0) -> None:
@@ -593,11 +595,11 @@ def ead_qk_norm_rope(rope: EadRope, positions, q, k, q_out, k_out, *, device=0, 
     be the same tensors); ``positions`` int32 ``[n]``."""
     n, dim = positions.shape[0], rope.head_dim
     _dense(positions, (n,), _t().int32, "positions")
-    heads_q, q_stride = _heads(q, n, dim, "q")
-    heads_kv, k_stride = _heads(k, n, dim, "k")
+    q_at, heads_q, q_stride = _heads(q, n, dim, "q")
+    k_at, heads_kv, k_stride = _heads(k, n, dim, "k")
     qo_stride = _rows3(q_out, (n, heads_q, dim), "q_out") if heads_q else 0
     ko_stride = _rows3(k_out, (n, heads_kv, dim), "k_out") if heads_kv else 0
-    rc = lib().ead_qk_norm_rope(rope.ref, positions.data_ptr(), n, _ptr(q), q_stride, heads_q, _ptr(k), k_stride, heads_kv, _ptr(q_out),
+    rc = lib().ead_qk_norm_rope(rope.ref, positions.data_ptr(), n, q_at, q_stride, heads_q, k_at, k_stride, heads_kv, _ptr(q_out),
                                 qo_stride, _ptr(k_out), ko_stride, device, stream)
     if rc:
         _check(rc, "ead_qk_norm_rope")
@@ -608,15 +610,17 @@ def ead_kv_rotate_write(rope: EadRope, cache: EadKvCache, batch: EadKvBatch, q, 
     """Norm and rotation of the step's queries into ``q_out``, of its keys, with the values, into the cache; ``positions`` int32
     ``[n_tokens]``, by default the tokens' places in their contexts."""
     n, dim = batch.n_tokens, cache.head_dim
-    heads_q, q_stride = _heads(q, n, dim, "q")
+    q_at, heads_q, q_stride = _heads(q, n, dim, "q")
     qo_stride = _rows3(q_out, (n, heads_q, dim), "q_out") if heads_q else 0
-    kv_stride = _rows3(k, (n, cache.heads_kv, dim), "k")
-    if _rows3(v, (n, cache.heads_kv, dim), "v") != kv_stride:
+    shape = (n, cache.heads_kv, dim)
+    kv_stride = _rows3(k, shape, "k")
+    if _rows3(v, shape, "v") != kv_stride:
         raise ValueError("k and v: want the same row stride")
     if positions is not None:
         _dense(positions, (n,), _t().int32, "positions")
-    rc = lib().ead_kv_rotate_write(rope.ref, cache.ref, batch.ref, _ptr(positions), _ptr(q), q_stride, heads_q, k.data_ptr(), v.data_ptr(),
-                                   kv_stride, _ptr(q_out), qo_stride, _ptr(status), device, stream)
+    rc = lib().ead_kv_rotate_write(rope.ref, cache.ref, batch.ref, None if positions is None else positions.data_ptr(), q_at, q_stride, heads_q,
+                                   k.data_ptr(), v.data_ptr(), kv_stride, q_out.data_ptr() if heads_q else None, qo_stride,
+                                   None if status is None else status.data_ptr(), device, stream)
     if rc:
         _check(rc, "ead_kv_rotate_write")
 
@@ -628,21 +632,38 @@ def ead_token_logprobs(logits, tokens, *, workspace, logprob=None, entropy=None,
     Results go into the tensors that are given; ``workspace`` is a zero-filled buffer of ``EAD_LOGPROB_WORKSPACE_BYTES`` that
     calls which may overlap must not share."""
     T = _t()
-    formats = {T.bfloat16: EAD_FMT_BF16, T.float16: EAD_FMT_F16, T.float32: EAD_FMT_F32}
-    n, V = logits.shape
-    stride = _rows2(logits, logits.shape, "logits", formats)
-    k = 0
-    for t, dtype, name in ((tokens, T.int32, "tokens"), (logprob, T.float32, "logprob"), (entropy, T.float32, "entropy"), (rank, T.int32, "rank")):
-        if t is not None:
-            _dense(t, (n,), dtype, name)
-    for t, dtype, name in ((top, T.int32, "top"), (top_logprob, T.float32, "top_logprob")):
-        if t is not None:
-            k = t.shape[-1] if top is None else top.shape[-1]
-            _dense(t, (n, k), dtype, name)
+    n, V = shape = logits.shape
+    dtype = logits.dtype
+    if dtype is T.bfloat16:
+        fmt = EAD_FMT_BF16
+    elif dtype is T.float32:
+        fmt = EAD_FMT_F32
+    elif dtype is T.float16:
+        fmt = EAD_FMT_F16
+    else:
+        raise ValueError(f"logits: {dtype}, want bfloat16, float16 or float32")
+    stride = _rows2(logits, shape, "logits", (dtype,))
+    f32, i32, rows, k = T.float32, T.int32, (n,), 0
+    if top is not None or top_logprob is not None:
+        k = (top if top is not None else top_logprob).shape[-1]
+    given = tokens, logprob, entropy, rank, top, top_logprob, status
+    at = [None if t is None else t.data_ptr() for t in given]
+    if tokens is not None:
+        _dense(tokens, rows, i32, "tokens")
+    if logprob is not None:
+        _dense(logprob, rows, f32, "logprob")
+    if entropy is not None:
+        _dense(entropy, rows, f32, "entropy")
+    if rank is not None:
+        _dense(rank, rows, i32, "rank")
+    if top is not None:
+        _dense(top, (n, k), i32, "top")
+    if top_logprob is not None:
+        _dense(top_logprob, (n, k), f32, "top_logprob")
     if workspace.nbytes < EAD_LOGPROB_WORKSPACE_BYTES:
         raise ValueError("workspace: want EAD_LOGPROB_WORKSPACE_BYTES bytes")
-    rc = lib().ead_token_logprobs(logits.data_ptr(), formats[logits.dtype], stride, n, V, _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(rank),
-                                  k, _ptr(top), _ptr(top_logprob), workspace.data_ptr(), _ptr(status), device, stream)
+    rc = lib().ead_token_logprobs(logits.data_ptr(), fmt, stride, n, V, at[0], at[1], at[2], at[3], k, at[4], at[5], workspace.data_ptr(),
+                                  at[6], device, stream)
     if rc:
         _check(rc, "ead_token_logprobs")
 

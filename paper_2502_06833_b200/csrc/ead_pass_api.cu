@@ -28,7 +28,7 @@ constexpr int kLinPairFixed = 100;
 constexpr double kLinJoinStages = 4;
 // Blocks of a call that scores few rows, per SM, and the least 16-byte vectors of a part.
 constexpr int kScoreBlocksPerSm = 2;
-constexpr int kScoreMinVectors = 256;
+constexpr int kScoreMinVectors = kScoreUnroll * kScoreThreads;
 
 // Passes of 512 values of a warp that quantises, and the warps per SM below which it has fewer.
 constexpr int kQuantMinPasses = 14;
@@ -407,7 +407,7 @@ extern "C" int ead_token_logprobs(const void *logits, int32_t format, int64_t st
     p.status = status;
     const int per = format == EAD_FMT_F32 ? 4 : 8, blocks = kScoreBlocksPerSm * d->sms;
     const int64_t vectors = (static_cast<int64_t>(V) + per - 1) / per;
-    int64_t parts = std::min<int64_t>(blocks / n_rows, vectors / kScoreMinVectors);
+    int64_t parts = std::min<int64_t>(blocks / n_rows, (vectors + kScoreMinVectors - 1) / kScoreMinVectors);
     parts = std::min<int64_t>(parts, kScoreMaxParts);
     if (p.k) parts = std::min<int64_t>(parts, kScoreMaxJoin / p.k);
     p.parts = static_cast<int>(std::max<int64_t>(parts, 1));

@@ -44,6 +44,14 @@ struct ScoreSums {
     int before;                                   // logits that come before the given token
 };
 
+// A vector of -infinity.
+template <int FMT>
+__device__ __forceinline__ uint4 nothing()
+{
+    const uint32_t w = FMT == kFmtF32 ? 0xff800000u : FMT == kFmtF16 ? 0xfc00fc00u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+}
+
 // Larger logits have larger keys; equal ones larger keys for lower indices.  0 is below every logit's key.
 __device__ __forceinline__ uint32_t order_bits(float z)
 {
@@ -431,10 +439,12 @@ struct ScoreThread {
     CountAbove<FMT> above;
     int before;
     __device__ __forceinline__ ScoreThread() : m(-INFINITY), second(-INFINITY), at(0), m_log2(LogitVec<FMT>::kFloor * kLog2e), s(0), t(0), before(0) {}
-    // U vectors from g on, kScoreThreads apart; EDGE: some of their columns may lie outside the row.  g_given: the given token's vector.
-    template <int U, bool EDGE>
-    __device__ __forceinline__ void take(const RowVectors<FMT> &row, const uint4 (&v)[U], int g, bool given, float z_given, uint32_t t_or_equal, uint32_t t_above, int token, int g_given)
+    // A run of vectors from g on, kScoreThreads apart; EDGE: some of their columns may lie outside the row, vectors from g_end on are not the
+    // part's and -infinity.  g_given: the given token's vector.
+    template <bool EDGE>
+    __device__ __forceinline__ void take(const RowVectors<FMT> &row, const uint4 (&v)[kScoreUnroll], int g, int g_end, bool given, float z_given, uint32_t t_or_equal, uint32_t t_above, int token, int g_given)
     {
+        constexpr int U = kScoreUnroll;
         float top = largest<FMT>(v[0]);
 #pragma unroll
         for (int u = 1; u < U; ++u) top = fmaxf(top, largest<FMT>(v[u]));
@@ -466,17 +476,20 @@ struct ScoreThread {
             }
         }
         if (given && top >= z_given) {
+            const bool all_before = g + (U - 1) * kScoreThreads < g_given, all_behind = g > g_given;
+            if (!EDGE && (all_before || all_behind) && z_given != -INFINITY) {
+                const uint32_t t = all_before ? t_or_equal : t_above;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int gu = g + u * kScoreThreads;
-                if (EDGE || gu == g_given || z_given == -INFINITY) {
+                for (int u = 0; u < U; ++u) above.add(v[u], t);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
                     float z[N];
                     unpack_logits<FMT>(v[u], z);
-                    const int col = row.column(gu);
+                    const int gu = g + u * kScoreThreads, col = row.column(gu);
+                    if (EDGE && gu >= g_end) break;
 #pragma unroll
                     for (int i = 0; i < N; ++i) before += z[i] > z_given || (z[i] == z_given && col + i < token && col + i >= 0);
-                } else {
-                    above.add(v[u], gu < g_given ? t_or_equal : t_above);
                 }
             }
         }
@@ -506,6 +519,8 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
         const RowVectors<FMT> vec(logits, p.V);
         const int g0 = static_cast<int>(static_cast<int64_t>(vec.n) * blockIdx.x / p.parts);
         const int g1 = static_cast<int>(static_cast<int64_t>(vec.n) * (blockIdx.x + 1) / p.parts);
+        // (on its way while the token and its logit are looked up)
+        if (g0 + static_cast<int>(threadIdx.x) < g1) asm volatile("prefetch.global.L1 [%0];" ::"l"(vec.base + 16 * (static_cast<int64_t>(g0) + threadIdx.x)));
         const int token = p.tokens ? __ldg(p.tokens + row) : -1;
         const bool given = p.rank && token >= 0 && token < p.V;
         const float z_given = given ? logit_at<FMT>(logits, token) : INFINITY;
@@ -514,16 +529,17 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
         ScoreThread<FMT> th;
         const int n = g1 - g0, whole_end = vec.whole(g1 - 1) ? n : n - 1;                // vectors of this part
         int i = 0;
-        auto one = [&] {
-            const int g = g0 + i + threadIdx.x;
-            if (g < g1) {
-                const uint4 v[1] = {vec.raw(g)};
-                th.template take<1, true>(vec, v, g, given, z_given, t_or_equal, t_above, token, g_given);
-            }
-            i += kScoreThreads;
-        };
-        if (!vec.whole(g0)) one();                // (whole_end may then be wrong for a row of one vector: no quick run fits)
         constexpr int kRun = kScoreUnroll * kScoreThreads;
+        auto edge = [&] {                         // a run that may meet an end of the row or of the part
+            const int g = g0 + i + threadIdx.x;
+            uint4 v[kScoreUnroll];
+#pragma unroll
+            for (int u = 0; u < kScoreUnroll; ++u)
+                v[u] = static_cast<int64_t>(g) + u * kScoreThreads < g1 ? vec.raw(g + u * kScoreThreads) : nothing<FMT>();
+            if (g < g1) th.template take<true>(vec, v, g, g1, given, z_given, t_or_equal, t_above, token, g_given);
+            i += kRun;
+        };
+        if (!vec.whole(g0)) edge();               // (whole_end may then be wrong for a row of one vector: no quick run fits)
         while (i + kRun <= whole_end) {
             const int stop = min(whole_end, i + kScoreSettle * kRun);
             for (; i + kRun <= stop; i += kRun) {
@@ -532,11 +548,11 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
                 uint4 v[kScoreUnroll];
 #pragma unroll
                 for (int u = 0; u < kScoreUnroll; ++u) v[u] = load_logits(from + 16 * u * kScoreThreads);
-                th.template take<kScoreUnroll, false>(vec, v, g, given, z_given, t_or_equal, t_above, token, g_given);
+                th.template take<false>(vec, v, g, g1, given, z_given, t_or_equal, t_above, token, g_given);
             }
             th.above.settle();
         }
-        while (i < n) one();
+        while (i < n) edge();
         th.before += th.above.total;
         if (p.k) find_top<FMT>(sh, vec, g0, g1, th.m, th.at, th.second, p.k);
         ScoreSums a = block_sums(sh, th.sums(), LogitVec<FMT>::kFloor);
