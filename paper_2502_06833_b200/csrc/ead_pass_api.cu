@@ -191,12 +191,15 @@ int launch_early(void (*kernel)(Params), dim3 grid, int threads, const Params &p
 template <int FMT, bool DENSE>
 int launch_rotate(RopeParams &p, int n_tokens, int sms, cudaStream_t s)
 {
+    const bool halves = p.rot == p.dim && !p.interleaved;
+    const int run = halves ? 2 * kRopeRun : kRopeRun;
     const int64_t values = (static_cast<int64_t>(p.heads_q) + (DENSE ? 1 : 2) * p.heads_kv) * p.dim;
-    const int runs = static_cast<int>((values + kRopeRun - 1) / kRopeRun);
+    const int runs = static_cast<int>((values + run - 1) / run);
     p.n_tokens = n_tokens;
     p.split = static_cast<int>(std::min<int64_t>(runs, std::max<int64_t>(1, int64_t{kRopeWarpsPerSm} * sms / n_tokens)));
     const int64_t blocks = (static_cast<int64_t>(n_tokens) * p.split + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
-    return launch_early(ead_rotate_kernel<FMT, DENSE>, static_cast<unsigned>(blocks), kRopeThreads, p, s);
+    return halves ? launch_early(ead_rotate_halves_kernel<FMT, DENSE>, static_cast<unsigned>(blocks), kRopeThreads, p, s)
+                  : launch_early(ead_rotate_kernel<FMT, DENSE>, static_cast<unsigned>(blocks), kRopeThreads, p, s);
 }
 
 template <int BLOCK, bool F32, bool PAIR>

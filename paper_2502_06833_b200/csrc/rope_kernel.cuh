@@ -13,6 +13,8 @@
 namespace ead {
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeDepth = 4;                     // runs on their way to shared memory, the one that is read among them
+constexpr int kRopeAhead = 2;                     // runs that are on their way together
 constexpr int kRopeRun = 256;                     // elements that a warp takes at a time
 
 struct RopeParams {
@@ -119,6 +121,75 @@ __device__ __forceinline__ void norm_and_rotate(const RopeParams &p, const RopeL
     }
 }
 
+// The warp's token and share of its heads, and the token's place.
+struct RopeToken {
+    int t, share, position, page, slot;
+};
+// False: no token.
+__device__ __forceinline__ bool token_of(const RopeParams &p, int warp, RopeToken &k)
+{
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kRopeThreads / 32) + warp;
+    k.t = p.split == 1 ? static_cast<int>(unit) : static_cast<int>(unit / p.split);
+    k.share = static_cast<int>(unit - static_cast<int64_t>(k.t) * p.split);
+    k.page = k.slot = 0;
+    return k.t < p.n_tokens;
+}
+// False: the token has no place, nothing of it is written.
+template <bool DENSE>
+__device__ __forceinline__ bool find_place(const RopeParams &p, int lane, RopeToken &k)
+{
+    if (DENSE) {
+        k.position = __ldg(p.positions + k.t);
+        return true;
+    }
+    const int b = find_sequence(p.batch.new_start, p.batch.B, k.t, lane);
+    const int first = __ldg(p.batch.new_start + b), last = __ldg(p.batch.new_start + b + 1);
+    const bool bad = first < 0 || k.t < first || k.t >= last || last > p.batch.n_tokens || last - first > p.batch.max_new;
+    const int cached = __ldg(p.batch.kv_len + b) - (last - k.t);
+    k.page = bad ? -1 : find_page(p.cache, p.batch, b, cached);
+    k.position = p.positions ? __ldg(p.positions + k.t) : cached;
+    k.slot = cached & (p.cache.page_size - 1);
+    if (k.page < 0 && lane == 0 && k.share == 0) flag_status(p.status, bad ? kStatusBadCount : kStatusBadPage);
+    return k.page >= 0;
+}
+
+// Where a token's values go in a pool of the cache, from element e0 of a head on: its first head's, and the scale's (e4m3).
+struct RopePlace {
+    uint8_t *pool, *scale;
+};
+template <int FMT>
+__device__ __forceinline__ RopePlace place_of(const KvCacheView &c, const RopeToken &k, uint8_t *values, uint8_t *scales, int e0)
+{
+    RopePlace r;
+    r.pool = values + (FMT == kFmtBf16 ? 2 : 1) * (pool_offset(c, k.page, 0, k.slot) + e0);
+    r.scale = FMT == kFmtE4m3 ? scales + scale_offset(c, k.page, 0, k.slot) + (e0 >> 5) : nullptr;
+    return r;
+}
+// 8 elements of a head; 4 lanes hold a block of 32.
+template <int FMT>
+__device__ __forceinline__ void put8(const RopePlace &at, int64_t offset, int scale_offset, bool live, const f32x2 (&y)[4], int lane)
+{
+    if (FMT == kFmtBf16) {
+        if (live) *reinterpret_cast<uint4 *>(at.pool + 2 * offset) = to_bf16x8(y);
+        return;
+    }
+    float f[8];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        unpack2(y[j], f[2 * j], f[2 * j + 1]);
+        amax = __vimax3_u32(amax, abs_bits(f[2 * j]), abs_bits(f[2 * j + 1]));
+    }
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+    const int byte = scale_byte(amax);
+    if (live) {
+        *reinterpret_cast<uint2 *>(at.pool + offset) = to_e4m3x8(f, inverse_scale(byte));
+        if ((lane & 3) == 0) at.scale[scale_offset] = static_cast<uint8_t>(byte);
+    }
+}
+
+// The form for heads that are rotated in part or in neighbouring pairs.
 // Warp (token, share of its heads); queries first, then keys, then (for the cache) values, each in runs of kRopeRun elements.
 template <int FMT, bool DENSE>
 __global__ void __launch_bounds__(kRopeThreads, 4) ead_rotate_kernel(RopeParams p)
@@ -127,35 +198,18 @@ __global__ void __launch_bounds__(kRopeThreads, 4) ead_rotate_kernel(RopeParams 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     griddep_wait();
     griddep_launch_dependents();
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kRopeThreads / 32) + warp;
-    const int t = p.split == 1 ? static_cast<int>(unit) : static_cast<int>(unit / p.split), share = static_cast<int>(unit - static_cast<int64_t>(t) * p.split);
-    if (t >= p.n_tokens) return;
-    const int nq = p.heads_q * p.dim, nk = p.heads_kv * p.dim;
+    RopeToken k;
+    if (!token_of(p, warp, k) || !find_place<DENSE>(p, lane, k)) return;
+    const int t = k.t, nq = p.heads_q * p.dim, nk = p.heads_kv * p.dim;
     const int runs_q = (nq + kRopeRun - 1) / kRopeRun, runs_k = (nk + kRopeRun - 1) / kRopeRun, runs = runs_q + (DENSE ? 1 : 2) * runs_k;
-    const int begin = runs * share / p.split, end = runs * (share + 1) / p.split;
-    int position, page = 0, slot = 0;
-    if (DENSE) {
-        position = __ldg(p.positions + t);
-    } else {
-        const int b = find_sequence(p.batch.new_start, p.batch.B, t, lane);
-        const int first = __ldg(p.batch.new_start + b), last = __ldg(p.batch.new_start + b + 1);
-        const bool bad = first < 0 || t < first || t >= last || last > p.batch.n_tokens || last - first > p.batch.max_new;
-        const int cached = __ldg(p.batch.kv_len + b) - (last - t);
-        page = bad ? -1 : find_page(p.cache, p.batch, b, cached);
-        position = p.positions ? __ldg(p.positions + t) : cached;
-        slot = cached & (p.cache.page_size - 1);
-        if (page < 0) {                           // no place: nothing of the token is written
-            if (lane == 0 && share == 0) flag_status(p.status, bad ? kStatusBadCount : kStatusBadPage);
-            return;
-        }
-    }
+    const int begin = runs * k.share / p.split, end = runs * (k.share + 1) / p.split;
     float2 *const turn = s_turn[warp];
     const int in_head = lane & ((p.dim >> 3) - 1), e0 = in_head * 8, half = p.rot >> 1, shift = p.dim == 128 ? 7 : 6;
     RopeLane l;
     l.turned = e0 < p.rot;
     l.partner = p.interleaved ? -1 : !l.turned ? lane : e0 < half ? lane + (half >> 3) : lane - (half >> 3);
     if (begin < runs_q + runs_k) {                // (the angles are not for values)
-        for (int i = lane; i < half; i += 32) turn[i] = rotation(position, __ldg(p.inv_freq + i));
+        for (int i = lane; i < half; i += 32) turn[i] = rotation(k.position, __ldg(p.inv_freq + i));
         __syncwarp();
     }
     // Runs r0 .. r1 - 1 of one kind; `done` takes a run's elements.
@@ -163,15 +217,18 @@ __global__ void __launch_bounds__(kRopeThreads, 4) ead_rotate_kernel(RopeParams 
         const uint8_t *from = row + 2 * (r0 * kRopeRun + lane * 8);
         int e = r0 * kRopeRun + lane * 8;         // of a run's first element
         auto load = [&](int ahead) { return e + ahead * kRopeRun < n ? *reinterpret_cast<const uint4 *>(from + 2 * ahead * kRopeRun) : make_uint4(0, 0, 0, 0); };
-        uint4 x0 = load(0), x1 = r0 + 1 < r1 ? load(1) : x0;
-        for (int r = r0; r < r1; r += 2, e += 2 * kRopeRun, from += 4 * kRopeRun) {
-            const uint4 y0 = x0;
-            if (r + 2 < r1) x0 = load(2);
-            done(e, e < n, y0);
-            if (r + 1 >= r1) break;
-            const uint4 y1 = x1;
-            if (r + 3 < r1) x1 = load(3);
-            done(e + kRopeRun, e + kRopeRun < n, y1);
+        uint4 ahead[kRopeAhead];
+#pragma unroll
+        for (int i = 0; i < kRopeAhead; ++i)
+            if (r0 + i < r1) ahead[i] = load(i);
+        for (int r = r0; r < r1; r += kRopeAhead, e += kRopeAhead * kRopeRun, from += 2 * kRopeAhead * kRopeRun) {
+#pragma unroll
+            for (int i = 0; i < kRopeAhead; ++i) {
+                if (r + i >= r1) break;
+                const uint4 x = ahead[i];
+                if (r + kRopeAhead + i < r1) ahead[i] = load(kRopeAhead + i);
+                done(e + i * kRopeRun, e + i * kRopeRun < n, x);
+            }
         }
     };
     const int q1 = min(end, runs_q), k0 = max(begin, runs_q) - runs_q, k1 = min(end, runs_q + runs_k) - runs_q;
@@ -184,45 +241,17 @@ __global__ void __launch_bounds__(kRopeThreads, 4) ead_rotate_kernel(RopeParams 
             if (live) *reinterpret_cast<uint4 *>(to + 2 * e) = to_bf16x8(y);
         });
     }
-    // a key or value of the cache
-    uint8_t *pool = nullptr, *scale = nullptr;
     const int64_t head_stride = DENSE ? 0 : p.cache.head_stride;
     const int scale_stride = DENSE ? 0 : p.cache.page_size * (p.cache.head_dim / kFmtBlock);
-    auto put = [&](int e, bool live, const f32x2 (&y)[4]) {
-        const int head = e >> shift;
-        const int64_t to = head * head_stride;
-        if (FMT == kFmtBf16) {
-            if (live) *reinterpret_cast<uint4 *>(pool + 2 * to) = to_bf16x8(y);
-            return;
-        }
-        float f[8];
-        uint32_t amax = 0;                        // 4 lanes hold a block of 32
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            unpack2(y[j], f[2 * j], f[2 * j + 1]);
-            amax = __vimax3_u32(amax, abs_bits(f[2 * j]), abs_bits(f[2 * j + 1]));
-        }
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const int byte = scale_byte(amax);
-        if (live) {
-            *reinterpret_cast<uint2 *>(pool + to) = to_e4m3x8(f, inverse_scale(byte));
-            if ((lane & 3) == 0) scale[head * scale_stride] = static_cast<uint8_t>(byte);
-        }
-    };
-    auto set_pool = [&](uint8_t *values, uint8_t *scales) {
-        pool = values + (FMT == kFmtBf16 ? 2 : 1) * (pool_offset(p.cache, page, 0, slot) + e0);
-        if (FMT == kFmtE4m3) scale = scales + scale_offset(p.cache, page, 0, slot) + (e0 >> 5);
-    };
     if (k0 < k1) {
         set_factors(p, l, p.k_weight, turn, lane);
         uint8_t *const to = DENSE ? p.k_out + 2 * t * p.k_out_stride : nullptr;
-        if (!DENSE) set_pool(p.cache.k, p.cache.k_scale);
+        const RopePlace at = DENSE ? RopePlace{} : place_of<FMT>(p.cache, k, p.cache.k, p.cache.k_scale, e0);
         stream(k0, k1, p.k + 2 * t * p.kv_stride, nk, [&](int e, bool live, const uint4 &x) {
             f32x2 y[4];
             norm_and_rotate(p, l, x, y);
             if (!DENSE)
-                put(e, live, y);
+                put8<FMT>(at, (e >> shift) * head_stride, (e >> shift) * scale_stride, live, y, lane);
             else if (live)
                 *reinterpret_cast<uint4 *>(to + 2 * e) = to_bf16x8(y);
         });
@@ -230,15 +259,182 @@ __global__ void __launch_bounds__(kRopeThreads, 4) ead_rotate_kernel(RopeParams 
     if (DENSE) return;
     const int v0 = max(begin, runs_q + runs_k) - runs_q - runs_k, v1 = end - runs_q - runs_k;
     if (v0 < v1) {
-        set_pool(p.cache.v, p.cache.v_scale);
+        const RopePlace at = place_of<FMT>(p.cache, k, p.cache.v, p.cache.v_scale, e0);
         stream(v0, v1, p.v + 2 * t * p.kv_stride, nk, [&](int e, bool live, const uint4 &x) {
-            if (FMT == kFmtBf16) {
-                if (live) *reinterpret_cast<uint4 *>(pool + 2 * (e >> shift) * head_stride) = x;
-                return;
-            }
             f32x2 y[4];
             unpack8(x, y);
-            put(e, live, y);
+            put8<FMT>(at, (e >> shift) * head_stride, (e >> shift) * scale_stride, live, y, lane);
+        });
+    }
+}
+
+// 16 bytes to the thread's own place in shared memory, without a register on the way.
+__device__ __forceinline__ void copy_async_16(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_async_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared_16(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// The form for heads that are rotated as a whole, pairs in their two halves: a lane holds 8 elements of either half, so partners meet in a register
+// and half as many lanes share a sum.  What the warp reads depends on the token alone: it is on its way to shared memory, kRopeDepth runs deep, while
+// the token's place and angles are found.  (A lane copies and reads its own pieces: no barrier.)
+template <int FMT, bool DENSE>
+__global__ void __launch_bounds__(kRopeThreads, 2) ead_rotate_halves_kernel(RopeParams p)
+{
+    __shared__ alignas(16) float2 s_turn[kRopeThreads / 32][64];
+    __shared__ alignas(16) uint8_t s_ring[kRopeThreads / 32][kRopeDepth][2][512];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    griddep_wait();
+    griddep_launch_dependents();
+    const int half = p.dim >> 1, per_head = half >> 3, in_head = lane & (per_head - 1), e0 = in_head * 8, heads_run = 32 / per_head, head0 = lane / per_head;
+    const int runs_q = (p.heads_q + heads_run - 1) / heads_run, runs_k = (p.heads_kv + heads_run - 1) / heads_run, runs = runs_q + (DENSE ? 1 : 2) * runs_k;
+    RopeToken k;
+    if (!token_of(p, warp, k)) return;
+    const int begin = runs * k.share / p.split, end = runs * (k.share + 1) / p.split;
+    const uint32_t ring = smem_u32(s_ring[warp]) + lane * 16;
+    const uint8_t *const row_q = p.q + 2 * (k.t * p.q_stride + e0), *const row_k = p.k + 2 * (k.t * p.kv_stride + e0);
+    const uint8_t *const row_v = DENSE ? nullptr : p.v + 2 * (k.t * p.kv_stride + e0);
+    int asked = begin, to = 0, from = 0;          // next run to ask for, its place, and the place of the next one to read
+    auto ask = [&] {
+        if (asked < end) {
+            const int r = asked < runs_q ? asked : asked < runs_q + runs_k ? asked - runs_q : asked - runs_q - runs_k;
+            const uint8_t *const row = asked < runs_q ? row_q : asked < runs_q + runs_k ? row_k : row_v;
+            const int head = r * heads_run + head0;
+            if (head < (asked < runs_q ? p.heads_q : p.heads_kv)) {
+                copy_async_16(ring + to * 1024, row + 2 * head * p.dim);
+                copy_async_16(ring + to * 1024 + 512, row + 2 * (head * p.dim + half));
+            }
+            ++asked;
+            to = to + 1 == kRopeDepth ? 0 : to + 1;
+        }
+        copy_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kRopeDepth - 1; ++i) ask();
+    if (!find_place<DENSE>(p, lane, k)) {
+        copy_async_wait<0>();
+        return;
+    }
+    float2 *const turn = s_turn[warp];
+    if (begin < runs_q + runs_k) {                // (the angles are not for values)
+        for (int i = lane; i < half; i += 32) turn[i] = rotation(k.position, __ldg(p.inv_freq + i));
+        __syncwarp();
+    }
+    // Runs r0 .. r1 - 1 of n heads; `done` takes a run's head and the two pieces.
+    auto stream = [&](int r0, int r1, int n, auto done) {
+        for (int r = r0; r < r1; ++r) {
+            ask();
+            copy_async_wait<kRopeDepth - 1>();
+            const int head = r * heads_run + head0;
+            const bool live = head < n;
+            uint4 x = make_uint4(0, 0, 0, 0), y = x;
+            if (live) {
+                x = ld_shared_16(ring + from * 1024);
+                y = ld_shared_16(ring + from * 1024 + 512);
+            }
+            from = from + 1 == kRopeDepth ? 0 : from + 1;
+            done(head, live, x, y);
+        }
+    };
+    const int64_t head_stride = DENSE ? 0 : p.cache.head_stride;
+    const int scale_stride = DENSE ? 0 : p.cache.page_size * (p.cache.head_dim / kFmtBlock);
+    auto put = [&](const RopePlace &at, int head, bool live, const f32x2 (&y)[4], const f32x2 (&z)[4]) {
+        const RopePlace high{at.pool + (FMT == kFmtBf16 ? 2 : 1) * half, FMT == kFmtE4m3 ? at.scale + (half >> 5) : nullptr};
+        put8<FMT>(at, head * head_stride, head * scale_stride, live, y, lane);
+        put8<FMT>(high, head * head_stride, head * scale_stride, live, z, lane);
+    };
+    // Queries or keys: `weight` and the angles in four factors per pair of elements.
+    auto turn_heads = [&](int r0, int r1, int n, const uint8_t *weight, auto done) {
+        f32x2 fy[4], gy[4], fz[4], gz[4];
+        {
+            uint4 w = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), u = w;             // ones
+            if (weight) {
+                w = __ldg(reinterpret_cast<const uint4 *>(weight + 2 * e0));
+                u = __ldg(reinterpret_cast<const uint4 *>(weight + 2 * (e0 + half)));
+            }
+            f32x2 wy[4], wz[4];
+            unpack8(w, wy);
+            unpack8(u, wz);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 cs = *reinterpret_cast<const float4 *>(turn + e0 + 2 * i);
+                const f32x2 c = pack2(cs.x, cs.z), sn = pack2(cs.y, cs.w);
+                fy[i] = mul2(wy[i], c);
+                gy[i] = mul2(wz[i], pack2(-cs.y, -cs.w));
+                fz[i] = mul2(wz[i], c);
+                gz[i] = mul2(wy[i], sn);
+            }
+        }
+        stream(r0, r1, n, [&](int head, bool live, const uint4 &x, const uint4 &v) {
+            f32x2 a[4], b[4], y[4], z[4];
+            unpack8(x, a);
+            unpack8(v, b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i] = fma2(a[i], fy[i], mul2(b[i], gy[i]));
+                z[i] = fma2(b[i], fz[i], mul2(a[i], gz[i]));
+            }
+            if (weight) {
+                f32x2 squares = mul2(a[0], a[0]);
+#pragma unroll
+                for (int i = 1; i < 4; ++i) squares = fma2(a[i], a[i], squares);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) squares = fma2(b[i], b[i], squares);
+                float sum, odd;
+                unpack2(squares, sum, odd);
+                sum += odd;
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                if (per_head == 8) sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                const float r = rsqrtf(sum * (per_head == 8 ? 1.f / 128 : 1.f / 64) + p.eps);
+                const f32x2 rr = pack2(r, r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y[i] = mul2(y[i], rr);
+                    z[i] = mul2(z[i], rr);
+                }
+            }
+            done(head, live, y, z);
+        });
+    };
+    auto to_rows = [&](uint8_t *row) {
+        return [=](int head, bool live, const f32x2 (&y)[4], const f32x2 (&z)[4]) {
+            uint8_t *const to = row + 2 * (head * p.dim + e0);
+            if (!live) return;
+            *reinterpret_cast<uint4 *>(to) = to_bf16x8(y);
+            *reinterpret_cast<uint4 *>(to + 2 * half) = to_bf16x8(z);
+        };
+    };
+    const int q1 = min(end, runs_q), k0 = max(begin, runs_q) - runs_q, k1 = min(end, runs_q + runs_k) - runs_q;
+    if (begin < q1) turn_heads(begin, q1, p.heads_q, p.q_weight, to_rows(p.q_out + 2 * k.t * p.q_out_stride));
+    if (k0 < k1) {
+        if constexpr (DENSE) {
+            turn_heads(k0, k1, p.heads_kv, p.k_weight, to_rows(p.k_out + 2 * k.t * p.k_out_stride));
+        } else {
+            const RopePlace at = place_of<FMT>(p.cache, k, p.cache.k, p.cache.k_scale, e0);
+            turn_heads(k0, k1, p.heads_kv, p.k_weight, [&](int head, bool live, const f32x2 (&y)[4], const f32x2 (&z)[4]) { put(at, head, live, y, z); });
+        }
+    }
+    if (DENSE) return;
+    const int v0 = max(begin, runs_q + runs_k) - runs_q - runs_k, v1 = end - runs_q - runs_k;
+    if (v0 < v1) {
+        const RopePlace at = place_of<FMT>(p.cache, k, p.cache.v, p.cache.v_scale, e0);
+        stream(v0, v1, p.heads_kv, [&](int head, bool live, const uint4 &x, const uint4 &v) {
+            f32x2 y[4], z[4];
+            unpack8(x, y);
+            unpack8(v, z);
+            put(at, head, live, y, z);
         });
     }
 }
