@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "ead_internal.cuh"
+#include "ptx_sm100.cuh"
 
 namespace ead {
 
@@ -38,14 +39,15 @@ __device__ __forceinline__ void flag_status(uint32_t *status, uint32_t bits)
 
 // Largest b with start[b] <= t, found by the whole warp: every lane probes one of 32 equally spaced
 // entries, so 1024 sequences take two dependent loads instead of a binary search's ten.
-// start[0] = 0 and start[B] > t.
+// start[0] = 0 and start[B] > t.  BEHIND: see ld_behind.
+template <bool BEHIND = false>
 __device__ __forceinline__ int find_sequence(const int32_t *start, int B, int t, int lane)
 {
     int lo = 0, n = B;                            // the answer is in [lo, lo + n)
     while (n > 1) {
         const int step = (n + 31) >> 5;
         const int at = lo + lane * step;
-        const bool le = lane * step < n && __ldg(start + at) <= t;
+        const bool le = lane * step < n && (BEHIND ? ld_behind(start + at) : __ldg(start + at)) <= t;
         const unsigned hits = __ballot_sync(0xffffffffu, le);
         const int last = 31 - __clz(hits | 1u);
         lo += last * step;
@@ -55,10 +57,12 @@ __device__ __forceinline__ int find_sequence(const int32_t *start, int B, int t,
 }
 
 // Page that holds position `pos` of sequence b, or -1 (nothing there, or an index outside the pool).
+template <bool BEHIND = false>
 __device__ __forceinline__ int find_page(const KvCacheView &c, const KvBatchView &bt, int b, int pos)
 {
     if (pos < 0 || pos >= bt.max_len) return -1;
-    const int page = __ldg(bt.page_table + static_cast<int64_t>(b) * bt.table_stride + (pos >> c.page_shift));
+    const int32_t *const entry = bt.page_table + static_cast<int64_t>(b) * bt.table_stride + (pos >> c.page_shift);
+    const int page = BEHIND ? ld_behind(entry) : __ldg(entry);
     return page >= 0 && page < c.n_pages ? page : -1;
 }
 

@@ -244,7 +244,7 @@ __device__ __forceinline__ uint32_t load_bytes(const uint8_t *p, int n)
 {
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 3u;
     const uint32_t *const word = reinterpret_cast<const uint32_t *>(p - off);
-    const uint32_t lo = __ldg(word), hi = __ldg(word + (static_cast<int>(off) + n > 4));
+    const uint32_t lo = ld_behind(word), hi = ld_behind(word + (static_cast<int>(off) + n > 4));
     return __funnelshift_r(lo, hi, 8 * off) & (n >= 4 ? 0xffffffffu : (1u << (8 * max(n, 0))) - 1);
 }
 
@@ -266,7 +266,7 @@ struct LinScales {
         if (BLOCK == 128) {                       // of four stages one byte each
             if ((odd & 3) == 0 && n == 4) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[0][j] = __ldg(reinterpret_cast<const uint32_t *>(row[j]));
+                for (int j = 0; j < 4; ++j) v[0][j] = ld_behind(reinterpret_cast<const uint32_t *>(row[j]));
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[0][j] = load_bytes(row[j], n);
@@ -274,7 +274,7 @@ struct LinScales {
         } else if ((odd & 15) == 0) {             // of four stages four bytes each
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(row[j]));
+                const uint4 x = ld_behind(reinterpret_cast<const uint4 *>(row[j]));
                 v[0][j] = x.x;
                 v[kSets - 3][j] = x.y;
                 v[kSets - 2][j] = x.z;
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(LinLayout<BLOCK, PAIR>::kThreads, 1)
             token0 = LinWork<PAIR>::token0(p, g);
             tokens = min(p.tile_tokens, p.T - token0);
             joins = !PAIR && p.split > 1 && g.tile >= p.whole;
-            bias = p.bias && feature0 + lane < p.N ? __uint_as_float(static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(p.bias) + feature0 + lane)) << 16) : 0.f;
+            bias = p.bias && feature0 + lane < p.N ? __uint_as_float(static_cast<uint32_t>(ld_behind(reinterpret_cast<const uint16_t *>(p.bias) + feature0 + lane)) << 16) : 0.f;
             if (!warp_wait(bar_acc_full + 8 * (n & 1), (n >> 1) & 1)) break;
             tc_fence_after_sync();
             const uint32_t acc = tmem + (n & 1) * L::kMaxTokens + (static_cast<uint32_t>(quadrant) << 21);

@@ -74,15 +74,15 @@ struct LogitVec {
 
 __device__ __forceinline__ uint4 load_logits(const uint8_t *p)
 {
-    return __ldg(reinterpret_cast<const uint4 *>(p));
+    return ld_behind(reinterpret_cast<const uint4 *>(p));
 }
 
 template <int FMT>
 __device__ __forceinline__ float logit_at(const uint8_t *row, int64_t i)
 {
-    if (FMT == kFmtF32) return __ldg(reinterpret_cast<const float *>(row) + i);
-    if (FMT == kFmtBf16) return __uint_as_float(static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(row) + i)) << 16);
-    return __half2float(__ushort_as_half(__ldg(reinterpret_cast<const uint16_t *>(row) + i)));
+    if (FMT == kFmtF32) return ld_behind(reinterpret_cast<const float *>(row) + i);
+    if (FMT == kFmtBf16) return __uint_as_float(static_cast<uint32_t>(ld_behind(reinterpret_cast<const uint16_t *>(row) + i)) << 16);
+    return __half2float(__ushort_as_half(ld_behind(reinterpret_cast<const uint16_t *>(row) + i)));
 }
 
 template <int FMT>
@@ -130,9 +130,9 @@ struct RowVectors {
             const bool in = c >= 0 && c < V;
             const int64_t at = static_cast<int64_t>(g) * N + i;
             if (FMT == kFmtF32) {
-                w[i] = in ? __ldg(reinterpret_cast<const uint32_t *>(base) + at) : 0xff800000u;
+                w[i] = in ? ld_behind(reinterpret_cast<const uint32_t *>(base) + at) : 0xff800000u;
             } else {
-                const uint32_t h = in ? __ldg(reinterpret_cast<const uint16_t *>(base) + at) : FMT == kFmtF16 ? 0xfc00u : 0xff80u;
+                const uint32_t h = in ? ld_behind(reinterpret_cast<const uint16_t *>(base) + at) : FMT == kFmtF16 ? 0xfc00u : 0xff80u;
                 w[i / 2] = (i & 1) ? w[i / 2] | h << 16 : h;
             }
         }
@@ -342,7 +342,7 @@ __device__ __forceinline__ void write_scores(const ScoreParams &p, const ScoreSh
         if (bad) flag_status(p.status, kStatusNonFinite);
         if (p.entropy) p.entropy[row] = bad ? nan : fmaxf((log2_s - a.t / a.s) * kLn2Score, 0.f);
         if (p.tokens) {
-            const int token = __ldg(p.tokens + row);
+            const int token = ld_behind(p.tokens + row);
             const bool given = token >= 0 && token < p.V;
             if (token >= p.V) flag_status(p.status, kStatusBadToken);
             if (p.logprob) {
@@ -521,7 +521,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
         const int g1 = static_cast<int>(static_cast<int64_t>(vec.n) * (blockIdx.x + 1) / p.parts);
         // (on its way while the token and its logit are looked up)
         if (g0 + static_cast<int>(threadIdx.x) < g1) asm volatile("prefetch.global.L1 [%0];" ::"l"(vec.base + 16 * (static_cast<int64_t>(g0) + threadIdx.x)));
-        const int token = p.tokens ? __ldg(p.tokens + row) : -1;
+        const int token = p.tokens ? ld_behind(p.tokens + row) : -1;
         const bool given = p.rank && token >= 0 && token < p.V;
         const float z_given = given ? logit_at<FMT>(logits, token) : INFINITY;
         const int g_given = given ? static_cast<int>((static_cast<int64_t>(token) + vec.shift) / N) : 0;

@@ -33,6 +33,14 @@ __device__ __forceinline__ void griddep_launch_dependents()
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// A load for kernels that may start before the one that writes what they read has ended: the read-only path (__ldg) is for what stays the same
+// for the kernel's whole life, and its loads may be moved above the wait.
+template <typename T>
+__device__ __forceinline__ T ld_behind(const T *p)
+{
+    return *p;
+}
+
 // ----------------------------------------------------------------- mbarrier
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
 {

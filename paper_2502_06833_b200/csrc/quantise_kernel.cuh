@@ -3,6 +3,7 @@
 // Every value is read once and every code written once, so HBM bounds both at size and the launch at one step.
 #pragma once
 #include "kv_format.cuh"
+#include "ptx_sm100.cuh"
 #include "rmsnorm_kernel.cuh"
 
 namespace ead {
@@ -23,13 +24,6 @@ __device__ __forceinline__ uint2 to_e4m3x8(const float (&y)[8], float inv)
 {
     return make_uint2(to_e4m3x2(y[0] * inv, y[1] * inv) | to_e4m3x2(y[2] * inv, y[3] * inv) << 16,
                       to_e4m3x2(y[4] * inv, y[5] * inv) | to_e4m3x2(y[6] * inv, y[7] * inv) << 16);
-}
-
-__device__ __forceinline__ uint4 load_stream(const void *p)
-{
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
 }
 
 // g / (1 + e^-g): the exponential and the quotient by the special function unit, a few units of the last 32-bit place off.
@@ -56,8 +50,8 @@ __global__ void __launch_bounds__(kQuantThreads) ead_quantise_rows_kernel(QuantP
             const int col = pass * kQuantPass + h * (kQuantPass / 2) + lane * 8;
             x[h] = g[h] = make_uint4(0, 0, 0, 0);
             if (col < p.cols) {
-                x[h] = load_stream(x_row + 2 * static_cast<int64_t>(col));
-                if (GATED) g[h] = load_stream(g_row + 2 * static_cast<int64_t>(col));
+                x[h] = ld_behind(reinterpret_cast<const uint4 *>(x_row + 2 * static_cast<int64_t>(col)));
+                if (GATED) g[h] = ld_behind(reinterpret_cast<const uint4 *>(g_row + 2 * static_cast<int64_t>(col)));
             }
         }
     };
@@ -119,7 +113,7 @@ __global__ void __launch_bounds__(kQuantThreads) ead_quantise_tiles_kernel(Quant
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         x[i] = make_uint4(0, 0, 0, 0);
-        if (col < p.cols && row0 + 16 * i < p.rows) x[i] = load_stream(p.x + 2 * ((row0 + 16 * i) * p.x_stride + col));
+        if (col < p.cols && row0 + 16 * i < p.rows) x[i] = ld_behind(reinterpret_cast<const uint4 *>(p.x + 2 * ((row0 + 16 * i) * p.x_stride + col)));
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

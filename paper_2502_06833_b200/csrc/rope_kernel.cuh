@@ -14,7 +14,7 @@ namespace ead {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeDepth = 4;                     // runs on their way to shared memory, the one that is read among them
-constexpr int kRopeAhead = 2;                     // runs that are on their way together
+constexpr int kRopePartDepth = 6;                 // the same for heads that are rotated in part
 constexpr int kRopeRun = 256;                     // elements that a warp takes at a time
 
 struct RopeParams {
@@ -73,8 +73,8 @@ __device__ __forceinline__ void set_factors(const RopeParams &p, RopeLane &l, co
     uint4 w = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), o = w;                 // ones
     if (weight) {
         const int in_head = lane & ((p.dim >> 3) - 1);
-        w = o = __ldg(reinterpret_cast<const uint4 *>(weight) + in_head);
-        if (l.partner >= 0) o = __ldg(reinterpret_cast<const uint4 *>(weight) + (l.partner & ((p.dim >> 3) - 1)));
+        w = o = ld_behind(reinterpret_cast<const uint4 *>(weight) + in_head);
+        if (l.partner >= 0) o = ld_behind(reinterpret_cast<const uint4 *>(weight) + (l.partner & ((p.dim >> 3) - 1)));
     }
     if (l.partner < 0) o = make_uint4(__byte_perm(w.x, 0, 0x1032), __byte_perm(w.y, 0, 0x1032), __byte_perm(w.z, 0, 0x1032), __byte_perm(w.w, 0, 0x1032));
     f32x2 a[4], b[4];
@@ -139,15 +139,15 @@ template <bool DENSE>
 __device__ __forceinline__ bool find_place(const RopeParams &p, int lane, RopeToken &k)
 {
     if (DENSE) {
-        k.position = __ldg(p.positions + k.t);
+        k.position = ld_behind(p.positions + k.t);
         return true;
     }
-    const int b = find_sequence(p.batch.new_start, p.batch.B, k.t, lane);
-    const int first = __ldg(p.batch.new_start + b), last = __ldg(p.batch.new_start + b + 1);
+    const int b = find_sequence<true>(p.batch.new_start, p.batch.B, k.t, lane);
+    const int first = ld_behind(p.batch.new_start + b), last = ld_behind(p.batch.new_start + b + 1);
     const bool bad = first < 0 || k.t < first || k.t >= last || last > p.batch.n_tokens || last - first > p.batch.max_new;
-    const int cached = __ldg(p.batch.kv_len + b) - (last - k.t);
-    k.page = bad ? -1 : find_page(p.cache, p.batch, b, cached);
-    k.position = p.positions ? __ldg(p.positions + k.t) : cached;
+    const int cached = ld_behind(p.batch.kv_len + b) - (last - k.t);
+    k.page = bad ? -1 : find_page<true>(p.cache, p.batch, b, cached);
+    k.position = p.positions ? ld_behind(p.positions + k.t) : cached;
     k.slot = cached & (p.cache.page_size - 1);
     if (k.page < 0 && lane == 0 && k.share == 0) flag_status(p.status, bad ? kStatusBadCount : kStatusBadPage);
     return k.page >= 0;
@@ -189,85 +189,6 @@ __device__ __forceinline__ void put8(const RopePlace &at, int64_t offset, int sc
     }
 }
 
-// The form for heads that are rotated in part or in neighbouring pairs.
-// Warp (token, share of its heads); queries first, then keys, then (for the cache) values, each in runs of kRopeRun elements.
-template <int FMT, bool DENSE>
-__global__ void __launch_bounds__(kRopeThreads, 4) ead_rotate_kernel(RopeParams p)
-{
-    __shared__ alignas(16) float2 s_turn[kRopeThreads / 32][64];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    griddep_wait();
-    griddep_launch_dependents();
-    RopeToken k;
-    if (!token_of(p, warp, k) || !find_place<DENSE>(p, lane, k)) return;
-    const int t = k.t, nq = p.heads_q * p.dim, nk = p.heads_kv * p.dim;
-    const int runs_q = (nq + kRopeRun - 1) / kRopeRun, runs_k = (nk + kRopeRun - 1) / kRopeRun, runs = runs_q + (DENSE ? 1 : 2) * runs_k;
-    const int begin = runs * k.share / p.split, end = runs * (k.share + 1) / p.split;
-    float2 *const turn = s_turn[warp];
-    const int in_head = lane & ((p.dim >> 3) - 1), e0 = in_head * 8, half = p.rot >> 1, shift = p.dim == 128 ? 7 : 6;
-    RopeLane l;
-    l.turned = e0 < p.rot;
-    l.partner = p.interleaved ? -1 : !l.turned ? lane : e0 < half ? lane + (half >> 3) : lane - (half >> 3);
-    if (begin < runs_q + runs_k) {                // (the angles are not for values)
-        for (int i = lane; i < half; i += 32) turn[i] = rotation(k.position, __ldg(p.inv_freq + i));
-        __syncwarp();
-    }
-    // Runs r0 .. r1 - 1 of one kind; `done` takes a run's elements.
-    auto stream = [&](int r0, int r1, const uint8_t *row, int n, auto done) {
-        const uint8_t *from = row + 2 * (r0 * kRopeRun + lane * 8);
-        int e = r0 * kRopeRun + lane * 8;         // of a run's first element
-        auto load = [&](int ahead) { return e + ahead * kRopeRun < n ? *reinterpret_cast<const uint4 *>(from + 2 * ahead * kRopeRun) : make_uint4(0, 0, 0, 0); };
-        uint4 ahead[kRopeAhead];
-#pragma unroll
-        for (int i = 0; i < kRopeAhead; ++i)
-            if (r0 + i < r1) ahead[i] = load(i);
-        for (int r = r0; r < r1; r += kRopeAhead, e += kRopeAhead * kRopeRun, from += 2 * kRopeAhead * kRopeRun) {
-#pragma unroll
-            for (int i = 0; i < kRopeAhead; ++i) {
-                if (r + i >= r1) break;
-                const uint4 x = ahead[i];
-                if (r + kRopeAhead + i < r1) ahead[i] = load(kRopeAhead + i);
-                done(e + i * kRopeRun, e + i * kRopeRun < n, x);
-            }
-        }
-    };
-    const int q1 = min(end, runs_q), k0 = max(begin, runs_q) - runs_q, k1 = min(end, runs_q + runs_k) - runs_q;
-    if (begin < q1) {
-        set_factors(p, l, p.q_weight, turn, lane);
-        uint8_t *const to = p.q_out + 2 * t * p.q_out_stride;
-        stream(begin, q1, p.q + 2 * t * p.q_stride, nq, [&](int e, bool live, const uint4 &x) {
-            f32x2 y[4];
-            norm_and_rotate(p, l, x, y);
-            if (live) *reinterpret_cast<uint4 *>(to + 2 * e) = to_bf16x8(y);
-        });
-    }
-    const int64_t head_stride = DENSE ? 0 : p.cache.head_stride;
-    const int scale_stride = DENSE ? 0 : p.cache.page_size * (p.cache.head_dim / kFmtBlock);
-    if (k0 < k1) {
-        set_factors(p, l, p.k_weight, turn, lane);
-        uint8_t *const to = DENSE ? p.k_out + 2 * t * p.k_out_stride : nullptr;
-        const RopePlace at = DENSE ? RopePlace{} : place_of<FMT>(p.cache, k, p.cache.k, p.cache.k_scale, e0);
-        stream(k0, k1, p.k + 2 * t * p.kv_stride, nk, [&](int e, bool live, const uint4 &x) {
-            f32x2 y[4];
-            norm_and_rotate(p, l, x, y);
-            if (!DENSE)
-                put8<FMT>(at, (e >> shift) * head_stride, (e >> shift) * scale_stride, live, y, lane);
-            else if (live)
-                *reinterpret_cast<uint4 *>(to + 2 * e) = to_bf16x8(y);
-        });
-    }
-    if (DENSE) return;
-    const int v0 = max(begin, runs_q + runs_k) - runs_q - runs_k, v1 = end - runs_q - runs_k;
-    if (v0 < v1) {
-        const RopePlace at = place_of<FMT>(p.cache, k, p.cache.v, p.cache.v_scale, e0);
-        stream(v0, v1, p.v + 2 * t * p.kv_stride, nk, [&](int e, bool live, const uint4 &x) {
-            f32x2 y[4];
-            unpack8(x, y);
-            put8<FMT>(at, (e >> shift) * head_stride, (e >> shift) * scale_stride, live, y, lane);
-        });
-    }
-}
-
 // 16 bytes to the thread's own place in shared memory, without a register on the way.
 __device__ __forceinline__ void copy_async_16(uint32_t to, const void *from)
 {
@@ -284,6 +205,97 @@ __device__ __forceinline__ uint4 ld_shared_16(uint32_t addr)
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
+}
+
+// The form for heads that are rotated in part or in neighbouring pairs.
+// Warp (token, share of its heads); queries first, then keys, then (for the cache) values, each in runs of kRopeRun elements.
+template <int FMT, bool DENSE>
+__global__ void __launch_bounds__(kRopeThreads, 4) ead_rotate_kernel(RopeParams p)
+{
+    __shared__ alignas(16) float2 s_turn[kRopeThreads / 32][64];
+    __shared__ alignas(16) uint8_t s_ring[kRopeThreads / 32][kRopePartDepth][512];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    griddep_wait();
+    griddep_launch_dependents();
+    RopeToken k;
+    if (!token_of(p, warp, k)) return;
+    const int t = k.t, nq = p.heads_q * p.dim, nk = p.heads_kv * p.dim;
+    const int runs_q = (nq + kRopeRun - 1) / kRopeRun, runs_k = (nk + kRopeRun - 1) / kRopeRun, runs = runs_q + (DENSE ? 1 : 2) * runs_k;
+    const int begin = runs * k.share / p.split, end = runs * (k.share + 1) / p.split;
+    const uint32_t ring = smem_u32(s_ring[warp]) + lane * 16;
+    const uint8_t *const row_q = p.q + 2 * t * p.q_stride, *const row_k = p.k + 2 * t * p.kv_stride, *const row_v = DENSE ? nullptr : p.v + 2 * t * p.kv_stride;
+    int asked = begin, to_place = 0, from_place = 0;      // next run to ask for, its place, and the place of the next one to read
+    auto ask = [&] {
+        if (asked < end) {
+            const int r = asked < runs_q ? asked : asked < runs_q + runs_k ? asked - runs_q : asked - runs_q - runs_k, e = r * kRopeRun + lane * 8;
+            const uint8_t *const row = asked < runs_q ? row_q : asked < runs_q + runs_k ? row_k : row_v;
+            if (e < (asked < runs_q ? nq : nk)) copy_async_16(ring + to_place * 512, row + 2 * e);
+            ++asked;
+            to_place = to_place + 1 == kRopePartDepth ? 0 : to_place + 1;
+        }
+        copy_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kRopePartDepth - 1; ++i) ask();
+    if (!find_place<DENSE>(p, lane, k)) {
+        copy_async_wait<0>();
+        return;
+    }
+    float2 *const turn = s_turn[warp];
+    const int in_head = lane & ((p.dim >> 3) - 1), e0 = in_head * 8, half = p.rot >> 1, shift = p.dim == 128 ? 7 : 6;
+    RopeLane l;
+    l.turned = e0 < p.rot;
+    l.partner = p.interleaved ? -1 : !l.turned ? lane : e0 < half ? lane + (half >> 3) : lane - (half >> 3);
+    if (begin < runs_q + runs_k) {                // (the angles are not for values)
+        for (int i = lane; i < half; i += 32) turn[i] = rotation(k.position, ld_behind(p.inv_freq + i));
+        __syncwarp();
+    }
+    // Runs r0 .. r1 - 1 of one kind with n elements; `done` takes a run's elements.
+    auto stream = [&](int r0, int r1, int n, auto done) {
+        for (int r = r0; r < r1; ++r) {
+            ask();
+            copy_async_wait<kRopePartDepth - 1>();
+            const int e = r * kRopeRun + lane * 8;
+            const uint4 x = e < n ? ld_shared_16(ring + from_place * 512) : make_uint4(0, 0, 0, 0);
+            from_place = from_place + 1 == kRopePartDepth ? 0 : from_place + 1;
+            done(e, e < n, x);
+        }
+    };
+    const int q1 = min(end, runs_q), k0 = max(begin, runs_q) - runs_q, k1 = min(end, runs_q + runs_k) - runs_q;
+    if (begin < q1) {
+        set_factors(p, l, p.q_weight, turn, lane);
+        uint8_t *const to = p.q_out + 2 * t * p.q_out_stride;
+        stream(begin, q1, nq, [&](int e, bool live, const uint4 &x) {
+            f32x2 y[4];
+            norm_and_rotate(p, l, x, y);
+            if (live) *reinterpret_cast<uint4 *>(to + 2 * e) = to_bf16x8(y);
+        });
+    }
+    const int64_t head_stride = DENSE ? 0 : p.cache.head_stride;
+    const int scale_stride = DENSE ? 0 : p.cache.page_size * (p.cache.head_dim / kFmtBlock);
+    if (k0 < k1) {
+        set_factors(p, l, p.k_weight, turn, lane);
+        uint8_t *const to = DENSE ? p.k_out + 2 * t * p.k_out_stride : nullptr;
+        const RopePlace at = DENSE ? RopePlace{} : place_of<FMT>(p.cache, k, p.cache.k, p.cache.k_scale, e0);
+        stream(k0, k1, nk, [&](int e, bool live, const uint4 &x) {
+            f32x2 y[4];
+            norm_and_rotate(p, l, x, y);
+            if (!DENSE)
+                put8<FMT>(at, (e >> shift) * head_stride, (e >> shift) * scale_stride, live, y, lane);
+            else if (live)
+                *reinterpret_cast<uint4 *>(to + 2 * e) = to_bf16x8(y);
+        });
+    }
+    if (DENSE) return;
+    const int v0 = max(begin, runs_q + runs_k) - runs_q - runs_k, v1 = end - runs_q - runs_k;
+    if (v0 < v1) {
+        const RopePlace at = place_of<FMT>(p.cache, k, p.cache.v, p.cache.v_scale, e0);
+        stream(v0, v1, nk, [&](int e, bool live, const uint4 &x) {
+            f32x2 y[4];
+            unpack8(x, y);
+            put8<FMT>(at, (e >> shift) * head_stride, (e >> shift) * scale_stride, live, y, lane);
+        });
+    }
 }
 
 // The form for heads that are rotated as a whole, pairs in their two halves: a lane holds 8 elements of either half, so partners meet in a register
@@ -328,7 +340,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) ead_rotate_halves_kernel(Rope
     }
     float2 *const turn = s_turn[warp];
     if (begin < runs_q + runs_k) {                // (the angles are not for values)
-        for (int i = lane; i < half; i += 32) turn[i] = rotation(k.position, __ldg(p.inv_freq + i));
+        for (int i = lane; i < half; i += 32) turn[i] = rotation(k.position, ld_behind(p.inv_freq + i));
         __syncwarp();
     }
     // Runs r0 .. r1 - 1 of n heads; `done` takes a run's head and the two pieces.
@@ -360,8 +372,8 @@ __global__ void __launch_bounds__(kRopeThreads, 2) ead_rotate_halves_kernel(Rope
         {
             uint4 w = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), u = w;             // ones
             if (weight) {
-                w = __ldg(reinterpret_cast<const uint4 *>(weight + 2 * e0));
-                u = __ldg(reinterpret_cast<const uint4 *>(weight + 2 * (e0 + half)));
+                w = ld_behind(reinterpret_cast<const uint4 *>(weight + 2 * e0));
+                u = ld_behind(reinterpret_cast<const uint4 *>(weight + 2 * (e0 + half)));
             }
             f32x2 wy[4], wz[4];
             unpack8(w, wy);
