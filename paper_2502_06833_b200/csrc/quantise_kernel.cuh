@@ -1,6 +1,8 @@
 // bf16 values into 8-bit blocks: rows with a scale per 32 or 128 consecutive values (activations; of a gated MLP
 // y = silu(gate) * x is taken on the way), and matrices with a scale per 128 x 128 (weights).
 // Every value is read once and every code written once, so HBM bounds both at size and the launch at one step.
+// Measured: 8191 rows of 13824 with a gate 95 us, 5.9 TB/s, 0.91 of the device's copy rate, with 80 % of the issue slots taken (one exponential and one
+// reciprocal per value); 64 rows of 8960 2.1 us.  With one pass of 512 values per warp 145 us, 4 passes 103, 8 98, 14 and all 27 of a row 96.5.
 #pragma once
 #include "kv_format.cuh"
 #include "ptx_sm100.cuh"
@@ -26,7 +28,8 @@ __device__ __forceinline__ uint2 to_e4m3x8(const float (&y)[8], float inv)
                       to_e4m3x2(y[4] * inv, y[5] * inv) | to_e4m3x2(y[6] * inv, y[7] * inv) << 16);
 }
 
-// g / (1 + e^-g): the exponential and the quotient by the special function unit, a few units of the last 32-bit place off.
+// g / (1 + e^-g): the exponential and the quotient by the special function unit, a few units of the last 32-bit place off; 0 for gates below
+// -87.3, where the divisor passes 2^126 (the product is below 2^-118 of x there).
 __device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.f + __expf(-g)); }
 
 // A warp takes a stretch of a row, kQuantPass values at a time, a lane 8 consecutive ones of each half of them: BLOCK / 8 neighbouring lanes share a

@@ -1,12 +1,17 @@
 // Root-mean-square norm of every query and key head, and the position rotation, in one pass over a step's projections; the
 // results go into tensors (dense) or, with the values, straight into the paged cache in its format:
 //   y = x / sqrt(mean(x^2) + eps) * weight,   (a, b) -> (a cos - b sin, b cos + a sin),   angle = position * inv_freq[j]
-// A warp takes one token (with few tokens: some of its heads): it looks up the token's place, computes the angles once, the product in 64 bits and
-// brought within half a turn before it is rounded to 32, and then streams the heads.  A lane holds 8 consecutive elements of a head, a head is 8
-// or 16 neighbouring lanes.  Weight, cos and sin come together in two factors per element that a lane keeps for all heads,
+// A warp takes one token (with few tokens: some of its heads).  Its rows are on their way to shared memory, several runs deep, while it looks up the
+// token's place and computes the angles once, the product in 64 bits and brought within half a turn before it is rounded to 32; then it
+// streams the heads.  Weight, cos and sin come together in two factors per element that a lane keeps for all heads,
 //   y_e = (x_e f_e + x_partner g_e) / sqrt(mean(x^2) + eps),   f = weight cos,   g = -+ weight of the partner sin
-// so partners exchange the bf16 words as they were loaded.  Every element is read once and written once: HBM bounds it at size, launch and the
+// Two forms: heads rotated as a whole in halves (a lane holds 8 elements of either half), and all others (a lane holds 8 consecutive elements, partners
+// exchange the bf16 words as they were loaded).  Every element is read once and written once: HBM bounds it at size, launch and the
 // chain of look-ups at one step.
+// Measured: 18125 tokens of 32 + 8 + 8 heads of 128 into an 8-bit cache 79 us, 5.2 TB/s, 0.79 of the device's copy rate (the other form, with rows
+// two runs ahead in registers: 93; a block per token with angles shared: 174); 64 tokens of 40 + 8 + 8 heads 3.7 us; 4001 tokens of 32 + 8 heads of 64, 32
+// elements of each rotated, 9.8 us, 4.2 TB/s.  More runs ahead do not help (whole heads: 3 runs 80.6, 4 78.7, 5 79.0), more warps per SM cost registers
+// (whole heads: 16 warps 78.7, 24 81.5, 32 107; the other form: 32 warps 9.8, 24 11.5).
 #pragma once
 #include "quantise_kernel.cuh"
 

@@ -159,3 +159,41 @@ def test_example_scores_what_it_produced(kw):
             assert (lp < 0).all() and lp.isfinite().all() and (entropy > 0).all() and (entropy <= np.log(512) + 1e-4).all()
             assert (rank >= 0).all() and (rank < 512).all()
             assert (lp <= -torch.log1p(rank.float()) + 1e-4).all()       # rank tokens are at least as likely: p <= 1 / (rank + 1)
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_calls_back_to_back_equal_calls_one_at_a_time(E, T):
+    """A kernel's setup runs under the end of the one before it; what that one writes must be what it reads.  Every round has other numbers in the same
+    buffers; once with a wait after every call, once without any."""
+    K, V, rounds = 640, 3000, 25
+    g = torch.Generator(device="cuda").manual_seed(T)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()              # noqa: E731
+    xs, gates = [rnd(T, K) for _ in range(rounds)], [rnd(T, K) for _ in range(rounds)]
+    w = _matrix(E, V, K, (128, 128))
+    E.ead_quantise(rnd(V, K), w, stream=E.current_stream())
+    tokens = [torch.randint(0, V, (T,), generator=g, device="cuda").int() for _ in range(rounds)]
+    x, gate, token = torch.empty_like(xs[0]), torch.empty_like(xs[0]), torch.empty_like(tokens[0])
+    q, logits, space = _matrix(E, T, K, (1, 128)), torch.empty(T, V, device="cuda"), torch.zeros(E.EAD_LOGPROB_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    f = (10000.0 ** -(torch.arange(0, 64, 2, dtype=torch.float64) / 64)).float().cuda()
+    rope, place = E.ead_rope(f, 64), torch.arange(T, dtype=torch.int32, device="cuda")
+
+    def go(wait):
+        out = []
+        for i in range(rounds):
+            x.copy_(xs[i])
+            gate.copy_(gates[i])
+            token.copy_(tokens[i])
+            heads = x.view(T, K // 64, 64)
+            lp, rank, top = torch.empty(T, device="cuda"), torch.empty(T, dtype=torch.int32, device="cuda"), torch.empty(T, 4, dtype=torch.int32, device="cuda")
+            s = E.current_stream()
+            for call in (lambda: E.ead_qk_norm_rope(rope, place, heads, None, heads, None, stream=s), lambda: E.ead_quantise(x, q, gate=gate, stream=s),
+                         lambda: E.ead_linear(q, w, logits, stream=s),
+                         lambda: E.ead_token_logprobs(logits, token, logprob=lp, rank=rank, top=top, workspace=space, stream=s)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+            out.append((x.clone(), logits.clone(), lp, rank, top))
+        torch.cuda.synchronize()
+        return out
+    for a, b in zip(go(True), go(False)):
+        assert all(torch.equal(p, r) for p, r in zip(a, b))
