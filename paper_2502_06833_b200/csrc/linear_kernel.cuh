@@ -22,7 +22,8 @@
 // pairs, groups of scales, clusters, one issuing thread 183 / 14.3 / 23; its loop unrolled, four warps for scales, parts fetched 32 at a time 131 / 11.5 / 17;
 // setup under the end of the kernel before 131 / 10.7 / 16; tiles by measured cost 115; eight warps for scales 113 / - / 14.5; a row's scales of four stages in one
 // load 111 / 10.8 / 13.8.  Tried and not kept: the first weights brought into L2 before the wait for the kernel before (64 tokens 11.2); a group's scales
-// loaded before the last one's arrival (the arrival waits for the loads).
+// loaded before the last one's arrival (the arrival waits for the loads); parts sent to the block that adds them up instead of fetched by it (one token 7.2,
+// 64 tokens 13.1: the barrier then waits for the remote stores).
 #pragma once
 #include "attn_common.cuh"
 

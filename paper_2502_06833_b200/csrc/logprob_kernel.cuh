@@ -12,6 +12,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "kv_format.cuh"
 #include "ptx_sm100.cuh"
 #include "rmsnorm_kernel.cuh"
@@ -242,28 +244,34 @@ __device__ __forceinline__ void sort_candidates(ScoreShared &sh, int n, int k)
     __syncthreads();
 }
 
-// Largest of a vector's logits; a NaN is passed over.
-template <int FMT>
-__device__ __forceinline__ float largest(const uint4 &v)
+// Largest of some vectors' logits, 16-bit ones two at a time; a NaN is passed over.
+template <int FMT, int U>
+__device__ __forceinline__ float largest(const uint4 (&v)[U])
 {
     if constexpr (FMT == kFmtF32) {
-        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
-    } else if constexpr (FMT == kFmtBf16) {
-        const __nv_bfloat162 *const h = reinterpret_cast<const __nv_bfloat162 *>(&v);
-        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        return fmaxf(__low2float(m), __high2float(m));
+        const float *const z = reinterpret_cast<const float *>(v);
+        float m = z[0];
+#pragma unroll
+        for (int i = 1; i < 4 * U; ++i) m = fmaxf(m, z[i]);
+        return m;
     } else {
-        const __half2 *const h = reinterpret_cast<const __half2 *>(&v);
-        const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        return fmaxf(__low2float(m), __high2float(m));
+        using H = std::conditional_t<FMT == kFmtBf16, __nv_bfloat162, __half2>;
+        const H *const h = reinterpret_cast<const H *>(v);
+        H m[4] = {h[0], h[1], h[2], h[3]};
+#pragma unroll
+        for (int i = 4; i < 4 * U; ++i) m[i & 3] = __hmax2(m[i & 3], h[i]);
+        m[0] = __hmax2(__hmax2(m[0], m[1]), __hmax2(m[2], m[3]));
+        return fmaxf(__low2float(m[0]), __high2float(m[0]));
     }
 }
+
 // Puts a vector's logits that reach the bound among the candidates.
 template <int FMT>
 __device__ __forceinline__ void add_candidates(ScoreShared &sh, const RowVectors<FMT> &row, const uint4 &v, int g, uint32_t bound)
 {
     constexpr int N = LogitVec<FMT>::kN;
-    if (bound && order_bits(largest<FMT>(v)) < bound) return;
+    const uint4 one[1] = {v};
+    if (bound && order_bits(largest<FMT>(one)) < bound) return;
     float z[N];
     unpack_logits<FMT>(v, z);
 #pragma unroll
@@ -449,9 +457,7 @@ struct ScoreThread {
     __device__ __forceinline__ void take(const RowVectors<FMT> &row, const uint4 (&v)[kScoreUnroll], int g, int g_end, bool given, float z_given, uint32_t t_or_equal, uint32_t t_above, int token, int g_given)
     {
         constexpr int U = kScoreUnroll;
-        float top = largest<FMT>(v[0]);
-#pragma unroll
-        for (int u = 1; u < U; ++u) top = fmaxf(top, largest<FMT>(v[u]));
+        const float top = largest<FMT>(v);
         if (top <= m) {
             second = fmaxf(second, top);
         } else if (top > m) {
