@@ -567,6 +567,7 @@ typedef struct ead_e4m3_matrix {
 /*
  * y = x, or y = x * gate / (1 + e^-gate) with a gate (the activations of a gated MLP), into 8-bit blocks: scales and codes as
  * defined above, for blocks of any of the three shapes.  A block with an x or gate that is not finite reads as NaNs.
+ * A gate below -87.3 gives 0; a product of finite numbers beyond the largest 32-bit one is the block's largest code.
  *   x, gate   dev, bf16 [rows, cols], x_stride and gate_stride elements apart; gate NULL: none (and none with 128 x 128 blocks)
  *   out       what is written; its codes' rows are block_cols wide stretches of y
  * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (rows x cols / 2048 above 2^32),
@@ -595,8 +596,8 @@ int ead_linear(const ead_e4m3_matrix *x, const ead_e4m3_matrix *w, const void *b
  *   y = x / sqrt(mean(x^2) + eps) * weight
  * (without one y = x), then its first rot_dim elements in pairs (a, b), pair j turned by position * inv_freq[j]:
  *   (a, b) -> (a cos - b sin, b cos + a sin)
- * Pair j is elements j and j + rot_dim / 2, or 2j and 2j + 1 (interleaved).  The angle is exact to 32 bits of a turn at any
- * position; arithmetic is in 32 bits, rounded once at the end.
+ * Pair j is elements j and j + rot_dim / 2, or 2j and 2j + 1 (interleaved).  The angle is taken in 64 bits and brought
+ * within half a turn before it is rounded to 32; arithmetic is in 32 bits, rounded once at the end.
  */
 typedef struct ead_rope {
     int32_t head_dim;        /* 64 or 128                                                        */

@@ -5,8 +5,8 @@
 // logit, and only the few threads whose maximum reaches it can hold one of the k.  A thread knows the run of four vectors its maximum is in and the
 // largest logit of its other runs, so nearly always that run alone is read again, and what reaches the bound is sorted.  With few rows a row is cut
 // into parts, one block each; the last block of a row to finish joins the parts in their order, so the result does not depend on who comes last.
-// Measured, 2041 rows of 152064 in bf16: entropy alone 105 us, 6.0 TB/s, 0.91 of the device's copy rate; with the rank of a token 125, with 20
-// alternatives 124, with both 142: the special function unit is busy 56 % (an exponential per logit), 62 % of the issue slots are taken, and a row's end
+// Measured, 2041 rows of 152064 in bf16: entropy alone 107 us, 5.9 TB/s, 0.90 of the device's copy rate; with the rank of a token 124, with 20
+// alternatives 124, with both 141: the special function unit is busy 56 % (an exponential per logit), 62 % of the issue slots are taken, and a row's end
 // (bound, second look, sort) is a chain of barriers that four other rows of the SM have to cover.  One row of 128256 in 32 bits 8.8 us, a chain of
 // look-ups, loads and the join.  On the way: a list per thread's strip read again 187, one element at a time 295; rows in two parts 174.
 #pragma once
