@@ -114,6 +114,7 @@ LinearPlan plan_linear(int T, int N, int kblocks, int block, const int *clusters
         }
         return best;
     }
+    if (clusters[2] < 1) return best;             // no pair fits (a device of which only a part is there): refused
     const int64_t pairs = clusters[2], feature_pairs = (features + 1) / 2, least = (T + int64_t{most} - 1) / most;
     int64_t cost = INT64_MAX;
     for (int64_t n = least; n <= least + pairs; ++n) {
