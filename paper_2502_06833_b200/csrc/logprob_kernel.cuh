@@ -189,6 +189,8 @@ struct ScoreShared {
     uint2 warp_range[kScoreThreads / 32];
     int run[kScoreThreads], strip[kScoreThreads]; // of threads whose maximum reaches the bound: its run's first vector, or the thread
     int n_runs, n_strips, n_cand, last;
+    int token;                                    // of thread 0 alone, for the row's end: the given token and its logit
+    float z_given;
 };
 
 // Sums over the block, in every thread.  (The tree is the same whatever the timing.)
@@ -343,8 +345,7 @@ __device__ __forceinline__ void find_top(ScoreShared &sh, const RowVectors<FMT> 
 }
 
 // The row's answers from its sums and its best keys.
-template <int FMT>
-__device__ __forceinline__ void write_scores(const ScoreParams &p, const ScoreShared &sh, int row, const uint8_t *logits, const ScoreSums &a)
+__device__ __forceinline__ void write_scores(const ScoreParams &p, const ScoreShared &sh, int row, const ScoreSums &a)
 {
     const float m = fmaxf(a.m, kLowest);
     // NaN or +infinity among the logits, or nothing but -infinity
@@ -354,12 +355,11 @@ __device__ __forceinline__ void write_scores(const ScoreParams &p, const ScoreSh
         if (bad) flag_status(p.status, kStatusNonFinite);
         if (p.entropy) p.entropy[row] = bad ? nan : fmaxf((log2_s - a.t / a.s) * kLn2Score, 0.f);
         if (p.tokens) {
-            const int token = ld_behind(p.tokens + row);
+            const int token = sh.token;
             const bool given = token >= 0 && token < p.V;
             if (token >= p.V) flag_status(p.status, kStatusBadToken);
             if (p.logprob) {
-                const float z = given ? logit_at<FMT>(logits, token) : 0.f;
-                p.logprob[row] = bad || !given ? nan : (z - m) - log2_s * kLn2Score;
+                p.logprob[row] = bad || !given ? nan : (sh.z_given - m) - log2_s * kLn2Score;
             }
             if (p.rank) p.rank[row] = bad || !given ? -1 : a.before;
         }
@@ -532,8 +532,13 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
         // (on its way while the token and its logit are looked up)
         if (g0 + static_cast<int>(threadIdx.x) < g1) asm volatile("prefetch.global.L1 [%0];" ::"l"(vec.base + 16 * (static_cast<int64_t>(g0) + threadIdx.x)));
         const int token = p.tokens ? ld_behind(p.tokens + row) : -1;
+        const float z_token = token >= 0 && token < p.V ? logit_at<FMT>(logits, token) : 0.f;
+        if (threadIdx.x == 0) {
+            sh.token = token;
+            sh.z_given = z_token;
+        }
         const bool given = p.rank && token >= 0 && token < p.V;
-        const float z_given = given ? logit_at<FMT>(logits, token) : INFINITY;
+        const float z_given = given ? z_token : INFINITY;
         const int g_given = given ? static_cast<int>((static_cast<int64_t>(token) + vec.shift) / N) : 0;
         const uint32_t t_or_equal = threshold<FMT>(z_given, false), t_above = threshold<FMT>(z_given, true);
         ScoreThread<FMT> th;
@@ -584,7 +589,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
             a.before = before;
         }
         if (p.parts == 1) {
-            write_scores<FMT>(p, sh, row, logits, a);
+            write_scores(p, sh, row, a);
             __syncthreads();
             continue;
         }
@@ -620,7 +625,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
             __syncthreads();
             sort_candidates(sh, sh.n_cand, p.k);
         }
-        write_scores<FMT>(p, sh, row, logits, all);
+        write_scores(p, sh, row, all);
         if (threadIdx.x == 0) *counter = 0;       // ready for the next call
         __syncthreads();
     }
