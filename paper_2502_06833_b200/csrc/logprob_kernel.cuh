@@ -5,9 +5,9 @@
 // logit, and only the few threads whose maximum reaches it can hold one of the k.  A thread knows the run of four vectors its maximum is in and the
 // largest logit of its other runs, so nearly always that run alone is read again, and what reaches the bound is sorted.  With few rows a row is cut
 // into parts, one block each; the last block of a row to finish joins the parts in their order, so the result does not depend on who comes last.
-// Measured, 2041 rows of 152064 in bf16: entropy alone 107 us, 5.9 TB/s, 0.90 of the device's copy rate; with the rank of a token 124, with 20
-// alternatives 124, with both 141: the special function unit is busy 56 % (an exponential per logit), 62 % of the issue slots are taken, and a row's end
-// (bound, second look, sort) is a chain of barriers that four other rows of the SM have to cover.  One row of 128256 in 32 bits 8.8 us, a chain of
+// Measured, 2041 rows of 152064 in bf16: entropy alone 106 us, 5.9 TB/s, 0.90 of the device's copy rate; with the rank of a token 122, with 20
+// alternatives 121, with both 139: the special function unit is busy 56 % (an exponential per logit), 62 % of the issue slots are taken, and a row's end
+// (bound, second look, sort) is a chain of barriers that four other rows of the SM have to cover.  One row of 128256 in 32 bits 8.5 us, a chain of
 // look-ups, loads and the join.  On the way: a list per thread's strip read again 187, one element at a time 295; rows in two parts 174.
 #pragma once
 #include <cuda_fp16.h>
@@ -193,18 +193,28 @@ struct ScoreShared {
     float z_given;
 };
 
-// Sums over the block, in every thread.  (The tree is the same whatever the timing.)
-__device__ __forceinline__ ScoreSums block_sums(ScoreShared &sh, ScoreSums a, float low)
+// Sums over the block in two halves with a barrier between: of each warp, into shared memory; and of the warps, in every thread.  (The tree is the
+// same whatever the timing.)
+__device__ __forceinline__ void warp_sums(ScoreShared &sh, ScoreSums a, float low)
 {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) a = join_sums(a, shuffle_xor(a, o), low);
     if ((threadIdx.x & 31) == 0) sh.warp_sums[threadIdx.x >> 5] = a;
-    __syncthreads();
-    a = sh.warp_sums[threadIdx.x & (kScoreThreads / 32 - 1)];
-    __syncthreads();                              // it may be written again
+}
+__device__ __forceinline__ ScoreSums sums_of_warps(const ScoreShared &sh, float low)
+{
+    ScoreSums a = sh.warp_sums[threadIdx.x & (kScoreThreads / 32 - 1)];
 #pragma unroll
     for (int o = 1; o < kScoreThreads / 32; o <<= 1) a = join_sums(a, shuffle_xor(a, o), low);
     return a;
+}
+// Both; whoever read earlier sums may still be at it.
+__device__ __forceinline__ ScoreSums block_sums(ScoreShared &sh, const ScoreSums &a, float low)
+{
+    __syncthreads();
+    warp_sums(sh, a, low);
+    __syncthreads();
+    return sums_of_warps(sh, low);
 }
 
 // A lower bound of the k-th largest of the threads' keys (32 bits, 0: none) that few more than k of them reach; 0 if fewer than k
@@ -569,8 +579,12 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
         }
         while (i < n) edge();
         th.before += th.above.total;
-        if (p.k) find_top<FMT>(sh, vec, g0, g1, th.m, th.at, th.second, p.k);
-        ScoreSums a = block_sums(sh, th.sums(), LogitVec<FMT>::kFloor);
+        warp_sums(sh, th.sums(), LogitVec<FMT>::kFloor);
+        if (p.k)
+            find_top<FMT>(sh, vec, g0, g1, th.m, th.at, th.second, p.k);      // (with barriers of its own)
+        else
+            __syncthreads();
+        ScoreSums a = sums_of_warps(sh, LogitVec<FMT>::kFloor);
         if (a.m > -INFINITY && a.m < INFINITY && !(a.m >= LogitVec<FMT>::kLow && a.m <= LogitVec<FMT>::kHigh)) {
             // logits at the ends of the type's range: once more, relative to the part's maximum
             ScoreSums x{a.m, 0.f, 0.f, 0};
