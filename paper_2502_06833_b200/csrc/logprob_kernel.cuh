@@ -23,6 +23,7 @@ namespace ead {
 constexpr int kScoreThreads = 256;
 constexpr int kScoreSettle = 1024;                // runs between settlements of a thread's counts
 constexpr int kScoreUnroll = 4;                   // vectors of a run: a thread has them on their way together
+constexpr int kScoreDepth = 2;                    // runs on their way to shared memory, the one that is read among them
 constexpr int kScoreMaxTop = 64;                  // alternatives
 constexpr int kScoreMaxParts = kScoreThreads;     // of a row, at most
 constexpr int kScoreMaxJoin = 2048;               // parts x alternatives, at most
@@ -183,7 +184,10 @@ __device__ __forceinline__ ScoreSums shuffle_xor(const ScoreSums &a, int o)
 
 struct ScoreShared {
     ScoreSums warp_sums[kScoreThreads / 32];
-    unsigned long long cand[kScoreCandidates];
+    union {                                       // (barriers stand between the last run and the first candidate)
+        uint4 ring[kScoreDepth][kScoreUnroll][kScoreThreads];
+        unsigned long long cand[kScoreCandidates];
+    };
     unsigned long long best[kScoreMaxTop];        // the k largest keys, descending; 0: none
     unsigned long long warp_key[kScoreThreads / 32];
     uint2 warp_range[kScoreThreads / 32];
@@ -539,8 +543,25 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
         const RowVectors<FMT> vec(logits, p.V);
         const int g0 = static_cast<int>(static_cast<int64_t>(vec.n) * blockIdx.x / p.parts);
         const int g1 = static_cast<int>(static_cast<int64_t>(vec.n) * (blockIdx.x + 1) / p.parts);
-        // (on its way while the token and its logit are looked up)
-        if (g0 + static_cast<int>(threadIdx.x) < g1) asm volatile("prefetch.global.L1 [%0];" ::"l"(vec.base + 16 * (static_cast<int64_t>(g0) + threadIdx.x)));
+        const int n = g1 - g0, whole_end = vec.whole(g1 - 1) ? n : n - 1;                // vectors of this part
+        constexpr int kRun = kScoreUnroll * kScoreThreads;
+        // Whole runs go to shared memory, a lane's vectors to its own places, the first ones while the token and its logit are looked up.
+        const uint32_t ring = smem_u32(&sh.ring[0][0][threadIdx.x]);
+        const bool starts_cut = !vec.whole(g0);
+        int i = 0, asked = starts_cut ? kRun : 0;
+        uint32_t to = ring, from = ring;
+        auto ask = [&] {
+            if (asked + kRun <= whole_end) {
+                const uint8_t *const at = vec.base + 16 * static_cast<int64_t>(g0 + asked + static_cast<int>(threadIdx.x));
+#pragma unroll
+                for (int u = 0; u < kScoreUnroll; ++u) copy_async_16(to + u * kScoreThreads * 16, at + u * kScoreThreads * 16);
+                asked += kRun;
+                to = to == ring + (kScoreDepth - 1) * kRun * 16 ? ring : to + kRun * 16;
+            }
+            copy_async_commit();
+        };
+#pragma unroll
+        for (int d = 0; d < kScoreDepth - 1; ++d) ask();
         const int token = p.tokens ? ld_behind(p.tokens + row) : -1;
         const float z_token = token >= 0 && token < p.V ? logit_at<FMT>(logits, token) : 0.f;
         if (threadIdx.x == 0) {
@@ -552,9 +573,6 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
         const int g_given = given ? static_cast<int>((static_cast<int64_t>(token) + vec.shift) / N) : 0;
         const uint32_t t_or_equal = threshold<FMT>(z_given, false), t_above = threshold<FMT>(z_given, true);
         ScoreThread<FMT> th;
-        const int n = g1 - g0, whole_end = vec.whole(g1 - 1) ? n : n - 1;                // vectors of this part
-        int i = 0;
-        constexpr int kRun = kScoreUnroll * kScoreThreads;
         auto edge = [&] {                         // a run that may meet an end of the row or of the part
             const int g = g0 + i + threadIdx.x;
             uint4 v[kScoreUnroll];
@@ -564,15 +582,17 @@ __global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(Sc
             if (g < g1) th.template take<true>(vec, v, g, g1, given, z_given, t_or_equal, t_above, token, g_given);
             i += kRun;
         };
-        if (!vec.whole(g0)) edge();               // (whole_end may then be wrong for a row of one vector: no quick run fits)
+        if (starts_cut) edge();                   // (whole_end may then be wrong for a row of one vector: no quick run fits)
         while (i + kRun <= whole_end) {
             const int stop = min(whole_end, i + kScoreSettle * kRun);
             for (; i + kRun <= stop; i += kRun) {
                 const int g = g0 + i + threadIdx.x;
-                const uint8_t *const from = vec.base + 16 * static_cast<int64_t>(g);
+                ask();
+                copy_async_wait<kScoreDepth - 1>();
                 uint4 v[kScoreUnroll];
 #pragma unroll
-                for (int u = 0; u < kScoreUnroll; ++u) v[u] = load_logits(from + 16 * u * kScoreThreads);
+                for (int u = 0; u < kScoreUnroll; ++u) v[u] = ld_shared_16(from + u * kScoreThreads * 16);
+                from = from == ring + (kScoreDepth - 1) * kRun * 16 ? ring : from + kRun * 16;
                 th.template take<false>(vec, v, g, g1, given, z_given, t_or_equal, t_above, token, g_given);
             }
             th.above.settle();

@@ -194,24 +194,6 @@ __device__ __forceinline__ void put8(const RopePlace &at, int64_t offset, int sc
     }
 }
 
-// 16 bytes to the thread's own place in shared memory, without a register on the way.
-__device__ __forceinline__ void copy_async_16(uint32_t to, const void *from)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_async_wait()
-{
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint4 ld_shared_16(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-
 // The form for heads that are rotated in part or in neighbouring pairs.
 // Warp (token, share of its heads); queries first, then keys, then (for the cache) values, each in runs of kRopeRun elements.
 template <int FMT, bool DENSE>
