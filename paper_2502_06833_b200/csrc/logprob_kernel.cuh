@@ -532,7 +532,7 @@ struct ScoreThread {
 
 // Block (x, y): part x of row y, y + gridDim.y, ...
 template <int FMT>
-__global__ void __launch_bounds__(kScoreThreads, 5) ead_token_logprobs_kernel(ScoreParams p)
+__global__ void __launch_bounds__(kScoreThreads, 4) ead_token_logprobs_kernel(ScoreParams p)
 {
     __shared__ ScoreShared sh;
     constexpr int N = LogitVec<FMT>::kN;
