@@ -58,6 +58,8 @@ class EadConfig(C.Structure):
                 ("vocab_offset_large", C.c_int32)]
 
 
+# Descriptions keep their tensors alive (`held`) and are passed by address (`ref`): a ctypes reference kept in the description itself would close
+# a cycle, and the tensors' memory would wait for the cyclic collector.
 class EadKvCache(C.Structure):
     """``struct ead_kv_cache``; made by ``ead_kv_cache``."""
     _fields_ = [("format", C.c_int32), ("heads_kv", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
@@ -417,7 +419,7 @@ def ead_kv_cache(k, v, k_scale=None, v_scale=None) -> EadKvCache:
     c = EadKvCache(EAD_FMT_E4M3 if e4m3 else EAD_FMT_BF16, k.shape[1], k.shape[3], k.shape[2], k.shape[0], 0,
                    *strides(k), _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
     c.held = (k, v, k_scale, v_scale)
-    c.ref = C.byref(c)
+    c.ref = C.addressof(c)
     return c
 
 
@@ -435,7 +437,7 @@ def ead_kv_batch(page_table, new_start, kv_len=None, *, n_tokens, max_new, max_l
     c = EadKvBatch(B, int(n_tokens), int(max_new), int(max_len), _ptr(new_start), _ptr(kv_len), _ptr(page_table),
                    max(page_table.stride(0) if B > 1 else page_table.shape[1], 1), 0)
     c.held = (page_table, new_start, kv_len)
-    c.ref = C.byref(c)
+    c.ref = C.addressof(c)
     return c
 
 
@@ -540,7 +542,7 @@ def ead_e4m3_matrix(codes, scale, *, block) -> EadE4m3Matrix:
     _dense(scale, (-(-rows // block[0]), -(-cols // block[1])), T.uint8, "scale")
     m = EadE4m3Matrix(rows, cols, block[0], block[1], stride, _ptr(codes), _ptr(scale), 0)
     m.held = (codes, scale)
-    m.ref = C.byref(m)
+    m.ref = C.addressof(m)
     return m
 
 
@@ -576,7 +578,7 @@ def ead_rope(inv_freq, head_dim, *, interleaved=False, q_weight=None, k_weight=N
             _dense(t, (head_dim,), T.bfloat16, name)
     r = EadRope(head_dim, 2 * inv_freq.numel(), int(bool(interleaved)), float(eps), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), 0)
     r.held = (inv_freq, q_weight, k_weight)
-    r.ref = C.byref(r)
+    r.ref = C.addressof(r)
     return r
 
 
