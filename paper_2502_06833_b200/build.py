@@ -10,6 +10,7 @@ import subprocess
 import sys
 
 _DIR = os.path.dirname(os.path.abspath(__file__))
+_ROOT = os.path.dirname(_DIR)
 _CSRC = os.path.join(_DIR, "csrc")
 _OBJ = os.path.join(_DIR, "build")
 LIB_PATH = os.path.join(_DIR, "libead_b200.so")
@@ -30,14 +31,18 @@ def _stale(target: str, deps) -> bool:
 
 
 def _deps(source: str):
-    """The source and this repository's headers that it was last compiled with; all headers before the first time."""
+    """What the object of a source depends on in this repository: this file (it has the flags), the source, and the headers that it was last compiled
+    with; all headers where no list of this checkout says which."""
+    headers = [os.path.join(_CSRC, f) for f in os.listdir(_CSRC)] + [os.path.join(_ROOT, "include", "ead.h")]
     try:
         with open(_object(source) + ".d") as f:
             words = f.read().replace("\\\n", " ").split()[1:]
     except OSError:
-        return [source] + [os.path.join(_CSRC, f) for f in os.listdir(_CSRC)]
-    root = os.path.dirname(_DIR)
-    return [source] + [w for w in map(os.path.abspath, words) if w.startswith(root + os.sep)]
+        words = []
+    words = [os.path.normpath(os.path.join(_DIR, w)) for w in words if w != ":"]      # (compiled in _DIR by paths relative to it: a copied tree has its own files)
+    if source in words:
+        headers = [w for w in words if w.startswith(_ROOT + os.sep)]
+    return [os.path.abspath(__file__), source, *headers]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -45,7 +50,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     jobs = []
     for s in SOURCES:
         if force or _stale(_object(s), _deps(s)):
-            cmd = [_nvcc(), *_FLAGS, "-MD", "-MF", _object(s) + ".d", "-c", s, "-o", _object(s)]
+            cmd = [_nvcc(), *_FLAGS, "-MD", "-MF", _object(s) + ".d", "-c", os.path.relpath(s, _DIR), "-o", _object(s)]
             jobs.append(subprocess.Popen(cmd[:1] + (["-Xptxas=-v"] if verbose else []) + cmd[1:], cwd=_DIR, text=True,
                                          stdout=subprocess.PIPE, stderr=subprocess.STDOUT))
     said = [j.communicate()[0] for j in jobs]
