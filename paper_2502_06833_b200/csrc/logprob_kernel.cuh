@@ -173,8 +173,9 @@ __device__ __forceinline__ ScoreSums join_sums(const ScoreSums &a, const ScoreSu
     r.m = fmaxf(a.m, b.m);
     const float m = fmaxf(r.m, low), da = below_max(fmaxf(a.m, low), m), db = below_max(fmaxf(b.m, low), m);
     const float ea = exp2_of(da), eb = exp2_of(db);
-    r.s = a.s * ea + b.s * eb;
-    r.t = fmaf(a.s, da, a.t) * ea + fmaf(b.s, db, b.t) * eb;
+    // roundings spelled out: a product drawn into the sum would make it matter which set comes first, and lanes that exchange sums have them either way
+    r.s = __fadd_rn(__fmul_rn(a.s, ea), __fmul_rn(b.s, eb));
+    r.t = __fadd_rn(__fmul_rn(fmaf(a.s, da, a.t), ea), __fmul_rn(fmaf(b.s, db, b.t), eb));
     r.before = a.before + b.before;
     return r;
 }

@@ -387,3 +387,17 @@ def test_token_logprobs_counts_settle_more_than_once(E, space, which):
     assert abs(got[0].item() - (given - top - math.log(total))) <= _sum_error(torch.bfloat16, V, 32) + 2.0 ** -21 * (1 + abs(given - top) + math.log(total))
     best = torch.sort(z[0], descending=True, stable=True).indices[:k]
     assert torch.equal(got[3][0].long(), best)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,V", [(64, 30001), (200, 30001), (64, 500)])
+def test_token_logprobs_says_the_same_twice(E, space, dtype, n, V):
+    """A given token that is among the alternatives has one log probability: the two outputs hold the same number."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = (3.0 * torch.randn(1, V, generator=g, device="cuda")).to(dtype).repeat(n, 1)
+    top = _score(E, z, torch.zeros(n, device="cuda"), 64, space)[0][3]
+    tokens = top[0].repeat(4)[:n]
+    got, _ = _score(E, z, tokens, 64, space)
+    assert torch.equal(got[2].long(), torch.arange(64, device="cuda").repeat(4)[:n])
+    # (of one row: rows begin at different places in 16 bytes and may be added up in another order)
+    assert torch.equal(got[0], got[4].gather(1, got[2].long()[:, None])[:, 0])
