@@ -567,7 +567,8 @@ typedef struct ead_e4m3_matrix {
 /*
  * y = x, or y = x * gate / (1 + e^-gate) with a gate (the activations of a gated MLP), into 8-bit blocks: scales and codes as
  * defined above, for blocks of any of the three shapes.  A block with an x or gate that is not finite reads as NaNs.
- * A gate below -87.3 gives 0; a product of finite numbers beyond the largest 32-bit one is the block's largest code.
+ * With a gate y is within 2^-20 + 1.25 x 2^-24 |gate| of itself before it is rounded to a code.  A gate below -87.3
+ * gives 0; a product of finite numbers beyond the largest 32-bit one is the block's largest code.
  *   x, gate   dev, bf16 [rows, cols], x_stride and gate_stride elements apart; gate NULL: none (and none with 128 x 128 blocks)
  *   out       what is written; its codes' rows are block_cols wide stretches of y
  * Errors: EAD_EINVALID_ARG, EAD_EALIGNMENT, EAD_ELIMIT (rows x cols / 2048 above 2^32),

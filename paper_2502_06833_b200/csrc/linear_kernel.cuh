@@ -12,11 +12,14 @@
 // Many tokens (PAIR = true): two blocks share a tile of 256 features (cta_group::2), each holds its features' weights and half of the
 // tokens: per product a third less passes through L2, which bounds the other form at size.
 //
-// What bounds it, measured.  4099 x 7168 x 5120: 111 us, 2.70 PFLOP/s, 0.81 of twice the device's bf16 burst rate; the tensor pipe is busy 80 % of
-// the time, at the clock that the power limit leaves.  A head of 152064 x 1536 for 61 tokens into 32 bits: 46 us, 5.9 TB/s, 0.90 of the copy rate.
+// What bounds it, measured.  4099 x 7168 x 5120: 111-114 us in short runs of a replayed graph, 2.64-2.70 PFLOP/s, 0.79-0.81 of twice the device's bf16
+// burst rate, with the tensor pipe busy 80 % of the time; 130-135 us in calls one after another, whose clock the power limit sets: 2.23-2.31 PFLOP/s,
+// 0.80-0.82 of twice the sustained rate.  A head of 152064 x 1536 for 61 tokens into 32 bits: 46-50 us either way, 5.4-5.9 TB/s, 0.83-0.90 of the copy rate.
+// The sizes below take 0.1-0.4 us more in calls.
 // 64 tokens x 7168 x 5120: 10.8 us: the 37 MB stream in 6 us, the rest is the way to the first product (2.5 us: launch, barriers, first loads from
 // HBM) and from the last one (2.3 us: parts through the cluster, output).  347 x 5000 x 4128: 13.8 us: 33 stages of about 350 cycles for
 // 256 cycles of products, which is what 24 KB in and 40 KB out of shared memory take, and the same two ends.  One token x 2048 x 1536: 4.3 us.
+// A narrow output of a long sum is served worst where pairs begin, as they have no cut along K: 1536 x 8960, 160 tokens 10.5-13.8 us, 161 19.4, 200 19.2.
 //
 // Steps that mattered (us; 4099 tokens / 64 / 347): blocks of 128 x 240 with two sets of scales in TMEM and parts joined through global memory 252 / 34 / 50;
 // pairs, groups of scales, clusters, one issuing thread 183 / 14.3 / 23; its loop unrolled, four warps for scales, parts fetched 32 at a time 131 / 11.5 / 17;

@@ -6,9 +6,11 @@
 // largest logit of its other runs, so nearly always that run alone is read again, and what reaches the bound is sorted.  With few rows a row is cut
 // into parts, one block each; the last block of a row to finish joins the parts in their order, so the result does not depend on who comes last.
 // Whole runs go to shared memory, a lane's vectors to its own places, so that the next run's loads are on their way under the arithmetic without a register.
-// Measured, 2041 rows of 152064 in bf16: entropy alone 97 us, 6.4 TB/s, 0.98 of the device's copy rate; with the rank of a token 112, with 20
-// alternatives 110, with both 124: 71 % of the issue slots are taken, the special function unit is busy 63 % (an exponential per logit), and a row's end
-// (bound, second look, sort) is a chain of barriers that three other rows of the SM have to cover.  One row of 128256 in 32 bits 8.5 us, a chain of
+// Measured in a replayed graph, 2041 rows of 152064 in bf16: entropy alone 97 us, 6.4 TB/s, 0.98 of the device's copy rate; with the rank of a token 112, with
+// 20 alternatives 110, with both 124 (132-140 in calls one after another; f16 128, 1021 rows in 32 bits 111): 71 % of the issue slots are taken, the
+// special function unit is busy 63 % (an exponential per logit), and a row's end (bound, second look, sort) is a chain of barriers that three other rows of
+// the SM have to cover.  A row with more equal logits at the bound than the list of candidates has places (fewer unmasked ones than alternatives, say) is
+// scanned once per alternative: 2041 rows of 152064 with 10 unmasked logits and 20 alternatives 7.4 ms.  One row of 128256 in 32 bits 8.5 us, a chain of
 // look-ups, loads and the join.  On the way: a list per thread's strip read again 187, one element at a time 295, rows in two parts 174, runs loaded into
 // registers with five blocks per SM 139.  Runs of 2, 3, 4, 5 vectors (five blocks per SM, four for 5): 155, 144, 132, 131; of 4 with 5, 4, 3 blocks per SM
 // 132, 124, 133.

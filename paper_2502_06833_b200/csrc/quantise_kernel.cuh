@@ -1,8 +1,10 @@
 // bf16 values into 8-bit blocks: rows with a scale per 32 or 128 consecutive values (activations; of a gated MLP
 // y = silu(gate) * x is taken on the way), and matrices with a scale per 128 x 128 (weights).
 // Every value is read once and every code written once, so HBM bounds both at size and the launch at one step.
-// Measured: 8191 rows of 13824 with a gate 95 us, 5.9 TB/s, 0.91 of the device's copy rate, with 80 % of the issue slots taken (one exponential and one
-// reciprocal per value); 64 rows of 8960 2.1 us.  With one pass of 512 values per warp 145 us, 4 passes 103, 8 98, 14 and all 27 of a row 96.5.
+// Measured: 8191 rows of 13824 with a gate 95-102 us in a replayed graph, 5.6-5.9 TB/s, 0.85-0.91 of the device's copy rate, with 80 % of the issue slots
+// taken (one exponential and one reciprocal per value), 104-111 us in calls one after another; 64 rows of 8960 2.1-3.0 us.  With one pass of 512 values per
+// warp 145 us, 4 passes 103, 8 98, 14 and all 27 of a row 96.5.  Weights in 128 x 128 blocks: 152064 x 1536 132 us, 5.3 TB/s, 7168 x 5120 24 us, 4.7 TB/s
+// (each block of threads has its tile's loads out at once and waits for all of them; a weight is brought into the format once).
 #pragma once
 #include "kv_format.cuh"
 #include "ptx_sm100.cuh"
@@ -28,8 +30,10 @@ __device__ __forceinline__ uint2 to_e4m3x8(const float (&y)[8], float inv)
                       to_e4m3x2(y[4] * inv, y[5] * inv) | to_e4m3x2(y[6] * inv, y[7] * inv) << 16);
 }
 
-// g / (1 + e^-g): the exponential and the quotient by the special function unit, a few units of the last 32-bit place off; 0 for gates below
-// -87.3, where the divisor passes 2^126 (the product is below 2^-118 of x there).
+// g / (1 + e^-g): the exponential and the quotient by the special function unit, 2^-22 each; the exponential's argument is rounded to 32 bits, which
+// adds 1.25 x 2^-24 |g|: the result is within 2^-20 + 1.25 x 2^-24 |g| of itself (2^-17 at -87), where a code's rounding takes 2^-4.  The argument
+// in an exact and a small part would bring 2^-20 at every gate for 103 us instead of 95 (8191 rows of 13824).  0 for gates below -87.3, where the divisor
+// passes 2^126 (the product is below 2^-118 of x there).
 __device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.f + __expf(-g)); }
 
 // A warp takes a stretch of a row, kQuantPass values at a time, a lane 8 consecutive ones of each half of them: BLOCK / 8 neighbouring lanes share a

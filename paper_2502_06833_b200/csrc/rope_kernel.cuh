@@ -8,9 +8,11 @@
 // Two forms: heads rotated as a whole in halves (a lane holds 8 elements of either half), and all others (a lane holds 8 consecutive elements, partners
 // exchange the bf16 words as they were loaded).  Every element is read once and written once: HBM bounds it at size, launch and the
 // chain of look-ups at one step.
-// Measured: 18125 tokens of 32 + 8 + 8 heads of 128 into an 8-bit cache 79 us, 5.2 TB/s, 0.79 of the device's copy rate (the other form, with rows
-// two runs ahead in registers: 93; a block per token with angles shared: 174); 64 tokens of 40 + 8 + 8 heads 3.7 us; 4001 tokens of 32 + 8 heads of 64, 32
-// elements of each rotated, 9.8 us, 4.2 TB/s.  More runs ahead do not help (whole heads: 3 runs 80.6, 4 78.7, 5 79.0), more warps per SM cost registers
+// Measured: 18125 tokens of 32 + 8 + 8 heads of 128 into an 8-bit cache 79 us in a replayed graph, 5.2 TB/s, 0.79 of the device's copy rate, 81-85 us in
+// calls one after another; into a bf16 cache 77 us, 5.8 TB/s.  (On the way: the other form, with rows two runs ahead in registers, 93; a block per token with angles
+// shared 174.)  The other form, half of each head or neighbouring pairs: 92-94 us into 8 bits, 84 into bf16, with 82 % of the issue slots taken (64
+// registers; into a cache 8 and 24 bytes of them spill).  64 tokens of 40 + 8 + 8 heads 3.7-4.0 us; 4001 tokens of 32 + 8 heads of 64, 32
+// elements of each rotated, 9.8-9.9 us, 4.1-4.2 TB/s.  More runs ahead do not help (whole heads: 3 runs 80.6, 4 78.7, 5 79.0), more warps per SM cost registers
 // (whole heads: 16 warps 78.7, 24 81.5, 32 107; the other form: 32 warps 9.8, 24 11.5).
 #pragma once
 #include "quantise_kernel.cuh"
